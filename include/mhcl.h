@@ -308,6 +308,77 @@ int mhcl_coeffs_logits_layers(const mhcl_desc *desc, int32_t L, const void *cons
 int mhcl_ds_chain(int32_t n, int32_t L, int64_t T, const float *H, float *colsum, float *l1,
                   float *prod, float *prod_colsum, float *prod_l1, void *stream);
 
+/* ---- the two ends of a language model around a stack of layers ------------- */
+/*
+ * Not the paper's: what turns tokens into the streams that the first layer reads, and the last layer's streams into
+ * the loss that training needs.  With V the vocabulary, T tokens, n streams of width C:
+ *
+ *     x[t][i]  = scale * table[ids[t]]                       for every stream i       (mhcl_embed)
+ *     h[t]     = gain * s / sqrt(mean(s^2) + eps),  s = sum_i x[t][i]                 (mhcl_streams_norm)
+ *     loss[t]  = log sum_v exp(z[t][v]) - z[t][targets[t]],  z[t] = h[t] W^T          (mhcl_head_loss)
+ *
+ * The conventions above hold here too (device pointers, no allocation, no synchronisation, results that are the same
+ * bits from call to call), with these differences:
+ *  - ids, targets, weight, loss and lse need only the alignment of their element type (tokens[1:] is fine).
+ *  - A negative id or target marks a place that holds no token: its streams are zeros and it adds nothing to any gradient,
+ *    its loss is 0.  One that is V or more is a mistake that the host cannot see: its streams and its loss are NaN, and so are its g_h
+ *    and all of g_W unless its weight is 0; nothing is read or written out of bounds for it; mhcl_embed_bwd leaves it out.
+ *  - Gradients of table and W have the type of table and W.
+ */
+enum { MHCL_I64 = 0, MHCL_I32 = 1 };           /* id_dtype */
+typedef struct {
+  int32_t n;         /* residual streams, 1..8 (read by mhcl_embed* and mhcl_streams_norm*)             */
+  int32_t C;         /* width; a positive multiple of 8, at most 32768                                  */
+  int64_t T;         /* tokens, 0 .. 2^31 - 1                                                           */
+  int32_t V;         /* rows of table or W, >= 1 (not read by mhcl_streams_norm*)                       */
+  int32_t io_dtype;  /* MHCL_BF16 | MHCL_F32: streams, h and their gradients                            */
+  int32_t w_dtype;   /* MHCL_BF16 | MHCL_F32: table, W and their gradients (mhcl_head_*: equal io_dtype) */
+  int32_t id_dtype;  /* MHCL_I64 | MHCL_I32: ids and targets                                            */
+  float scale;       /* mhcl_embed*: factor of the rows, finite                                         */
+  float eps;         /* mhcl_streams_norm*: >= 0, added to the mean square                              */
+} mhcl_ends_desc;
+
+/* operations that need workspace, for mhcl_ends_workspace_bytes() */
+enum { MHCL_OP_EMBED_BWD = 0, MHCL_OP_STREAMS_NORM_BWD = 1, MHCL_OP_HEAD_LOSS = 2, MHCL_OP_HEAD_LOSS_GRAD = 3 };
+
+/* Bytes of workspace `op` needs for `desc`; 0 if desc or op is invalid or unsupported.  Host only. */
+size_t mhcl_ends_workspace_bytes(const mhcl_ends_desc *desc, int op);
+
+/* in : table [V,C] w, ids [T];  out: x [T,n,C] io */
+int mhcl_embed(const mhcl_ends_desc *desc, const void *table, const void *ids, void *x, void *stream);
+
+/* Backward of mhcl_embed: g_table[v] = scale * sum over the t with ids[t] = v, in order, and over the streams, of g_x[t][i].
+ * Sums are fp32 and rounded once.  accumulate != 0: added to what g_table holds (the gradient that a head of the same
+ * weights left there; rows without a token are then not touched), else overwritten, zeros where no token is.
+ * in : ids [T], g_x [T,n,C] io;  out: g_table [V,C] w */
+int mhcl_embed_bwd(const mhcl_ends_desc *desc, const void *ids, const void *g_x, void *g_table, int accumulate,
+                   void *ws, size_t ws_bytes, void *stream);
+
+/* in : x [T,n,C] io, gain [C] f32;  out: h [T,C] io */
+int mhcl_streams_norm(const mhcl_ends_desc *desc, const void *x, const float *gain, void *h, void *stream);
+
+/* Backward of mhcl_streams_norm; the norm's factor is recomputed from x.
+ * in : x [T,n,C], gain [C] f32, g_h [T,C] io;  out: g_x [T,n,C] io (every stream has the same gradient), g_gain [C] f32 */
+int mhcl_streams_norm_bwd(const mhcl_ends_desc *desc, const void *x, const float *gain, const void *g_h, void *g_x,
+                          float *g_gain, void *ws, size_t ws_bytes, void *stream);
+
+/* Softmax cross entropy of h W^T with the targets; logits never reach memory.  lse[t] = log sum_v exp(z[t][v]) is written for
+ * every token, counted or not.  Logits and sums are fp32, of bf16 operands as they are; fp32 operands enter as three bf16
+ * parts each (24 significant bits), six products of parts, so that an infinity among them makes NaN of the logits it meets.
+ * in : h [T,C] io, W [V,C] io, targets [T];  out: loss [T], lse [T] f32 */
+int mhcl_head_loss(const mhcl_ends_desc *desc, const void *h, const void *W, const void *targets, float *loss, float *lse,
+                   void *ws, size_t ws_bytes, void *stream);
+
+/* The same and the gradients of sum_t weight[t] loss[t]: g_h = g W, g_W = g^T h with g[t] = weight[t] (softmax(z[t]) - onehot(targets[t])).
+ * weight NULL: that of the mean, 1 / (number of targets that are not negative).  A place without a target, or of weight 0, adds
+ * nothing, whatever h holds there, NaN included.  bf16: g enters the two products rounded to bf16, once.
+ * The workspace holds a block of tokens' softmax numerators (16 bits each for bf16; at most MHCL_HEAD_BLOCK_BYTES, a block being
+ * at least 256 tokens, and blocks of fewer tokens than T add up g_W in fp32).
+ * in : h, W, targets as above, weight [T] f32 or NULL;  out: loss [T], lse [T] f32, g_h [T,C], g_W [V,C] io */
+#define MHCL_HEAD_BLOCK_BYTES (2ull << 30)
+int mhcl_head_loss_grad(const mhcl_ends_desc *desc, const void *h, const void *W, const void *targets, const float *weight,
+                        float *loss, float *lse, void *g_h, void *g_W, void *ws, size_t ws_bytes, void *stream);
+
 /* ---- measurement aids (no part of the method) --------------------------- */
 
 /* Kernel stages that can be bracketed with events. */

@@ -11,6 +11,11 @@ from .binding import (  # noqa: F401
     mhcl_coeffs, mhcl_pre, mhcl_post, mhcl_fwd_coeffs_pre, mhcl_post_bwd, mhcl_pre_bwd,
     mhcl_coeffs_bwd, mhcl_bwd_fused, mhcl_logits, mhcl_coeffs_logits, mhcl_coeffs_logits_layers, mhcl_ds_chain, mhcl_fwd_coeffs_pre_static,
     STATIC_SCRATCH_BYTES,
+    I64, I32, OP_EMBED_BWD, OP_STREAMS_NORM_BWD, OP_HEAD_LOSS, OP_HEAD_LOSS_GRAD, EndsDesc, ends_workspace_bytes,
+    mhcl_embed, mhcl_embed_bwd, mhcl_streams_norm, mhcl_streams_norm_bwd, mhcl_head_loss, mhcl_head_loss_grad,
 )
 from .layer import GpuLayer, desc_for, empty_stream, place_stream  # noqa: F401,E402
 from .autograd import HyperConnection, HyperConnectionStack, init_params  # noqa: F401,E402
+from .ends import (  # noqa: F401,E402
+    embed_tokens, embed_tokens_grad, streams_norm, streams_norm_grad, head_loss, head_loss_grad,
+)

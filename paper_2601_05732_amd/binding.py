@@ -19,6 +19,8 @@ _LIB_PATH = os.path.join(_HERE, "libmhcl.so")
 BF16, F32 = 0, 1
 RES_LITE, RES_SK, RES_SUBSET = 0, 1, 2
 OP_COEFFS, OP_COEFFS_BWD, OP_FWD_COEFFS_PRE, OP_BWD_FUSED, OP_COEFFS_LAYERS = 0, 1, 2, 3, 4
+I64, I32 = 0, 1
+OP_EMBED_BWD, OP_STREAMS_NORM_BWD, OP_HEAD_LOSS, OP_HEAD_LOSS_GRAD = 0, 1, 2, 3   # of the ends, ends_workspace_bytes
 
 _SYMBOLS = [
     "mhcl_status_string", "mhcl_validate", "mhcl_logit_count", "mhcl_workspace_bytes",
@@ -26,6 +28,8 @@ _SYMBOLS = [
     "mhcl_post_bwd", "mhcl_pre_bwd", "mhcl_coeffs_bwd", "mhcl_bwd_fused",
     "mhcl_logits", "mhcl_ds_chain", "mhcl_profile_next_call", "mhcl_debug_copy",
     "mhcl_fwd_coeffs_pre_static", "mhcl_coeffs_logits", "mhcl_coeffs_logits_layers", "mhcl_streams_in", "mhcl_streams_out",
+    "mhcl_ends_workspace_bytes", "mhcl_embed", "mhcl_embed_bwd", "mhcl_streams_norm", "mhcl_streams_norm_bwd",
+    "mhcl_head_loss", "mhcl_head_loss_grad",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20   # MHCL_STATIC_SCRATCH_BYTES
 
@@ -41,6 +45,29 @@ class _CDesc(ctypes.Structure):
                 ("io_dtype", ctypes.c_int32), ("res_mode", ctypes.c_int32),
                 ("sk_iters", ctypes.c_int32), ("eps", ctypes.c_float),
                 ("n_perm", ctypes.c_int32), ("perm", ctypes.c_void_p)]
+
+
+class _CEndsDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("C", ctypes.c_int32), ("T", ctypes.c_int64), ("V", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("w_dtype", ctypes.c_int32), ("id_dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+_DTYPE = {torch.bfloat16: BF16, torch.float32: F32}
+_ID_DTYPE = {torch.int64: I64, torch.int32: I32}
+
+
+class EndsDesc:
+    """Mirror of ``mhcl_ends_desc``, with torch's types."""
+    __slots__ = ("n", "C", "T", "V", "io", "w", "ids", "c")
+
+    def __init__(self, C, T, n=1, V=1, io=torch.bfloat16, w=torch.float32, ids=torch.int64, scale=1.0, eps=1e-6):
+        if io not in _DTYPE or w not in _DTYPE or ids not in _ID_DTYPE:
+            raise ValueError(f"types {io}, {w}, {ids}: streams and weights are bfloat16 or float32, tokens int64 or int32")
+        if not (-2 ** 31 <= C < 2 ** 31 and -2 ** 31 <= V < 2 ** 31 and -2 ** 31 <= n < 2 ** 31):
+            raise ValueError(f"n = {n}, C = {C}, V = {V}: out of range")
+        self.n, self.C, self.T, self.V, self.io, self.w, self.ids = n, C, T, V, io, w, ids
+        self.c = _CEndsDesc(n, C, T, V, _DTYPE[io], _DTYPE[w], _ID_DTYPE[ids], scale, eps)
 
 
 class Desc:
@@ -116,6 +143,15 @@ def lib():
         L.mhcl_streams_in.argtypes = L.mhcl_streams_out.argtypes = [P] + [V] * 3
         L.mhcl_coeffs_logits_layers.argtypes = [P, ctypes.c_int32] + [V] * 8 + [Z, V]
         L.mhcl_ds_chain.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int64] + [V] * 7
+        E = ctypes.POINTER(_CEndsDesc)
+        L.mhcl_ends_workspace_bytes.restype = Z
+        L.mhcl_ends_workspace_bytes.argtypes = [E, ctypes.c_int]
+        L.mhcl_embed.argtypes = [E] + [V] * 4
+        L.mhcl_embed_bwd.argtypes = [E] + [V] * 3 + [ctypes.c_int, V, Z, V]
+        L.mhcl_streams_norm.argtypes = [E] + [V] * 4
+        L.mhcl_streams_norm_bwd.argtypes = [E] + [V] * 6 + [Z, V]
+        L.mhcl_head_loss.argtypes = [E] + [V] * 6 + [Z, V]
+        L.mhcl_head_loss_grad.argtypes = [E] + [V] * 9 + [Z, V]
         _lib = L
     return _lib
 
@@ -328,3 +364,60 @@ def mhcl_ds_chain(n, L, T, H, colsum, l1, prod, prod_colsum, prod_l1):
         _ptr(l1, f, (L, T), "l1"), _ptr(prod, f, (T, n, n), "prod"),
         _ptr(prod_colsum, f, (L, T, n), "prod_colsum"), _ptr(prod_l1, f, (L, T), "prod_l1"),
         _stream()), "mhcl_ds_chain")
+
+
+# ---- the two ends of a language model ---------------------------------------------------------
+
+
+def ends_workspace_bytes(d: EndsDesc, op: int) -> int:
+    return lib().mhcl_ends_workspace_bytes(ctypes.byref(d.c), op)
+
+
+def new_ends_workspace(d: EndsDesc, op: int, device="cuda"):
+    return torch.empty(ends_workspace_bytes(d, op), dtype=torch.uint8, device=device)
+
+
+def mhcl_embed(d, table, ids, x):
+    _check(lib().mhcl_embed(ctypes.byref(d.c), _ptr(table, d.w, (d.V, d.C), "table"), _ptr(ids, d.ids, (d.T,), "ids"),
+                            _ptr(x, d.io, (d.T, d.n, d.C), "x"), _stream()), "mhcl_embed")
+
+
+def mhcl_embed_bwd(d, ids, g_x, g_table, accumulate, ws):
+    wp, wb = _ws(ws)
+    _check(lib().mhcl_embed_bwd(
+        ctypes.byref(d.c), _ptr(ids, d.ids, (d.T,), "ids"), _ptr(g_x, d.io, (d.T, d.n, d.C), "g_x"),
+        _ptr(g_table, d.w, (d.V, d.C), "g_table"), int(accumulate), wp, wb, _stream()), "mhcl_embed_bwd")
+
+
+def mhcl_streams_norm(d, x, gain, h):
+    _check(lib().mhcl_streams_norm(ctypes.byref(d.c), _ptr(x, d.io, (d.T, d.n, d.C), "x"),
+                                   _ptr(gain, torch.float32, (d.C,), "gain"), _ptr(h, d.io, (d.T, d.C), "h"), _stream()),
+           "mhcl_streams_norm")
+
+
+def mhcl_streams_norm_bwd(d, x, gain, g_h, g_x, g_gain, ws):
+    f = torch.float32
+    wp, wb = _ws(ws)
+    _check(lib().mhcl_streams_norm_bwd(
+        ctypes.byref(d.c), _ptr(x, d.io, (d.T, d.n, d.C), "x"), _ptr(gain, f, (d.C,), "gain"),
+        _ptr(g_h, d.io, (d.T, d.C), "g_h"), _ptr(g_x, d.io, (d.T, d.n, d.C), "g_x"), _ptr(g_gain, f, (d.C,), "g_gain"),
+        wp, wb, _stream()), "mhcl_streams_norm_bwd")
+
+
+def mhcl_head_loss(d, h, W, targets, loss, lse, ws):
+    f = torch.float32
+    wp, wb = _ws(ws)
+    _check(lib().mhcl_head_loss(
+        ctypes.byref(d.c), _ptr(h, d.io, (d.T, d.C), "h"), _ptr(W, d.w, (d.V, d.C), "W"),
+        _ptr(targets, d.ids, (d.T,), "targets"), _ptr(loss, f, (d.T,), "loss"), _ptr(lse, f, (d.T,), "lse"), wp, wb,
+        _stream()), "mhcl_head_loss")
+
+
+def mhcl_head_loss_grad(d, h, W, targets, weight, loss, lse, g_h, g_W, ws):
+    f = torch.float32
+    wp, wb = _ws(ws)
+    _check(lib().mhcl_head_loss_grad(
+        ctypes.byref(d.c), _ptr(h, d.io, (d.T, d.C), "h"), _ptr(W, d.w, (d.V, d.C), "W"),
+        _ptr(targets, d.ids, (d.T,), "targets"), None if weight is None else _ptr(weight, f, (d.T,), "weight"),
+        _ptr(loss, f, (d.T,), "loss"), _ptr(lse, f, (d.T,), "lse"), _ptr(g_h, d.io, (d.T, d.C), "g_h"),
+        _ptr(g_W, d.w, (d.V, d.C), "g_W"), wp, wb, _stream()), "mhcl_head_loss_grad")

@@ -1,0 +1,530 @@
+// The ends of a language model, first part: token embedding into the streams with the table's gradient, and the norm of
+// the streams' sum with its backward.
+#include "mhcl_common.h"
+#include "mhcl_ends.h"
+
+namespace mhcl {
+namespace {
+
+constexpr int kBlock = 256;
+
+template <typename F>
+hipError_t dispatch_id(int id_dtype, F &&f) {
+  if (id_dtype == MHCL_I64) return f(int64_t{});
+  return f(int32_t{});
+}
+
+// an id as 32 bits: -1 where there is no token, V where it is none of the vocabulary's
+template <typename ID>
+__device__ __forceinline__ int32_t token_of(const ID *ids, int64_t t, int32_t V) {
+  const ID id = ids[t];
+  return id < 0 ? -1 : (id >= V ? V : static_cast<int32_t>(id));
+}
+
+// VEC elements of type W (a row's piece; VEC * sizeof(W) is 8, 16 or 32 bytes) as fp32, and back
+template <typename W, int VEC>
+__device__ __forceinline__ void load_as(const void *p, size_t elem, float (&v)[VEC]) {
+  if constexpr (W::kVec == VEC) {
+    W::load(p, elem, v);
+  } else if constexpr (W::kVec == 4) {   // 8 floats
+    float lo[4], hi[4];
+    F32::load(p, elem, lo);
+    F32::load(p, elem + 4, hi);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = lo[e], v[e + 4] = hi[e];
+  } else {                               // 4 bf16
+    const uint2 q = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + elem);
+    v[0] = bf16lo(q.x); v[1] = bf16hi(q.x); v[2] = bf16lo(q.y); v[3] = bf16hi(q.y);
+  }
+}
+template <typename W, int VEC>
+__device__ __forceinline__ void store_as(void *p, size_t elem, const float (&v)[VEC]) {
+  if constexpr (W::kVec == VEC) {
+    W::store(p, elem, v);
+  } else if constexpr (W::kVec == 4) {
+    const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
+    F32::store(p, elem, lo);
+    F32::store(p, elem + 4, hi);
+  } else {
+    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p) + elem) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  }
+}
+
+// ---------------------------------------------------------------- embedding
+// x[t][i] = scale table[ids[t]]: one thread per 16-byte piece of a row of C, which it reads once and writes n times.
+// Bound by the writes.
+template <typename IO, typename W, typename ID>
+__global__ __launch_bounds__(kBlock) void embed_kernel(const void *__restrict__ table, const ID *__restrict__ ids,
+                                                       void *__restrict__ x, int n, int C, int64_t T, int32_t V, float scale) {
+  constexpr int VEC = IO::kVec;
+  const int vpr = C / VEC;
+  const int64_t idx = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x;
+  const int64_t t = idx / vpr;
+  if (t >= T) return;
+  const int c = static_cast<int>(idx - t * vpr) * VEC;
+  const int32_t id = token_of(ids, t, V);
+  float v[VEC];
+  if (id >= 0 && id < V) {
+    load_as<W, VEC>(table, static_cast<size_t>(id) * C + c, v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] *= scale;
+  } else {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = id < 0 ? 0.f : __uint_as_float(0x7fc00000u);
+  }
+  for (int i = 0; i < n; ++i) IO::store(x, (t * n + i) * C + c, v);
+}
+
+// Tokens by id: a token's place is the number of tokens with a smaller id, or the same id and an earlier place.  A block
+// ranks 64 tokens, one a lane; its sixteen waves share out the tokens compared with, whose ids are wave-uniform.
+constexpr int kRankWaves = 16;
+template <typename ID>
+__global__ __launch_bounds__(64 * kRankWaves) void rank_kernel(const ID *__restrict__ ids, int32_t *__restrict__ key,
+                                                               int32_t *__restrict__ pos, int32_t T, int32_t V) {
+  __shared__ int32_t count[kRankWaves][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t t = blockIdx.x * 64 + lane;
+  // (what has no place in the table goes last)
+  const auto key_of = [&](int32_t j) {
+    const ID id = ids[j];
+    return id < 0 || id >= V ? V : static_cast<int32_t>(id);
+  };
+  const int32_t mine = t < T ? key_of(t) : V;
+  const int32_t per = ((T + kRankWaves - 1) / kRankWaves + 63) / 64 * 64;
+  const int32_t first = wave * per, last = min(T, first + per);
+  int32_t smaller = 0;
+  for (int32_t j0 = first; j0 < last; j0 += 64) {
+    const int32_t theirs = j0 + lane < last ? key_of(j0 + lane) : 0x7fffffff;
+#pragma unroll
+    for (int k = 0; k < 64; ++k) {
+      const int32_t other = __builtin_amdgcn_readlane(theirs, k);
+      smaller += (other < mine || (other == mine && j0 + k < t)) ? 1 : 0;
+    }
+  }
+  count[wave][lane] = smaller;
+  __syncthreads();
+  if (wave == 0 && t < T) {
+    int32_t place = 0;
+#pragma unroll
+    for (int w = 0; w < kRankWaves; ++w) place += count[w][lane];
+    key[place] = mine;
+    pos[place] = t;
+  }
+}
+
+// Sums of kChunk sorted tokens, TX threads for a row's columns (grid.y: the pieces of VEC TX columns), one chunk per
+// threadIdx.y.  A row whose tokens all lie in the chunk is written; of a row shared with other chunks the sum goes to
+// part[chunk][0] where it continues from the chunk before, else (it begins here) to part[chunk][1].
+template <typename IO, typename W, bool ACC>
+__device__ __forceinline__ void embed_write(void *g_table, size_t elem, const float (&sum)[IO::kVec], float scale) {
+  constexpr int VEC = IO::kVec;
+  float v[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) v[e] = sum[e] * scale;
+  if constexpr (ACC) {
+    float old[VEC];
+    load_as<W, VEC>(g_table, elem, old);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] += old[e];
+  }
+  store_as<W, VEC>(g_table, elem, v);
+}
+template <typename IO, typename W, bool ACC>
+__global__ __launch_bounds__(kBlock) void embed_sum_kernel(const int32_t *__restrict__ key, const int32_t *__restrict__ pos,
+                                                           const void *__restrict__ g_x, void *__restrict__ g_table,
+                                                           float *__restrict__ part, int n, int C, int32_t T, int32_t V, float scale) {
+  constexpr int VEC = IO::kVec;
+  const int32_t chunk = blockIdx.x * blockDim.y + threadIdx.y;
+  const int64_t s = static_cast<int64_t>(chunk) * kChunk;
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * VEC;
+  if (s >= T || c >= C) return;
+  const int count = static_cast<int>(min<int64_t>(kChunk, T - s));
+  float sum[VEC] = {};
+  int32_t cur = key[s];
+  bool from_before = s > 0 && key[s - 1] == cur;
+  for (int k = 0; k < count; ++k) {
+    const int32_t id = key[s + k];
+    if (id != cur) {
+      if (cur < V) {
+        if (from_before) store_as<F32, VEC>(part, static_cast<size_t>(chunk) * 2 * C + c, sum);
+        else embed_write<IO, W, ACC>(g_table, static_cast<size_t>(cur) * C + c, sum, scale);
+      }
+      cur = id;
+      from_before = false;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
+    }
+    if (id >= V) return;   // (those come last)
+    const int64_t row = static_cast<int64_t>(pos[s + k]) * n;
+    float own[VEC] = {};
+    for (int i = 0; i < n; ++i) {
+      float v[VEC];
+      IO::load(g_x, (row + i) * C + c, v);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) own[e] += v[e];
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) sum[e] += own[e];
+  }
+  const bool goes_on = s + count < T && key[s + count] == cur;
+  if (!from_before && !goes_on) {
+    embed_write<IO, W, ACC>(g_table, static_cast<size_t>(cur) * C + c, sum, scale);
+    return;
+  }
+  store_as<F32, VEC>(part, (static_cast<size_t>(chunk) * 2 + (from_before ? 0 : 1)) * C + c, sum);
+}
+
+// The rows that lie in several chunks: a block looks at one chunk's last row, and where that begins in this chunk and goes
+// on, adds the parts of the chunks after it, in order: sixteen threads of a column take a range of them each.
+constexpr int kJoinRows = 16;
+template <typename W, bool ACC>
+__global__ __launch_bounds__(64 * kJoinRows) void embed_join_kernel(const int32_t *__restrict__ key, const float *__restrict__ part,
+                                                                    void *__restrict__ g_table, int C, int32_t T, int32_t V, float scale) {
+  __shared__ float red[kJoinRows][64];
+  const int64_t chunk = blockIdx.x;
+  const int64_t e = (chunk + 1) * kChunk;
+  if (e >= T) return;
+  const int32_t id = key[e - 1];
+  if (id >= V || key[e] != id) return;                                  // ends here
+  const int64_t s = chunk * kChunk;
+  if (key[s] == id && s > 0 && key[s - 1] == id) return;                // began before
+  // its last chunk: the one of the last token with this id
+  int64_t lo = e, hi = T;                                               // key[lo] == id, key[hi] > id
+  while (hi - lo > 1) {
+    const int64_t mid = (lo + hi) / 2;
+    if (key[mid] == id) lo = mid;
+    else hi = mid;
+  }
+  const int64_t parts = lo / kChunk - chunk;                            // after this chunk's
+  const int c = blockIdx.y * 64 + threadIdx.x;
+  const int64_t per = (parts + kJoinRows - 1) / kJoinRows;
+  const int64_t k0 = threadIdx.y * per, k1 = min(parts, k0 + per);
+  float sum = 0.f;
+  if (c < C) {
+    if (threadIdx.y == 0) sum = part[(chunk * 2 + 1) * C + c];
+#pragma unroll 8
+    for (int64_t k = k0; k < k1; ++k) sum += part[(chunk + 1 + k) * 2 * C + c];
+  }
+  red[threadIdx.y][threadIdx.x] = sum;
+  __syncthreads();
+  if (threadIdx.y != 0 || c >= C) return;
+  sum = pairwise_sum<kJoinRows>([&](int k) { return red[k][threadIdx.x]; }) * scale;
+  const size_t at = static_cast<size_t>(id) * C + c;
+  if constexpr (W::kVec == 8) {
+    uint16_t *g = static_cast<uint16_t *>(g_table);
+    if constexpr (ACC) sum += bf16_to_f32(g[at]);
+    g[at] = f32_to_bf16(sum);
+  } else {
+    float *g = static_cast<float *>(g_table);
+    if constexpr (ACC) sum += g[at];
+    g[at] = sum;
+  }
+}
+
+// Zeros in the rows of no token: a wave looks up 64 rows, one a lane, among the sorted ids.
+__global__ __launch_bounds__(kBlock) void embed_zero_kernel(const int32_t *__restrict__ key, uint4 *__restrict__ g_table,
+                                                            int chunks16, int32_t T, int32_t V) {
+  const int lane = threadIdx.x & 63;
+  const int64_t v0 = (static_cast<int64_t>(blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6)) * 64;
+  if (v0 >= V) return;
+  const int64_t v = v0 + lane;
+  int32_t lo = 0, hi = T;   // first place whose id is v or more
+  while (lo < hi) {
+    const int32_t mid = lo + (hi - lo) / 2;
+    if (key[mid] < v) lo = mid + 1;
+    else hi = mid;
+  }
+  const bool absent = v < V && (lo >= T || key[lo] != v);
+  uint64_t rows = __ballot(absent);
+  while (rows) {
+    const int r = __ffsll(static_cast<unsigned long long>(rows)) - 1;
+    rows &= rows - 1;
+    uint4 *row = g_table + (v0 + r) * chunks16;
+    for (int c = lane; c < chunks16; c += 64) row[c] = make_uint4(0, 0, 0, 0);
+  }
+}
+
+// ---------------------------------------------------------------- norm of the streams' sum
+// A token's row of C is held by L threads, CH pieces of 16 bytes each; a block has kTokens(L) tokens at a time.
+constexpr int norm_tokens(int L) { return L >= 256 ? 1 : 256 / L; }
+
+// sum over the L threads of a token, in each of them
+template <int L>
+__device__ __forceinline__ float row_sum(float v, float *red) {
+  v = wave_sum(v);
+  if constexpr (L > 64) {
+    constexpr int waves = L / 64;
+    __syncthreads();                       // (red may still be read from the sum before)
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = pairwise_sum<waves>([&](int k) { return red[k]; });
+  }
+  return v;
+}
+
+template <typename IO, int N, int VEC>
+__device__ __forceinline__ void stream_sum(const void *x, int64_t t, int n, int C, int c, float (&s)[VEC]) {
+  if constexpr (N > 0) {
+    float v[N][VEC];
+#pragma unroll
+    for (int i = 0; i < N; ++i) IO::load(x, (t * N + i) * C + c, v[i]);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      s[e] = v[0][e];
+#pragma unroll
+      for (int i = 1; i < N; ++i) s[e] += v[i][e];
+    }
+  } else {
+    IO::load(x, t * n * C + c, s);
+    for (int i = 1; i < n; ++i) {
+      float v[VEC];
+      IO::load(x, (t * n + i) * C + c, v);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[e] += v[e];
+    }
+  }
+}
+
+// h = gain s / sqrt(mean(s^2) + eps), s the sum of a token's streams in fp32; one pass, bound by memory
+template <typename IO, int N, int L, int CH>
+__global__ __launch_bounds__(L *norm_tokens(L)) void norm_kernel(const void *__restrict__ x, const float *__restrict__ gain,
+                                                                 void *__restrict__ h, int n, int C, int64_t T, float eps) {
+  constexpr int VEC = IO::kVec;
+  __shared__ float red[16];
+  const int lane = threadIdx.x % L;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * norm_tokens(L) + threadIdx.x / L;
+  if (t >= T) return;                      // (whole waves; with more than a wave a token the block has one token)
+  float s[CH][VEC], sq = 0.f;
+#pragma unroll
+  for (int k = 0; k < CH; ++k) {
+    const int c = (k * L + lane) * VEC;
+    if (c < C) {
+      stream_sum<IO, N>(x, t, n, C, c, s[k]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sq = fmaf(s[k][e], s[k][e], sq);
+    }
+  }
+  const float r = rms_factor(row_sum<L>(sq, red), C, eps);
+#pragma unroll
+  for (int k = 0; k < CH; ++k) {
+    const int c = (k * L + lane) * VEC;
+    if (c < C) {
+      float g[VEC];
+      load_as<F32, VEC>(gain, c, g);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) g[e] *= s[k][e] * r;
+      IO::store(h, t * C + c, g);
+    }
+  }
+}
+
+// u = s r, g = g_h gain:  g_s = r (g - u mean(g u)), written to every stream; g_gain = sum_t g_h u.  A block takes every
+// gridDim-th token and keeps its part of g_gain in registers.
+template <typename IO, int N, int L, int CH>
+__global__ __launch_bounds__(L *norm_tokens(L)) void norm_bwd_kernel(const void *__restrict__ x, const float *__restrict__ gain,
+                                                                     const void *__restrict__ g_h, void *__restrict__ g_x,
+                                                                     float *__restrict__ part, int n, int C, int64_t T, float eps) {
+  constexpr int VEC = IO::kVec, TOK = norm_tokens(L);
+  __shared__ float red[16];
+  const int lane = threadIdx.x % L, row = threadIdx.x / L;
+  float acc[CH][VEC] = {};
+  for (int64_t t = static_cast<int64_t>(blockIdx.x) * TOK + row; t < T; t += static_cast<int64_t>(gridDim.x) * TOK) {
+    float s[CH][VEC], g[CH][VEC], sq = 0.f, gs = 0.f;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int c = (k * L + lane) * VEC;
+      if (c < C) {
+        stream_sum<IO, N>(x, t, n, C, c, s[k]);
+        float w[VEC];
+        IO::load(g_h, t * C + c, g[k]);
+        load_as<F32, VEC>(gain, c, w);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          sq = fmaf(s[k][e], s[k][e], sq);
+          gs = fmaf(g[k][e] * w[e], s[k][e], gs);
+        }
+      }
+    }
+    const float r = rms_factor(row_sum<L>(sq, red), C, eps);
+    const float m = row_sum<L>(gs, red) / static_cast<float>(C) * r * r;   // mean(g u) r
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int c = (k * L + lane) * VEC;
+      if (c < C) {
+        float w[VEC], o[VEC];
+        load_as<F32, VEC>(gain, c, w);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float u = s[k][e] * r;
+          acc[k][e] = fmaf(g[k][e], u, acc[k][e]);
+          o[e] = r * (g[k][e] * w[e]) - u * m;
+        }
+        for (int i = 0; i < n; ++i) IO::store(g_x, (t * n + i) * C + c, o);
+      }
+    }
+  }
+  // the tokens of a block that share it add up, in order
+  if constexpr (TOK > 1) {
+    __shared__ float sums[TOK][64 * VEC];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sums[row][e * 64 + lane] = acc[k][e];
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) acc[k][e] = pairwise_sum<TOK>([&](int j) { return sums[j][e * 64 + lane]; });
+    }
+  }
+  if (row == 0) {
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int c = (k * L + lane) * VEC;
+      if (c < C) store_as<F32, VEC>(part, static_cast<size_t>(blockIdx.x) * C + c, acc[k]);
+    }
+  }
+}
+
+// g_gain[c] = the sum of its column of `part`, in order: sixteen threads of a column take a range of the rows each
+__global__ __launch_bounds__(1024) void gain_sum_kernel(const float *__restrict__ part, float *__restrict__ g_gain, int rows, int C) {
+  __shared__ float red[16][64];
+  const int c = blockIdx.x * 64 + threadIdx.x;
+  const int per = (rows + 15) / 16, k0 = threadIdx.y * per, k1 = min(rows, k0 + per);
+  float sum = 0.f;
+  if (c < C) {
+#pragma unroll 8
+    for (int k = k0; k < k1; ++k) sum += part[static_cast<size_t>(k) * C + c];
+  }
+  red[threadIdx.y][threadIdx.x] = sum;
+  __syncthreads();
+  if (threadIdx.y == 0 && c < C) g_gain[c] = pairwise_sum<16>([&](int k) { return red[k][threadIdx.x]; });
+}
+
+__global__ __launch_bounds__(kBlock) void zero_kernel(uint32_t *__restrict__ p, size_t words) {
+  const size_t i = static_cast<size_t>(blockIdx.x) * kBlock + threadIdx.x;
+  if (i < words) p[i] = 0;
+}
+
+inline unsigned blocks(int64_t items, int64_t each) { return static_cast<unsigned>((items + each - 1) / each); }
+
+template <typename F>
+hipError_t dispatch_io_w(const mhcl_ends_desc &d, F &&f) {
+  return dispatch_io(d.io_dtype, [&](auto io) {
+    return dispatch_io(d.w_dtype, [&](auto w) { return f(io, w); });
+  });
+}
+
+// L, CH of a row of `pieces` 16-byte pieces: few threads where a row is short, so that a block has several tokens; no more
+// than two pieces a thread while the block can grow
+template <typename F>
+hipError_t dispatch_row(int pieces, F &&f) {
+  const auto go = [&](auto l, auto ch) { return f(l, ch); };
+  if (pieces <= 64) return go(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+  if (pieces <= 128) return go(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+  if (pieces <= 256) return go(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+  if (pieces <= 512) return go(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
+  if (pieces <= 1024) return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
+  if (pieces <= 2048) return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
+  return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 8>{});
+}
+// number of streams: known to the kernel up to four
+template <typename F>
+hipError_t dispatch_streams(int n, F &&f) {
+  switch (n) {
+    case 1: return f(std::integral_constant<int, 1>{});
+    case 2: return f(std::integral_constant<int, 2>{});
+    case 3: return f(std::integral_constant<int, 3>{});
+    case 4: return f(std::integral_constant<int, 4>{});
+  }
+  return f(std::integral_constant<int, 0>{});
+}
+
+}  // namespace
+
+hipError_t launch_zero(void *p, size_t bytes, hipStream_t s) {
+  const size_t words = bytes / 4;
+  if (words == 0) return hipSuccess;
+  hipLaunchKernelGGL(zero_kernel, dim3(blocks(words, kBlock)), dim3(kBlock), 0, s, static_cast<uint32_t *>(p), words);
+  return hipGetLastError();
+}
+
+hipError_t launch_embed(const mhcl_ends_desc &d, const void *table, const void *ids, void *x, hipStream_t s) {
+  return dispatch_io_w(d, [&](auto io, auto w) {
+    return dispatch_id(d.id_dtype, [&](auto id) {
+      using IO = decltype(io);
+      using ID = decltype(id);
+      hipLaunchKernelGGL((embed_kernel<IO, decltype(w), ID>), dim3(blocks(d.T * (d.C / IO::kVec), kBlock)), dim3(kBlock), 0, s,
+                         table, static_cast<const ID *>(ids), x, d.n, d.C, d.T, d.V, d.scale);
+      return hipGetLastError();
+    });
+  });
+}
+
+hipError_t launch_embed_bwd(const mhcl_ends_desc &d, const void *ids, const void *g_x, void *g_table, bool accumulate,
+                            const EmbedBwdWs &w, hipStream_t s) {
+  const int32_t T = static_cast<int32_t>(d.T);
+  hipError_t e = dispatch_id(d.id_dtype, [&](auto id) {
+    using ID = decltype(id);
+    hipLaunchKernelGGL((rank_kernel<ID>), dim3(blocks(T, 64)), dim3(64 * kRankWaves), 0, s, static_cast<const ID *>(ids), w.key,
+                       w.pos, T, d.V);
+    return hipGetLastError();
+  });
+  if (e != hipSuccess) return e;
+  if (!accumulate) {
+    const int chunks16 = static_cast<int>(d.C * dtype_bytes(d.w_dtype) / 16);
+    hipLaunchKernelGGL(embed_zero_kernel, dim3(blocks(d.V, kBlock)), dim3(kBlock), 0, s, w.key, static_cast<uint4 *>(g_table),
+                       chunks16, T, d.V);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  const unsigned chunks = blocks(T, kChunk);
+  return dispatch_io_w(d, [&](auto io, auto wt) {
+    using IO = decltype(io);
+    using W = decltype(wt);
+    const int pieces = d.C / IO::kVec;
+    int tx = 1;
+    while (tx < kBlock && tx < pieces) tx *= 2;
+    const int ty = kBlock / tx;
+    const auto go = [&](auto acc) {
+      constexpr bool ACC = decltype(acc)::value;
+      hipLaunchKernelGGL((embed_sum_kernel<IO, W, ACC>), dim3(blocks(chunks, ty), blocks(pieces, tx)), dim3(tx, ty), 0, s, w.key,
+                         w.pos, g_x, g_table, w.part, d.n, d.C, T, d.V, d.scale);
+      hipLaunchKernelGGL((embed_join_kernel<W, ACC>), dim3(chunks, blocks(d.C, 64)), dim3(64, kJoinRows), 0, s, w.key, w.part,
+                         g_table, d.C, T, d.V, d.scale);
+      return hipGetLastError();
+    };
+    return accumulate ? go(std::true_type{}) : go(std::false_type{});
+  });
+}
+
+hipError_t launch_streams_norm(const mhcl_ends_desc &d, const void *x, const float *gain, void *h, hipStream_t s) {
+  return dispatch_io(d.io_dtype, [&](auto io) {
+    using IO = decltype(io);
+    return dispatch_row(d.C / IO::kVec, [&](auto l, auto ch) {
+      return dispatch_streams(d.n, [&](auto nn) {
+        constexpr int L = decltype(l)::value;
+        hipLaunchKernelGGL((norm_kernel<IO, decltype(nn)::value, L, decltype(ch)::value>), dim3(blocks(d.T, norm_tokens(L))),
+                           dim3(L * norm_tokens(L)), 0, s, x, gain, h, d.n, d.C, d.T, d.eps);
+        return hipGetLastError();
+      });
+    });
+  });
+}
+
+hipError_t launch_streams_norm_bwd(const mhcl_ends_desc &d, const void *x, const float *gain, const void *g_h, void *g_x,
+                                   float *g_gain, float *part, hipStream_t s) {
+  return dispatch_io(d.io_dtype, [&](auto io) {
+    using IO = decltype(io);
+    return dispatch_row(d.C / IO::kVec, [&](auto l, auto ch) {
+      return dispatch_streams(d.n, [&](auto nn) {
+        constexpr int L = decltype(l)::value;
+        const unsigned want = blocks(d.T, norm_tokens(L)), grid = want < kNormBwdBlocks ? want : kNormBwdBlocks;
+        hipLaunchKernelGGL((norm_bwd_kernel<IO, decltype(nn)::value, L, decltype(ch)::value>), dim3(grid),
+                           dim3(L * norm_tokens(L)), 0, s, x, gain, g_h, g_x, part, d.n, d.C, d.T, d.eps);
+        hipLaunchKernelGGL(gain_sum_kernel, dim3(blocks(d.C, 64)), dim3(64, 16), 0, s, part, g_gain, static_cast<int>(grid), d.C);
+        return hipGetLastError();
+      });
+    });
+  });
+}
+
+}  // namespace mhcl

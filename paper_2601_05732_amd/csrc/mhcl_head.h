@@ -1,0 +1,43 @@
+// Host-side declarations of the head's softmax cross entropy (mhcl_head.hip).
+#pragma once
+#include "mhcl_ends.h"
+
+namespace mhcl {
+
+// How the three products of the head are tiled: rows of the vocabulary and tokens of a block of threads, and the rows of one of its
+// waves, which is what a softmax's partial maximum and sum stand for.
+struct HeadTile {
+  int bm, bn, gran;
+};
+constexpr HeadTile kTileBig{256, 256, 128}, kTileMid{128, 128, 64}, kTileSlim{128, 32, 32};
+
+struct HeadPlan {
+  int parts;            // bf16 numbers that an operand's element is taken as: 1, or 3 for fp32
+  int pairs;            // products of parts
+  HeadTile logits, gh, gw;
+  int64_t tokens;       // of a block
+  int64_t ld;           // row of the softmax's numerators: V, filled up to whole tiles
+  int64_t granules;     // partial sums of a row
+  int gh_splits;        // of the vocabulary in the product for g_h
+  HeadPlan(const mhcl_ends_desc &d, bool grad);
+};
+
+struct HeadWs {
+  HeadPlan plan;
+  uint16_t *hp, *Wp;    // [parts][tokens][C]: h, zeros where a token does not count; [parts][V][C] (fp32 only)
+  char *E;              // [tokens][ld] numerators: 16 bits each, then g in bf16 in their place; fp32: floats
+  uint16_t *G;          // [parts][tokens][ld] g
+  float2 *stat;         // [tokens][granules] maximum and sum
+  float *zt;            // [tokens] the targets' logits
+  float *inv;           // [1] weight of the mean
+  float *slabs;         // [gh_splits][tokens][C]
+  float *gW;            // [V][C] sums over blocks of tokens
+  size_t bytes;
+  HeadWs(const mhcl_ends_desc &d, bool grad, void *ws);
+};
+
+// g_h, g_W null: the loss alone.  weight null: that of the mean.
+hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, const void *targets, const float *weight,
+                       float *loss, float *lse, void *g_h, void *g_W, const HeadWs &w, hipStream_t s);
+
+}  // namespace mhcl

@@ -1,0 +1,647 @@
+// The head's softmax cross entropy and its gradients.
+//
+//   z = h W^T                       [T, V]   never in memory
+//   g = weight (softmax(z) - onehot)
+//   g_h = g W,  g_W = g^T h
+//
+// Three matrix products of 2 T C V operations each.  The first one's epilogue takes, for each token, the maximum m and the sum of
+// exp(z - m) over the rows of the vocabulary that a wave holds (a "granule"), and for the gradients leaves exp(z - m) in 16
+// bits; a pass over a row then joins the granules, knows lse, and turns the numerators into g in place.  (Forming z again
+// instead, once lse is known, is a fourth product: 2 C operations for each number in place of 4 bytes.)
+#include "mhcl_common.h"
+#include "mhcl_head.h"
+#include "mhcl_mfma.h"
+
+namespace mhcl {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kBK = 64;                       // depth of a step: 128 bytes of a row
+constexpr float kLog2e = 1.4426950408889634f;
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_void;
+
+__device__ uint4 g_zeros;                     // what a step reads in place of what lies outside of an operand
+
+// ---------------------------------------------------------------- products
+// D[m][n] = sum_k A[m][k] B[n][k] over bf16 operands.  An operand lies in memory with k innermost (KINNER: row m or n starts at p + m ld),
+// or with m or n innermost (row k starts at p + k ld), in `part` elements long parts.  rows: its extent in m or n; depth: in k.
+struct Operand {
+  const uint16_t *p;
+  int64_t ld, part;
+  int64_t rows, depth;
+};
+
+// The pairs of parts whose products are added, small ones first: with three parts of 8 bits, what is left out is below 2^-26 of
+// the product.
+struct PartPairs {
+  signed char a[6], b[6];
+};
+constexpr PartPairs kOnePair{{0}, {0}}, kSixPairs{{1, 0, 2, 0, 1, 0}, {1, 2, 0, 1, 0, 0}};
+
+struct GemmArgs {
+  Operand A, B;
+  PartPairs pairs;
+  int n_pairs;
+  int tiles_m, tiles_n, splits;
+};
+
+// One operand's tile of R rows by kBK in LDS, in 16-byte pieces, as the loads that go straight to LDS leave it (piece i at
+// 16 i), so that a piece's place is chosen by which piece of memory a thread asks for.
+//  KINNER: piece (row, c) of a row's eight at 8 row + (c ^ (row / 2 % 8)): the 16 rows that a fragment reads at one c lie in
+//   all 64 banks once.
+//  else: row k holds R / 8 pieces; the pairs of pieces (16 numbers, what a transposing read takes of a row) are exchanged
+//   by k: pair m16 of row k at m16 ^ (k % 4 + 4 (k / 8 % 2)), so that the eight rows that half a wave reads lie in all banks.
+template <int R, int NT, bool KINNER>
+struct TileLoader {
+  static constexpr int PER = R * 8 / NT;
+  const uint16_t *p[PER];
+  int k[PER];            // of the piece, within the tile
+  bool in[PER];          // whether its row is one of the operand's (rows outside give results that nobody reads)
+  int64_t step;          // elements from one step to the next
+  __device__ __forceinline__ void init(const Operand &o, int64_t row0) {
+    const int tid = threadIdx.x;
+    step = KINNER ? kBK : kBK * o.ld;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int piece = i * NT + tid;
+      if constexpr (KINNER) {
+        const int row = piece >> 3, c = (piece & 7) ^ ((row >> 1) & 7);
+        const int64_t g = row0 + row < o.rows ? row0 + row : o.rows - 1;
+        k[i] = c * 8;
+        in[i] = true;
+        p[i] = o.p + g * o.ld + c * 8;
+      } else {
+        constexpr int PPR = R / 8;
+        const int kr = piece / PPR, slot = piece % PPR;
+        const int m = (((slot >> 1) ^ ((kr & 3) | ((kr >> 3) & 1) << 2)) * 2 + (slot & 1)) * 8;
+        k[i] = kr;
+        in[i] = row0 + m < o.rows;
+        p[i] = o.p + kr * o.ld + (in[i] ? row0 + m : 0);
+      }
+    }
+  }
+  __device__ __forceinline__ void move(int64_t elements) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) p[i] += elements;
+  }
+  // left: depth that is left of the operand from this step on
+  __device__ __forceinline__ void load(uint4 *tile, int64_t left) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const void *src = k[i] < left ? static_cast<const void *>(p[i]) : static_cast<const void *>(&g_zeros);
+      __builtin_amdgcn_global_load_lds((global_void *)src, (lds_void *)(tile + i * NT + wave * 64), 16, 0, 0);
+    }
+    move(step);
+  }
+};
+
+// Fragment of 16 rows from row0 on (a multiple of 16), k = 32 s + 8 q .. + 7 for lane (r, q)
+template <int R, bool KINNER>
+__device__ __forceinline__ u32x4 fragment(const uint4 *tile, int row0, int s) {
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  if constexpr (KINNER) {
+    return *reinterpret_cast<const u32x4 *>(tile + (row0 + r) * 8 + ((s * 4 + q) ^ ((r >> 1) & 7)));
+  } else {
+    // 16 lanes read rows k .. k + 3, 32 bytes of each, and get a column of four each
+    const int k = s * 32 + q * 8 + (r >> 2), m16 = (row0 >> 4) ^ ((r >> 2) | (q & 1) << 2);
+    const char *at = reinterpret_cast<const char *>(tile) + k * (R * 2) + m16 * 32 + (r & 3) * 8;
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * R * 2));
+    const u32x2 l = __builtin_bit_cast(u32x2, lo), h = __builtin_bit_cast(u32x2, hi);
+    return u32x4{l[0], l[1], h[0], h[1]};
+  }
+}
+
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
+__device__ __forceinline__ void barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Tile (tm, tn, split) of this block: blocks of one XCD (every eighth) take neighbouring tiles, in strips of eight tiles of m
+__device__ __forceinline__ void tile_of(const GemmArgs &g, int &tm, int &tn, int &split) {
+  const int total = g.tiles_m * g.tiles_n * g.splits;
+  const int b = blockIdx.x, each = total / 8, more = total % 8, xcd = b % 8;
+  int i = xcd * each + min(xcd, more) + b / 8;
+  const int per = g.tiles_m * g.tiles_n;
+  split = i / per;
+  i -= split * per;
+  constexpr int STRIP = 8;
+  const int strip = i / (STRIP * g.tiles_n), m0 = strip * STRIP, width = min(STRIP, g.tiles_m - m0);
+  i -= strip * STRIP * g.tiles_n;
+  tm = m0 + i % width;
+  tn = i / width;
+}
+
+// A block of WM x WN waves computes a BM x BN tile; wave (wm, wn) rows wm BM / WM of it and columns wn BN / WN on.
+// The epilogue gets acc[fm][fn]: lane (r, q) holds m = 16 fm + 4 q + 0..3 of the wave's rows, n = 16 fn + r of its columns.
+template <int BM, int BN, int WM, int WN, bool AK, bool BK, typename Epilogue>
+__global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, const Epilogue epilogue) {
+  constexpr int NT = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
+  __shared__ uint4 a0[BM * 8], a1[BM * 8], b0[BN * 8], b1[BN * 8];
+  int tm, tn, split;
+  tile_of(g, tm, tn, split);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+  const int64_t depth = g.A.depth < g.B.depth ? g.B.depth : g.A.depth;
+  const int steps = static_cast<int>((depth + kBK - 1) / kBK);
+  const int64_t total = static_cast<int64_t>(steps) * g.n_pairs;
+  const int64_t first = total * split / g.splits, last = total * (split + 1) / g.splits;
+  TileLoader<BM, NT, AK> la;
+  TileLoader<BN, NT, BK> lb;
+  la.init(g.A, static_cast<int64_t>(tm) * BM);
+  lb.init(g.B, static_cast<int64_t>(tn) * BN);
+  int pair = static_cast<int>(first / steps), at = static_cast<int>(first % steps);   // of the next load
+  la.move(g.pairs.a[pair] * g.A.part + at * la.step);
+  lb.move(g.pairs.b[pair] * g.B.part + at * lb.step);
+  f32x4 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // multiplies one step's tiles while the next one's are on their way (past the last step: zeros, or what another split needs)
+  const auto step = [&](const uint4 *__restrict__ a, const uint4 *__restrict__ b, uint4 *__restrict__ a_next, uint4 *__restrict__ b_next)
+      __attribute__((always_inline)) {
+    la.load(a_next, g.A.depth - static_cast<int64_t>(at) * kBK);
+    lb.load(b_next, g.B.depth - static_cast<int64_t>(at) * kBK);
+    if (++at == steps && pair + 1 < g.n_pairs) {
+      la.move((g.pairs.a[pair + 1] - g.pairs.a[pair]) * g.A.part - steps * la.step);
+      lb.move((g.pairs.b[pair + 1] - g.pairs.b[pair]) * g.B.part - steps * lb.step);
+      ++pair;
+      at = 0;
+    }
+    if (a == nullptr) return;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      u32x4 fa[FM], fb[FN];
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fa[i] = fragment<BM, AK>(a, (wm * FM + i) * 16, s);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[j] = fragment<BN, BK>(b, (wn * FN + j) * 16, s);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = mfma16(fa[i], fb[j], acc[i][j]);
+    }
+  };
+  step(nullptr, nullptr, a0, b0);
+  wait_loads();
+  barrier();
+  for (int64_t left = last - first; left > 0; left -= 2) {
+    step(a0, b0, a1, b1);
+    wait_loads();
+    barrier();
+    if (left > 1) step(a1, b1, a0, b0);
+    wait_loads();
+    barrier();
+  }
+  epilogue.template operator()<FM, FN>(acc, static_cast<int64_t>(tm) * BM + wm * (FM * 16), static_cast<int64_t>(tn) * BN + wn * (FN * 16),
+                                       split);
+}
+
+// ---- epilogues
+// e in [0, 1] as 16 bits: 6 of the exponent, 10 of the mantissa (2^-63 .. 1 to 2^-11 of itself, less is 0)
+constexpr uint32_t kCodeBase = 64u << 23;
+__device__ __forceinline__ uint32_t encode(float e) {
+  return static_cast<uint32_t>(max(0, static_cast<int32_t>(__float_as_uint(e) + 0x1000u - kCodeBase))) >> 13;
+}
+__device__ __forceinline__ float decode(uint32_t code) { return code ? __uint_as_float((code << 13) + kCodeBase) : 0.f; }
+
+// exp(x), x <= 0: the instruction for bf16 operands (relative error 2^-23 |x|), the library's for fp32 ones
+template <bool WIDE>
+__device__ __forceinline__ float exp_of(float x) {
+  if constexpr (WIDE) return expf(x);
+  return __builtin_amdgcn_exp2f(x * kLog2e);
+}
+
+// m: vocabulary, n: tokens.  STORE: the numerators too.  WIDE: fp32 numerators.
+template <typename ID, bool STORE, bool WIDE>
+struct LogitsEpilogue {
+  const ID *targets;
+  float2 *stat;
+  float *zt;
+  char *E;
+  int64_t T, V, ld, granules;
+  template <int FM, int FN>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int) const {
+    const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    if (m0 + FM * 16 > V) {   // rows beyond the vocabulary
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool out = m0 + 16 * i + 4 * q + e >= V;
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i][j][e] = out ? -INFINITY : acc[i][j][e];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const int64_t t = n0 + 16 * j + r;
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[i][j][e]);
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const int64_t y = t < T ? static_cast<int64_t>(targets[t]) - m0 - 4 * q : -1;
+      if (__ballot(y >= 0 && y < FM * 16) != 0) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (y == 16 * i + e) zt[t] = acc[i][j][e];
+      }
+      const float base = top == -INFINITY ? 0.f : top;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          acc[i][j][e] = exp_of<WIDE>(acc[i][j][e] - base);
+          sum += acc[i][j][e];
+        }
+        if constexpr (STORE) {
+          if (t < T) {
+            const int64_t elem = t * ld + m0 + 16 * i + 4 * q;
+            if constexpr (WIDE) {
+              *reinterpret_cast<f32x4 *>(E + elem * 4) = acc[i][j];
+            } else {
+              const f32x4 v = acc[i][j];
+              *reinterpret_cast<uint2 *>(E + elem * 2) =
+                  make_uint2(encode(v[0]) | encode(v[1]) << 16, encode(v[2]) | encode(v[3]) << 16);
+            }
+          }
+        }
+      }
+      sum += __shfl_xor(sum, 16, 64);
+      sum += __shfl_xor(sum, 32, 64);
+      if (q == 0 && t < T) stat[t * granules + m0 / (FM * 16)] = make_float2(top, sum);
+    }
+  }
+};
+
+// out[n][m], m innermost: fp32 slabs of splits (out32 != null), added to `add` if that is there; else rounded to bf16
+struct StoreEpilogue {
+  float *out32;
+  uint16_t *out16;
+  const float *add;
+  int64_t M, N, slab;     // elements of a split's slab
+  template <int FM, int FN>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int split) const {
+    const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const int64_t n = n0 + 16 * j + r;
+      if (n >= N) continue;
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const int64_t m = m0 + 16 * i + 4 * q;
+        if (m >= M) continue;       // (M is a multiple of 8)
+        const int64_t elem = n * M + m;
+        f32x4 v = acc[i][j];
+        if (add) v += *reinterpret_cast<const f32x4 *>(add + elem);
+        if (out32) *reinterpret_cast<f32x4 *>(out32 + split * slab + elem) = v;
+        else *reinterpret_cast<uint2 *>(out16 + elem) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------- rows
+// the weight of the mean: 1 / (targets that are not negative)
+template <typename ID>
+__global__ __launch_bounds__(1024) void count_kernel(const ID *__restrict__ targets, int64_t T, float *__restrict__ inv) {
+  __shared__ float red[16];
+  int64_t count = 0;
+  for (int64_t t = threadIdx.x; t < T; t += 1024) count += targets[t] >= 0 ? 1 : 0;
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) count += __shfl_xor(static_cast<int>(count), off, 64);
+  if ((threadIdx.x & 63) == 0) reinterpret_cast<int *>(red)[threadIdx.x >> 6] = static_cast<int>(count);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int all = 0;
+    for (int i = 0; i < 16; ++i) all += reinterpret_cast<int *>(red)[i];
+    *inv = all > 0 ? 1.f / static_cast<float>(all) : 0.f;
+  }
+}
+
+// joins a row's granules, in a fixed order: (maximum, sum of exp(z - maximum)) in every lane of a wave
+__device__ __forceinline__ float2 join_granules(const float2 *stat, int64_t granules, int lane, int lanes) {
+  float top = -INFINITY, sum = 0.f;
+  for (int64_t p = lane; p < granules; p += lanes) top = fmaxf(top, stat[p].x);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+  return make_float2(top, sum);
+}
+
+struct RowArgs {
+  const void *h;
+  const float *weight, *inv;
+  const float2 *stat;
+  const float *zt;
+  float *loss, *lse;
+  char *E;
+  uint16_t *G, *hp;
+  int64_t T, ld, granules;
+  int32_t V;
+  int C, gran_log2;
+};
+
+// loss and lse of a token, one wave each
+template <typename ID>
+__global__ __launch_bounds__(kBlock) void loss_kernel(const RowArgs a, const ID *__restrict__ targets) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
+  if (t >= a.T) return;
+  const float2 *stat = a.stat + t * a.granules;
+  const float top = join_granules(stat, a.granules, lane, 64).x, base = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+  for (int64_t p = lane; p < a.granules; p += 64) sum += stat[p].y * expf(stat[p].x - base);
+  sum = wave_sum(sum);
+  if (lane == 0) {
+    const int64_t y = static_cast<int64_t>(targets[t]);
+    a.lse[t] = base + logf(sum);
+    a.loss[t] = y < 0 ? 0.f : (y < a.V ? logf(sum) + (base - a.zt[t]) : __uint_as_float(0x7fc00000u));
+  }
+}
+
+// The same, one block a token, and the row's numerators turned into g: bf16 in their place, or (PARTS = 3) three bf16 parts of each; h's
+// row into hp, zeros where the weight is 0.
+template <typename ID, int PARTS>
+__global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *__restrict__ targets) {
+  __shared__ float red[2][kBlock / 64];
+  const int64_t t = blockIdx.x;
+  const int tid = threadIdx.x;
+  const float2 *stat = a.stat + t * a.granules;
+  float top = -INFINITY, sum = 0.f;
+  for (int64_t p = tid; p < a.granules; p += kBlock) top = fmaxf(top, stat[p].x);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+  if ((tid & 63) == 0) red[0][tid >> 6] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kBlock / 64; ++w) top = fmaxf(top, red[0][w]);
+  const float base = top == -INFINITY ? 0.f : top;
+  for (int64_t p = tid; p < a.granules; p += kBlock) sum += stat[p].y * expf(stat[p].x - base);
+  sum = wave_sum(sum);
+  if ((tid & 63) == 0) red[1][tid >> 6] = sum;
+  __syncthreads();
+  sum = pairwise_sum<kBlock / 64>([&](int w) { return red[1][w]; });
+  // (not by way of lse, in which log(sum) is lost where the logits are large)
+  const int64_t y = static_cast<int64_t>(targets[t]);
+  const float bad = __uint_as_float(0x7fc00000u);
+  const float loss = y < 0 ? 0.f : (y < a.V ? logf(sum) + (base - a.zt[t]) : bad);
+  if (tid == 0) {
+    a.lse[t] = base + logf(sum);
+    a.loss[t] = loss;
+  }
+  const float given = y < 0 ? 0.f : (a.weight ? a.weight[t] : *a.inv);
+  const bool counts = given != 0.f;
+  const float weight = y < a.V ? given : bad;
+  const float hit = weight * expm1f(-loss);      // p - 1 of the target
+  const float scale = weight / sum;
+  for (int64_t v = tid * 8; v < a.ld; v += kBlock * 8) {
+    float g[8];
+    if (counts) {
+      const float f = scale * expf(stat[v >> a.gran_log2].x - base);
+      if constexpr (PARTS == 1) {
+        const uint4 c = *reinterpret_cast<const uint4 *>(a.E + (t * a.ld + v) * 2);
+        const uint32_t code[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          g[2 * i] = decode(code[i] & 0xffffu) * f;
+          g[2 * i + 1] = decode(code[i] >> 16) * f;
+        }
+      } else {
+        F32::load(a.E, t * a.ld + v, reinterpret_cast<float(&)[4]>(g[0]));
+        F32::load(a.E, t * a.ld + v + 4, reinterpret_cast<float(&)[4]>(g[4]));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] *= f;
+      }
+      if (y >= v && y < v + 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = y == v + i ? hit : g[i];
+      }
+      if (v + 8 > a.V) {                         // (a row of NaN leaves the fill-up finite)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = v + i < a.V ? g[i] : 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = 0.f;
+    }
+    if constexpr (PARTS == 1) {
+      BF16::store(a.E, t * a.ld + v, g);
+    } else {
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) {
+        float part[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          part[i] = bf16_to_f32(f32_to_bf16(g[i]));
+          g[i] -= part[i];
+        }
+        BF16::store(a.G, (p * a.T + t) * a.ld + v, part);
+      }
+    }
+  }
+  const float none[8] = {};
+  for (int c = tid * 8; c < a.C; c += kBlock * 8) {
+    if constexpr (PARTS == 1) {
+      float v[8];
+      BF16::load(a.h, t * a.C + c, v);
+      if (counts) BF16::store(a.hp, t * a.C + c, v);
+      else BF16::store(a.hp, t * a.C + c, none);
+    } else if (!counts) {                        // (the parts are there from before the first product)
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) BF16::store(a.hp, (p * a.T + t) * a.C + c, none);
+    }
+  }
+}
+
+// fp32 as three bf16 parts, each the rounded rest: `count` elements (a multiple of 8), parts `part` elements apart
+__global__ __launch_bounds__(kBlock) void split_kernel(const float *__restrict__ in, uint16_t *__restrict__ out, int64_t count, int64_t part) {
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 8;
+  if (i >= count) return;
+  float v[8];
+  F32::load(in, i, reinterpret_cast<float(&)[4]>(v[0]));
+  F32::load(in, i + 4, reinterpret_cast<float(&)[4]>(v[4]));
+#pragma unroll
+  for (int p = 0; p < 3; ++p) {
+    float h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      h[e] = bf16_to_f32(f32_to_bf16(v[e]));
+      v[e] -= h[e];
+    }
+    BF16::store(out, p * part + i, h);
+  }
+}
+
+// out = the sum of `slabs` slabs of `count` floats (a multiple of 4), in order
+template <typename IO>
+__global__ __launch_bounds__(kBlock) void slab_sum_kernel(const float *__restrict__ in, void *__restrict__ out, int slabs, int64_t count) {
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4;
+  if (i >= count) return;
+  f32x4 s = *reinterpret_cast<const f32x4 *>(in + i);
+#pragma unroll 4
+  for (int k = 1; k < slabs; ++k) s += *reinterpret_cast<const f32x4 *>(in + k * count + i);
+  if constexpr (IO::kVec == 4) *reinterpret_cast<f32x4 *>(static_cast<float *>(out) + i) = s;
+  else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + i) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+unsigned blocks(int64_t items, int64_t each) { return static_cast<unsigned>(ceil_div(items, each)); }
+
+template <typename F>
+hipError_t dispatch_id(int id_dtype, F &&f) {
+  if (id_dtype == MHCL_I64) return f(int64_t{});
+  return f(int32_t{});
+}
+
+template <bool AK, bool BK, typename Epilogue>
+hipError_t launch_gemm(const HeadTile &tile, Operand A, Operand B, int64_t M, int64_t N, int parts, int splits, const Epilogue &e, hipStream_t s) {
+  GemmArgs g;
+  g.A = A;
+  g.B = B;
+  g.pairs = parts == 1 ? kOnePair : kSixPairs;
+  g.n_pairs = parts == 1 ? 1 : 6;
+  g.tiles_m = static_cast<int>(ceil_div(M, tile.bm));
+  g.tiles_n = static_cast<int>(ceil_div(N, tile.bn));
+  g.splits = splits;
+  const dim3 grid(static_cast<unsigned>(g.tiles_m * g.tiles_n * splits));
+  if (tile.bm == 256) hipLaunchKernelGGL((gemm_kernel<256, 256, 2, 4, AK, BK, Epilogue>), grid, dim3(512), 0, s, g, e);
+  else if (tile.bn == 128) hipLaunchKernelGGL((gemm_kernel<128, 128, 2, 2, AK, BK, Epilogue>), grid, dim3(256), 0, s, g, e);
+  else if constexpr (BK) hipLaunchKernelGGL((gemm_kernel<128, 32, 4, 1, AK, BK, Epilogue>), grid, dim3(256), 0, s, g, e);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+constexpr int64_t kChipBlocks = 256;
+
+// the largest tile of which there are enough for the chip
+HeadTile tile_for(int64_t M, int64_t N, bool slim) {
+  if (slim && N <= 64) return kTileSlim;
+  return ceil_div(M, 256) * ceil_div(N, 256) >= kChipBlocks ? kTileBig : kTileMid;
+}
+
+}  // namespace
+
+HeadPlan::HeadPlan(const mhcl_ends_desc &d, bool grad) {
+  parts = d.io_dtype == MHCL_BF16 ? 1 : 3;
+  pairs = parts == 1 ? 1 : 6;
+  tokens = d.T;
+  const int64_t row = ceil_div(d.V, 256) * 256;
+  const int64_t row_bytes = grad ? row * (parts == 1 ? 2 : 4 + 2 * parts) : row / 32 * 8;
+  const int64_t fit = static_cast<int64_t>(MHCL_HEAD_BLOCK_BYTES) / row_bytes / 256 * 256;
+  if (tokens > fit) tokens = fit < 256 ? 256 : fit;
+  if (tokens > d.T) tokens = d.T;
+  logits = tile_for(d.V, tokens, true);
+  gh = tile_for(d.C, tokens, true);
+  gw = tile_for(d.C, d.V, false);
+  ld = ceil_div(d.V, logits.bm) * logits.bm;   // (what the first product's tiles cover)
+  granules = ld / logits.gran;
+  gh_splits = 1;
+  if (grad) {
+    // enough blocks for the chip, each with at least eight steps
+    const int64_t tiles = ceil_div(d.C, gh.bm) * ceil_div(tokens, gh.bn), steps = ceil_div(d.V, kBK) * pairs;
+    int64_t k = (2 * kChipBlocks) / (tiles > 0 ? tiles : 1);
+    if (k > steps / 8) k = steps / 8;
+    if (k > 64) k = 64;
+    gh_splits = k < 1 ? 1 : static_cast<int>(k);
+  }
+}
+
+HeadWs::HeadWs(const mhcl_ends_desc &d, bool grad, void *ws) : plan(d, grad) {
+  WsCursor c(ws);
+  const size_t T = static_cast<size_t>(plan.tokens), P = plan.parts, V = static_cast<size_t>(d.V), C = static_cast<size_t>(d.C), ld = static_cast<size_t>(plan.ld);
+  hp = grad || P > 1 ? c.take<uint16_t>(P * T * C) : nullptr;
+  Wp = P > 1 ? c.take<uint16_t>(P * V * C) : nullptr;
+  E = grad ? c.take<char>(T * ld * (P == 1 ? 2 : 4)) : nullptr;
+  G = !grad || P == 1 ? reinterpret_cast<uint16_t *>(E) : c.take<uint16_t>(P * T * ld);
+  stat = c.take<float2>(T * static_cast<size_t>(plan.granules));
+  zt = c.take<float>(T);
+  inv = c.take<float>(1);
+  slabs = plan.gh_splits > 1 ? c.take<float>(static_cast<size_t>(plan.gh_splits) * T * C) : nullptr;
+  gW = grad && P == 1 && plan.tokens < d.T ? c.take<float>(V * C) : nullptr;
+  bytes = c.off;
+}
+
+hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, const void *targets, const float *weight,
+                       float *loss, float *lse, void *g_h, void *g_W, const HeadWs &w, hipStream_t s) {
+  return dispatch_id(d.id_dtype, [&](auto id) -> hipError_t {
+    using ID = decltype(id);
+    const HeadPlan &p = w.plan;
+    const bool grad = g_W != nullptr, wide = p.parts > 1;
+    const int64_t C = d.C, V = d.V, esize = wide ? 4 : 2;
+    const ID *all = static_cast<const ID *>(targets);
+    hipError_t e;
+    if (wide) {
+      hipLaunchKernelGGL(split_kernel, dim3(blocks(V * C, kBlock * 8)), dim3(kBlock), 0, s, static_cast<const float *>(W), w.Wp, V * C, V * C);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (grad && !weight) {
+      hipLaunchKernelGGL((count_kernel<ID>), dim3(1), dim3(1024), 0, s, all, d.T, w.inv);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    const uint16_t *Wb = wide ? w.Wp : static_cast<const uint16_t *>(W);
+    for (int64_t t0 = 0; t0 < d.T; t0 += p.tokens) {
+      const int64_t T = d.T - t0 < p.tokens ? d.T - t0 : p.tokens;
+      const void *hb = static_cast<const char *>(h) + t0 * C * esize;
+      const ID *y = all + t0;
+      if (wide) {
+        hipLaunchKernelGGL(split_kernel, dim3(blocks(T * C, kBlock * 8)), dim3(kBlock), 0, s, static_cast<const float *>(hb), w.hp, T * C, T * C);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
+      const Operand Wk{Wb, C, V * C, V, C}, hk{wide ? w.hp : static_cast<const uint16_t *>(hb), C, T * C, T, C};
+      const auto logits = [&](auto store, auto is_wide) {
+        const LogitsEpilogue<ID, decltype(store)::value, decltype(is_wide)::value> ep{y, w.stat, w.zt, w.E, T, V, p.ld, p.granules};
+        return launch_gemm<true, true>(p.logits, Wk, hk, V, T, p.parts, 1, ep, s);
+      };
+      if (grad) e = wide ? logits(std::true_type{}, std::true_type{}) : logits(std::true_type{}, std::false_type{});
+      else e = wide ? logits(std::false_type{}, std::true_type{}) : logits(std::false_type{}, std::false_type{});
+      if (e != hipSuccess) return e;
+      int gran_log2 = 0;
+      while ((1 << gran_log2) < p.logits.gran) ++gran_log2;
+      const RowArgs a{hb, weight ? weight + t0 : nullptr, w.inv, w.stat, w.zt, loss + t0, lse + t0, w.E, w.G, w.hp, T, p.ld, p.granules, d.V, d.C, gran_log2};
+      if (!grad) {
+        hipLaunchKernelGGL((loss_kernel<ID>), dim3(blocks(T, kBlock / 64)), dim3(kBlock), 0, s, a, y);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        continue;
+      }
+      if (wide) hipLaunchKernelGGL((row_kernel<ID, 3>), dim3(static_cast<unsigned>(T)), dim3(kBlock), 0, s, a, y);
+      else hipLaunchKernelGGL((row_kernel<ID, 1>), dim3(static_cast<unsigned>(T)), dim3(kBlock), 0, s, a, y);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      // g_h [T, C]: m over C, k over the vocabulary
+      {
+        const Operand Wm{Wb, C, V * C, C, V}, gk{w.G, p.ld, T * p.ld, T, p.ld};
+        void *out = static_cast<char *>(g_h) + t0 * C * esize;
+        StoreEpilogue ep{p.gh_splits > 1 ? w.slabs : (wide ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out), nullptr, C, T, T * C};
+        if ((e = launch_gemm<false, true>(p.gh, Wm, gk, C, T, p.parts, p.gh_splits, ep, s)) != hipSuccess) return e;
+        if (p.gh_splits > 1) {
+          if (wide) hipLaunchKernelGGL((slab_sum_kernel<F32>), dim3(blocks(T * C, kBlock * 4)), dim3(kBlock), 0, s, w.slabs, out, p.gh_splits, T * C);
+          else hipLaunchKernelGGL((slab_sum_kernel<BF16>), dim3(blocks(T * C, kBlock * 4)), dim3(kBlock), 0, s, w.slabs, out, p.gh_splits, T * C);
+          if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
+      }
+      // g_W [V, C]: m over C, n over the vocabulary, k over the tokens; the blocks of tokens add up in fp32
+      {
+        const Operand hm{w.hp, C, T * C, C, T}, gm{w.G, p.ld, T * p.ld, p.ld, T};
+        const bool last = t0 + T == d.T;
+        float *sums = wide ? static_cast<float *>(g_W) : w.gW;
+        StoreEpilogue ep{wide || !last ? sums : nullptr, static_cast<uint16_t *>(g_W), t0 > 0 ? sums : nullptr, C, V, 0};
+        if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, p.parts, 1, ep, s)) != hipSuccess) return e;
+      }
+    }
+    return hipSuccess;
+  });
+}
+
+}  // namespace mhcl
