@@ -29,7 +29,7 @@ struct HeadWs {
   uint16_t *G;          // [parts][tokens][ld] g
   float2 *stat;         // [tokens][granules] maximum and sum
   float *zt;            // [tokens] the targets' logits
-  float *inv;           // [1] weight of the mean
+  float *common;        // [1] what all weights are multiples of
   float *slabs;         // [gh_splits][tokens][C]
   float *gW;            // [V][C] sums over blocks of tokens
   size_t bytes;

@@ -287,8 +287,9 @@ struct LogitsEpilogue {
   }
 };
 
-// out[n][m], m innermost: fp32 slabs of splits (out32 != null), added to `add` if that is there; else rounded to bf16
+// out[n][m], m innermost, times *scale: fp32 slabs of splits (out32 != null), added to `add` if that is there; else rounded to bf16
 struct StoreEpilogue {
+  const float *scale;
   float *out32;
   uint16_t *out16;
   const float *add;
@@ -296,6 +297,7 @@ struct StoreEpilogue {
   template <int FM, int FN>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int split) const {
     const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    const float factor = *scale;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int64_t n = n0 + 16 * j + r;
@@ -305,7 +307,7 @@ struct StoreEpilogue {
         const int64_t m = m0 + 16 * i + 4 * q;
         if (m >= M) continue;       // (M is a multiple of 8)
         const int64_t elem = n * M + m;
-        f32x4 v = acc[i][j];
+        f32x4 v = acc[i][j] * factor;
         if (add) v += *reinterpret_cast<const f32x4 *>(add + elem);
         if (out32) *reinterpret_cast<f32x4 *>(out32 + split * slab + elem) = v;
         else *reinterpret_cast<uint2 *>(out16 + elem) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
@@ -315,35 +317,42 @@ struct StoreEpilogue {
 };
 
 // ---------------------------------------------------------------- rows
-// the weight of the mean: 1 / (targets that are not negative)
+// The factor c that all weights have in common, which the two products multiply their sums by: a token's g is rounded with weight / c
+// alone, so that equal weights do not round a whole gradient's scale (16384 tokens, the mean's 1 / 15560 in bf16: g_h, g_W off by 0.0030 of their
+// 2-norms with the weight in g, 0.0024 without).  The mean's: c = 1 / (targets that are not negative), weight / c = 1.  The caller's: c
+// the largest |weight| of a target that is not negative (1 where that is no positive number).
 template <typename ID>
-__global__ __launch_bounds__(1024) void count_kernel(const ID *__restrict__ targets, int64_t T, float *__restrict__ inv) {
+__global__ __launch_bounds__(1024) void common_weight_kernel(const ID *__restrict__ targets, const float *__restrict__ weight, int64_t T,
+                                                             float *__restrict__ common) {
   __shared__ float red[16];
-  int64_t count = 0;
-  for (int64_t t = threadIdx.x; t < T; t += 1024) count += targets[t] >= 0 ? 1 : 0;
+  float most = 0.f;
+  int count = 0;
+  for (int64_t t = threadIdx.x; t < T; t += 1024) {
+    const bool counts = targets[t] >= 0;
+    count += counts ? 1 : 0;
+    if (weight && counts) most = fmaxf(most, fabsf(weight[t]));
+  }
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) count += __shfl_xor(static_cast<int>(count), off, 64);
-  if ((threadIdx.x & 63) == 0) reinterpret_cast<int *>(red)[threadIdx.x >> 6] = static_cast<int>(count);
+  for (int off = 32; off > 0; off >>= 1) {
+    most = fmaxf(most, __shfl_xor(most, off, 64));
+    count += __shfl_xor(count, off, 64);
+  }
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = weight ? most : __int_as_float(count);
   __syncthreads();
   if (threadIdx.x == 0) {
     int all = 0;
-    for (int i = 0; i < 16; ++i) all += reinterpret_cast<int *>(red)[i];
-    *inv = all > 0 ? 1.f / static_cast<float>(all) : 0.f;
+    for (int i = 0; i < 16; ++i) {
+      most = fmaxf(most, weight ? red[i] : 0.f);
+      all += weight ? 0 : __float_as_int(red[i]);
+    }
+    if (!weight) most = all > 0 ? 1.f / static_cast<float>(all) : 0.f;
+    *common = most > 0.f && most <= 3.4028235e38f ? most : 1.f;
   }
-}
-
-// joins a row's granules, in a fixed order: (maximum, sum of exp(z - maximum)) in every lane of a wave
-__device__ __forceinline__ float2 join_granules(const float2 *stat, int64_t granules, int lane, int lanes) {
-  float top = -INFINITY, sum = 0.f;
-  for (int64_t p = lane; p < granules; p += lanes) top = fmaxf(top, stat[p].x);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-  return make_float2(top, sum);
 }
 
 struct RowArgs {
   const void *h;
-  const float *weight, *inv;
+  const float *weight, *common;
   const float2 *stat;
   const float *zt;
   float *loss, *lse;
@@ -361,8 +370,11 @@ __global__ __launch_bounds__(kBlock) void loss_kernel(const RowArgs a, const ID 
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
   if (t >= a.T) return;
   const float2 *stat = a.stat + t * a.granules;
-  const float top = join_granules(stat, a.granules, lane, 64).x, base = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
+  float top = -INFINITY, sum = 0.f;
+  for (int64_t p = lane; p < a.granules; p += 64) top = fmaxf(top, stat[p].x);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+  const float base = top == -INFINITY ? 0.f : top;
   for (int64_t p = lane; p < a.granules; p += 64) sum += stat[p].y * expf(stat[p].x - base);
   sum = wave_sum(sum);
   if (lane == 0) {
@@ -402,7 +414,7 @@ __global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *
     a.lse[t] = base + logf(sum);
     a.loss[t] = loss;
   }
-  const float given = y < 0 ? 0.f : (a.weight ? a.weight[t] : *a.inv);
+  const float given = y < 0 ? 0.f : (a.weight ? a.weight[t] / *a.common : 1.f);
   const bool counts = given != 0.f;
   const float weight = y < a.V ? given : bad;
   const float hit = weight * expm1f(-loss);      // p - 1 of the target
@@ -568,7 +580,7 @@ HeadWs::HeadWs(const mhcl_ends_desc &d, bool grad, void *ws) : plan(d, grad) {
   G = !grad || P == 1 ? reinterpret_cast<uint16_t *>(E) : c.take<uint16_t>(P * T * ld);
   stat = c.take<float2>(T * static_cast<size_t>(plan.granules));
   zt = c.take<float>(T);
-  inv = c.take<float>(1);
+  common = c.take<float>(1);
   slabs = plan.gh_splits > 1 ? c.take<float>(static_cast<size_t>(plan.gh_splits) * T * C) : nullptr;
   gW = grad && P == 1 && plan.tokens < d.T ? c.take<float>(V * C) : nullptr;
   bytes = c.off;
@@ -587,8 +599,8 @@ hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, co
       hipLaunchKernelGGL(split_kernel, dim3(blocks(V * C, kBlock * 8)), dim3(kBlock), 0, s, static_cast<const float *>(W), w.Wp, V * C, V * C);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    if (grad && !weight) {
-      hipLaunchKernelGGL((count_kernel<ID>), dim3(1), dim3(1024), 0, s, all, d.T, w.inv);
+    if (grad) {
+      hipLaunchKernelGGL((common_weight_kernel<ID>), dim3(1), dim3(1024), 0, s, all, weight, d.T, w.common);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     const uint16_t *Wb = wide ? w.Wp : static_cast<const uint16_t *>(W);
@@ -610,7 +622,7 @@ hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, co
       if (e != hipSuccess) return e;
       int gran_log2 = 0;
       while ((1 << gran_log2) < p.logits.gran) ++gran_log2;
-      const RowArgs a{hb, weight ? weight + t0 : nullptr, w.inv, w.stat, w.zt, loss + t0, lse + t0, w.E, w.G, w.hp, T, p.ld, p.granules, d.V, d.C, gran_log2};
+      const RowArgs a{hb, weight ? weight + t0 : nullptr, w.common, w.stat, w.zt, loss + t0, lse + t0, w.E, w.G, w.hp, T, p.ld, p.granules, d.V, d.C, gran_log2};
       if (!grad) {
         hipLaunchKernelGGL((loss_kernel<ID>), dim3(blocks(T, kBlock / 64)), dim3(kBlock), 0, s, a, y);
         if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -623,7 +635,7 @@ hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, co
       {
         const Operand Wm{Wb, C, V * C, C, V}, gk{w.G, p.ld, T * p.ld, T, p.ld};
         void *out = static_cast<char *>(g_h) + t0 * C * esize;
-        StoreEpilogue ep{p.gh_splits > 1 ? w.slabs : (wide ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out), nullptr, C, T, T * C};
+        StoreEpilogue ep{w.common, p.gh_splits > 1 ? w.slabs : (wide ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out), nullptr, C, T, T * C};
         if ((e = launch_gemm<false, true>(p.gh, Wm, gk, C, T, p.parts, p.gh_splits, ep, s)) != hipSuccess) return e;
         if (p.gh_splits > 1) {
           if (wide) hipLaunchKernelGGL((slab_sum_kernel<F32>), dim3(blocks(T * C, kBlock * 4)), dim3(kBlock), 0, s, w.slabs, out, p.gh_splits, T * C);
@@ -636,7 +648,7 @@ hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, co
         const Operand hm{w.hp, C, T * C, C, T}, gm{w.G, p.ld, T * p.ld, p.ld, T};
         const bool last = t0 + T == d.T;
         float *sums = wide ? static_cast<float *>(g_W) : w.gW;
-        StoreEpilogue ep{wide || !last ? sums : nullptr, static_cast<uint16_t *>(g_W), t0 > 0 ? sums : nullptr, C, V, 0};
+        StoreEpilogue ep{w.common, wide || !last ? sums : nullptr, static_cast<uint16_t *>(g_W), t0 > 0 ? sums : nullptr, C, V, 0};
         if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, p.parts, 1, ep, s)) != hipSuccess) return e;
       }
     }
