@@ -21,9 +21,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(1))) const void global_void;
-
-__device__ uint4 g_zeros;                     // what a step reads in place of what lies outside of an operand
 
 // ---------------------------------------------------------------- products
 // D[m][n] = sum_k A[m][k] B[n][k] over bf16 operands.  An operand lies in memory with k innermost (KINNER: row m or n starts at p + m ld),
@@ -34,12 +31,12 @@ struct Operand {
   int64_t rows, depth;
 };
 
-// The pairs of parts whose products are added, small ones first: with three parts of 8 bits, what is left out is below 2^-26 of
-// the product.
+// The pairs of parts whose products are added, small ones first, four bits for each: of three parts of 8 bits all but the
+// three products below 2^-23 of the whole.
 struct PartPairs {
-  signed char a[6], b[6];
+  uint32_t a, b;
 };
-constexpr PartPairs kOnePair{{0}, {0}}, kSixPairs{{1, 0, 2, 0, 1, 0}, {1, 2, 0, 1, 0, 0}};
+constexpr PartPairs kOnePair{0, 0}, kSixPairs{0x010201, 0x001021};   // (1,1) (0,2) (2,0) (0,1) (1,0) (0,0) from the low end
 
 struct GemmArgs {
   Operand A, B;
@@ -54,70 +51,81 @@ struct GemmArgs {
 //   all 64 banks once.
 //  else: row k holds R / 8 pieces; the pairs of pieces (16 numbers, what a transposing read takes of a row) are exchanged
 //   by k: pair m16 of row k at m16 ^ (k % 4 + 4 (k / 8 % 2)), so that the eight rows that half a wave reads lie in all banks.
+// A thread's pieces lie the same distance apart, so that they share one offset; the loads' own range check gives zeros past
+// the operand's end.  (Rows of m or n outside of the operand give results that nobody reads.)
 template <int R, int NT, bool KINNER>
 struct TileLoader {
   static constexpr int PER = R * 8 / NT;
-  const uint16_t *p[PER];
-  int k[PER];            // of the piece, within the tile
-  bool in[PER];          // whether its row is one of the operand's (rows outside give results that nobody reads)
-  int64_t step;          // elements from one step to the next
+  static constexpr int kRows = KINNER ? NT / 8 : NT / (R / 8);   // rows of memory from one piece to the next
+  static_assert(kRows % 16 == 0 || PER == 1, "the exchange of pieces is the same for all of a thread's");
+  const char *base, *end;   // of the tile and the next step; of the operand (its part)
+  int64_t step;             // bytes from one step to the next
+  int apart;                // bytes from one piece to the next (a tile's are less than 2^31: the host sees to it)
+  uint32_t at;              // bytes from `base` to the thread's first piece
+  int depth;                // KINNER: k of the thread's pieces within the tile
   __device__ __forceinline__ void init(const Operand &o, int64_t row0) {
     const int tid = threadIdx.x;
-    step = KINNER ? kBK : kBK * o.ld;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int piece = i * NT + tid;
-      if constexpr (KINNER) {
-        const int row = piece >> 3, c = (piece & 7) ^ ((row >> 1) & 7);
-        const int64_t g = row0 + row < o.rows ? row0 + row : o.rows - 1;
-        k[i] = c * 8;
-        in[i] = true;
-        p[i] = o.p + g * o.ld + c * 8;
-      } else {
-        constexpr int PPR = R / 8;
-        const int kr = piece / PPR, slot = piece % PPR;
-        const int m = (((slot >> 1) ^ ((kr & 3) | ((kr >> 3) & 1) << 2)) * 2 + (slot & 1)) * 8;
-        k[i] = kr;
-        in[i] = row0 + m < o.rows;
-        p[i] = o.p + kr * o.ld + (in[i] ? row0 + m : 0);
-      }
+    step = (KINNER ? kBK : kBK * o.ld) * 2;
+    apart = static_cast<int>(kRows * o.ld * 2);
+    base = reinterpret_cast<const char *>(o.p) + row0 * (KINNER ? o.ld : 1) * 2;
+    end = reinterpret_cast<const char *>(o.p) + (KINNER ? o.rows : o.depth) * o.ld * 2;
+    if constexpr (KINNER) {
+      depth = ((tid & 7) ^ ((tid >> 4) & 7)) * 8;
+      at = static_cast<uint32_t>(((tid >> 3) * o.ld + depth) * 2);
+    } else {
+      const int kr = tid / (R / 8), slot = tid % (R / 8);
+      const int m = (((slot >> 1) ^ ((kr & 3) | ((kr >> 3) & 1) << 2)) * 2 + (slot & 1)) * 8;
+      depth = 0;
+      at = static_cast<uint32_t>((kr * o.ld + m) * 2);
     }
   }
-  __device__ __forceinline__ void move(int64_t elements) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) p[i] += elements;
-  }
-  // left: depth that is left of the operand from this step on
-  __device__ __forceinline__ void load(uint4 *tile, int64_t left) {
+  __device__ __forceinline__ void to_part(int64_t bytes) { base += bytes, end += bytes; }
+  // left: depth that is left of the operand from this step on, 0 or less for a tile of zeros
+  __device__ __forceinline__ void load(uint4 *tile, int left) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t rest = end - base;
+    const int range = left <= 0 || rest <= 0 ? 0 : (rest > 0x7fffffff ? 0x7fffffff : static_cast<int>(rest));
+    uint32_t from = at;
+    if constexpr (KINNER) from = depth < left ? at : 0x80000000u;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const void *src = k[i] < left ? static_cast<const void *>(p[i]) : static_cast<const void *>(&g_zeros);
-      __builtin_amdgcn_global_load_lds((global_void *)src, (lds_void *)(tile + i * NT + wave * 64), 16, 0, 0);
-    }
-    move(step);
+    for (int i = 0; i < PER; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + i * apart), 0, max(range - i * apart, 0), 0x00020000),
+          (lds_void *)(tile + i * NT + wave * 64), 16, from, 0, 0, 0);
+    base += step;
   }
 };
 
-// Fragment of 16 rows from row0 on (a multiple of 16), k = 32 s + 8 q .. + 7 for lane (r, q)
+// Fragments of 16 rows, k = 32 s + 8 q .. + 7 for lane (r, q).  lane_at: the lane's place in fragment 0 at s = 0, in bytes.
 template <int R, bool KINNER>
-__device__ __forceinline__ u32x4 fragment(const uint4 *tile, int row0, int s) {
+__device__ __forceinline__ int lane_at() {
   const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  if constexpr (KINNER) return r * 128 | (q ^ ((r >> 1) & 7)) << 4;
+  // 16 lanes read rows k .. k + 3, 32 bytes of each, and get a column of four each
+  return (q * 8 + (r >> 2)) * (R * 2) | ((r >> 2) | (q & 1) << 2) << 5 | (r & 3) << 3;
+}
+template <int R, bool KINNER>
+__device__ __forceinline__ u32x4 fragment(const uint4 *tile, int at, int f, int s) {
+  const char *p = reinterpret_cast<const char *>(tile);
   if constexpr (KINNER) {
-    return *reinterpret_cast<const u32x4 *>(tile + (row0 + r) * 8 + ((s * 4 + q) ^ ((r >> 1) & 7)));
+    return *reinterpret_cast<const u32x4 *>(p + (at ^ s << 6) + f * 2048);
   } else {
-    // 16 lanes read rows k .. k + 3, 32 bytes of each, and get a column of four each
-    const int k = s * 32 + q * 8 + (r >> 2), m16 = (row0 >> 4) ^ ((r >> 2) | (q & 1) << 2);
-    const char *at = reinterpret_cast<const char *>(tile) + k * (R * 2) + m16 * 32 + (r & 3) * 8;
+    const char *from = p + (at ^ f << 5) + s * (32 * R * 2);
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * R * 2));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)from);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(from + 4 * R * 2));
     const u32x2 l = __builtin_bit_cast(u32x2, lo), h = __builtin_bit_cast(u32x2, hi);
     return u32x4{l[0], l[1], h[0], h[1]};
   }
 }
 
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
+// (the addresses of exchanged pieces take an instruction each; kept from step to step they would take a register each)
+template <bool KINNER>
+__device__ __forceinline__ int formed_here(int at) {
+  if constexpr (!KINNER) asm volatile("" : "+v"(at));
+  return at;
+}
+__device__ __forceinline__ void wait_all() { __builtin_amdgcn_s_waitcnt(0x0070); }   // vmcnt(0) lgkmcnt(0)
 __device__ __forceinline__ void barrier() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_barrier();
@@ -157,48 +165,80 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, con
   la.init(g.A, static_cast<int64_t>(tm) * BM);
   lb.init(g.B, static_cast<int64_t>(tn) * BN);
   int pair = static_cast<int>(first / steps), at = static_cast<int>(first % steps);   // of the next load
-  la.move(g.pairs.a[pair] * g.A.part + at * la.step);
-  lb.move(g.pairs.b[pair] * g.B.part + at * lb.step);
+  const auto part_of = [](uint32_t parts, int i) { return static_cast<int>(parts >> (4 * i) & 15); };
+  la.to_part(part_of(g.pairs.a, pair) * g.A.part * 2);
+  lb.to_part(part_of(g.pairs.b, pair) * g.B.part * 2);
+  la.base += at * la.step;
+  lb.base += at * lb.step;
   f32x4 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // multiplies one step's tiles while the next one's are on their way (past the last step: zeros, or what another split needs)
-  const auto step = [&](const uint4 *__restrict__ a, const uint4 *__restrict__ b, uint4 *__restrict__ a_next, uint4 *__restrict__ b_next)
-      __attribute__((always_inline)) {
-    la.load(a_next, g.A.depth - static_cast<int64_t>(at) * kBK);
-    lb.load(b_next, g.B.depth - static_cast<int64_t>(at) * kBK);
-    if (++at == steps && pair + 1 < g.n_pairs) {
-      la.move((g.pairs.a[pair + 1] - g.pairs.a[pair]) * g.A.part - steps * la.step);
-      lb.move((g.pairs.b[pair + 1] - g.pairs.b[pair]) * g.B.part - steps * lb.step);
-      ++pair;
-      at = 0;
-    }
-    if (a == nullptr) return;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u32x4 fa[FM], fb[FN];
-#pragma unroll
-      for (int i = 0; i < FM; ++i) fa[i] = fragment<BM, AK>(a, (wm * FM + i) * 16, s);
-#pragma unroll
-      for (int j = 0; j < FN; ++j) fb[j] = fragment<BN, BK>(b, (wn * FN + j) * 16, s);
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = mfma16(fa[i], fb[j], acc[i][j]);
-    }
+  int64_t to_load = last - first;
+  const auto load = [&](uint4 *a, uint4 *b) __attribute__((always_inline)) {
+    const int done = to_load-- > 0 ? at * kBK : 0x7fffffff;   // past the last step: zeros
+    la.load(a, static_cast<int>(g.A.depth) - done);
+    lb.load(b, static_cast<int>(g.B.depth) - done);
+    // on to the next pair of parts after the last step of one (without a branch, which costs registers)
+    const int over = ++at == steps ? -1 : 0;
+    la.to_part((part_of(g.pairs.a, pair - over) - part_of(g.pairs.a, pair)) * g.A.part * 2);
+    lb.to_part((part_of(g.pairs.b, pair - over) - part_of(g.pairs.b, pair)) * g.B.part * 2);
+    la.base -= (steps & over) * la.step;
+    lb.base -= (steps & over) * lb.step;
+    pair -= over;
+    at &= ~over;
   };
-  step(nullptr, nullptr, a0, b0);
-  wait_loads();
+  // A step is four groups of products, (k half s, half hm of the rows), whose fragments are read one group ahead.  Once the last
+  // group's have arrived the stage is free and the next one's tiles are needed: there the waves meet, and
+  // the next step's first fragments are on their way while the last group multiplies.
+  constexpr int HM = FM / 2;
+  // (of the wave's first rows; FM, FN are powers of two)
+  const int at_a = AK ? lane_at<BM, AK>() + wm * FM * 2048 : lane_at<BM, AK>() ^ (wm * FM) << 5;
+  const int at_b = BK ? lane_at<BN, BK>() + wn * FN * 2048 : lane_at<BN, BK>() ^ (wn * FN) << 5;
+  u32x4 fa[2][HM], fb[2][FN];
+  const auto read_a = [&](const uint4 *a, int s, int hm) __attribute__((always_inline)) {
+    const int here = formed_here<AK>(at_a);
+#pragma unroll
+    for (int i = 0; i < HM; ++i) fa[hm][i] = fragment<BM, AK>(a, here, hm * HM + i, s);
+  };
+  const auto read_b = [&](const uint4 *b, int s) __attribute__((always_inline)) {
+    const int here = formed_here<BK>(at_b);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) fb[s][j] = fragment<BN, BK>(b, here, j, s);
+  };
+  const auto products = [&](int s, int hm) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < HM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[hm * HM + i][j] = mfma16(fa[hm][i], fb[s][j], acc[hm * HM + i][j]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const auto step = [&](const uint4 *a, const uint4 *b, uint4 *a_next, uint4 *b_next) __attribute__((always_inline)) {
+    load(a_next, b_next);
+    read_a(a, 0, 1);
+    products(0, 0);
+    read_b(b, 1);
+    read_a(a, 1, 0);
+    products(0, 1);
+    read_a(a, 1, 1);
+    products(1, 0);
+    wait_all();
+    barrier();
+    read_a(a_next, 0, 0);
+    read_b(b_next, 0);
+    products(1, 1);
+  };
+  load(a0, b0);
+  wait_all();
   barrier();
+  read_a(a0, 0, 0);
+  read_b(b0, 0);
+  // (steps in pairs, so that a stage's place is known where it is read; after an odd last one a step of zeros)
   for (int64_t left = last - first; left > 0; left -= 2) {
     step(a0, b0, a1, b1);
-    wait_loads();
-    barrier();
-    if (left > 1) step(a1, b1, a0, b0);
-    wait_loads();
-    barrier();
+    step(a1, b1, a0, b0);
   }
   epilogue.template operator()<FM, FN>(acc, static_cast<int64_t>(tm) * BM + wm * (FM * 16), static_cast<int64_t>(tn) * BN + wn * (FN * 16),
                                        split);
