@@ -41,7 +41,6 @@ constexpr PartPairs kOnePair{0, 0}, kSixPairs{0x010201, 0x001021};   // (1,1) (0
 struct GemmArgs {
   Operand A, B;
   PartPairs pairs;
-  int n_pairs;
   int tiles_m, tiles_n, splits;
 };
 
@@ -51,24 +50,25 @@ struct GemmArgs {
 //   all 64 banks once.
 //  else: row k holds R / 8 pieces; the pairs of pieces (16 numbers, what a transposing read takes of a row) are exchanged
 //   by k: pair m16 of row k at m16 ^ (k % 4 + 4 (k / 8 % 2)), so that the eight rows that half a wave reads lie in all banks.
-// A thread's pieces lie the same distance apart, so that they share one offset; the loads' own range check gives zeros past
-// the operand's end.  (Rows of m or n outside of the operand give results that nobody reads.)
+// A thread's pieces lie the same distance apart; the loads' own range check gives zeros past the operand's end.  (Rows of m or n
+// outside of the operand give results that nobody reads.)
 template <int R, int NT, bool KINNER>
 struct TileLoader {
   static constexpr int PER = R * 8 / NT;
   static constexpr int kRows = KINNER ? NT / 8 : NT / (R / 8);   // rows of memory from one piece to the next
   static_assert(kRows % 16 == 0 || PER == 1, "the exchange of pieces is the same for all of a thread's");
-  const char *base, *end;   // of the tile and the next step; of the operand (its part)
-  int64_t step;             // bytes from one step to the next
+  const char *base;         // of the tile and the next step
+  int64_t rest, step;       // bytes from there to the operand's (its part's) end; from one step to the next
   int apart;                // bytes from one piece to the next (a tile's are less than 2^31: the host sees to it)
-  uint32_t at;              // bytes from `base` to the thread's first piece
+  uint32_t at, from;        // bytes from `base` to the thread's first piece; the same, or out of range, for this step
   int depth;                // KINNER: k of the thread's pieces within the tile
   __device__ __forceinline__ void init(const Operand &o, int64_t row0) {
     const int tid = threadIdx.x;
+    const int64_t skip = row0 * (KINNER ? o.ld : 1) * 2;
     step = (KINNER ? kBK : kBK * o.ld) * 2;
     apart = static_cast<int>(kRows * o.ld * 2);
-    base = reinterpret_cast<const char *>(o.p) + row0 * (KINNER ? o.ld : 1) * 2;
-    end = reinterpret_cast<const char *>(o.p) + (KINNER ? o.rows : o.depth) * o.ld * 2;
+    base = reinterpret_cast<const char *>(o.p) + skip;
+    rest = (KINNER ? o.rows : o.depth) * o.ld * 2 - skip;
     if constexpr (KINNER) {
       depth = ((tid & 7) ^ ((tid >> 4) & 7)) * 8;
       at = static_cast<uint32_t>(((tid >> 3) * o.ld + depth) * 2);
@@ -79,20 +79,17 @@ struct TileLoader {
       at = static_cast<uint32_t>((kr * o.ld + m) * 2);
     }
   }
-  __device__ __forceinline__ void to_part(int64_t bytes) { base += bytes, end += bytes; }
+  __device__ __forceinline__ void skip(int64_t bytes) { base += bytes, rest -= bytes; }
   // left: depth that is left of the operand from this step on, 0 or less for a tile of zeros
-  __device__ __forceinline__ void load(uint4 *tile, int left) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t rest = end - base;
-    const int range = left <= 0 || rest <= 0 ? 0 : (rest > 0x7fffffff ? 0x7fffffff : static_cast<int>(rest));
-    uint32_t from = at;
+  __device__ __forceinline__ void aim(int left) {
+    from = at;
     if constexpr (KINNER) from = depth < left ? at : 0x80000000u;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + i * apart), 0, max(range - i * apart, 0), 0x00020000),
-          (lds_void *)(tile + i * NT + wave * 64), 16, from, 0, 0, 0);
-    base += step;
+    else from = left > 0 ? at : 0x80000000u;
+  }
+  __device__ __forceinline__ void piece(uint4 *tile, int wave, int i) const {
+    const int range = rest <= 0 ? 0 : (rest > 0x7fffffff ? 0x7fffffff : static_cast<int>(rest));
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, range, 0x00020000),
+                                             (lds_void *)(tile + i * NT + wave * 64), 16, from + i * apart, 0, 0, 0);
   }
 };
 
@@ -125,6 +122,10 @@ __device__ __forceinline__ int formed_here(int at) {
   if constexpr (!KINNER) asm volatile("" : "+v"(at));
   return at;
 }
+template <int LOADS>
+__device__ __forceinline__ void wait_all_but() {   // the last LOADS (< 16) loads
+  __builtin_amdgcn_s_waitcnt(0x0070 | LOADS);
+}
 __device__ __forceinline__ void wait_all() { __builtin_amdgcn_s_waitcnt(0x0070); }   // vmcnt(0) lgkmcnt(0)
 __device__ __forceinline__ void barrier() {
   asm volatile("" ::: "memory");
@@ -149,7 +150,7 @@ __device__ __forceinline__ void tile_of(const GemmArgs &g, int &tm, int &tn, int
 
 // A block of WM x WN waves computes a BM x BN tile; wave (wm, wn) rows wm BM / WM of it and columns wn BN / WN on.
 // The epilogue gets acc[fm][fn]: lane (r, q) holds m = 16 fm + 4 q + 0..3 of the wave's rows, n = 16 fn + r of its columns.
-template <int BM, int BN, int WM, int WN, bool AK, bool BK, typename Epilogue>
+template <int BM, int BN, int WM, int WN, bool AK, bool BK, int PAIRS, typename Epilogue>
 __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, const Epilogue epilogue) {
   constexpr int NT = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
   __shared__ uint4 a0[BM * 8], a1[BM * 8], b0[BN * 8], b1[BN * 8];
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, con
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
   const int64_t depth = g.A.depth < g.B.depth ? g.B.depth : g.A.depth;
   const int steps = static_cast<int>((depth + kBK - 1) / kBK);
-  const int64_t total = static_cast<int64_t>(steps) * g.n_pairs;
+  const int64_t total = static_cast<int64_t>(steps) * PAIRS;
   const int64_t first = total * split / g.splits, last = total * (split + 1) / g.splits;
   TileLoader<BM, NT, AK> la;
   TileLoader<BN, NT, BK> lb;
@@ -166,28 +167,37 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, con
   lb.init(g.B, static_cast<int64_t>(tn) * BN);
   int pair = static_cast<int>(first / steps), at = static_cast<int>(first % steps);   // of the next load
   const auto part_of = [](uint32_t parts, int i) { return static_cast<int>(parts >> (4 * i) & 15); };
-  la.to_part(part_of(g.pairs.a, pair) * g.A.part * 2);
-  lb.to_part(part_of(g.pairs.b, pair) * g.B.part * 2);
-  la.base += at * la.step;
-  lb.base += at * lb.step;
+  la.skip(part_of(g.pairs.a, pair) * g.A.part * 2 + at * la.step);
+  lb.skip(part_of(g.pairs.b, pair) * g.B.part * 2 + at * lb.step);
+  la.rest += part_of(g.pairs.a, pair) * g.A.part * 2;
+  lb.rest += part_of(g.pairs.b, pair) * g.B.part * 2;
   f32x4 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int64_t to_load = last - first;
-  const auto load = [&](uint4 *a, uint4 *b) __attribute__((always_inline)) {
+  int to_load = static_cast<int>(last - first);
+  const auto aim = [&]() __attribute__((always_inline)) {
     const int done = to_load-- > 0 ? at * kBK : 0x7fffffff;   // past the last step: zeros
-    la.load(a, static_cast<int>(g.A.depth) - done);
-    lb.load(b, static_cast<int>(g.B.depth) - done);
-    // on to the next pair of parts after the last step of one (without a branch, which costs registers)
-    const int over = ++at == steps ? -1 : 0;
-    la.to_part((part_of(g.pairs.a, pair - over) - part_of(g.pairs.a, pair)) * g.A.part * 2);
-    lb.to_part((part_of(g.pairs.b, pair - over) - part_of(g.pairs.b, pair)) * g.B.part * 2);
-    la.base -= (steps & over) * la.step;
-    lb.base -= (steps & over) * lb.step;
-    pair -= over;
-    at &= ~over;
+    la.aim(static_cast<int>(g.A.depth) - done);
+    lb.aim(static_cast<int>(g.B.depth) - done);
+  };
+  // (on to the next pair of parts after the last step of one, without a branch, which costs registers)
+  const auto next = [&]() __attribute__((always_inline)) {
+    ++at;
+    la.skip(la.step);
+    lb.skip(lb.step);
+    if constexpr (PAIRS > 1) {
+      const int over = at == steps ? -1 : 0;
+      const int64_t a = (part_of(g.pairs.a, pair - over) - part_of(g.pairs.a, pair)) * g.A.part * 2;
+      const int64_t b = (part_of(g.pairs.b, pair - over) - part_of(g.pairs.b, pair)) * g.B.part * 2;
+      la.skip(a - (steps & over) * la.step);
+      lb.skip(b - (steps & over) * lb.step);
+      la.rest += a;
+      lb.rest += b;
+      pair -= over;
+      at &= ~over;
+    }
   };
   // A step is four groups of products, (k half s, half hm of the rows), whose fragments are read one group ahead.  Once the last
   // group's have arrived the stage is free and the next one's tiles are needed: there the waves meet, and
@@ -207,31 +217,53 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, con
 #pragma unroll
     for (int j = 0; j < FN; ++j) fb[s][j] = fragment<BN, BK>(b, here, j, s);
   };
-  const auto products = [&](int s, int hm) __attribute__((always_inline)) {
+  // one row of fragments after the other, `between(i)` after row i
+  const auto products = [&](int s, int hm, auto between) __attribute__((always_inline)) {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < HM; ++i)
+    for (int i = 0; i < HM; ++i) {
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[hm * HM + i][j] = mfma16(fa[hm][i], fb[s][j], acc[hm * HM + i][j]);
-    __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_sched_barrier(0);
+      between(i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
-  const auto step = [&](const uint4 *a, const uint4 *b, uint4 *a_next, uint4 *b_next) __attribute__((always_inline)) {
-    load(a_next, b_next);
+  const auto nothing = [](int) {};
+  const auto step = [&](uint4 *a, uint4 *b, const uint4 *a_next, const uint4 *b_next) __attribute__((always_inline)) {
     read_a(a, 0, 1);
-    products(0, 0);
+    products(0, 0, nothing);
     read_b(b, 1);
     read_a(a, 1, 0);
-    products(0, 1);
+    products(0, 1, nothing);
     read_a(a, 1, 1);
-    products(1, 0);
+    products(1, 0, nothing);
     wait_all();
     barrier();
     read_a(a_next, 0, 0);
     read_b(b_next, 0);
-    products(1, 1);
+    aim();
+    // the tiles after the next take this step's place
+    products(1, 1, [&](int i) __attribute__((always_inline)) {
+      constexpr int PA = (la.PER + HM - 1) / HM, PB = (lb.PER + HM - 1) / HM;
+#pragma unroll
+      for (int p = i * PA; p < (i + 1) * PA && p < la.PER; ++p) la.piece(a, wave, p);
+#pragma unroll
+      for (int p = i * PB; p < (i + 1) * PB && p < lb.PER; ++p) lb.piece(b, wave, p);
+    });
+    next();
+  };
+  const auto load = [&](uint4 *a, uint4 *b) __attribute__((always_inline)) {
+    aim();
+#pragma unroll
+    for (int p = 0; p < la.PER; ++p) la.piece(a, wave, p);
+#pragma unroll
+    for (int p = 0; p < lb.PER; ++p) lb.piece(b, wave, p);
+    next();
   };
   load(a0, b0);
-  wait_all();
+  load(a1, b1);
+  wait_all_but<la.PER + lb.PER>();
   barrier();
   read_a(a0, 0, 0);
   read_b(b0, 0);
@@ -262,6 +294,7 @@ __device__ __forceinline__ float exp_of(float x) {
 // m: vocabulary, n: tokens.  STORE: the numerators too.  WIDE: fp32 numerators.
 template <typename ID, bool STORE, bool WIDE>
 struct LogitsEpilogue {
+  static constexpr int kWide = WIDE;   // with one product of parts (0), six (1), either (2)
   const ID *targets;
   float2 *stat;
   float *zt;
@@ -329,6 +362,7 @@ struct LogitsEpilogue {
 
 // out[n][m], m innermost, times *scale: fp32 slabs of splits (out32 != null), added to `add` if that is there; else rounded to bf16
 struct StoreEpilogue {
+  static constexpr int kWide = 2;
   const float *scale;
   float *out32;
   uint16_t *out16;
@@ -564,16 +598,21 @@ hipError_t launch_gemm(const HeadTile &tile, Operand A, Operand B, int64_t M, in
   g.A = A;
   g.B = B;
   g.pairs = parts == 1 ? kOnePair : kSixPairs;
-  g.n_pairs = parts == 1 ? 1 : 6;
   g.tiles_m = static_cast<int>(ceil_div(M, tile.bm));
   g.tiles_n = static_cast<int>(ceil_div(N, tile.bn));
   g.splits = splits;
   const dim3 grid(static_cast<unsigned>(g.tiles_m * g.tiles_n * splits));
-  if (tile.bm == 256) hipLaunchKernelGGL((gemm_kernel<256, 256, 2, 4, AK, BK, Epilogue>), grid, dim3(512), 0, s, g, e);
-  else if (tile.bn == 128) hipLaunchKernelGGL((gemm_kernel<128, 128, 2, 2, AK, BK, Epilogue>), grid, dim3(256), 0, s, g, e);
-  else if constexpr (BK) hipLaunchKernelGGL((gemm_kernel<128, 32, 4, 1, AK, BK, Epilogue>), grid, dim3(256), 0, s, g, e);
-  else return hipErrorInvalidValue;
-  return hipGetLastError();
+  const auto go = [&](auto pairs) {
+    constexpr int P = decltype(pairs)::value;
+    if (tile.bm == 256) hipLaunchKernelGGL((gemm_kernel<256, 256, 2, 4, AK, BK, P, Epilogue>), grid, dim3(512), 0, s, g, e);
+    else if (tile.bn == 128) hipLaunchKernelGGL((gemm_kernel<128, 128, 2, 2, AK, BK, P, Epilogue>), grid, dim3(256), 0, s, g, e);
+    else if constexpr (BK) hipLaunchKernelGGL((gemm_kernel<128, 32, 4, 1, AK, BK, P, Epilogue>), grid, dim3(256), 0, s, g, e);
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+  };
+  if constexpr (Epilogue::kWide == 0) return go(std::integral_constant<int, 1>{});
+  else if constexpr (Epilogue::kWide == 1) return go(std::integral_constant<int, 6>{});
+  else return parts == 1 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 6>{});
 }
 
 constexpr int64_t kChipBlocks = 256;
