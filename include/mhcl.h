@@ -329,7 +329,7 @@ enum { MHCL_I64 = 0, MHCL_I32 = 1 };           /* id_dtype */
 typedef struct {
   int32_t n;         /* residual streams, 1..8 (read by mhcl_embed* and mhcl_streams_norm*)             */
   int32_t C;         /* width; a positive multiple of 8, at most 32768                                  */
-  int64_t T;         /* tokens, 0 .. 2^31 - 1                                                           */
+  int64_t T;         /* tokens, 0 .. 2^30                                                               */
   int32_t V;         /* rows of table or W, >= 1 (not read by mhcl_streams_norm*)                       */
   int32_t io_dtype;  /* MHCL_BF16 | MHCL_F32: streams, h and their gradients                            */
   int32_t w_dtype;   /* MHCL_BF16 | MHCL_F32: table, W and their gradients (mhcl_head_*: equal io_dtype) */

@@ -50,18 +50,44 @@ __device__ __forceinline__ void store_as(void *p, size_t elem, const float (&v)[
   }
 }
 
+// sum of a token's n streams (N of them where N > 0), in order, one piece; ONCE: read past the caches
+template <typename IO, int N, bool ONCE, int VEC>
+__device__ __forceinline__ void stream_sum(const void *x, int64_t t, int n, int C, int c, float (&s)[VEC]) {
+  if constexpr (N > 0) {
+    float v[N][VEC];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (ONCE) IO::load_once(x, (t * N + i) * C + c, v[i]);
+      else IO::load(x, (t * N + i) * C + c, v[i]);
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      s[e] = v[0][e];
+#pragma unroll
+      for (int i = 1; i < N; ++i) s[e] += v[i][e];
+    }
+  } else {
+    IO::load(x, t * n * C + c, s);
+    for (int i = 1; i < n; ++i) {
+      float v[VEC];
+      IO::load(x, (t * n + i) * C + c, v);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[e] += v[e];
+    }
+  }
+}
+
 // ---------------------------------------------------------------- embedding
 // x[t][i] = scale table[ids[t]]: one thread per 16-byte piece of a row of C, which it reads once and writes n times.
-// Bound by the writes.
+// Bound by the writes: 32768 tokens, n = 4, C = 4096, bf16 204 us, 5.3 TB/s (two tokens a thread 223; stores past the caches 210); 16384,
+// C = 1024, fp32 table 33 us.
 template <typename IO, typename W, typename ID>
 __global__ __launch_bounds__(kBlock) void embed_kernel(const void *__restrict__ table, const ID *__restrict__ ids,
                                                        void *__restrict__ x, int n, int C, int64_t T, int32_t V, float scale) {
   constexpr int VEC = IO::kVec;
-  const int vpr = C / VEC;
-  const int64_t idx = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x;
-  const int64_t t = idx / vpr;
-  if (t >= T) return;
-  const int c = static_cast<int>(idx - t * vpr) * VEC;
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * VEC;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * blockDim.y + threadIdx.y;
+  if (c >= C || t >= T) return;
   const int32_t id = token_of(ids, t, V);
   float v[VEC];
   if (id >= 0 && id < V) {
@@ -75,30 +101,35 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(const void *__restrict__ 
   for (int i = 0; i < n; ++i) IO::store(x, (t * n + i) * C + c, v);
 }
 
-// Tokens by id: a token's place is the number of tokens with a smaller id, or the same id and an earlier place.  A block
+// Tokens by id, equal ids in the order of the tokens.  What has no place in the table (id V here) goes last.
+template <typename ID>
+__device__ __forceinline__ int32_t key_of(const ID *ids, int32_t t, int32_t V) {
+  const ID id = ids[t];
+  return id < 0 || id >= V ? V : static_cast<int32_t>(id);
+}
+
+// Few tokens, one launch: a token's place is the number of tokens with a smaller id, or the same id and an earlier place.  A block
 // ranks 64 tokens, one a lane; its sixteen waves share out the tokens compared with, whose ids are wave-uniform.
 constexpr int kRankWaves = 16;
 template <typename ID>
 __global__ __launch_bounds__(64 * kRankWaves) void rank_kernel(const ID *__restrict__ ids, int32_t *__restrict__ key,
-                                                               int32_t *__restrict__ pos, int32_t T, int32_t V) {
+                                                               int32_t *__restrict__ pos, int32_t *__restrict__ shared_rows, int32_t T, int32_t V) {
   __shared__ int32_t count[kRankWaves][64];
+  if (blockIdx.x == 0 && threadIdx.x == 0) *shared_rows = 0;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int32_t t = blockIdx.x * 64 + lane;
-  // (what has no place in the table goes last)
-  const auto key_of = [&](int32_t j) {
-    const ID id = ids[j];
-    return id < 0 || id >= V ? V : static_cast<int32_t>(id);
-  };
-  const int32_t mine = t < T ? key_of(t) : V;
+  const int32_t t0 = blockIdx.x * 64, t = t0 + lane;
+  const int32_t mine = t < T ? key_of(ids, t, V) : V;
   const int32_t per = ((T + kRankWaves - 1) / kRankWaves + 63) / 64 * 64;
   const int32_t first = wave * per, last = min(T, first + per);
   int32_t smaller = 0;
   for (int32_t j0 = first; j0 < last; j0 += 64) {
-    const int32_t theirs = j0 + lane < last ? key_of(j0 + lane) : 0x7fffffff;
+    const int32_t theirs = j0 + lane < last ? key_of(ids, j0 + lane, V) : 0x7fffffff;
+    const int32_t below = j0 < t0 ? mine + 1 : mine;   // equal ids count where they come before
 #pragma unroll
-    for (int k = 0; k < 64; ++k) {
-      const int32_t other = __builtin_amdgcn_readlane(theirs, k);
-      smaller += (other < mine || (other == mine && j0 + k < t)) ? 1 : 0;
+    for (int k = 0; k < 64; ++k) smaller += __builtin_amdgcn_readlane(theirs, k) < below ? 1 : 0;
+    if (j0 == t0) {
+#pragma unroll
+      for (int k = 0; k < 64; ++k) smaller += __builtin_amdgcn_readlane(theirs, k) == mine && k < lane ? 1 : 0;
     }
   }
   count[wave][lane] = smaller;
@@ -112,7 +143,113 @@ __global__ __launch_bounds__(64 * kRankWaves) void rank_kernel(const ID *__restr
   }
 }
 
-// Sums of kChunk sorted tokens, TX threads for a row's columns (grid.y: the pieces of VEC TX columns), one chunk per
+// Many tokens: by digits of the id, the lowest first.  A block has a range of `per` tokens; digit_count_kernel counts its digits,
+// digit_place_kernel moves its tokens behind all of smaller digits and those of the same digit in earlier blocks.  (us, the ranks
+// above / two passes of digits: 4096 tokens 10.6 / 17.2, 8192 17.6 / 20.5, 16384 31.4 / 23.2; 10^6 - / 136.)
+constexpr int kDigitMost = 9, kDigits = 1 << kDigitMost, kSortBlocks = 64, kSortThreads = 512, kSortTile = 2048;
+
+struct Unsorted {   // keys and places of a pass: from the ids (the first one) or from what the pass before left
+  const void *ids;
+  const int32_t *key, *pos;
+  template <typename ID, bool FIRST>
+  __device__ __forceinline__ int32_t at(int32_t i, int32_t V) const {
+    if constexpr (FIRST) return key_of(static_cast<const ID *>(ids), i, V);
+    return key[i];
+  }
+};
+
+template <typename ID, bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void digit_count_kernel(const Unsorted in, int32_t *__restrict__ counts, int32_t *__restrict__ shared_rows,
+                                                                   int32_t T, int32_t V, int32_t per, int shift, int bits) {
+  __shared__ int32_t count[kDigits];
+  if (blockIdx.x == 0 && threadIdx.x == 0) *shared_rows = 0;
+  for (int d = threadIdx.x; d < kDigits; d += kSortThreads) count[d] = 0;
+  __syncthreads();
+  const int32_t first = blockIdx.x * per, last = min(T, first + per);
+  for (int32_t i = first + threadIdx.x; i < last; i += kSortThreads)
+    atomicAdd(&count[in.at<ID, FIRST>(i, V) >> shift & ((1 << bits) - 1)], 1);   // (whole numbers: any order)
+  __syncthreads();
+  for (int d = threadIdx.x; d < kDigits; d += kSortThreads) counts[blockIdx.x * kDigits + d] = count[d];
+}
+
+template <typename ID, bool FIRST>
+__global__ __launch_bounds__(kSortThreads) void digit_place_kernel(const Unsorted in, const int32_t *__restrict__ counts,
+                                                                   int32_t *__restrict__ key, int32_t *__restrict__ pos, int32_t T, int32_t V,
+                                                                   int32_t per, int shift, int bits) {
+  static_assert(kDigits == kSortThreads, "a thread for each digit");
+  constexpr int WAVES = kSortThreads / 64, ROUNDS = kSortTile / kSortThreads;
+  __shared__ int32_t next[kDigits], count[WAVES][kDigits], sums[WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  {
+    // where this block's tokens of digit `tid` begin
+    int32_t before = 0, all = 0;
+    for (int b = 0; b < static_cast<int>(gridDim.x); ++b) {
+      const int32_t c = counts[b * kDigits + tid];
+      before += b < static_cast<int>(blockIdx.x) ? c : 0;
+      all += c;
+    }
+    int32_t upto = all;                                // sum over the digits up to this one
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+      const int32_t v = __shfl_up(upto, off, 64);
+      upto += lane >= off ? v : 0;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += sums[w];
+    next[tid] = upto - all + before;
+  }
+  const int32_t first = blockIdx.x * per, last = min(T, first + per);
+  for (int32_t tile = first; tile < last; tile += kSortTile) {
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) count[w][tid] = 0;
+    __syncthreads();
+    // a wave takes neighbouring tokens, 64 at a time: a token's place among those of its digit in the wave
+    int32_t k[ROUNDS], p[ROUNDS], place[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      const int32_t i = tile + wave * (64 * ROUNDS) + r * 64 + lane;
+      const bool there = i < last;
+      k[r] = there ? in.at<ID, FIRST>(i, V) : 0;
+      p[r] = there ? (FIRST ? i : in.pos[i]) : -1;
+      const int digit = k[r] >> shift & ((1 << bits) - 1);
+      uint64_t same = __ballot(there);
+#pragma unroll
+      for (int b = 0; b < kDigitMost; ++b) {
+        const bool one = digit >> b & 1;
+        const uint64_t ones = __ballot(one);
+        same &= one ? ones : ~ones;
+      }
+      const int lower = __popcll(same & ((uint64_t{1} << lane) - 1));
+      place[r] = there ? count[wave][digit] + lower : 0;
+      __builtin_amdgcn_wave_barrier();                 // (all of a wave's lanes have read before one of them writes)
+      if (there && lower == 0) count[wave][digit] += __popcll(same);
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    {
+      int32_t begin = next[tid];
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const int32_t c = count[w][tid];
+        count[w][tid] = begin;
+        begin += c;
+      }
+      next[tid] = begin;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      if (p[r] < 0) continue;
+      const int32_t to = count[wave][k[r] >> shift & ((1 << bits) - 1)] + place[r];
+      key[to] = k[r];
+      pos[to] = p[r];
+    }
+    __syncthreads();
+  }
+}
+
+// Sums of `span` sorted tokens (a chunk), TX threads for a row's columns (grid.y: the pieces of VEC TX columns), one chunk per
 // threadIdx.y.  A row whose tokens all lie in the chunk is written; of a row shared with other chunks the sum goes to
 // part[chunk][0] where it continues from the chunk before, else (it begins here) to part[chunk][1].
 template <typename IO, typename W, bool ACC>
@@ -129,95 +266,102 @@ __device__ __forceinline__ void embed_write(void *g_table, size_t elem, const fl
   }
   store_as<W, VEC>(g_table, elem, v);
 }
-template <typename IO, typename W, bool ACC>
+// N: the number of streams where it is four or less, else 0; the rows of four tokens are asked for together then.  A chunk in which a
+// shared row begins joins the list of those.
+template <typename IO, typename W, bool ACC, int N, bool ONCE>
 __global__ __launch_bounds__(kBlock) void embed_sum_kernel(const int32_t *__restrict__ key, const int32_t *__restrict__ pos,
                                                            const void *__restrict__ g_x, void *__restrict__ g_table,
-                                                           float *__restrict__ part, int n, int C, int32_t T, int32_t V, float scale) {
-  constexpr int VEC = IO::kVec;
+                                                           float *__restrict__ part, int32_t *__restrict__ shared_rows, int span, int n,
+                                                           int C, int32_t T, int32_t V, float scale) {
+  constexpr int VEC = IO::kVec, GROUP = N > 0 ? 4 : 1;
   const int32_t chunk = blockIdx.x * blockDim.y + threadIdx.y;
-  const int64_t s = static_cast<int64_t>(chunk) * kChunk;
+  const int64_t s = static_cast<int64_t>(chunk) * span;
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * VEC;
   if (s >= T || c >= C) return;
-  const int count = static_cast<int>(min<int64_t>(kChunk, T - s));
+  const int64_t end = min<int64_t>(s + span, T);
   float sum[VEC] = {};
   int32_t cur = key[s];
+  if (cur >= V) return;                                 // (those come last)
   bool from_before = s > 0 && key[s - 1] == cur;
-  for (int k = 0; k < count; ++k) {
-    const int32_t id = key[s + k];
-    if (id != cur) {
-      if (cur < V) {
+  for (int64_t k = s; k < end; k += GROUP) {
+    int32_t id[GROUP];
+    float own[GROUP][VEC];
+#pragma unroll
+    for (int j = 0; j < GROUP; ++j) {
+      id[j] = k + j < end ? key[k + j] : V;
+      // (in place of what is not summed, the chunk's first token: without a branch the loads go out together)
+      stream_sum<IO, N, ONCE>(g_x, pos[id[j] < V ? k + j : s], n, C, c, own[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < GROUP; ++j) {
+      if (id[j] >= V) break;
+      if (id[j] != cur) {
         if (from_before) store_as<F32, VEC>(part, static_cast<size_t>(chunk) * 2 * C + c, sum);
         else embed_write<IO, W, ACC>(g_table, static_cast<size_t>(cur) * C + c, sum, scale);
+        cur = id[j];
+        from_before = false;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
       }
-      cur = id;
-      from_before = false;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) sum[e] = 0.f;
+      for (int e = 0; e < VEC; ++e) sum[e] += own[j][e];
     }
-    if (id >= V) return;   // (those come last)
-    const int64_t row = static_cast<int64_t>(pos[s + k]) * n;
-    float own[VEC] = {};
-    for (int i = 0; i < n; ++i) {
-      float v[VEC];
-      IO::load(g_x, (row + i) * C + c, v);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) own[e] += v[e];
-    }
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) sum[e] += own[e];
   }
-  const bool goes_on = s + count < T && key[s + count] == cur;
+  const bool goes_on = end < T && key[end] == cur;
   if (!from_before && !goes_on) {
     embed_write<IO, W, ACC>(g_table, static_cast<size_t>(cur) * C + c, sum, scale);
     return;
   }
   store_as<F32, VEC>(part, (static_cast<size_t>(chunk) * 2 + (from_before ? 0 : 1)) * C + c, sum);
+  if (!from_before && c == 0) shared_rows[1 + atomicAdd(shared_rows, 1)] = chunk;   // (their order changes nothing)
 }
 
-// The rows that lie in several chunks: a block looks at one chunk's last row, and where that begins in this chunk and goes
-// on, adds the parts of the chunks after it, in order: sixteen threads of a column take a range of them each.
-constexpr int kJoinRows = 16;
+// The rows that lie in several chunks, 256 columns at a time: the last row of the chunk in which it begins and the first ones of the
+// chunks after it, in order; four threads of a column take a range of them each.  The blocks share out the list that the sums have left
+// (a block for every chunk and 64 columns instead, most of which end at once: 32768 tokens, C = 4096 458 us, all of it launch).
+constexpr int kJoinRows = 4, kJoinBlocks = 2048;
 template <typename W, bool ACC>
 __global__ __launch_bounds__(64 * kJoinRows) void embed_join_kernel(const int32_t *__restrict__ key, const float *__restrict__ part,
-                                                                    void *__restrict__ g_table, int C, int32_t T, int32_t V, float scale) {
-  __shared__ float red[kJoinRows][64];
-  const int64_t chunk = blockIdx.x;
-  const int64_t e = (chunk + 1) * kChunk;
-  if (e >= T) return;
-  const int32_t id = key[e - 1];
-  if (id >= V || key[e] != id) return;                                  // ends here
-  const int64_t s = chunk * kChunk;
-  if (key[s] == id && s > 0 && key[s - 1] == id) return;                // began before
-  // its last chunk: the one of the last token with this id
-  int64_t lo = e, hi = T;                                               // key[lo] == id, key[hi] > id
-  while (hi - lo > 1) {
-    const int64_t mid = (lo + hi) / 2;
-    if (key[mid] == id) lo = mid;
-    else hi = mid;
-  }
-  const int64_t parts = lo / kChunk - chunk;                            // after this chunk's
-  const int c = blockIdx.y * 64 + threadIdx.x;
-  const int64_t per = (parts + kJoinRows - 1) / kJoinRows;
-  const int64_t k0 = threadIdx.y * per, k1 = min(parts, k0 + per);
-  float sum = 0.f;
-  if (c < C) {
-    if (threadIdx.y == 0) sum = part[(chunk * 2 + 1) * C + c];
+                                                                    const int32_t *__restrict__ shared_rows, void *__restrict__ g_table,
+                                                                    int span, int C, int32_t T, int32_t V, float scale) {
+  __shared__ float4 red[kJoinRows][64];
+  const int tiles = (C + 255) / 256;
+  const int64_t items = static_cast<int64_t>(*shared_rows) * tiles;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t chunk = shared_rows[1 + item / tiles];
+    const int c = static_cast<int>(item % tiles) * 256 + threadIdx.x * 4;
+    const int64_t e = (chunk + 1) * span;
+    const int32_t id = key[e - 1];
+    // its last chunk: the one of the last token with this id
+    int64_t lo = e, hi = T;                                               // key[lo] == id, key[hi] > id
+    while (hi - lo > 1) {
+      const int64_t mid = (lo + hi) / 2;
+      if (key[mid] == id) lo = mid;
+      else hi = mid;
+    }
+    const int64_t parts = lo / span - chunk;                            // after this chunk's
+    const int64_t per = (parts + kJoinRows - 1) / kJoinRows;
+    const int64_t k0 = threadIdx.y * per, k1 = min(parts, k0 + per);
+    float sum[4] = {};
+    if (c < C) {
+      if (threadIdx.y == 0) F32::load(part, (chunk * 2 + 1) * C + c, sum);
 #pragma unroll 8
-    for (int64_t k = k0; k < k1; ++k) sum += part[(chunk + 1 + k) * 2 * C + c];
-  }
-  red[threadIdx.y][threadIdx.x] = sum;
-  __syncthreads();
-  if (threadIdx.y != 0 || c >= C) return;
-  sum = pairwise_sum<kJoinRows>([&](int k) { return red[k][threadIdx.x]; }) * scale;
-  const size_t at = static_cast<size_t>(id) * C + c;
-  if constexpr (W::kVec == 8) {
-    uint16_t *g = static_cast<uint16_t *>(g_table);
-    if constexpr (ACC) sum += bf16_to_f32(g[at]);
-    g[at] = f32_to_bf16(sum);
-  } else {
-    float *g = static_cast<float *>(g_table);
-    if constexpr (ACC) sum += g[at];
-    g[at] = sum;
+      for (int64_t k = k0; k < k1; ++k) {
+        float v[4];
+        F32::load(part, (chunk + 1 + k) * 2 * C + c, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += v[i];
+      }
+    }
+    red[threadIdx.y][threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    __syncthreads();
+    if (threadIdx.y == 0 && c < C) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        sum[i] = pairwise_sum<kJoinRows>([&](int k) { return reinterpret_cast<const float *>(&red[k][threadIdx.x])[i]; });
+      embed_write<F32, W, ACC>(g_table, static_cast<size_t>(id) * C + c, sum, scale);
+    }
+    __syncthreads();
   }
 }
 
@@ -262,31 +406,9 @@ __device__ __forceinline__ float row_sum(float v, float *red) {
   return v;
 }
 
-template <typename IO, int N, int VEC>
-__device__ __forceinline__ void stream_sum(const void *x, int64_t t, int n, int C, int c, float (&s)[VEC]) {
-  if constexpr (N > 0) {
-    float v[N][VEC];
-#pragma unroll
-    for (int i = 0; i < N; ++i) IO::load(x, (t * N + i) * C + c, v[i]);
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      s[e] = v[0][e];
-#pragma unroll
-      for (int i = 1; i < N; ++i) s[e] += v[i][e];
-    }
-  } else {
-    IO::load(x, t * n * C + c, s);
-    for (int i = 1; i < n; ++i) {
-      float v[VEC];
-      IO::load(x, (t * n + i) * C + c, v);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) s[e] += v[e];
-    }
-  }
-}
-
-// h = gain s / sqrt(mean(s^2) + eps), s the sum of a token's streams in fp32; one pass, bound by memory
-template <typename IO, int N, int L, int CH>
+// h = gain s / sqrt(mean(s^2) + eps), s the sum of a token's streams in fp32; one pass, bound by memory: 32768 tokens, n = 4, C = 4096,
+// bf16 219 us, 6.1 TB/s.  Streams that the last-level cache cannot hold are read past the caches (kept: 248).
+template <typename IO, int N, int L, int CH, bool ONCE>
 __global__ __launch_bounds__(L *norm_tokens(L)) void norm_kernel(const void *__restrict__ x, const float *__restrict__ gain,
                                                                  void *__restrict__ h, int n, int C, int64_t T, float eps) {
   constexpr int VEC = IO::kVec;
@@ -299,7 +421,7 @@ __global__ __launch_bounds__(L *norm_tokens(L)) void norm_kernel(const void *__r
   for (int k = 0; k < CH; ++k) {
     const int c = (k * L + lane) * VEC;
     if (c < C) {
-      stream_sum<IO, N>(x, t, n, C, c, s[k]);
+      stream_sum<IO, N, ONCE>(x, t, n, C, c, s[k]);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) sq = fmaf(s[k][e], s[k][e], sq);
     }
@@ -334,7 +456,7 @@ __global__ __launch_bounds__(L *norm_tokens(L)) void norm_bwd_kernel(const void 
     for (int k = 0; k < CH; ++k) {
       const int c = (k * L + lane) * VEC;
       if (c < C) {
-        stream_sum<IO, N>(x, t, n, C, c, s[k]);
+        stream_sum<IO, N, false>(x, t, n, C, c, s[k]);
         float w[VEC];
         IO::load(g_h, t * C + c, g[k]);
         load_as<F32, VEC>(gain, c, w);
@@ -407,6 +529,13 @@ __global__ __launch_bounds__(kBlock) void zero_kernel(uint32_t *__restrict__ p, 
 
 inline unsigned blocks(int64_t items, int64_t each) { return static_cast<unsigned>((items + each - 1) / each); }
 
+// threads for a row of `pieces` pieces, and for as many rows as a block then has threads for
+inline dim3 row_block(int pieces) {
+  int x = 1;
+  while (x < kBlock && x < pieces) x *= 2;
+  return dim3(x, kBlock / x);
+}
+
 template <typename F>
 hipError_t dispatch_io_w(const mhcl_ends_desc &d, F &&f) {
   return dispatch_io(d.io_dtype, [&](auto io) {
@@ -441,6 +570,10 @@ hipError_t dispatch_streams(int n, F &&f) {
 
 }  // namespace
 
+// About a thousand chunks, for the chip, of 8 to 32 tokens: shorter ones leave more rows to be joined. (us, sums and joins at 8 / 16 / 32:
+// 3001 tokens, n = 4, C = 768, f32 15.4 / 18.0 / 27.1; 16384, C = 1024, bf16 63.2 / 63.4 / 67.9; 32768, C = 4096 350 / 331 / 313.)
+int32_t EmbedBwdWs::embed_chunk(const mhcl_ends_desc &d) { return d.T < 16384 ? 8 : (d.T < 32768 ? 16 : 32); }
+
 hipError_t launch_zero(void *p, size_t bytes, hipStream_t s) {
   const size_t words = bytes / 4;
   if (words == 0) return hipSuccess;
@@ -453,22 +586,56 @@ hipError_t launch_embed(const mhcl_ends_desc &d, const void *table, const void *
     return dispatch_id(d.id_dtype, [&](auto id) {
       using IO = decltype(io);
       using ID = decltype(id);
-      hipLaunchKernelGGL((embed_kernel<IO, decltype(w), ID>), dim3(blocks(d.T * (d.C / IO::kVec), kBlock)), dim3(kBlock), 0, s,
-                         table, static_cast<const ID *>(ids), x, d.n, d.C, d.T, d.V, d.scale);
+      const dim3 block = row_block(d.C / IO::kVec);
+      hipLaunchKernelGGL((embed_kernel<IO, decltype(w), ID>),
+                         dim3(blocks(d.T, block.y), blocks(d.C / IO::kVec, block.x)), block, 0, s, table, static_cast<const ID *>(ids), x, d.n, d.C, d.T, d.V, d.scale);
       return hipGetLastError();
     });
+  });
+}
+
+// Gradients above the size of the L2s are read past them (us of the sums, kept / past them, n = 4, C = 1024, bf16: 17 MB 9.8 / 11.8,
+// 34 MB 15.6 / 14.0, 67 MB 27.0 / 18.4, 134 MB 54.6 / 36.1; C = 4096, 1.07 GB 293 / 242).
+constexpr int64_t kOnceBytes = int64_t{32} << 20;
+
+// up to so many tokens by comparing each with each
+constexpr int32_t kRankTokens = 8192;
+
+static hipError_t sort_tokens(const mhcl_ends_desc &d, const void *ids, const EmbedBwdWs &w, hipStream_t s) {
+  const int32_t T = static_cast<int32_t>(d.T);
+  return dispatch_id(d.id_dtype, [&](auto id) {
+    using ID = decltype(id);
+    if (T <= kRankTokens) {
+      hipLaunchKernelGGL((rank_kernel<ID>), dim3(blocks(T, 64)), dim3(64 * kRankWaves), 0, s, static_cast<const ID *>(ids), w.key,
+                         w.pos, w.shared_rows, T, d.V);
+      return hipGetLastError();
+    }
+    int bits = 1;
+    while (d.V >> bits) ++bits;                          // ids are 0 .. V
+    const int passes = (bits + kDigitMost - 1) / kDigitMost, each = (bits + passes - 1) / passes;
+    const int32_t per = static_cast<int32_t>((T + int64_t{kSortBlocks} * kSortTile - 1) / (int64_t{kSortBlocks} * kSortTile) * kSortTile);
+    const dim3 grid(blocks(T, per)), block(kSortThreads);
+    for (int p = 0; p < passes; ++p) {
+      // the last pass leaves its result in key and pos, the ones before by turns there and in the other two
+      const bool home = (passes - 1 - p) % 2 == 0;
+      int32_t *key = home ? w.key : w.key2, *pos = home ? w.pos : w.pos2;
+      const Unsorted in{ids, home ? w.key2 : w.key, home ? w.pos2 : w.pos};
+      if (p == 0) {
+        hipLaunchKernelGGL((digit_count_kernel<ID, true>), grid, block, 0, s, in, w.counts, w.shared_rows, T, d.V, per, 0, each);
+        hipLaunchKernelGGL((digit_place_kernel<ID, true>), grid, block, 0, s, in, w.counts, key, pos, T, d.V, per, 0, each);
+      } else {
+        hipLaunchKernelGGL((digit_count_kernel<ID, false>), grid, block, 0, s, in, w.counts, w.shared_rows, T, d.V, per, p * each, each);
+        hipLaunchKernelGGL((digit_place_kernel<ID, false>), grid, block, 0, s, in, w.counts, key, pos, T, d.V, per, p * each, each);
+      }
+    }
+    return hipGetLastError();
   });
 }
 
 hipError_t launch_embed_bwd(const mhcl_ends_desc &d, const void *ids, const void *g_x, void *g_table, bool accumulate,
                             const EmbedBwdWs &w, hipStream_t s) {
   const int32_t T = static_cast<int32_t>(d.T);
-  hipError_t e = dispatch_id(d.id_dtype, [&](auto id) {
-    using ID = decltype(id);
-    hipLaunchKernelGGL((rank_kernel<ID>), dim3(blocks(T, 64)), dim3(64 * kRankWaves), 0, s, static_cast<const ID *>(ids), w.key,
-                       w.pos, T, d.V);
-    return hipGetLastError();
-  });
+  hipError_t e = sort_tokens(d, ids, w, s);
   if (e != hipSuccess) return e;
   if (!accumulate) {
     const int chunks16 = static_cast<int>(d.C * dtype_bytes(d.w_dtype) / 16);
@@ -476,21 +643,24 @@ hipError_t launch_embed_bwd(const mhcl_ends_desc &d, const void *ids, const void
                        chunks16, T, d.V);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  const unsigned chunks = blocks(T, kChunk);
+  const unsigned chunks = static_cast<unsigned>(w.chunks);
   return dispatch_io_w(d, [&](auto io, auto wt) {
     using IO = decltype(io);
     using W = decltype(wt);
     const int pieces = d.C / IO::kVec;
-    int tx = 1;
-    while (tx < kBlock && tx < pieces) tx *= 2;
-    const int ty = kBlock / tx;
+    const dim3 block = row_block(pieces);
     const auto go = [&](auto acc) {
       constexpr bool ACC = decltype(acc)::value;
-      hipLaunchKernelGGL((embed_sum_kernel<IO, W, ACC>), dim3(blocks(chunks, ty), blocks(pieces, tx)), dim3(tx, ty), 0, s, w.key,
-                         w.pos, g_x, g_table, w.part, d.n, d.C, T, d.V, d.scale);
-      hipLaunchKernelGGL((embed_join_kernel<W, ACC>), dim3(chunks, blocks(d.C, 64)), dim3(64, kJoinRows), 0, s, w.key, w.part,
-                         g_table, d.C, T, d.V, d.scale);
-      return hipGetLastError();
+      return dispatch_streams(d.n, [&](auto nn) {
+        constexpr int N = decltype(nn)::value;
+        const bool once = d.T * d.n * d.C * static_cast<int64_t>(dtype_bytes(d.io_dtype)) > kOnceBytes;
+        hipLaunchKernelGGL((once ? embed_sum_kernel<IO, W, ACC, N, true> : embed_sum_kernel<IO, W, ACC, N, false>), dim3(blocks(chunks, block.y), blocks(pieces, block.x)),
+                           block, 0, s, w.key, w.pos, g_x, g_table, w.part, w.shared_rows, w.chunk, d.n, d.C, T, d.V, d.scale);
+        const int64_t most = static_cast<int64_t>(chunks) * blocks(d.C, 256);
+        hipLaunchKernelGGL((embed_join_kernel<W, ACC>), dim3(most < kJoinBlocks ? static_cast<unsigned>(most) : kJoinBlocks),
+                           dim3(64, kJoinRows), 0, s, w.key, w.part, w.shared_rows, g_table, w.chunk, d.C, T, d.V, d.scale);
+        return hipGetLastError();
+      });
     };
     return accumulate ? go(std::true_type{}) : go(std::false_type{});
   });
@@ -501,8 +671,9 @@ hipError_t launch_streams_norm(const mhcl_ends_desc &d, const void *x, const flo
     using IO = decltype(io);
     return dispatch_row(d.C / IO::kVec, [&](auto l, auto ch) {
       return dispatch_streams(d.n, [&](auto nn) {
-        constexpr int L = decltype(l)::value;
-        hipLaunchKernelGGL((norm_kernel<IO, decltype(nn)::value, L, decltype(ch)::value>), dim3(blocks(d.T, norm_tokens(L))),
+        constexpr int L = decltype(l)::value, CH = decltype(ch)::value, N = decltype(nn)::value;
+        const bool once = d.T * d.n * d.C * static_cast<int64_t>(dtype_bytes(d.io_dtype)) > kLastLevelCache;
+        hipLaunchKernelGGL((once ? norm_kernel<IO, N, L, CH, true> : norm_kernel<IO, N, L, CH, false>), dim3(blocks(d.T, norm_tokens(L))),
                            dim3(L * norm_tokens(L)), 0, s, x, gain, h, d.n, d.C, d.T, d.eps);
         return hipGetLastError();
       });

@@ -31,7 +31,7 @@ int check_ends(const mhcl_ends_desc *d, End end) {
   if (end == End::kNorm && !(d->eps >= 0.f)) return MHCL_ERR_INVALID_ARG;
   if (end == End::kHead && d->w_dtype != d->io_dtype) return MHCL_ERR_UNSUPPORTED;
   // index arithmetic: tokens and rows of the vocabulary in 32 bits, with room for a sentinel; at most 2^31 - 1 blocks a launch
-  if (d->C > 32768 || d->T > (int64_t{1} << 31) - 1) return MHCL_ERR_UNSUPPORTED;
+  if (d->C > 32768 || d->T > (1 << 30)) return MHCL_ERR_UNSUPPORTED;
   if (end != End::kNorm && d->V > (1 << 30)) return MHCL_ERR_UNSUPPORTED;
   if (d->T * (d->C / 4) / 256 > (int64_t{1} << 31) - 1) return MHCL_ERR_UNSUPPORTED;
   return MHCL_OK;
