@@ -272,9 +272,41 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, con
     step(a0, b0, a1, b1);
     step(a1, b1, a0, b0);
   }
+  // the stages are free for the epilogue once the last loads (of zeros) have arrived and every wave has read its fragments
+  wait_all();
+  barrier();
+  constexpr int NW = WM * WN, EACH = NW > 4 ? NW / 4 : 1;
+  static_assert(FM * FN * 256 * 2 * EACH <= (BN < BM ? BN : BM) * 128, "a wave's 16-bit results fit its part of the stages");
+  const int which = wave / EACH % 4;
+  uint4 *const scratch = which == 0 ? a0 : (which == 1 ? a1 : (which == 2 ? b0 : b1));
   epilogue.template operator()<FM, FN>(acc, static_cast<int64_t>(tm) * BM + wm * (FM * 16), static_cast<int64_t>(tn) * BN + wn * (FN * 16),
-                                       split);
+                                       split, scratch + wave % EACH * (FM * FN * 32));
 }
+
+// A wave's results, four 16-bit numbers in each of its lanes' places (16 i + 4 q .. + 3 of row 16 j + r), go to memory by way
+// of LDS: from the registers a store would write 32 bytes of each of 16 rows, so it writes whole rows of the wave's (256 bytes and
+// fewer, no faster one by one: 16384 tokens, 65536 rows, 64 deep: 1056 us from the registers, LDSUS this way).
+template <int FM, int FN>
+struct RowsOut {
+  static constexpr int CPR = FM * 2;          // 16-byte pieces of a row
+  uint4 *lds;
+  __device__ __forceinline__ void put(int i, int j, uint2 v) {
+    const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    const int piece = (2 * i + (q >> 1)) ^ (r & (CPR - 1));
+    *reinterpret_cast<uint2 *>(reinterpret_cast<char *>(lds + (16 * j + r) * CPR + piece) + (q & 1) * 8) = v;
+  }
+  // out(row, piece, value): row of the wave's, 16-byte piece of it
+  template <typename F>
+  __device__ __forceinline__ void flush(F out) {
+    const int lane = threadIdx.x & 63;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < FN * 16 * CPR / 64; ++k) {
+      const int row = (k * 64 + lane) / CPR, piece = lane % CPR;
+      out(row, piece, lds[row * CPR + (piece ^ (row & 15 & (CPR - 1)))]);
+    }
+  }
+};
 
 // ---- epilogues
 // e in [0, 1] as 16 bits: 6 of the exponent, 10 of the mantissa (2^-63 .. 1 to 2^-11 of itself, less is 0)
@@ -301,8 +333,9 @@ struct LogitsEpilogue {
   char *E;
   int64_t T, V, ld, granules;
   template <int FM, int FN>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int) const {
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int, uint4 *lds) const {
     const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    RowsOut<FM, FN> rows{lds};
     if (m0 + FM * 16 > V) {   // rows beyond the vocabulary
 #pragma unroll
       for (int i = 0; i < FM; ++i)
@@ -341,22 +374,19 @@ struct LogitsEpilogue {
           sum += acc[i][j][e];
         }
         if constexpr (STORE) {
-          if (t < T) {
-            const int64_t elem = t * ld + m0 + 16 * i + 4 * q;
-            if constexpr (WIDE) {
-              *reinterpret_cast<f32x4 *>(E + elem * 4) = acc[i][j];
-            } else {
-              const f32x4 v = acc[i][j];
-              *reinterpret_cast<uint2 *>(E + elem * 2) =
-                  make_uint2(encode(v[0]) | encode(v[1]) << 16, encode(v[2]) | encode(v[3]) << 16);
-            }
-          }
+          const f32x4 v = acc[i][j];
+          if constexpr (!WIDE) rows.put(i, j, make_uint2(encode(v[0]) | encode(v[1]) << 16, encode(v[2]) | encode(v[3]) << 16));
+          else if (t < T) *reinterpret_cast<f32x4 *>(E + (t * ld + m0 + 16 * i + 4 * q) * 4) = v;
         }
       }
       sum += __shfl_xor(sum, 16, 64);
       sum += __shfl_xor(sum, 32, 64);
       if (q == 0 && t < T) stat[t * granules + m0 / (FM * 16)] = make_float2(top, sum);
     }
+    if constexpr (STORE && !WIDE)
+      rows.flush([&](int row, int piece, uint4 v) {
+        if (n0 + row < T) *reinterpret_cast<uint4 *>(E + ((n0 + row) * ld + m0 + piece * 8) * 2) = v;
+      });
   }
 };
 
@@ -369,9 +399,24 @@ struct StoreEpilogue {
   const float *add;
   int64_t M, N, slab;     // elements of a split's slab
   template <int FM, int FN>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int split) const {
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int split, uint4 *lds) const {
     const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
     const float factor = *scale;
+    if (!out32 && !add) {
+      RowsOut<FM, FN> rows{lds};
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+          const f32x4 v = acc[i][j] * factor;
+          rows.put(i, j, make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])));
+        }
+      rows.flush([&](int row, int piece, uint4 v) {
+        const int64_t n = n0 + row, m = m0 + piece * 8;
+        if (n < N && m < M) *reinterpret_cast<uint4 *>(out16 + n * M + m) = v;
+      });
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int64_t n = n0 + 16 * j + r;
