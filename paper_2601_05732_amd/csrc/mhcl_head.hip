@@ -31,16 +31,14 @@ struct Operand {
   int64_t rows, depth;
 };
 
-// The pairs of parts whose products are added, small ones first, four bits for each: of three parts of 8 bits all but the
-// three products below 2^-23 of the whole.
-struct PartPairs {
-  uint32_t a, b;
-};
-constexpr PartPairs kOnePair{0, 0}, kSixPairs{0x010201, 0x001021};   // (1,1) (0,2) (2,0) (0,1) (1,0) (0,0) from the low end
+// The pairs of parts whose products are added, small ones first: of three parts of 8 bits all but the three products below 2^-23 of
+// the whole.  (1, 1) (0, 2) (2, 0) (0, 1) (1, 0) (0, 0), a hexadecimal digit each from the low end; and two more than the way from
+// each to the next.  (An array would be kept in memory.)
+constexpr uint32_t kPartsA = 0x010201, kPartsB = 0x001021, kWayA = 0x213041, kWayB = 0x221303;
+__device__ __forceinline__ int digit(uint32_t digits, int i) { return static_cast<int>(digits >> (4 * i) & 15); }
 
 struct GemmArgs {
   Operand A, B;
-  PartPairs pairs;
   int tiles_m, tiles_n, splits;
 };
 
@@ -58,14 +56,14 @@ struct TileLoader {
   static constexpr int kRows = KINNER ? NT / 8 : NT / (R / 8);   // rows of memory from one piece to the next
   static_assert(kRows % 16 == 0 || PER == 1, "the exchange of pieces is the same for all of a thread's");
   const char *base;         // of the tile and the next step
-  int64_t rest, step;       // bytes from there to the operand's (its part's) end; from one step to the next
-  int apart;                // bytes from one piece to the next (a tile's are less than 2^31: the host sees to it)
+  int64_t rest;             // bytes from there to the operand's (its part's) end
+  int step, apart;          // bytes from one step to the next; from one piece to the next (a tile's are less than 2^31: the host sees to it)
   uint32_t at, from;        // bytes from `base` to the thread's first piece; the same, or out of range, for this step
   int depth;                // KINNER: k of the thread's pieces within the tile
   __device__ __forceinline__ void init(const Operand &o, int64_t row0) {
     const int tid = threadIdx.x;
     const int64_t skip = row0 * (KINNER ? o.ld : 1) * 2;
-    step = (KINNER ? kBK : kBK * o.ld) * 2;
+    step = static_cast<int>((KINNER ? kBK : kBK * o.ld) * 2);
     apart = static_cast<int>(kRows * o.ld * 2);
     base = reinterpret_cast<const char *>(o.p) + skip;
     rest = (KINNER ? o.rows : o.depth) * o.ld * 2 - skip;
@@ -124,7 +122,8 @@ __device__ __forceinline__ int formed_here(int at) {
 }
 template <int LOADS>
 __device__ __forceinline__ void wait_all_but() {   // the last LOADS (< 16) loads
-  __builtin_amdgcn_s_waitcnt(0x0070 | LOADS);
+  static_assert(LOADS < 64, "what the counter holds");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (LOADS & 15) | (LOADS >> 4) << 14);
 }
 __device__ __forceinline__ void wait_all() { __builtin_amdgcn_s_waitcnt(0x0070); }   // vmcnt(0) lgkmcnt(0)
 __device__ __forceinline__ void barrier() {
@@ -133,10 +132,11 @@ __device__ __forceinline__ void barrier() {
   asm volatile("" ::: "memory");
 }
 
-// Tile (tm, tn, split) of this block: blocks of one XCD (every eighth) take neighbouring tiles, in strips of eight tiles of m
-__device__ __forceinline__ void tile_of(const GemmArgs &g, int &tm, int &tn, int &split) {
+// The b-th tile (tm, tn, split), b being a block's number and then every gridDim.x-th: blocks of one XCD (every eighth) take
+// neighbouring tiles, in strips of eight tiles of m
+__device__ __forceinline__ void tile_of(const GemmArgs &g, int b, int &tm, int &tn, int &split) {
   const int total = g.tiles_m * g.tiles_n * g.splits;
-  const int b = blockIdx.x, each = total / 8, more = total % 8, xcd = b % 8;
+  const int each = total / 8, more = total % 8, xcd = b % 8;
   int i = xcd * each + min(xcd, more) + b / 8;
   const int per = g.tiles_m * g.tiles_n;
   split = i / per;
@@ -148,35 +148,36 @@ __device__ __forceinline__ void tile_of(const GemmArgs &g, int &tm, int &tn, int
   tn = i / width;
 }
 
-// A block of WM x WN waves computes a BM x BN tile; wave (wm, wn) rows wm BM / WM of it and columns wn BN / WN on.
+// A block of WM x WN waves computes BM x BN tiles; wave (wm, wn) rows wm BM / WM of one and columns wn BN / WN on.
 // The epilogue gets acc[fm][fn]: lane (r, q) holds m = 16 fm + 4 q + 0..3 of the wave's rows, n = 16 fn + r of its columns.
+// The next tile's first loads are on their way during the epilogue, and the epilogue's stores during the next tile's first step.
 template <int BM, int BN, int WM, int WN, bool AK, bool BK, int PAIRS, typename Epilogue>
 __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, const Epilogue epilogue) {
   constexpr int NT = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
   __shared__ uint4 a0[BM * 8], a1[BM * 8], b0[BN * 8], b1[BN * 8];
-  int tm, tn, split;
-  tile_of(g, tm, tn, split);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
   const int64_t depth = g.A.depth < g.B.depth ? g.B.depth : g.A.depth;
   const int steps = static_cast<int>((depth + kBK - 1) / kBK);
-  const int64_t total = static_cast<int64_t>(steps) * PAIRS;
-  const int64_t first = total * split / g.splits, last = total * (split + 1) / g.splits;
+  const int tiles = g.tiles_m * g.tiles_n * g.splits;
+  int tile = blockIdx.x, tm, tn, split;
   TileLoader<BM, NT, AK> la;
   TileLoader<BN, NT, BK> lb;
-  la.init(g.A, static_cast<int64_t>(tm) * BM);
-  lb.init(g.B, static_cast<int64_t>(tn) * BN);
-  int pair = static_cast<int>(first / steps), at = static_cast<int>(first % steps);   // of the next load
-  const auto part_of = [](uint32_t parts, int i) { return static_cast<int>(parts >> (4 * i) & 15); };
-  la.skip(part_of(g.pairs.a, pair) * g.A.part * 2 + at * la.step);
-  lb.skip(part_of(g.pairs.b, pair) * g.B.part * 2 + at * lb.step);
-  la.rest += part_of(g.pairs.a, pair) * g.A.part * 2;
-  lb.rest += part_of(g.pairs.b, pair) * g.B.part * 2;
+  int pair, at, to_load, to_do;   // of the next load; steps to load, and to multiply
+  const auto begin = [&]() __attribute__((always_inline)) {
+    tile_of(g, tile, tm, tn, split);
+    const int64_t total = static_cast<int64_t>(steps) * PAIRS;
+    const int64_t first = total * split / g.splits, last = total * (split + 1) / g.splits;
+    to_load = to_do = static_cast<int>(last - first);
+    la.init(g.A, static_cast<int64_t>(tm) * BM);
+    lb.init(g.B, static_cast<int64_t>(tn) * BN);
+    pair = static_cast<int>(first / steps), at = static_cast<int>(first % steps);
+    const int64_t from_a = digit(PAIRS > 1 ? kPartsA : 0, pair) * g.A.part * 2, from_b = digit(PAIRS > 1 ? kPartsB : 0, pair) * g.B.part * 2;
+    la.skip(from_a + static_cast<int64_t>(at) * la.step);
+    lb.skip(from_b + static_cast<int64_t>(at) * lb.step);
+    la.rest += from_a;
+    lb.rest += from_b;
+  };
   f32x4 acc[FM][FN];
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int to_load = static_cast<int>(last - first);
   const auto aim = [&]() __attribute__((always_inline)) {
     const int done = to_load-- > 0 ? at * kBK : 0x7fffffff;   // past the last step: zeros
     la.aim(static_cast<int>(g.A.depth) - done);
@@ -188,15 +189,14 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, con
     la.skip(la.step);
     lb.skip(lb.step);
     if constexpr (PAIRS > 1) {
-      const int over = at == steps ? -1 : 0;
-      const int64_t a = (part_of(g.pairs.a, pair - over) - part_of(g.pairs.a, pair)) * g.A.part * 2;
-      const int64_t b = (part_of(g.pairs.b, pair - over) - part_of(g.pairs.b, pair)) * g.B.part * 2;
-      la.skip(a - (steps & over) * la.step);
-      lb.skip(b - (steps & over) * lb.step);
-      la.rest += a;
-      lb.rest += b;
-      pair -= over;
-      at &= ~over;
+      const int64_t over = at == steps ? -1 : 0;
+      const int64_t span_a = static_cast<int64_t>(steps) * la.step, span_b = static_cast<int64_t>(steps) * lb.step;
+      la.base += over & ((digit(kWayA, pair) - 2) * g.A.part * 2 - span_a);
+      lb.base += over & ((digit(kWayB, pair) - 2) * g.B.part * 2 - span_b);
+      la.rest += over & span_a;
+      lb.rest += over & span_b;
+      pair -= static_cast<int>(over);
+      at &= static_cast<int>(~over);
     }
   };
   // A step is four groups of products, (k half s, half hm of the rows), whose fragments are read one group ahead.  Once the last
@@ -261,66 +261,67 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, con
     for (int p = 0; p < lb.PER; ++p) lb.piece(b, wave, p);
     next();
   };
+  begin();
   load(a0, b0);
   load(a1, b1);
-  wait_all_but<la.PER + lb.PER>();
-  barrier();
-  read_a(a0, 0, 0);
-  read_b(b0, 0);
-  // (steps in pairs, so that a stage's place is known where it is read; after an odd last one a step of zeros)
-  for (int64_t left = last - first; left > 0; left -= 2) {
-    step(a0, b0, a1, b1);
-    step(a1, b1, a0, b0);
+  bool stored = false;            // whether every wave's stores of the last epilogue were what stores<>() says at least
+  for (;;) {
+    if (stored) wait_all_but<la.PER + lb.PER + Epilogue::template stores<FM, FN>()>();
+    else wait_all();
+    barrier();
+    read_a(a0, 0, 0);
+    read_b(b0, 0);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // (steps in pairs, so that a stage's place is known where it is read; after an odd last one a step of zeros)
+    for (int left = to_do; left > 0; left -= 2) {
+      step(a0, b0, a1, b1);
+      step(a1, b1, a0, b0);
+    }
+    const int64_t m0 = static_cast<int64_t>(tm) * BM + wm * (FM * 16), n0 = static_cast<int64_t>(tn) * BN + wn * (FN * 16);
+    const int this_split = split;
+    const auto held = epilogue.template hold<FN>(n0);
+    // the stages are free once the last loads (of zeros) have arrived and every wave has read its fragments
+    wait_all();
+    barrier();
+    stored = epilogue.whole(static_cast<int64_t>(tm + 1) * BM, static_cast<int64_t>(tn + 1) * BN);
+    tile += gridDim.x;
+    const bool more = tile < tiles;
+    if (more) {
+      begin();
+      load(a0, b0);
+      load(a1, b1);
+    }
+    epilogue.template operator()<FM, FN>(acc, held, m0, n0, this_split);
+    if (!more) break;
   }
-  // the stages are free for the epilogue once the last loads (of zeros) have arrived and every wave has read its fragments
-  wait_all();
-  barrier();
-  constexpr int NW = WM * WN, EACH = NW > 4 ? NW / 4 : 1;
-  static_assert(FM * FN * 256 * 2 * EACH <= (BN < BM ? BN : BM) * 128, "a wave's 16-bit results fit its part of the stages");
-  const int which = wave / EACH % 4;
-  uint4 *const scratch = which == 0 ? a0 : (which == 1 ? a1 : (which == 2 ? b0 : b1));
-  epilogue.template operator()<FM, FN>(acc, static_cast<int64_t>(tm) * BM + wm * (FM * 16), static_cast<int64_t>(tn) * BN + wn * (FN * 16),
-                                       split, scratch + wave % EACH * (FM * FN * 32));
 }
 
-// A wave's results, four 16-bit numbers in each of its lanes' places (16 i + 4 q .. + 3 of row 16 j + r), go to memory by way
-// of LDS: from the registers a store would write 32 bytes of each of 16 rows, so it writes whole rows of the wave's (256 bytes and
-// fewer, no faster one by one: 16384 tokens, 65536 rows, 64 deep: 1056 us from the registers, LDSUS this way).
-template <int FM, int FN>
-struct RowsOut {
-  static constexpr int CPR = FM * 2;          // 16-byte pieces of a row
-  uint4 *lds;
-  __device__ __forceinline__ void put(int i, int j, uint2 v) {
-    const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-    const int piece = (2 * i + (q >> 1)) ^ (r & (CPR - 1));
-    *reinterpret_cast<uint2 *>(reinterpret_cast<char *>(lds + (16 * j + r) * CPR + piece) + (q & 1) * 8) = v;
-  }
-  // out(row, piece, value): row of the wave's, 16-byte piece of it
-  template <typename F>
-  __device__ __forceinline__ void flush(F out) {
-    const int lane = threadIdx.x & 63;
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int k = 0; k < FN * 16 * CPR / 64; ++k) {
-      const int row = (k * 64 + lane) / CPR, piece = lane % CPR;
-      out(row, piece, lds[row * CPR + (piece ^ (row & 15 & (CPR - 1)))]);
-    }
-  }
-};
+// Four 16-bit results of a lane (r, q) at 16 i + 4 q and as many at 16 (i + 1) + 4 q become eight, for one 16-byte store, at 16 (i + q % 2) +
+// 8 (q / 2): the lanes of odd q exchange the former for the latter of the lanes sixteen before.  (A store of 8 bytes writes 32 bytes
+// of each of 16 rows: 16384 tokens, 65536 rows, 64 deep, us: 8 bytes 1166, whole rows by way of LDS 1064.)
+__device__ __forceinline__ uint4 join_pairs(uint2 lower, uint2 upper) {
+  const auto x = __builtin_amdgcn_permlane16_swap(lower.x, upper.x, false, false);
+  const auto y = __builtin_amdgcn_permlane16_swap(lower.y, upper.y, false, false);
+  return make_uint4(x[0], y[0], x[1], y[1]);
+}
 
 // ---- epilogues
-// e in [0, 1] as 16 bits: 6 of the exponent, 10 of the mantissa (2^-63 .. 1 to 2^-11 of itself, less is 0)
-constexpr uint32_t kCodeBase = 64u << 23;
-__device__ __forceinline__ uint32_t encode(float e) {
-  return static_cast<uint32_t>(max(0, static_cast<int32_t>(__float_as_uint(e) + 0x1000u - kCodeBase))) >> 13;
+// A number e in [0, 1] as 16 bits: 6 of the exponent, 10 of the mantissa (2^-61 .. 1 to 2^-11 of itself, what is less may be 0).  These are
+// bits 28 .. 13 of e 2^-64, which an exponential gives at once.
+constexpr float kCodeExp = -64.f, kCodeScale = 0x1p64f;
+__device__ __forceinline__ uint32_t encode2(float lo, float hi) {   // of two e 2^-64
+  return (__float_as_uint(lo) + 0x1000u) >> 13 | ((__float_as_uint(hi) + 0x1000u) << 3 & 0xffff0000u);
 }
-__device__ __forceinline__ float decode(uint32_t code) { return code ? __uint_as_float((code << 13) + kCodeBase) : 0.f; }
+__device__ __forceinline__ float decode(uint32_t code) { return code ? __uint_as_float((code << 13) + (64u << 23)) : 0.f; }
 
-// exp(x), x <= 0: the instruction for bf16 operands (relative error 2^-23 |x|), the library's for fp32 ones
+// exp(x), x <= 0: the library's for fp32 operands; for bf16 ones 2^-64 exp(x) by the instruction (relative error 2^-23 |x|)
 template <bool WIDE>
 __device__ __forceinline__ float exp_of(float x) {
   if constexpr (WIDE) return expf(x);
-  return __builtin_amdgcn_exp2f(x * kLog2e);
+  return __builtin_amdgcn_exp2f(fmaf(x, kLog2e, kCodeExp));
 }
 
 // m: vocabulary, n: tokens.  STORE: the numerators too.  WIDE: fp32 numerators.
@@ -332,10 +333,28 @@ struct LogitsEpilogue {
   float *zt;
   char *E;
   int64_t T, V, ld, granules;
+  // what the epilogue reads, read ahead of it
+  template <int FN>
+  struct Targets {
+    int64_t y[FN];
+  };
+  template <int FN>
+  __device__ __forceinline__ Targets<FN> hold(int64_t n0) const {
+    Targets<FN> h;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const int64_t t = n0 + 16 * j + (threadIdx.x & 15);
+      h.y[j] = t < T ? static_cast<int64_t>(targets[t]) : -1;
+    }
+    return h;
+  }
+  // stores of a wave where all of a tile's tokens are there
   template <int FM, int FN>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int, uint4 *lds) const {
+  static constexpr int stores() { return FN * (1 + (!STORE ? 0 : (WIDE ? FM : FM / 2))); }
+  __device__ __forceinline__ bool whole(int64_t, int64_t n_end) const { return n_end <= T; }
+  template <int FM, int FN>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], const Targets<FN> &held, int64_t m0, int64_t n0, int) const {
     const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-    RowsOut<FM, FN> rows{lds};
     if (m0 + FM * 16 > V) {   // rows beyond the vocabulary
 #pragma unroll
       for (int i = 0; i < FM; ++i)
@@ -356,7 +375,7 @@ struct LogitsEpilogue {
         for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[i][j][e]);
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const int64_t y = t < T ? static_cast<int64_t>(targets[t]) - m0 - 4 * q : -1;
+      const int64_t y = held.y[j] - m0 - 4 * q;
       if (__ballot(y >= 0 && y < FM * 16) != 0) {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
@@ -373,20 +392,22 @@ struct LogitsEpilogue {
           acc[i][j][e] = exp_of<WIDE>(acc[i][j][e] - base);
           sum += acc[i][j][e];
         }
-        if constexpr (STORE) {
-          const f32x4 v = acc[i][j];
-          if constexpr (!WIDE) rows.put(i, j, make_uint2(encode(v[0]) | encode(v[1]) << 16, encode(v[2]) | encode(v[3]) << 16));
-          else if (t < T) *reinterpret_cast<f32x4 *>(E + (t * ld + m0 + 16 * i + 4 * q) * 4) = v;
+        if constexpr (STORE && WIDE) {
+          if (t < T) *reinterpret_cast<f32x4 *>(E + (t * ld + m0 + 16 * i + 4 * q) * 4) = acc[i][j];
+        } else if constexpr (STORE) {
+          if (i % 2 == 1) {
+            const f32x4 u = acc[i - 1][j], v = acc[i][j];
+            const uint4 eight = join_pairs(make_uint2(encode2(u[0], u[1]), encode2(u[2], u[3])),
+                                           make_uint2(encode2(v[0], v[1]), encode2(v[2], v[3])));
+            if (t < T) *reinterpret_cast<uint4 *>(E + (t * ld + m0 + 16 * (i - 1 + (q & 1)) + 8 * (q >> 1)) * 2) = eight;
+          }
         }
       }
       sum += __shfl_xor(sum, 16, 64);
       sum += __shfl_xor(sum, 32, 64);
+      if constexpr (!WIDE) sum *= kCodeScale;
       if (q == 0 && t < T) stat[t * granules + m0 / (FM * 16)] = make_float2(top, sum);
     }
-    if constexpr (STORE && !WIDE)
-      rows.flush([&](int row, int piece, uint4 v) {
-        if (n0 + row < T) *reinterpret_cast<uint4 *>(E + ((n0 + row) * ld + m0 + piece * 8) * 2) = v;
-      });
   }
 };
 
@@ -398,38 +419,34 @@ struct StoreEpilogue {
   uint16_t *out16;
   const float *add;
   int64_t M, N, slab;     // elements of a split's slab
+  template <int FN>
+  __device__ __forceinline__ float hold(int64_t) const { return *scale; }
   template <int FM, int FN>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], int64_t m0, int64_t n0, int split, uint4 *lds) const {
+  static constexpr int stores() { return FN * FM / 2; }   // (in fp32 twice as many)
+  __device__ __forceinline__ bool whole(int64_t m_end, int64_t n_end) const { return m_end <= M && n_end <= N; }
+  template <int FM, int FN>
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], float factor, int64_t m0, int64_t n0, int split) const {
     const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-    const float factor = *scale;
-    if (!out32 && !add) {
-      RowsOut<FM, FN> rows{lds};
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          const f32x4 v = acc[i][j] * factor;
-          rows.put(i, j, make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])));
-        }
-      rows.flush([&](int row, int piece, uint4 v) {
-        const int64_t n = n0 + row, m = m0 + piece * 8;
-        if (n < N && m < M) *reinterpret_cast<uint4 *>(out16 + n * M + m) = v;
-      });
-      return;
-    }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int64_t n = n0 + 16 * j + r;
-      if (n >= N) continue;
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const int64_t m = m0 + 16 * i + 4 * q;
-        if (m >= M) continue;       // (M is a multiple of 8)
-        const int64_t elem = n * M + m;
-        f32x4 v = acc[i][j] * factor;
-        if (add) v += *reinterpret_cast<const f32x4 *>(add + elem);
-        if (out32) *reinterpret_cast<f32x4 *>(out32 + split * slab + elem) = v;
-        else *reinterpret_cast<uint2 *>(out16 + elem) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      for (int i = 0; i < FM; i += 2) {
+        uint2 part[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int64_t m = m0 + 16 * (i + k) + 4 * q, elem = n * M + m;      // (M is a multiple of 8)
+          const bool there = n < N && m < M;
+          f32x4 v = acc[i + k][j] * factor;
+          if (add && there) v += *reinterpret_cast<const f32x4 *>(add + elem);
+          if (out32 && there) *reinterpret_cast<f32x4 *>(out32 + split * slab + elem) = v;
+          part[k] = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        }
+        if (!out32) {
+          const uint4 eight = join_pairs(part[0], part[1]);
+          const int64_t m = m0 + 16 * (i + (q & 1)) + 8 * (q >> 1);
+          if (n < N && m < M) *reinterpret_cast<uint4 *>(out16 + n * M + m) = eight;
+        }
       }
     }
   }
@@ -628,6 +645,8 @@ __global__ __launch_bounds__(kBlock) void slab_sum_kernel(const float *__restric
   else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + i) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
 }
 
+constexpr int64_t kChipBlocks = 256;
+
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 unsigned blocks(int64_t items, int64_t each) { return static_cast<unsigned>(ceil_div(items, each)); }
 
@@ -642,15 +661,18 @@ hipError_t launch_gemm(const HeadTile &tile, Operand A, Operand B, int64_t M, in
   GemmArgs g;
   g.A = A;
   g.B = B;
-  g.pairs = parts == 1 ? kOnePair : kSixPairs;
   g.tiles_m = static_cast<int>(ceil_div(M, tile.bm));
   g.tiles_n = static_cast<int>(ceil_div(N, tile.bn));
   g.splits = splits;
-  const dim3 grid(static_cast<unsigned>(g.tiles_m * g.tiles_n * splits));
+  // as many blocks as the chip holds (of the smallest tile, which waits for memory, one for every tile)
+  const unsigned tiles = static_cast<unsigned>(g.tiles_m * g.tiles_n * splits), most = tile.bm == 256 ? kChipBlocks : 2 * kChipBlocks;
+  const dim3 grid(tile.bn < 128 || tiles < most ? tiles : most);
   const auto go = [&](auto pairs) {
     constexpr int P = decltype(pairs)::value;
-    if (tile.bm == 256) hipLaunchKernelGGL((gemm_kernel<256, 256, 2, 4, AK, BK, P, Epilogue>), grid, dim3(512), 0, s, g, e);
-    else if (tile.bn == 128) hipLaunchKernelGGL((gemm_kernel<128, 128, 2, 2, AK, BK, P, Epilogue>), grid, dim3(256), 0, s, g, e);
+    if (tile.bm == 256) {
+      if constexpr (P == 1 || (AK && BK)) hipLaunchKernelGGL((gemm_kernel<256, 256, 2, 4, AK, BK, P, Epilogue>), grid, dim3(512), 0, s, g, e);
+      else return hipErrorInvalidValue;
+    } else if (tile.bn == 128) hipLaunchKernelGGL((gemm_kernel<128, 128, 2, 2, AK, BK, P, Epilogue>), grid, dim3(256), 0, s, g, e);
     else if constexpr (BK) hipLaunchKernelGGL((gemm_kernel<128, 32, 4, 1, AK, BK, P, Epilogue>), grid, dim3(256), 0, s, g, e);
     else return hipErrorInvalidValue;
     return hipGetLastError();
@@ -660,12 +682,11 @@ hipError_t launch_gemm(const HeadTile &tile, Operand A, Operand B, int64_t M, in
   else return parts == 1 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 6>{});
 }
 
-constexpr int64_t kChipBlocks = 256;
-
-// the largest tile of which there are enough for the chip
-HeadTile tile_for(int64_t M, int64_t N, bool slim) {
+// the largest tile of which there are enough for the chip.  (For the gradients' products of fp32 operands the middle one: the largest
+// one's registers do not hold what the six products of parts need besides.  us, 2048 tokens, C = 768, 50257 rows, g_W, largest / middle: 1257 / 1155.)
+HeadTile tile_for(int64_t M, int64_t N, bool slim, bool big) {
   if (slim && N <= 64) return kTileSlim;
-  return ceil_div(M, 256) * ceil_div(N, 256) >= kChipBlocks ? kTileBig : kTileMid;
+  return big && ceil_div(M, 256) * ceil_div(N, 256) >= kChipBlocks ? kTileBig : kTileMid;
 }
 
 }  // namespace
@@ -679,9 +700,9 @@ HeadPlan::HeadPlan(const mhcl_ends_desc &d, bool grad) {
   const int64_t fit = static_cast<int64_t>(MHCL_HEAD_BLOCK_BYTES) / row_bytes / 256 * 256;
   if (tokens > fit) tokens = fit < 256 ? 256 : fit;
   if (tokens > d.T) tokens = d.T;
-  logits = tile_for(d.V, tokens, true);
-  gh = tile_for(d.C, tokens, true);
-  gw = tile_for(d.C, d.V, false);
+  logits = tile_for(d.V, tokens, true, true);
+  gh = tile_for(d.C, tokens, true, parts == 1);
+  gw = tile_for(d.C, d.V, false, parts == 1);
   ld = ceil_div(d.V, logits.bm) * logits.bm;   // (what the first product's tiles cover)
   granules = ld / logits.gran;
   gh_splits = 1;
