@@ -29,7 +29,7 @@ _SYMBOLS = [
     "mhcl_logits", "mhcl_ds_chain", "mhcl_profile_next_call", "mhcl_debug_copy",
     "mhcl_fwd_coeffs_pre_static", "mhcl_coeffs_logits", "mhcl_coeffs_logits_layers", "mhcl_streams_in", "mhcl_streams_out",
     "mhcl_ends_workspace_bytes", "mhcl_embed", "mhcl_embed_bwd", "mhcl_streams_norm", "mhcl_streams_norm_bwd",
-    "mhcl_head_loss", "mhcl_head_loss_grad",
+    "mhcl_head_loss", "mhcl_head_loss_grad", "mhcl_head_total", "mhcl_scale",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20   # MHCL_STATIC_SCRATCH_BYTES
 
@@ -152,6 +152,8 @@ def lib():
         L.mhcl_streams_norm_bwd.argtypes = [E] + [V] * 6 + [Z, V]
         L.mhcl_head_loss.argtypes = [E] + [V] * 6 + [Z, V]
         L.mhcl_head_loss_grad.argtypes = [E] + [V] * 9 + [Z, V]
+        L.mhcl_head_total.argtypes = [E] + [V] * 5
+        L.mhcl_scale.argtypes = [V, ctypes.c_int, ctypes.c_int64, V, V]
         _lib = L
     return _lib
 
@@ -421,3 +423,18 @@ def mhcl_head_loss_grad(d, h, W, targets, weight, loss, lse, g_h, g_W, ws):
         _ptr(targets, d.ids, (d.T,), "targets"), None if weight is None else _ptr(weight, f, (d.T,), "weight"),
         _ptr(loss, f, (d.T,), "loss"), _ptr(lse, f, (d.T,), "lse"), _ptr(g_h, d.io, (d.T, d.C), "g_h"),
         _ptr(g_W, d.w, (d.V, d.C), "g_W"), wp, wb, _stream()), "mhcl_head_loss_grad")
+
+
+def mhcl_head_total(d, targets, loss, weight, total):
+    f = torch.float32
+    _check(lib().mhcl_head_total(
+        ctypes.byref(d.c), _ptr(targets, d.ids, (d.T,), "targets"), _ptr(loss, f, (d.T,), "loss"),
+        None if weight is None else _ptr(weight, f, (d.T,), "weight"), _ptr(total, f, (1,), "total"), _stream()), "mhcl_head_total")
+
+
+def mhcl_scale(t, factor):
+    """t *= factor, a GPU tensor of one fp32 number."""
+    if t.dtype not in _DTYPE:
+        raise ValueError(f"dtype {t.dtype}: bfloat16 or float32")
+    _check(lib().mhcl_scale(_ptr(t, t.dtype, t.shape, "t"), _DTYPE[t.dtype], t.numel(),
+                            _ptr(factor.reshape(1), torch.float32, (1,), "factor"), _stream()), "mhcl_scale")

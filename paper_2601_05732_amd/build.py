@@ -1,5 +1,5 @@
-"""Builds libmhcl.so (HIP, gfx950 only) next to this file with hipcc, the graph nodes of autograd.py
-(torch_ext/autograd.cpp -> _autograd_native.so), and the stand-alone
+"""Builds libmhcl.so (HIP, gfx950 only) next to this file with hipcc, the graph nodes of autograd.py and the quick calls of
+ends.py (torch_ext/ -> _autograd_native.so), and the stand-alone
 memory-system probe (probe/memsys_probe.hip -> memsys_probe) that `bench.py --memsys` runs."""
 from __future__ import annotations
 
@@ -16,7 +16,7 @@ OBJ_DIR = os.path.join(_HERE, "_build")
 PROBE_SRC = os.path.join(_HERE, "probe", "memsys_probe.hip")
 PROBE = os.path.join(_HERE, "memsys_probe")
 
-AUTOGRAD_SRC = os.path.join(_HERE, "torch_ext", "autograd.cpp")
+EXT_SRC = [os.path.join(_HERE, "torch_ext", f) for f in ("autograd.cpp", "ends.cpp")]
 AUTOGRAD = os.path.join(_HERE, "_autograd_native.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -63,22 +63,33 @@ def build_library(verbose: bool = False) -> str:
 
 
 def build_autograd(verbose: bool = False) -> str:
-    """The graph nodes of autograd.py as a Python extension (host code; linked with libmhcl.so and torch)."""
+    """The graph nodes of autograd.py and the quick calls of ends.py as a Python extension (host code; linked with
+    libmhcl.so and torch)."""
     from torch.utils.cpp_extension import include_paths
     import torch
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     name = os.path.basename(AUTOGRAD).split(".")[0]
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", f"-DTORCH_EXTENSION_NAME={name}",
-           "-DTORCH_API_INCLUDE_EXTENSION_H", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           *[f"-I{p}" for p in include_paths()], "-I/opt/rocm/include",
-           f"-I{sysconfig.get_paths()['include']}", AUTOGRAD_SRC, "-o", AUTOGRAD, f"-L{lib}", "-ltorch_python", "-ltorch",
-           "-ltorch_cpu", "-lc10", "-lc10_hip", f"-L{_HERE}", "-lmhcl", "-Wl,-rpath,$ORIGIN"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"g++ failed on {AUTOGRAD_SRC}:\n{r.stderr}")
+    flags = ["-O2", "-std=c++17", "-fPIC", "-w", f"-DTORCH_EXTENSION_NAME={name}",
+             "-DTORCH_API_INCLUDE_EXTENSION_H", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+             *[f"-I{p}" for p in include_paths()], "-I/opt/rocm/include",
+             f"-I{sysconfig.get_paths()['include']}"]
+    objs = [os.path.join(OBJ_DIR, os.path.basename(s) + ".o") for s in EXT_SRC]
+    os.makedirs(OBJ_DIR, exist_ok=True)
+    cmds = [["g++", *flags, "-c", src, "-o", obj] for src, obj in zip(EXT_SRC, objs)]
+    link = ["g++", "-shared", *objs, "-o", AUTOGRAD, f"-L{lib}", "-ltorch_python", "-ltorch",
+            "-ltorch_cpu", "-lc10", "-lc10_hip", f"-L{_HERE}", "-lmhcl", "-Wl,-rpath,$ORIGIN"]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        return cmd, subprocess.run(cmd, capture_output=True, text=True)
+
+    with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
+        done = list(ex.map(run, cmds))
+    for cmd, r in done + ([run(link)] if all(r.returncode == 0 for _, r in done) else []):
+        if r.returncode != 0:
+            raise RuntimeError(f"{' '.join(cmd)} failed:\n{r.stderr}")
     return AUTOGRAD
 
 

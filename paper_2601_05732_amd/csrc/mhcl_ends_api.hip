@@ -133,4 +133,26 @@ int mhcl_head_loss_grad(const mhcl_ends_desc *desc, const void *h, const void *W
   return MHCL_OK;
 }
 
+int mhcl_head_total(const mhcl_ends_desc *desc, const void *targets, const float *loss, const float *weight, float *total,
+                    void *stream) {
+  if (int e = check_ends(desc, End::kHead)) return e;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!aligned(total, 4)) return MHCL_ERR_INVALID_ARG;
+  if (desc->T == 0) {
+    MHCL_HIP(launch_zero(total, 4, s));
+    return MHCL_OK;
+  }
+  if (!ids_ok(*desc, targets) || !aligned(loss, 4) || (weight && !aligned(weight, 4))) return MHCL_ERR_INVALID_ARG;
+  MHCL_HIP(launch_head_total(*desc, targets, loss, weight, total, s));
+  return MHCL_OK;
+}
+
+int mhcl_scale(void *p, int dtype, int64_t count, const float *factor, void *stream) {
+  if (!dtype_ok(dtype) || count < 0 || !aligned(factor, 4)) return MHCL_ERR_INVALID_ARG;
+  if (count == 0) return MHCL_OK;
+  if (!all16(p)) return MHCL_ERR_INVALID_ARG;
+  MHCL_HIP(launch_scale(p, dtype, count, factor, static_cast<hipStream_t>(stream)));
+  return MHCL_OK;
+}
+
 }  // extern "C"

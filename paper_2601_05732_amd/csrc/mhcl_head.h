@@ -40,4 +40,8 @@ struct HeadWs {
 hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, const void *targets, const float *weight,
                        float *loss, float *lse, void *g_h, void *g_W, const HeadWs &w, hipStream_t s);
 
+hipError_t launch_head_total(const mhcl_ends_desc &d, const void *targets, const float *loss, const float *weight, float *total,
+                             hipStream_t s);
+hipError_t launch_scale(void *p, int dtype, int64_t count, const float *factor, hipStream_t s);
+
 }  // namespace mhcl

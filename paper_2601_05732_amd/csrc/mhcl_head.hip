@@ -614,6 +614,62 @@ __global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *
   }
 }
 
+// sum of weight loss over the targets that are not negative, weights of 0 left out, or their mean; one block, in fp64
+template <typename ID>
+__global__ __launch_bounds__(1024) void total_kernel(const ID *__restrict__ targets, const float *__restrict__ loss,
+                                                     const float *__restrict__ weight, int64_t T, float *__restrict__ total) {
+  __shared__ double red[2][16];
+  double sum = 0., count = 0.;
+  for (int64_t t = threadIdx.x; t < T; t += 1024) {
+    const float w = targets[t] < 0 ? 0.f : (weight ? weight[t] : 1.f);
+    if (w != 0.f) sum += static_cast<double>(w) * loss[t];
+    count += w != 0.f ? 1. : 0.;
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    sum += __shfl_xor(sum, off, 64);
+    count += __shfl_xor(count, off, 64);
+  }
+  if ((threadIdx.x & 63) == 0) {
+    red[0][threadIdx.x >> 6] = sum;
+    red[1][threadIdx.x >> 6] = count;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) {
+      sum += red[0][i];
+      count += red[1][i];
+    }
+    *total = static_cast<float>(weight ? sum : (count > 0. ? sum / count : 0.));
+  }
+}
+
+template <typename IO>
+__global__ __launch_bounds__(kBlock) void scale_kernel(void *__restrict__ p, int64_t count, const float *__restrict__ factor) {
+  const float f = *factor;
+  if (f == 1.f) return;
+  constexpr int VEC = IO::kVec;
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * kBlock * VEC;
+  for (int64_t i = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * VEC; i < count; i += stride) {
+    if (i + VEC <= count) {
+      float v[VEC];
+      IO::load(p, i, v);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[e] *= f;
+      IO::store(p, i, v);
+    } else {
+      for (int64_t e = i; e < count; ++e) {
+        if constexpr (VEC == 8) {
+          uint16_t *q = static_cast<uint16_t *>(p);
+          q[e] = f32_to_bf16(bf16_to_f32(q[e]) * f);
+        } else {
+          static_cast<float *>(p)[e] *= f;
+        }
+      }
+    }
+  }
+}
+
 // fp32 as three bf16 parts, each the rounded rest: `count` elements (a multiple of 8), parts `part` elements apart
 __global__ __launch_bounds__(kBlock) void split_kernel(const float *__restrict__ in, uint16_t *__restrict__ out, int64_t count, int64_t part) {
   const int64_t i = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 8;
@@ -798,6 +854,24 @@ hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, co
       }
     }
     return hipSuccess;
+  });
+}
+
+hipError_t launch_head_total(const mhcl_ends_desc &d, const void *targets, const float *loss, const float *weight, float *total,
+                             hipStream_t s) {
+  return dispatch_id(d.id_dtype, [&](auto id) {
+    using ID = decltype(id);
+    hipLaunchKernelGGL((total_kernel<ID>), dim3(1), dim3(1024), 0, s, static_cast<const ID *>(targets), loss, weight, d.T, total);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_scale(void *p, int dtype, int64_t count, const float *factor, hipStream_t s) {
+  return dispatch_io(dtype, [&](auto io) {
+    using IO = decltype(io);
+    const int64_t want = ceil_div(count, kBlock * IO::kVec);
+    hipLaunchKernelGGL((scale_kernel<IO>), dim3(static_cast<unsigned>(want < 4096 ? want : 4096)), dim3(kBlock), 0, s, p, count, factor);
+    return hipGetLastError();
   });
 }
 

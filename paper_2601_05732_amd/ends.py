@@ -3,13 +3,17 @@ the streams' sum, and the head's softmax cross entropy, each with its gradients.
 
 The functions here allocate the results and make one call into ``libmhcl.so`` (``mhcl_embed`` and so on; include/mhcl.h has
 the formulas), which computes everything.  Tensors may be strided or at any address: what the library cannot read as it is
-gets copied first.
+gets copied first.  Calls with tensors that it can read go through the extension in C++ (``torch_ext/ends.cpp``: the same at less
+than half of the host time), where that is built.
+
+:class:`TokenEmbedding`, :class:`StreamsNorm` and :class:`Head` are the same under ``torch.autograd``.
 """
 from __future__ import annotations
 
 import torch
 
 from . import binding as mhcl
+from .autograd import _native
 from .layer import PHASE_G_X, PHASE_X, empty_stream
 
 
@@ -35,6 +39,9 @@ def _need(ok: bool, what: str):
 def embed_tokens(table: torch.Tensor, ids: torch.Tensor, n: int, scale: float = 1.0, dtype=None) -> torch.Tensor:
     """``x [T, n, C]`` with ``x[t, i] = scale * table[ids[t]]`` for every stream i, in `dtype` (default: the table's);
     zeros where ``ids[t]`` is negative, NaN where it is V or more.  table [V, C], ids [T] int64 or int32."""
+    native = _native()
+    if native is not None and (x := native.embed(table, ids, n, scale, dtype or table.dtype)) is not None:
+        return x
     _same_device(table, ids)
     _need(table.dim() == 2 and ids.dim() == 1, f"table [V, C] and ids [T], got {tuple(table.shape)} and {tuple(ids.shape)}")
     V, C = table.shape
@@ -48,6 +55,9 @@ def embed_tokens(table: torch.Tensor, ids: torch.Tensor, n: int, scale: float = 
 def embed_tokens_grad(ids: torch.Tensor, g_x: torch.Tensor, V: int, scale: float = 1.0, dtype=None, into=None) -> torch.Tensor:
     """The gradient [V, C] on `embed_tokens`' table, in `dtype` (default: that of g_x [T, n, C]).  into: a tensor [V, C] that
     it is added to (and that is returned) instead."""
+    native = _native()
+    if native is not None and (g := native.embed_grad(ids, g_x, V, scale, dtype or g_x.dtype, into)) is not None:
+        return g
     _same_device(ids, g_x, into)
     _need(g_x.dim() == 3 and ids.shape == g_x.shape[:1], f"ids [T] and g_x [T, n, C], got {tuple(ids.shape)} and {tuple(g_x.shape)}")
     T, n, C = g_x.shape
@@ -67,6 +77,9 @@ def _norm_desc(x, gain, eps):
 
 def streams_norm(x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6) -> torch.Tensor:
     """``h [T, C] = gain * s / sqrt(mean(s^2) + eps)`` of the sum s of the streams of x [T, n, C]; gain [C] fp32."""
+    native = _native()
+    if native is not None and (h := native.norm(x, gain, eps)) is not None:
+        return h
     _same_device(x, gain)
     d = _norm_desc(x, gain, eps)
     h = torch.empty(d.T, d.C, device=x.device, dtype=x.dtype)
@@ -76,6 +89,9 @@ def streams_norm(x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6) -> torc
 
 def streams_norm_grad(x: torch.Tensor, gain: torch.Tensor, g_h: torch.Tensor, eps: float = 1e-6):
     """``g_x [T, n, C], g_gain [C]`` of `streams_norm` for the gradient g_h [T, C] on its result."""
+    native = _native()
+    if native is not None and (g := native.norm_grad(x, gain, g_h, eps)) is not None:
+        return g
     _same_device(x, gain, g_h)
     d = _norm_desc(x, gain, eps)
     g_x = empty_stream(x.shape, x.dtype, x.device, PHASE_G_X)
@@ -94,6 +110,9 @@ def _head_desc(h, W, targets):
 def head_loss(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor):
     """``loss [T], lse [T]`` (fp32): the softmax cross entropy of the logits h W^T with the targets, 0 where a target is negative,
     and the logits' log-sum-exp.  h [T, C], W [V, C] of one type."""
+    native = _native()
+    if native is not None and (out := native.head(h, W, targets)) is not None:
+        return out
     _same_device(h, W, targets)
     d = _head_desc(h, W, targets)
     loss, lse = (torch.empty(d.T, device=h.device, dtype=torch.float32) for _ in range(2))
@@ -105,6 +124,9 @@ def head_loss(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor):
 def head_loss_grad(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, weight=None):
     """``loss [T], lse [T], g_h [T, C], g_W [V, C]``: `head_loss` and the gradients of ``sum(weight * loss)``; weight [T] fp32,
     or None for the mean over the targets that are not negative."""
+    native = _native()
+    if native is not None and (out := native.head_grad(h, W, targets, weight)) is not None:
+        return out
     _same_device(h, W, targets, weight)
     d = _head_desc(h, W, targets)
     loss, lse = (torch.empty(d.T, device=h.device, dtype=torch.float32) for _ in range(2))
@@ -113,3 +135,107 @@ def head_loss_grad(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, weig
     mhcl.mhcl_head_loss_grad(d, _dense(h), _dense(W), targets.contiguous(), None if weight is None else weight.contiguous(),
                              loss, lse, g_h, g_W, ws)
     return loss, lse, g_h, g_W
+
+
+# ---- under torch.autograd --------------------------------------------------------------------
+
+
+class _Embed(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, n, scale, dtype):
+        ctx.save_for_backward(ids)
+        ctx.V, ctx.scale, ctx.dtype = table.shape[0], scale, table.dtype
+        return embed_tokens(table, ids, n, scale, dtype)
+
+    @staticmethod
+    def backward(ctx, g_x):
+        ids, = ctx.saved_tensors
+        return embed_tokens_grad(ids, g_x, ctx.V, ctx.scale, ctx.dtype), None, None, None, None
+
+
+class _Norm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gain, eps):
+        ctx.save_for_backward(x, gain)
+        ctx.eps = eps
+        return streams_norm(x, gain, eps)
+
+    @staticmethod
+    def backward(ctx, g_h):
+        x, gain = ctx.saved_tensors
+        return *streams_norm_grad(x, gain, g_h, ctx.eps), None
+
+
+class _HeadTotal(torch.autograd.Function):
+    """The gradients are taken with the loss, for a gradient of 1 on it: the softmax's numerators, which both need, are formed
+    once.  The backward multiplies them by what it gets, unless that is 1 (the device looks)."""
+
+    @staticmethod
+    def forward(ctx, h, W, targets, weight):
+        loss, _, g_h, g_W = head_loss_grad(h, W, targets, weight)
+        ctx.grads = (g_h, g_W)
+        return _total(h, W, targets, loss, weight)
+
+    @staticmethod
+    def backward(ctx, g):
+        if ctx.grads is None:
+            raise RuntimeError("the head's gradients went out with its first backward: run the head again for another one")
+        g_h, g_W = ctx.grads
+        ctx.grads = None
+        for t, needed in zip((g_h, g_W), ctx.needs_input_grad):
+            if needed:
+                mhcl.mhcl_scale(t, g)
+        return g_h, g_W, None, None
+
+
+def _total(h, W, targets, loss, weight):
+    d = _head_desc(h, W, targets)
+    total = torch.empty(1, device=h.device, dtype=torch.float32)
+    mhcl.mhcl_head_total(d, targets.contiguous(), loss, None if weight is None else weight.contiguous(), total)
+    return total[0]
+
+
+class TokenEmbedding(torch.nn.Module):
+    """Token ids [T] to the streams x [T, n, C] of the first layer; negative ids hold no token."""
+
+    def __init__(self, V: int, C: int, n: int, scale: float = 1.0, dtype=torch.bfloat16, table_dtype=torch.float32,
+                 std: float = 0.02, device="cuda"):
+        super().__init__()
+        self.n, self.scale, self.dtype = n, scale, dtype
+        self.table = torch.nn.Parameter(torch.empty(V, C, device=device, dtype=table_dtype).normal_(0.0, std))
+
+    def forward(self, ids):
+        return _Embed.apply(self.table, ids, self.n, self.scale, self.dtype)
+
+
+class StreamsNorm(torch.nn.Module):
+    """RMS norm of the sum of the streams x [T, n, C], or of one row h [T, C], with a gain; [T, C]."""
+
+    def __init__(self, C: int, eps: float = 1e-6, device="cuda"):
+        super().__init__()
+        self.eps = eps
+        self.gain = torch.nn.Parameter(torch.ones(C, device=device))
+
+    def forward(self, x):
+        return _Norm.apply(x if x.dim() == 3 else x.unsqueeze(1), self.gain, self.eps)
+
+
+class Head(torch.nn.Module):
+    """The mean of the softmax cross entropy of h W^T with the next tokens [T] over those that are not negative, or, with weight [T],
+    the sum of weight times it.  W [V, C] is of h's type; `table`: the parameter of an embedding of that type, shared."""
+
+    def __init__(self, V: int, C: int, dtype=torch.bfloat16, std: float = 0.02, device="cuda", table=None):
+        super().__init__()
+        if table is not None and (table.shape != (V, C) or table.dtype is not dtype):
+            raise ValueError(f"table must be [{V}, {C}] of {dtype}, got {tuple(table.shape)} of {table.dtype}")
+        self.W = table if table is not None else torch.nn.Parameter(torch.empty(V, C, device=device, dtype=dtype).normal_(0.0, std))
+
+    def forward(self, h, targets, weight=None):
+        if torch.is_grad_enabled() and (h.requires_grad or self.W.requires_grad):
+            return _HeadTotal.apply(h, self.W, targets, weight)
+        return _total(h, self.W, targets, self.score(h, targets)[0], weight)
+
+    @torch.no_grad()
+    def score(self, h, targets):
+        """``loss [T], lse [T]`` of each token."""
+        return head_loss(h, self.W, targets)

@@ -5,57 +5,16 @@
 //
 // autograd.py decides which calls come here: plain GPU tensors outside of function transforms, tracing and
 // dispatch modes, with every shape, type and layout checked.  What the library itself refuses is raised as its status.
-#include <torch/extension.h>
-
-#include <c10/hip/HIPStream.h>
-
 #include <tuple>
 
-#include "../../include/mhcl.h"
+#include "native.h"
 
 namespace {
 
-using at::Tensor;
+using namespace native;
 using torch::autograd::AutogradContext;
 using torch::autograd::Function;
 using torch::autograd::variable_list;
-
-// Raises what binding.py raises for the same status. As a Python exception from here on: a backward runs in autograd's
-// threads, which carry those over to the caller as they are and make a RuntimeError of all others.
-[[noreturn]] void raise(int status, const char *where) {
-  py::gil_scoped_acquire gil;
-  const py::object type = py::module_::import("paper_2601_05732_amd.binding").attr("MhclError"), error = type(status, where);
-  PyErr_SetObject(type.ptr(), error.ptr());
-  python_error e;
-  e.persist();
-  throw e;
-}
-void check(int status, const char *where) {
-  if (status != MHCL_OK) raise(status, where);
-}
-
-void *stream() { return c10::hip::getCurrentHIPStream().stream(); }
-
-// an empty tensor has no storage: NULL
-template <typename T = void>
-T *ptr(const Tensor &t) {
-  return t.numel() == 0 ? nullptr : static_cast<T *>(t.data_ptr());
-}
-Tensor floats(const Tensor &like, at::IntArrayRef shape) { return at::empty(shape, like.options().dtype(at::kFloat)); }
-
-// as layer.empty_stream: contiguous, first byte `phase` bytes past a 1 KiB boundary
-Tensor empty_stream(const Tensor &like, at::IntArrayRef shape, int64_t phase) {
-  int64_t numel = 1;
-  std::vector<int64_t> strides(shape.size());
-  for (size_t i = shape.size(); i-- > 0;) {
-    strides[i] = numel;
-    numel *= shape[i];
-  }
-  const int64_t size = like.element_size();
-  const Tensor buf = at::empty({numel + 1024 / size}, like.options());
-  const uintptr_t lead = (static_cast<uintptr_t>(phase) - reinterpret_cast<uintptr_t>(buf.data_ptr())) & 1023u;
-  return buf.as_strided(shape, strides, static_cast<int64_t>(lead) / size);
-}
 
 // What the nodes of a layer share: its description, and what the post node leaves for the coefficient node.
 struct Link final : torch::CustomClassHolder {
@@ -229,5 +188,6 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
         }));
   m.def("streams_in", wrap([](const Tensor &x0, const LinkPtr &link) { return StreamsIn::apply(x0, link); }));
   m.def("readable", torch::wrap_pybind_function(&readable));
+  bind_ends(m);
   m.def("streams_out", wrap([](const Tensor &x, const LinkPtr &link) { return StreamsOut::apply(x, link); }));
 }
