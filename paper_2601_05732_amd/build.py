@@ -10,7 +10,8 @@ import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-CSRC = os.path.join(_HERE, "csrc")
+CSRC = os.path.join(_HERE, "csrc")             # the layers (bench.py's figures go by what lies there)
+CSRC_ENDS = os.path.join(_HERE, "csrc_ends")   # the ends of a language model
 LIB = os.path.join(_HERE, "libmhcl.so")
 OBJ_DIR = os.path.join(_HERE, "_build")
 PROBE_SRC = os.path.join(_HERE, "probe", "memsys_probe.hip")
@@ -28,7 +29,7 @@ FLAGS = [
 
 
 def sources():
-    return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".hip"))
+    return sorted(os.path.join(d, f) for d in (CSRC, CSRC_ENDS) for f in os.listdir(d) if f.endswith(".hip"))
 
 
 def build_library(verbose: bool = False) -> str:

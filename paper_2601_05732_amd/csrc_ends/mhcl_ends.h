@@ -1,7 +1,7 @@
 // Host-side declarations of the two ends of a language model: mhcl_ends.hip (embedding, norm), mhcl_head.hip
 // (cross entropy), mhcl_ends_api.hip (their C ABI).
 #pragma once
-#include "mhcl_internal.h"
+#include "../csrc/mhcl_internal.h"
 
 namespace mhcl {
 

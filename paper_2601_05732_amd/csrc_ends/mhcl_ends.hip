@@ -1,6 +1,6 @@
 // The ends of a language model, first part: token embedding into the streams with the table's gradient, and the norm of
 // the streams' sum with its backward.
-#include "mhcl_common.h"
+#include "../csrc/mhcl_common.h"
 #include "mhcl_ends.h"
 
 namespace mhcl {

@@ -8,9 +8,9 @@
 // exp(z - m) over the rows of the vocabulary that a wave holds (a "granule"), and for the gradients leaves exp(z - m) in 16
 // bits; a pass over a row then joins the granules, knows lse, and turns the numerators into g in place.  (Forming z again
 // instead, once lse is known, is a fourth product: 2 C operations for each number in place of 4 bytes.)
-#include "mhcl_common.h"
+#include "../csrc/mhcl_common.h"
 #include "mhcl_head.h"
-#include "mhcl_mfma.h"
+#include "../csrc/mhcl_mfma.h"
 
 namespace mhcl {
 namespace {
