@@ -499,21 +499,53 @@ struct RowArgs {
   int C, gran_log2;
 };
 
-// loss and lse of a token, one wave each
-template <typename ID>
-__global__ __launch_bounds__(kBlock) void loss_kernel(const RowArgs a, const ID *__restrict__ targets) {
-  const int lane = threadIdx.x & 63;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
-  if (t >= a.T) return;
-  const float2 *stat = a.stat + t * a.granules;
-  float top = -INFINITY, sum = 0.f;
-  for (int64_t p = lane; p < a.granules; p += 64) top = fmaxf(top, stat[p].x);
+// sum, and the largest, of a value over the WAVES waves of a token
+template <int WAVES>
+__device__ __forceinline__ float rows_sum(float v, float *red) {
+  v = wave_sum(v);
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = pairwise_sum<WAVES>([&](int w) { return red[w]; });
+  }
+  return v;
+}
+template <int WAVES>
+__device__ __forceinline__ float rows_max(float v, float *red) {
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-  const float base = top == -INFINITY ? 0.f : top;
-  for (int64_t p = lane; p < a.granules; p += 64) sum += stat[p].y * expf(stat[p].x - base);
-  sum = wave_sum(sum);
-  if (lane == 0) {
+  for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v = fmaxf(v, red[w]);
+  }
+  return v;
+}
+
+// a row's maximum (0 where there is none) and the sum of exp(z - that) from its granules
+template <int WAVES>
+__device__ __forceinline__ void join_granules(const float2 *stat, int64_t granules, float (*red)[16], float &base, float &sum) {
+  const int tid = threadIdx.x % (WAVES * 64);
+  float top = -INFINITY;
+  sum = 0.f;
+  for (int64_t p = tid; p < granules; p += WAVES * 64) top = fmaxf(top, stat[p].x);
+  top = rows_max<WAVES>(top, red[0]);
+  base = top == -INFINITY ? 0.f : top;
+  for (int64_t p = tid; p < granules; p += WAVES * 64) sum += stat[p].y * expf(stat[p].x - base);
+  sum = rows_sum<WAVES>(sum, red[1]);
+}
+
+// loss and lse of a token: one wave each, or (WAVES > 1) a block each
+template <typename ID, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * 64) void loss_kernel(const RowArgs a, const ID *__restrict__ targets) {
+  __shared__ float red[2][16];
+  constexpr int TOKENS = WAVES == 1 ? kBlock / 64 : 1;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * TOKENS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
+  if (t >= a.T) return;
+  float base, sum;
+  join_granules<WAVES>(a.stat + t * a.granules, a.granules, red, base, sum);
+  if (threadIdx.x % (WAVES * 64) == 0) {
     const int64_t y = static_cast<int64_t>(targets[t]);
     a.lse[t] = base + logf(sum);
     a.loss[t] = y < 0 ? 0.f : (y < a.V ? logf(sum) + (base - a.zt[t]) : __uint_as_float(0x7fc00000u));
@@ -524,24 +556,12 @@ __global__ __launch_bounds__(kBlock) void loss_kernel(const RowArgs a, const ID 
 // row into hp, zeros where the weight is 0.
 template <typename ID, int PARTS>
 __global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *__restrict__ targets) {
-  __shared__ float red[2][kBlock / 64];
+  __shared__ float red[2][16];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x;
   const float2 *stat = a.stat + t * a.granules;
-  float top = -INFINITY, sum = 0.f;
-  for (int64_t p = tid; p < a.granules; p += kBlock) top = fmaxf(top, stat[p].x);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-  if ((tid & 63) == 0) red[0][tid >> 6] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kBlock / 64; ++w) top = fmaxf(top, red[0][w]);
-  const float base = top == -INFINITY ? 0.f : top;
-  for (int64_t p = tid; p < a.granules; p += kBlock) sum += stat[p].y * expf(stat[p].x - base);
-  sum = wave_sum(sum);
-  if ((tid & 63) == 0) red[1][tid >> 6] = sum;
-  __syncthreads();
-  sum = pairwise_sum<kBlock / 64>([&](int w) { return red[1][w]; });
+  float base, sum;
+  join_granules<kBlock / 64>(stat, a.granules, red, base, sum);
   // (not by way of lse, in which log(sum) is lost where the logits are large)
   const int64_t y = static_cast<int64_t>(targets[t]);
   const float bad = __uint_as_float(0x7fc00000u);
@@ -740,8 +760,10 @@ hipError_t launch_gemm(const HeadTile &tile, Operand A, Operand B, int64_t M, in
 
 // the largest tile of which there are enough for the chip.  (For the gradients' products of fp32 operands the middle one: the largest
 // one's registers do not hold what the six products of parts need besides.  us, 2048 tokens, C = 768, 50257 rows, g_W, largest / middle: 1257 / 1155.)
-HeadTile tile_for(int64_t M, int64_t N, bool slim, bool big) {
-  if (slim && N <= 64) return kTileSlim;
+// The smallest one for the few tokens of a step of decoding, or where the middle one leaves half the chip without work; `parts`: into how
+// many the depth can be split.  (us, 333 tokens, C = 520, 1003 rows, logits and g_h, middle / smallest: 16.4, 12.4 / 11.0, 7.8.)
+HeadTile tile_for(int64_t M, int64_t N, int64_t parts, bool slim, bool big) {
+  if (slim && (N <= 64 || ceil_div(M, 128) * ceil_div(N, 128) * parts < kChipBlocks / 2)) return kTileSlim;
   return big && ceil_div(M, 256) * ceil_div(N, 256) >= kChipBlocks ? kTileBig : kTileMid;
 }
 
@@ -756,15 +778,16 @@ HeadPlan::HeadPlan(const mhcl_ends_desc &d, bool grad) {
   const int64_t fit = static_cast<int64_t>(MHCL_HEAD_BLOCK_BYTES) / row_bytes / 256 * 256;
   if (tokens > fit) tokens = fit < 256 ? 256 : fit;
   if (tokens > d.T) tokens = d.T;
-  logits = tile_for(d.V, tokens, true, true);
-  gh = tile_for(d.C, tokens, true, parts == 1);
-  gw = tile_for(d.C, d.V, false, parts == 1);
+  const int64_t steps = ceil_div(d.V, kBK) * pairs;   // of the product for g_h
+  logits = tile_for(d.V, tokens, 1, true, true);
+  gh = tile_for(d.C, tokens, steps / 8 > 0 ? steps / 8 : 1, true, parts == 1);
+  gw = tile_for(d.C, d.V, 1, false, parts == 1);
   ld = ceil_div(d.V, logits.bm) * logits.bm;   // (what the first product's tiles cover)
   granules = ld / logits.gran;
   gh_splits = 1;
   if (grad) {
     // enough blocks for the chip, each with at least eight steps
-    const int64_t tiles = ceil_div(d.C, gh.bm) * ceil_div(tokens, gh.bn), steps = ceil_div(d.V, kBK) * pairs;
+    const int64_t tiles = ceil_div(d.C, gh.bm) * ceil_div(tokens, gh.bn);
     int64_t k = (2 * kChipBlocks) / (tiles > 0 ? tiles : 1);
     if (k > steps / 8) k = steps / 8;
     if (k > 64) k = 64;
@@ -825,7 +848,9 @@ hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, co
       while ((1 << gran_log2) < p.logits.gran) ++gran_log2;
       const RowArgs a{hb, weight ? weight + t0 : nullptr, w.common, w.stat, w.zt, loss + t0, lse + t0, w.E, w.G, w.hp, T, p.ld, p.granules, d.V, d.C, gran_log2};
       if (!grad) {
-        hipLaunchKernelGGL((loss_kernel<ID>), dim3(blocks(T, kBlock / 64)), dim3(kBlock), 0, s, a, y);
+        // (us, 50257 rows in granules of 32: a wave / a block of sixteen for one token 11.2 / 4.6)
+        if (T < 1024) hipLaunchKernelGGL((loss_kernel<ID, 16>), dim3(static_cast<unsigned>(T)), dim3(1024), 0, s, a, y);
+        else hipLaunchKernelGGL((loss_kernel<ID, 1>), dim3(blocks(T, kBlock / 64)), dim3(kBlock), 0, s, a, y);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         continue;
       }
