@@ -330,7 +330,8 @@ typedef struct {
   int32_t n;         /* residual streams, 1..8 (read by mhcl_embed* and mhcl_streams_norm*)             */
   int32_t C;         /* width; a positive multiple of 8, at most 32768                                  */
   int64_t T;         /* tokens, 0 .. 2^30                                                               */
-  int32_t V;         /* rows of table or W, >= 1 (not read by mhcl_streams_norm*)                       */
+  int32_t V;         /* rows of table or W, >= 1 (not read by mhcl_streams_norm*);                      */
+                     /* at most 2^30, for mhcl_head_* 2^22 - 256                                         */
   int32_t io_dtype;  /* MHCL_BF16 | MHCL_F32: streams, h and their gradients                            */
   int32_t w_dtype;   /* MHCL_BF16 | MHCL_F32: table, W and their gradients (mhcl_head_*: equal io_dtype) */
   int32_t id_dtype;  /* MHCL_I64 | MHCL_I32: ids and targets                                            */

@@ -33,6 +33,8 @@ int check_ends(const mhcl_ends_desc *d, End end) {
   // index arithmetic: tokens and rows of the vocabulary in 32 bits, with room for a sentinel; at most 2^31 - 1 blocks a launch
   if (d->C > 32768 || d->T > (1 << 30)) return MHCL_ERR_UNSUPPORTED;
   if (end != End::kNorm && d->V > (1 << 30)) return MHCL_ERR_UNSUPPORTED;
+  // (the head's products reach over 256 rows of numerators, 128 of fp32, by 31-bit offsets in bytes)
+  if (end == End::kHead && d->V > kHeadMostRows) return MHCL_ERR_UNSUPPORTED;
   if (d->T * (d->C / 4) / 256 > (int64_t{1} << 31) - 1) return MHCL_ERR_UNSUPPORTED;
   return MHCL_OK;
 }

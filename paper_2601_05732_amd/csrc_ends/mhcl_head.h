@@ -11,9 +11,10 @@ struct HeadTile {
 };
 constexpr HeadTile kTileBig{256, 256, 128}, kTileMid{128, 128, 64}, kTileSlim{128, 32, 32};
 
+constexpr int32_t kHeadMostRows = (1 << 22) - 256;   // of the vocabulary
+
 struct HeadPlan {
-  int parts;            // bf16 numbers that an operand's element is taken as: 1, or 3 for fp32
-  int pairs;            // products of parts
+  bool wide;            // fp32 operands
   HeadTile logits, gh, gw;
   int64_t tokens;       // of a block
   int64_t ld;           // row of the softmax's numerators: V, filled up to whole tiles
@@ -24,9 +25,8 @@ struct HeadPlan {
 
 struct HeadWs {
   HeadPlan plan;
-  uint16_t *hp, *Wp;    // [parts][tokens][C]: h, zeros where a token does not count; [parts][V][C] (fp32 only)
-  char *E;              // [tokens][ld] numerators: 16 bits each, then g in bf16 in their place; fp32: floats
-  uint16_t *G;          // [parts][tokens][ld] g
+  char *hp;             // [tokens][C]: h, zeros where a token does not count
+  char *E;              // [tokens][ld] numerators in 16 bits, then g in bf16 in their place; fp32: 32 bits each
   float2 *stat;         // [tokens][granules] maximum and sum
   float *zt;            // [tokens] the targets' logits
   float *common;        // [1] what all weights are multiples of

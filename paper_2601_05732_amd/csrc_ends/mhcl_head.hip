@@ -16,88 +16,98 @@ namespace mhcl {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kBK = 64;                       // depth of a step: 128 bytes of a row
 constexpr float kLog2e = 1.4426950408889634f;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lds_void;
 
 // ---------------------------------------------------------------- products
-// D[m][n] = sum_k A[m][k] B[n][k] over bf16 operands.  An operand lies in memory with k innermost (KINNER: row m or n starts at p + m ld),
-// or with m or n innermost (row k starts at p + k ld), in `part` elements long parts.  rows: its extent in m or n; depth: in k.
+// D[m][n] = sum_k A[m][k] B[n][k].  An operand lies in memory with k innermost (KINNER: row m or n starts at p + m ld), or with m or n
+// innermost (row k starts at p + k ld).  rows: its extent in m or n; depth: in k.  Elements are bf16, or fp32 (WIDE), which the
+// fragments in registers split into three bf16 parts of 8 significant bits each; six of the nine products of parts are added, small ones
+// first, the other three being below 2^-23 of the whole.  (The fp32 matrix instruction does a sixteenth of the bf16 one's operations a
+// cycle, and six products are more exact.)
 struct Operand {
-  const uint16_t *p;
-  int64_t ld, part;
+  const void *p;
+  int64_t ld;
   int64_t rows, depth;
 };
-
-// The pairs of parts whose products are added, small ones first: of three parts of 8 bits all but the three products below 2^-23 of
-// the whole.  (1, 1) (0, 2) (2, 0) (0, 1) (1, 0) (0, 0), a hexadecimal digit each from the low end; and two more than the way from
-// each to the next.  (An array would be kept in memory.)
-constexpr uint32_t kPartsA = 0x010201, kPartsB = 0x001021, kWayA = 0x213041, kWayB = 0x221303;
-__device__ __forceinline__ int digit(uint32_t digits, int i) { return static_cast<int>(digits >> (4 * i) & 15); }
 
 struct GemmArgs {
   Operand A, B;
   int tiles_m, tiles_n, splits;
 };
 
-// One operand's tile of R rows by kBK in LDS, in 16-byte pieces, as the loads that go straight to LDS leave it (piece i at
+// One operand's tile of R rows by 128 bytes in LDS, in 16-byte pieces, as the loads that go straight to LDS leave it (piece i at
 // 16 i), so that a piece's place is chosen by which piece of memory a thread asks for.
 //  KINNER: piece (row, c) of a row's eight at 8 row + (c ^ (row / 2 % 8)): the 16 rows that a fragment reads at one c lie in
 //   all 64 banks once.
-//  else: row k holds R / 8 pieces; the pairs of pieces (16 numbers, what a transposing read takes of a row) are exchanged
+//  else, bf16: row k holds R / 8 pieces; the pairs of pieces (16 numbers, what a transposing read takes of a row) are exchanged
 //   by k: pair m16 of row k at m16 ^ (k % 4 + 4 (k / 8 % 2)), so that the eight rows that half a wave reads lie in all banks.
+//  else, fp32: row k holds R / 4 pieces; its units of four (16 numbers) are exchanged: unit m16 of row k at m16 ^ (k / 8), so that
+//   the four rows that a read takes lie in all banks.
 // A thread's pieces lie the same distance apart; the loads' own range check gives zeros past the operand's end.  (Rows of m or n
 // outside of the operand give results that nobody reads.)
-template <int R, int NT, bool KINNER>
+template <int R, int NT, bool KINNER, bool WIDE>
 struct TileLoader {
-  static constexpr int PER = R * 8 / NT;
-  static constexpr int kRows = KINNER ? NT / 8 : NT / (R / 8);   // rows of memory from one piece to the next
-  static_assert(kRows % 16 == 0 || PER == 1, "the exchange of pieces is the same for all of a thread's");
+  static constexpr int PER = R * 8 / NT, ES = WIDE ? 4 : 2, DEPTH = 128 / ES, PPR = R * ES / 16;
+  static constexpr int kRows = KINNER ? NT / 8 : NT / PPR;   // rows of memory from one piece to the next
+  static_assert(PER == 1 || (KINNER || !WIDE ? kRows % 16 == 0 : kRows == 8), "how the exchange of pieces goes on from one to the next");
   const char *base;         // of the tile and the next step
-  int64_t rest;             // bytes from there to the operand's (its part's) end
+  int64_t rest;             // bytes from there to the operand's end
   int step, apart;          // bytes from one step to the next; from one piece to the next (a tile's are less than 2^31: the host sees to it)
   uint32_t at, from;        // bytes from `base` to the thread's first piece; the same, or out of range, for this step
+  uint32_t unit;            // fp32, not KINNER: its unit's bytes, which the pieces exchange
   int depth;                // KINNER: k of the thread's pieces within the tile
   __device__ __forceinline__ void init(const Operand &o, int64_t row0) {
     const int tid = threadIdx.x;
-    const int64_t skip = row0 * (KINNER ? o.ld : 1) * 2;
-    step = static_cast<int>((KINNER ? kBK : kBK * o.ld) * 2);
-    apart = static_cast<int>(kRows * o.ld * 2);
-    base = reinterpret_cast<const char *>(o.p) + skip;
-    rest = (KINNER ? o.rows : o.depth) * o.ld * 2 - skip;
+    const int64_t skip = row0 * (KINNER ? o.ld : 1) * ES;
+    step = static_cast<int>((KINNER ? DEPTH : DEPTH * o.ld) * ES);
+    apart = static_cast<int>(kRows * o.ld * ES);
+    base = static_cast<const char *>(o.p) + skip;
+    rest = (KINNER ? o.rows : o.depth) * o.ld * ES - skip;
+    depth = 0;
+    unit = 0;
     if constexpr (KINNER) {
-      depth = ((tid & 7) ^ ((tid >> 4) & 7)) * 8;
-      at = static_cast<uint32_t>(((tid >> 3) * o.ld + depth) * 2);
+      const int c = (tid & 7) ^ ((tid >> 4) & 7);
+      depth = c * (16 / ES);
+      at = static_cast<uint32_t>((tid >> 3) * o.ld * ES + c * 16);
+    } else if constexpr (WIDE) {
+      const int slot = tid % PPR;
+      unit = (slot >> 2) << 6;
+      at = static_cast<uint32_t>(tid / PPR * o.ld * ES + (slot & 3) * 16);
     } else {
-      const int kr = tid / (R / 8), slot = tid % (R / 8);
+      const int kr = tid / PPR, slot = tid % PPR;
       const int m = (((slot >> 1) ^ ((kr & 3) | ((kr >> 3) & 1) << 2)) * 2 + (slot & 1)) * 8;
-      depth = 0;
-      at = static_cast<uint32_t>((kr * o.ld + m) * 2);
+      at = static_cast<uint32_t>((kr * o.ld + m) * ES);
     }
   }
   __device__ __forceinline__ void skip(int64_t bytes) { base += bytes, rest -= bytes; }
   // left: depth that is left of the operand from this step on, 0 or less for a tile of zeros
-  __device__ __forceinline__ void aim(int left) {
-    from = at;
-    if constexpr (KINNER) from = depth < left ? at : 0x80000000u;
-    else from = left > 0 ? at : 0x80000000u;
-  }
+  __device__ __forceinline__ void aim(int left) { from = depth < left ? at : 0x80000000u; }
   __device__ __forceinline__ void piece(uint4 *tile, int wave, int i) const {
     const int range = rest <= 0 ? 0 : (rest > 0x7fffffff ? 0x7fffffff : static_cast<int>(rest));
+    uint32_t offset = from + i * apart;
+    if constexpr (!KINNER && WIDE) offset += unit ^ i << 6;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, range, 0x00020000),
-                                             (lds_void *)(tile + i * NT + wave * 64), 16, from + i * apart, 0, 0, 0);
+                                             (lds_void *)(tile + i * NT + wave * 64), 16, offset, 0, 0, 0);
   }
 };
 
 // Fragments of 16 rows, k = 32 s + 8 q .. + 7 for lane (r, q).  lane_at: the lane's place in fragment 0 at s = 0, in bytes.
-template <int R, bool KINNER>
+template <int R, bool KINNER, bool WIDE>
 __device__ __forceinline__ int lane_at() {
   const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-  if constexpr (KINNER) return r * 128 | (q ^ ((r >> 1) & 7)) << 4;
+  if constexpr (KINNER) return r * 128 | ((WIDE ? 2 * q : q) ^ ((r >> 1) & 7)) << 4;
+  if constexpr (WIDE) return q * 8 * (R * 4) | q << 6 | r << 2;
   // 16 lanes read rows k .. k + 3, 32 bytes of each, and get a column of four each
   return (q * 8 + (r >> 2)) * (R * 2) | ((r >> 2) | (q & 1) << 2) << 5 | (r & 3) << 3;
+}
+// the same for the fragments from the first-th on (a power of two of them, first a multiple of it)
+template <int R, bool KINNER, bool WIDE>
+__device__ __forceinline__ int lane_at(int first) {
+  if constexpr (KINNER) return lane_at<R, KINNER, WIDE>() + first * 2048;
+  return lane_at<R, KINNER, WIDE>() ^ first << (WIDE ? 6 : 5);
 }
 template <int R, bool KINNER>
 __device__ __forceinline__ u32x4 fragment(const uint4 *tile, int at, int f, int s) {
@@ -113,6 +123,42 @@ __device__ __forceinline__ u32x4 fragment(const uint4 *tile, int at, int f, int 
     return u32x4{l[0], l[1], h[0], h[1]};
   }
 }
+// fp32: eight numbers, and their parts
+struct Eight {
+  f32x4 v[2];
+};
+template <int R, bool KINNER>
+__device__ __forceinline__ Eight wide_fragment(const uint4 *tile, int at, int f) {
+  const char *p = reinterpret_cast<const char *>(tile);
+  Eight e;
+  if constexpr (KINNER) {
+    e.v[0] = *reinterpret_cast<const f32x4 *>(p + at + f * 2048);
+    e.v[1] = *reinterpret_cast<const f32x4 *>(p + (at ^ 16) + f * 2048);
+  } else {
+    const char *from = p + (at ^ f << 6);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e.v[i / 4][i % 4] = *reinterpret_cast<const float *>(from + i * (R * 4));
+  }
+  return e;
+}
+struct Parts {
+  u32x4 p[3];
+};
+__device__ __forceinline__ Parts parts_of(const Eight &e) {
+  Parts r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo = e.v[i / 2][i % 2 * 2], hi = e.v[i / 2][i % 2 * 2 + 1];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const uint32_t two = cvt_pk_bf16(lo, hi);
+      r.p[k][i] = two;
+      lo -= bf16lo(two);
+      hi -= bf16hi(two);
+    }
+  }
+  return r;
+}
 
 // (the addresses of exchanged pieces take an instruction each; kept from step to step they would take a register each)
 template <bool KINNER>
@@ -121,7 +167,7 @@ __device__ __forceinline__ int formed_here(int at) {
   return at;
 }
 template <int LOADS>
-__device__ __forceinline__ void wait_all_but() {   // the last LOADS (< 16) loads
+__device__ __forceinline__ void wait_all_but() {   // the last LOADS loads
   static_assert(LOADS < 64, "what the counter holds");
   __builtin_amdgcn_s_waitcnt(0x0070 | (LOADS & 15) | (LOADS >> 4) << 14);
 }
@@ -151,61 +197,48 @@ __device__ __forceinline__ void tile_of(const GemmArgs &g, int b, int &tm, int &
 // A block of WM x WN waves computes BM x BN tiles; wave (wm, wn) rows wm BM / WM of one and columns wn BN / WN on.
 // The epilogue gets acc[fm][fn]: lane (r, q) holds m = 16 fm + 4 q + 0..3 of the wave's rows, n = 16 fn + r of its columns.
 // The next tile's first loads are on their way during the epilogue, and the epilogue's stores during the next tile's first step.
-template <int BM, int BN, int WM, int WN, bool AK, bool BK, int PAIRS, typename Epilogue>
-__global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, const Epilogue epilogue) {
+template <int BM, int BN, int WM, int WN, bool AK, bool BK, typename Epilogue>
+__global__ __launch_bounds__(WM *WN * 64, 2) void gemm_kernel(const GemmArgs g, const Epilogue epilogue) {
+  constexpr bool WIDE = Epilogue::kWide;
   constexpr int NT = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
   __shared__ uint4 a0[BM * 8], a1[BM * 8], b0[BN * 8], b1[BN * 8];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+  TileLoader<BM, NT, AK, WIDE> la;
+  TileLoader<BN, NT, BK, WIDE> lb;
   const int64_t depth = g.A.depth < g.B.depth ? g.B.depth : g.A.depth;
-  const int steps = static_cast<int>((depth + kBK - 1) / kBK);
+  const int steps = static_cast<int>((depth + la.DEPTH - 1) / la.DEPTH);
   const int tiles = g.tiles_m * g.tiles_n * g.splits;
   int tile = blockIdx.x, tm, tn, split;
-  TileLoader<BM, NT, AK> la;
-  TileLoader<BN, NT, BK> lb;
-  int pair, at, to_load, to_do;   // of the next load; steps to load, and to multiply
+  int at, to_load, to_do;         // step of the next load; steps to load, and to multiply
   const auto begin = [&]() __attribute__((always_inline)) {
     tile_of(g, tile, tm, tn, split);
-    const int64_t total = static_cast<int64_t>(steps) * PAIRS;
-    const int64_t first = total * split / g.splits, last = total * (split + 1) / g.splits;
-    to_load = to_do = static_cast<int>(last - first);
+    at = static_cast<int>(static_cast<int64_t>(steps) * split / g.splits);
+    to_load = to_do = static_cast<int>(static_cast<int64_t>(steps) * (split + 1) / g.splits) - at;
     la.init(g.A, static_cast<int64_t>(tm) * BM);
     lb.init(g.B, static_cast<int64_t>(tn) * BN);
-    pair = static_cast<int>(first / steps), at = static_cast<int>(first % steps);
-    const int64_t from_a = digit(PAIRS > 1 ? kPartsA : 0, pair) * g.A.part * 2, from_b = digit(PAIRS > 1 ? kPartsB : 0, pair) * g.B.part * 2;
-    la.skip(from_a + static_cast<int64_t>(at) * la.step);
-    lb.skip(from_b + static_cast<int64_t>(at) * lb.step);
-    la.rest += from_a;
-    lb.rest += from_b;
+    la.skip(static_cast<int64_t>(at) * la.step);
+    lb.skip(static_cast<int64_t>(at) * lb.step);
   };
   f32x4 acc[FM][FN];
   const auto aim = [&]() __attribute__((always_inline)) {
-    const int done = to_load-- > 0 ? at * kBK : 0x7fffffff;   // past the last step: zeros
+    const int done = to_load-- > 0 ? at * la.DEPTH : 0x7fffffff;   // past the last step: zeros
     la.aim(static_cast<int>(g.A.depth) - done);
     lb.aim(static_cast<int>(g.B.depth) - done);
   };
-  // (on to the next pair of parts after the last step of one, without a branch, which costs registers)
   const auto next = [&]() __attribute__((always_inline)) {
     ++at;
     la.skip(la.step);
     lb.skip(lb.step);
-    if constexpr (PAIRS > 1) {
-      const int64_t over = at == steps ? -1 : 0;
-      const int64_t span_a = static_cast<int64_t>(steps) * la.step, span_b = static_cast<int64_t>(steps) * lb.step;
-      la.base += over & ((digit(kWayA, pair) - 2) * g.A.part * 2 - span_a);
-      lb.base += over & ((digit(kWayB, pair) - 2) * g.B.part * 2 - span_b);
-      la.rest += over & span_a;
-      lb.rest += over & span_b;
-      pair -= static_cast<int>(over);
-      at &= static_cast<int>(~over);
-    }
+  };
+  constexpr int HM = FM / 2;
+  const int at_a = lane_at<BM, AK, WIDE>(wm * FM), at_b = lane_at<BN, BK, WIDE>(wn * FN);
+  const auto piece_of = [&](uint4 *a, uint4 *b, int p) __attribute__((always_inline)) {
+    if (p < la.PER) la.piece(a, wave, p);
+    else if (p < la.PER + lb.PER) lb.piece(b, wave, p - la.PER);
   };
   // A step is four groups of products, (k half s, half hm of the rows), whose fragments are read one group ahead.  Once the last
   // group's have arrived the stage is free and the next one's tiles are needed: there the waves meet, and
   // the next step's first fragments are on their way while the last group multiplies.
-  constexpr int HM = FM / 2;
-  // (of the wave's first rows; FM, FN are powers of two)
-  const int at_a = AK ? lane_at<BM, AK>() + wm * FM * 2048 : lane_at<BM, AK>() ^ (wm * FM) << 5;
-  const int at_b = BK ? lane_at<BN, BK>() + wn * FN * 2048 : lane_at<BN, BK>() ^ (wn * FN) << 5;
   u32x4 fa[2][HM], fb[2][FN];
   const auto read_a = [&](const uint4 *a, int s, int hm) __attribute__((always_inline)) {
     const int here = formed_here<AK>(at_a);
@@ -245,20 +278,65 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, con
     aim();
     // the tiles after the next take this step's place
     products(1, 1, [&](int i) __attribute__((always_inline)) {
-      constexpr int PA = (la.PER + HM - 1) / HM, PB = (lb.PER + HM - 1) / HM;
+      constexpr int EACH = (la.PER + lb.PER + HM - 1) / HM;
 #pragma unroll
-      for (int p = i * PA; p < (i + 1) * PA && p < la.PER; ++p) la.piece(a, wave, p);
+      for (int p = i * EACH; p < (i + 1) * EACH; ++p) piece_of(a, b, p);
+    });
+    next();
+  };
+  // fp32: two groups, (half hm of the rows), six products of parts each; the second one's numbers are read under the first one's products and the next
+  // step's under the second one's.
+  Eight ea[HM], eb[FN];
+  Parts pa[HM], pb[FN];
+  const auto read_wide_a = [&](const uint4 *a, int hm) __attribute__((always_inline)) {
+    const int here = formed_here<AK>(at_a);
 #pragma unroll
-      for (int p = i * PB; p < (i + 1) * PB && p < lb.PER; ++p) lb.piece(b, wave, p);
+    for (int i = 0; i < HM; ++i) ea[i] = wide_fragment<BM, AK>(a, here, hm * HM + i);
+  };
+  const auto read_wide_b = [&](const uint4 *b) __attribute__((always_inline)) {
+    const int here = formed_here<BK>(at_b);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) eb[j] = wide_fragment<BN, BK>(b, here, j);
+  };
+  const auto wide_products = [&](int hm, auto between) __attribute__((always_inline)) {
+    constexpr int A[6] = {1, 0, 2, 0, 1, 0}, B[6] = {1, 2, 0, 1, 0, 0};
+#pragma unroll
+    for (int k = 0; k < 6; ++k) {
+#pragma unroll
+      for (int i = 0; i < HM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[hm * HM + i][j] = mfma16(pa[i].p[A[k]], pb[j].p[B[k]], acc[hm * HM + i][j]);
+      between(k);
+    }
+  };
+  const auto wide_step = [&](uint4 *a, uint4 *b, const uint4 *a_next, const uint4 *b_next) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j) pb[j] = parts_of(eb[j]);
+#pragma unroll
+    for (int i = 0; i < HM; ++i) pa[i] = parts_of(ea[i]);
+    read_wide_a(a, 1);
+    wide_products(0, nothing);
+#pragma unroll
+    for (int i = 0; i < HM; ++i) pa[i] = parts_of(ea[i]);
+    __builtin_amdgcn_sched_barrier(0);
+    wait_all();
+    barrier();
+    read_wide_a(a_next, 0);
+    read_wide_b(b_next);
+    aim();
+    wide_products(1, [&](int k) __attribute__((always_inline)) {
+      constexpr int EACH = (la.PER + lb.PER + 5) / 6;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int p = k * EACH; p < (k + 1) * EACH; ++p) piece_of(a, b, p);
+      __builtin_amdgcn_sched_barrier(0);
     });
     next();
   };
   const auto load = [&](uint4 *a, uint4 *b) __attribute__((always_inline)) {
     aim();
 #pragma unroll
-    for (int p = 0; p < la.PER; ++p) la.piece(a, wave, p);
-#pragma unroll
-    for (int p = 0; p < lb.PER; ++p) lb.piece(b, wave, p);
+    for (int p = 0; p < la.PER + lb.PER; ++p) piece_of(a, b, p);
     next();
   };
   begin();
@@ -269,16 +347,26 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_kernel(const GemmArgs g, con
     if (stored) wait_all_but<la.PER + lb.PER + Epilogue::template stores<FM, FN>()>();
     else wait_all();
     barrier();
-    read_a(a0, 0, 0);
-    read_b(b0, 0);
+    if constexpr (WIDE) {
+      read_wide_a(a0, 0);
+      read_wide_b(b0);
+    } else {
+      read_a(a0, 0, 0);
+      read_b(b0, 0);
+    }
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     // (steps in pairs, so that a stage's place is known where it is read; after an odd last one a step of zeros)
     for (int left = to_do; left > 0; left -= 2) {
-      step(a0, b0, a1, b1);
-      step(a1, b1, a0, b0);
+      if constexpr (WIDE) {
+        wide_step(a0, b0, a1, b1);
+        wide_step(a1, b1, a0, b0);
+      } else {
+        step(a0, b0, a1, b1);
+        step(a1, b1, a0, b0);
+      }
     }
     const int64_t m0 = static_cast<int64_t>(tm) * BM + wm * (FM * 16), n0 = static_cast<int64_t>(tn) * BN + wn * (FN * 16);
     const int this_split = split;
@@ -327,7 +415,7 @@ __device__ __forceinline__ float exp_of(float x) {
 // m: vocabulary, n: tokens.  STORE: the numerators too.  WIDE: fp32 numerators.
 template <typename ID, bool STORE, bool WIDE>
 struct LogitsEpilogue {
-  static constexpr int kWide = WIDE;   // with one product of parts (0), six (1), either (2)
+  static constexpr bool kWide = WIDE;
   const ID *targets;
   float2 *stat;
   float *zt;
@@ -412,8 +500,9 @@ struct LogitsEpilogue {
 };
 
 // out[n][m], m innermost, times *scale: fp32 slabs of splits (out32 != null), added to `add` if that is there; else rounded to bf16
+template <bool WIDE>
 struct StoreEpilogue {
-  static constexpr int kWide = 2;
+  static constexpr bool kWide = WIDE;
   const float *scale;
   float *out32;
   uint16_t *out16;
@@ -422,7 +511,7 @@ struct StoreEpilogue {
   template <int FN>
   __device__ __forceinline__ float hold(int64_t) const { return *scale; }
   template <int FM, int FN>
-  static constexpr int stores() { return FN * FM / 2; }   // (in fp32 twice as many)
+  static constexpr int stores() { return FN * (WIDE ? FM : FM / 2); }   // (into fp32 slabs twice as many)
   __device__ __forceinline__ bool whole(int64_t m_end, int64_t n_end) const { return m_end <= M && n_end <= N; }
   template <int FM, int FN>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], float factor, int64_t m0, int64_t n0, int split) const {
@@ -492,8 +581,7 @@ struct RowArgs {
   const float2 *stat;
   const float *zt;
   float *loss, *lse;
-  char *E;
-  uint16_t *G, *hp;
+  char *E, *hp;
   int64_t T, ld, granules;
   int32_t V;
   int C, gran_log2;
@@ -552,9 +640,9 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * 64) void loss_kernel(
   }
 }
 
-// The same, one block a token, and the row's numerators turned into g: bf16 in their place, or (PARTS = 3) three bf16 parts of each; h's
-// row into hp, zeros where the weight is 0.
-template <typename ID, int PARTS>
+// The same, one block a token, and the row's numerators turned into g in their place, bf16 or (IO = F32) fp32; h's row into hp, zeros
+// where the weight is 0.
+template <typename ID, typename IO>
 __global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *__restrict__ targets) {
   __shared__ float red[2][16];
   const int64_t t = blockIdx.x;
@@ -579,7 +667,7 @@ __global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *
     float g[8];
     if (counts) {
       const float f = scale * expf(stat[v >> a.gran_log2].x - base);
-      if constexpr (PARTS == 1) {
+      if constexpr (IO::kVec == 8) {
         const uint4 c = *reinterpret_cast<const uint4 *>(a.E + (t * a.ld + v) * 2);
         const uint32_t code[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
@@ -605,32 +693,19 @@ __global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *
 #pragma unroll
       for (int i = 0; i < 8; ++i) g[i] = 0.f;
     }
-    if constexpr (PARTS == 1) {
+    if constexpr (IO::kVec == 8) {
       BF16::store(a.E, t * a.ld + v, g);
     } else {
-#pragma unroll
-      for (int p = 0; p < PARTS; ++p) {
-        float part[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          part[i] = bf16_to_f32(f32_to_bf16(g[i]));
-          g[i] -= part[i];
-        }
-        BF16::store(a.G, (p * a.T + t) * a.ld + v, part);
-      }
+      F32::store(a.E, t * a.ld + v, reinterpret_cast<const float(&)[4]>(g[0]));
+      F32::store(a.E, t * a.ld + v + 4, reinterpret_cast<const float(&)[4]>(g[4]));
     }
   }
-  const float none[8] = {};
-  for (int c = tid * 8; c < a.C; c += kBlock * 8) {
-    if constexpr (PARTS == 1) {
-      float v[8];
-      BF16::load(a.h, t * a.C + c, v);
-      if (counts) BF16::store(a.hp, t * a.C + c, v);
-      else BF16::store(a.hp, t * a.C + c, none);
-    } else if (!counts) {                        // (the parts are there from before the first product)
+  for (int c = tid * IO::kVec; c < a.C; c += kBlock * IO::kVec) {
+    float v[IO::kVec];
+    IO::load(a.h, t * a.C + c, v);
 #pragma unroll
-      for (int p = 0; p < PARTS; ++p) BF16::store(a.hp, (p * a.T + t) * a.C + c, none);
-    }
+    for (int i = 0; i < IO::kVec; ++i) v[i] = counts ? v[i] : 0.f;
+    IO::store(a.hp, t * a.C + c, v);
   }
 }
 
@@ -690,25 +765,6 @@ __global__ __launch_bounds__(kBlock) void scale_kernel(void *__restrict__ p, int
   }
 }
 
-// fp32 as three bf16 parts, each the rounded rest: `count` elements (a multiple of 8), parts `part` elements apart
-__global__ __launch_bounds__(kBlock) void split_kernel(const float *__restrict__ in, uint16_t *__restrict__ out, int64_t count, int64_t part) {
-  const int64_t i = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 8;
-  if (i >= count) return;
-  float v[8];
-  F32::load(in, i, reinterpret_cast<float(&)[4]>(v[0]));
-  F32::load(in, i + 4, reinterpret_cast<float(&)[4]>(v[4]));
-#pragma unroll
-  for (int p = 0; p < 3; ++p) {
-    float h[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      h[e] = bf16_to_f32(f32_to_bf16(v[e]));
-      v[e] -= h[e];
-    }
-    BF16::store(out, p * part + i, h);
-  }
-}
-
 // out = the sum of `slabs` slabs of `count` floats (a multiple of 4), in order
 template <typename IO>
 __global__ __launch_bounds__(kBlock) void slab_sum_kernel(const float *__restrict__ in, void *__restrict__ out, int slabs, int64_t count) {
@@ -733,33 +789,25 @@ hipError_t dispatch_id(int id_dtype, F &&f) {
 }
 
 template <bool AK, bool BK, typename Epilogue>
-hipError_t launch_gemm(const HeadTile &tile, Operand A, Operand B, int64_t M, int64_t N, int parts, int splits, const Epilogue &e, hipStream_t s) {
-  GemmArgs g;
-  g.A = A;
-  g.B = B;
-  g.tiles_m = static_cast<int>(ceil_div(M, tile.bm));
-  g.tiles_n = static_cast<int>(ceil_div(N, tile.bn));
-  g.splits = splits;
+hipError_t launch_gemm(const HeadTile &tile, const Operand &A, const Operand &B, int64_t M, int64_t N, int splits, const Epilogue &e, hipStream_t s) {
+  const GemmArgs g{A, B, static_cast<int>(ceil_div(M, tile.bm)), static_cast<int>(ceil_div(N, tile.bn)), splits};
   // as many blocks as the chip holds (of the smallest tile, which waits for memory, one for every tile)
   const unsigned tiles = static_cast<unsigned>(g.tiles_m * g.tiles_n * splits), most = tile.bm == 256 ? kChipBlocks : 2 * kChipBlocks;
   const dim3 grid(tile.bn < 128 || tiles < most ? tiles : most);
-  const auto go = [&](auto pairs) {
-    constexpr int P = decltype(pairs)::value;
-    if (tile.bm == 256) {
-      if constexpr (P == 1 || (AK && BK)) hipLaunchKernelGGL((gemm_kernel<256, 256, 2, 4, AK, BK, P, Epilogue>), grid, dim3(512), 0, s, g, e);
-      else return hipErrorInvalidValue;
-    } else if (tile.bn == 128) hipLaunchKernelGGL((gemm_kernel<128, 128, 2, 2, AK, BK, P, Epilogue>), grid, dim3(256), 0, s, g, e);
-    else if constexpr (BK) hipLaunchKernelGGL((gemm_kernel<128, 32, 4, 1, AK, BK, P, Epilogue>), grid, dim3(256), 0, s, g, e);
+  if (tile.bm == 256) {
+    if constexpr (!Epilogue::kWide) hipLaunchKernelGGL((gemm_kernel<256, 256, 2, 4, AK, BK, Epilogue>), grid, dim3(512), 0, s, g, e);
     else return hipErrorInvalidValue;
-    return hipGetLastError();
-  };
-  if constexpr (Epilogue::kWide == 0) return go(std::integral_constant<int, 1>{});
-  else if constexpr (Epilogue::kWide == 1) return go(std::integral_constant<int, 6>{});
-  else return parts == 1 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 6>{});
+  } else if (tile.bn == 128) {
+    hipLaunchKernelGGL((gemm_kernel<128, 128, 2, 2, AK, BK, Epilogue>), grid, dim3(256), 0, s, g, e);
+  } else {
+    if constexpr (BK) hipLaunchKernelGGL((gemm_kernel<128, 32, 4, 1, AK, BK, Epilogue>), grid, dim3(256), 0, s, g, e);
+    else return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
 }
 
-// the largest tile of which there are enough for the chip.  (For the gradients' products of fp32 operands the middle one: the largest
-// one's registers do not hold what the six products of parts need besides.  us, 2048 tokens, C = 768, 50257 rows, g_W, largest / middle: 1257 / 1155.)
+// the largest tile of which there are enough for the chip (of fp32 operands the middle one: the largest one's registers do not hold their
+// numbers and parts besides the sums)
 // The smallest one for the few tokens of a step of decoding, or where the middle one leaves half the chip without work; `parts`: into how
 // many the depth can be split.  (us, 333 tokens, C = 520, 1003 rows, logits and g_h, middle / smallest: 16.4, 12.4 / 11.0, 7.8.)
 HeadTile tile_for(int64_t M, int64_t N, int64_t parts, bool slim, bool big) {
@@ -770,18 +818,17 @@ HeadTile tile_for(int64_t M, int64_t N, int64_t parts, bool slim, bool big) {
 }  // namespace
 
 HeadPlan::HeadPlan(const mhcl_ends_desc &d, bool grad) {
-  parts = d.io_dtype == MHCL_BF16 ? 1 : 3;
-  pairs = parts == 1 ? 1 : 6;
+  wide = d.io_dtype == MHCL_F32;
   tokens = d.T;
   const int64_t row = ceil_div(d.V, 256) * 256;
-  const int64_t row_bytes = grad ? row * (parts == 1 ? 2 : 4 + 2 * parts) : row / 32 * 8;
+  const int64_t row_bytes = grad ? row * (wide ? 4 : 2) : row / 32 * 8;
   const int64_t fit = static_cast<int64_t>(MHCL_HEAD_BLOCK_BYTES) / row_bytes / 256 * 256;
   if (tokens > fit) tokens = fit < 256 ? 256 : fit;
   if (tokens > d.T) tokens = d.T;
-  const int64_t steps = ceil_div(d.V, kBK) * pairs;   // of the product for g_h
-  logits = tile_for(d.V, tokens, 1, true, true);
-  gh = tile_for(d.C, tokens, steps / 8 > 0 ? steps / 8 : 1, true, parts == 1);
-  gw = tile_for(d.C, d.V, 1, false, parts == 1);
+  const int64_t steps = ceil_div(d.V, wide ? 32 : 64);   // of the product for g_h
+  logits = tile_for(d.V, tokens, 1, true, !wide);
+  gh = tile_for(d.C, tokens, steps / 8 > 0 ? steps / 8 : 1, true, !wide);
+  gw = tile_for(d.C, d.V, 1, false, !wide);
   ld = ceil_div(d.V, logits.bm) * logits.bm;   // (what the first product's tiles cover)
   granules = ld / logits.gran;
   gh_splits = 1;
@@ -797,88 +844,88 @@ HeadPlan::HeadPlan(const mhcl_ends_desc &d, bool grad) {
 
 HeadWs::HeadWs(const mhcl_ends_desc &d, bool grad, void *ws) : plan(d, grad) {
   WsCursor c(ws);
-  const size_t T = static_cast<size_t>(plan.tokens), P = plan.parts, V = static_cast<size_t>(d.V), C = static_cast<size_t>(d.C), ld = static_cast<size_t>(plan.ld);
-  hp = grad || P > 1 ? c.take<uint16_t>(P * T * C) : nullptr;
-  Wp = P > 1 ? c.take<uint16_t>(P * V * C) : nullptr;
-  E = grad ? c.take<char>(T * ld * (P == 1 ? 2 : 4)) : nullptr;
-  G = !grad || P == 1 ? reinterpret_cast<uint16_t *>(E) : c.take<uint16_t>(P * T * ld);
+  const size_t T = static_cast<size_t>(plan.tokens), V = static_cast<size_t>(d.V), C = static_cast<size_t>(d.C), es = dtype_bytes(d.io_dtype);
+  hp = grad ? c.take<char>(T * C * es) : nullptr;
+  E = grad ? c.take<char>(T * static_cast<size_t>(plan.ld) * es) : nullptr;
   stat = c.take<float2>(T * static_cast<size_t>(plan.granules));
   zt = c.take<float>(T);
   common = c.take<float>(1);
   slabs = plan.gh_splits > 1 ? c.take<float>(static_cast<size_t>(plan.gh_splits) * T * C) : nullptr;
-  gW = grad && P == 1 && plan.tokens < d.T ? c.take<float>(V * C) : nullptr;
+  gW = grad && !plan.wide && plan.tokens < d.T ? c.take<float>(V * C) : nullptr;
   bytes = c.off;
 }
 
+namespace {
+
+// the head of IO operands (bf16 or fp32)
+template <typename ID, typename IO>
+hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, const ID *targets, const float *weight, float *loss,
+                    float *lse, void *g_h, void *g_W, const HeadWs &w, hipStream_t s) {
+  constexpr bool WIDE = IO::kVec == 4;
+  const HeadPlan &p = w.plan;
+  const bool grad = g_W != nullptr;
+  const int64_t C = d.C, V = d.V, es = WIDE ? 4 : 2;
+  hipError_t e;
+  if (grad) {
+    hipLaunchKernelGGL((common_weight_kernel<ID>), dim3(1), dim3(1024), 0, s, targets, weight, d.T, w.common);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  int gran_log2 = 0;
+  while ((1 << gran_log2) < p.logits.gran) ++gran_log2;
+  for (int64_t t0 = 0; t0 < d.T; t0 += p.tokens) {
+    const int64_t T = d.T - t0 < p.tokens ? d.T - t0 : p.tokens;
+    const void *hb = static_cast<const char *>(h) + t0 * C * es;
+    const ID *y = targets + t0;
+    const Operand Wk{W, C, V, C}, hk{hb, C, T, C};
+    const RowArgs a{hb, weight ? weight + t0 : nullptr, w.common, w.stat, w.zt, loss + t0, lse + t0, w.E, w.hp, T, p.ld, p.granules, d.V, d.C, gran_log2};
+    if (!grad) {
+      const LogitsEpilogue<ID, false, WIDE> ep{y, w.stat, w.zt, w.E, T, V, p.ld, p.granules};
+      if ((e = launch_gemm<true, true>(p.logits, Wk, hk, V, T, 1, ep, s)) != hipSuccess) return e;
+      // (us, 50257 rows in granules of 32: a wave / a block of sixteen for one token 11.2 / 4.6)
+      if (T < 1024) hipLaunchKernelGGL((loss_kernel<ID, 16>), dim3(static_cast<unsigned>(T)), dim3(1024), 0, s, a, y);
+      else hipLaunchKernelGGL((loss_kernel<ID, 1>), dim3(blocks(T, kBlock / 64)), dim3(kBlock), 0, s, a, y);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      continue;
+    }
+    {
+      const LogitsEpilogue<ID, true, WIDE> ep{y, w.stat, w.zt, w.E, T, V, p.ld, p.granules};
+      if ((e = launch_gemm<true, true>(p.logits, Wk, hk, V, T, 1, ep, s)) != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((row_kernel<ID, IO>), dim3(static_cast<unsigned>(T)), dim3(kBlock), 0, s, a, y);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    // g_h [T, C]: m over C, k over the vocabulary
+    {
+      const Operand Wm{W, C, C, V}, gk{w.E, p.ld, T, p.ld};
+      void *out = static_cast<char *>(g_h) + t0 * C * es;
+      const StoreEpilogue<WIDE> ep{w.common, p.gh_splits > 1 ? w.slabs : (WIDE ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out),
+                                   nullptr, C, T, T * C};
+      if ((e = launch_gemm<false, true>(p.gh, Wm, gk, C, T, p.gh_splits, ep, s)) != hipSuccess) return e;
+      if (p.gh_splits > 1) {
+        hipLaunchKernelGGL((slab_sum_kernel<IO>), dim3(blocks(T * C, kBlock * 4)), dim3(kBlock), 0, s, w.slabs, out, p.gh_splits, T * C);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
+    }
+    // g_W [V, C]: m over C, n over the vocabulary, k over the tokens; the blocks of tokens add up in fp32
+    {
+      const Operand hm{w.hp, C, C, T}, gm{w.E, p.ld, p.ld, T};
+      const bool last = t0 + T == d.T;
+      float *sums = WIDE ? static_cast<float *>(g_W) : w.gW;
+      const StoreEpilogue<WIDE> ep{w.common, WIDE || !last ? sums : nullptr, static_cast<uint16_t *>(g_W), t0 > 0 ? sums : nullptr, C, V, 0};
+      if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, 1, ep, s)) != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
 hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, const void *targets, const float *weight,
                        float *loss, float *lse, void *g_h, void *g_W, const HeadWs &w, hipStream_t s) {
-  return dispatch_id(d.id_dtype, [&](auto id) -> hipError_t {
-    using ID = decltype(id);
-    const HeadPlan &p = w.plan;
-    const bool grad = g_W != nullptr, wide = p.parts > 1;
-    const int64_t C = d.C, V = d.V, esize = wide ? 4 : 2;
-    const ID *all = static_cast<const ID *>(targets);
-    hipError_t e;
-    if (wide) {
-      hipLaunchKernelGGL(split_kernel, dim3(blocks(V * C, kBlock * 8)), dim3(kBlock), 0, s, static_cast<const float *>(W), w.Wp, V * C, V * C);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    if (grad) {
-      hipLaunchKernelGGL((common_weight_kernel<ID>), dim3(1), dim3(1024), 0, s, all, weight, d.T, w.common);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    const uint16_t *Wb = wide ? w.Wp : static_cast<const uint16_t *>(W);
-    for (int64_t t0 = 0; t0 < d.T; t0 += p.tokens) {
-      const int64_t T = d.T - t0 < p.tokens ? d.T - t0 : p.tokens;
-      const void *hb = static_cast<const char *>(h) + t0 * C * esize;
-      const ID *y = all + t0;
-      if (wide) {
-        hipLaunchKernelGGL(split_kernel, dim3(blocks(T * C, kBlock * 8)), dim3(kBlock), 0, s, static_cast<const float *>(hb), w.hp, T * C, T * C);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-      }
-      const Operand Wk{Wb, C, V * C, V, C}, hk{wide ? w.hp : static_cast<const uint16_t *>(hb), C, T * C, T, C};
-      const auto logits = [&](auto store, auto is_wide) {
-        const LogitsEpilogue<ID, decltype(store)::value, decltype(is_wide)::value> ep{y, w.stat, w.zt, w.E, T, V, p.ld, p.granules};
-        return launch_gemm<true, true>(p.logits, Wk, hk, V, T, p.parts, 1, ep, s);
-      };
-      if (grad) e = wide ? logits(std::true_type{}, std::true_type{}) : logits(std::true_type{}, std::false_type{});
-      else e = wide ? logits(std::false_type{}, std::true_type{}) : logits(std::false_type{}, std::false_type{});
-      if (e != hipSuccess) return e;
-      int gran_log2 = 0;
-      while ((1 << gran_log2) < p.logits.gran) ++gran_log2;
-      const RowArgs a{hb, weight ? weight + t0 : nullptr, w.common, w.stat, w.zt, loss + t0, lse + t0, w.E, w.G, w.hp, T, p.ld, p.granules, d.V, d.C, gran_log2};
-      if (!grad) {
-        // (us, 50257 rows in granules of 32: a wave / a block of sixteen for one token 11.2 / 4.6)
-        if (T < 1024) hipLaunchKernelGGL((loss_kernel<ID, 16>), dim3(static_cast<unsigned>(T)), dim3(1024), 0, s, a, y);
-        else hipLaunchKernelGGL((loss_kernel<ID, 1>), dim3(blocks(T, kBlock / 64)), dim3(kBlock), 0, s, a, y);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-        continue;
-      }
-      if (wide) hipLaunchKernelGGL((row_kernel<ID, 3>), dim3(static_cast<unsigned>(T)), dim3(kBlock), 0, s, a, y);
-      else hipLaunchKernelGGL((row_kernel<ID, 1>), dim3(static_cast<unsigned>(T)), dim3(kBlock), 0, s, a, y);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-      // g_h [T, C]: m over C, k over the vocabulary
-      {
-        const Operand Wm{Wb, C, V * C, C, V}, gk{w.G, p.ld, T * p.ld, T, p.ld};
-        void *out = static_cast<char *>(g_h) + t0 * C * esize;
-        StoreEpilogue ep{w.common, p.gh_splits > 1 ? w.slabs : (wide ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out), nullptr, C, T, T * C};
-        if ((e = launch_gemm<false, true>(p.gh, Wm, gk, C, T, p.parts, p.gh_splits, ep, s)) != hipSuccess) return e;
-        if (p.gh_splits > 1) {
-          if (wide) hipLaunchKernelGGL((slab_sum_kernel<F32>), dim3(blocks(T * C, kBlock * 4)), dim3(kBlock), 0, s, w.slabs, out, p.gh_splits, T * C);
-          else hipLaunchKernelGGL((slab_sum_kernel<BF16>), dim3(blocks(T * C, kBlock * 4)), dim3(kBlock), 0, s, w.slabs, out, p.gh_splits, T * C);
-          if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
-      }
-      // g_W [V, C]: m over C, n over the vocabulary, k over the tokens; the blocks of tokens add up in fp32
-      {
-        const Operand hm{w.hp, C, T * C, C, T}, gm{w.G, p.ld, T * p.ld, p.ld, T};
-        const bool last = t0 + T == d.T;
-        float *sums = wide ? static_cast<float *>(g_W) : w.gW;
-        StoreEpilogue ep{w.common, wide || !last ? sums : nullptr, static_cast<uint16_t *>(g_W), t0 > 0 ? sums : nullptr, C, V, 0};
-        if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, p.parts, 1, ep, s)) != hipSuccess) return e;
-      }
-    }
-    return hipSuccess;
+  return dispatch_id(d.id_dtype, [&](auto id) {
+    return dispatch_io(d.io_dtype, [&](auto io) {
+      using ID = decltype(id);
+      return run_head<ID, decltype(io)>(d, h, W, static_cast<const ID *>(targets), weight, loss, lse, g_h, g_W, w, s);
+    });
   });
 }
 

@@ -112,3 +112,16 @@ def test_tensors_of_the_cpu_are_left_to_python_and_refused():
 def test_a_shared_table_has_to_fit():
     with pytest.raises(ValueError, match="table must be"):
         ends.Head(10, 64, dtype=torch.bfloat16, device="cpu", table=torch.nn.Parameter(torch.ones(10, 64)))
+
+
+@pytest.mark.parametrize("io", ["BF16", "F32"])
+def test_the_head_s_vocabulary_is_bounded_where_its_offsets_are(io):
+    kw = dict(io_dtype=getattr(mhcl, io), w_dtype=getattr(mhcl, io))
+    most = 2 ** 22 - 256       # 256 rows of as many numerators of two bytes, or 128 of four, are just under 2^31 bytes
+    for op in (mhcl.OP_HEAD_LOSS, mhcl.OP_HEAD_LOSS_GRAD):
+        assert _bytes(_desc(V=most, **kw), op) > 0
+        assert _bytes(_desc(V=most + 1, **kw), op) == 0
+    d = _desc(V=most + 1, **kw)
+    for name in ("head", "head_grad"):
+        assert _calls(d)[name]() == 2, name
+    assert _bytes(_desc(V=most + 1, **kw), mhcl.OP_EMBED_BWD) > 0      # a table may have more
