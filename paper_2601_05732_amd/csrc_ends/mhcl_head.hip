@@ -144,7 +144,13 @@ __device__ __forceinline__ Eight wide_fragment(const uint4 *tile, int at, int f)
 struct Parts {
   u32x4 p[3];
 };
+// The rest after a part is a product of the pair of parts with (-1, 0) or (0, -1) added to the number: one instruction, and exact, since the
+// rest is one of the fp32 numbers.  (An infinity's rest is NaN and its neighbour's too: both meet in the same sums.)
 __device__ __forceinline__ Parts parts_of(const Eight &e) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  uint32_t first = 0x0000bf80u, second = 0xbf800000u;
+  asm("" : "+s"(first));      // (as a constant in the instruction it would stand for both halves)
+  asm("" : "+s"(second));
   Parts r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -153,8 +159,9 @@ __device__ __forceinline__ Parts parts_of(const Eight &e) {
     for (int k = 0; k < 3; ++k) {
       const uint32_t two = cvt_pk_bf16(lo, hi);
       r.p[k][i] = two;
-      lo -= bf16lo(two);
-      hi -= bf16hi(two);
+      const bf16x2 pair = __builtin_bit_cast(bf16x2, two);
+      lo = __builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(bf16x2, first), lo, false);
+      hi = __builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(bf16x2, second), hi, false);
     }
   }
   return r;
