@@ -204,11 +204,24 @@ __device__ __forceinline__ void tile_of(const GemmArgs &g, int b, int &tm, int &
 // A block of WM x WN waves computes BM x BN tiles; wave (wm, wn) rows wm BM / WM of one and columns wn BN / WN on.
 // The epilogue gets acc[fm][fn]: lane (r, q) holds m = 16 fm + 4 q + 0..3 of the wave's rows, n = 16 fn + r of its columns.
 // The next tile's first loads are on their way during the epilogue, and the epilogue's stores during the next tile's first step.
-template <int BM, int BN, int WM, int WN, bool AK, bool BK, typename Epilogue>
+// STAGES steps' tiles are in LDS or on their way there: two where products hide the way, four of the smallest tile, whose products are few
+// (us, 333 tokens, C = 520, 1003 rows, logits / g_h: two 11.0 / 7.6, four 8.1 / 6.4; four of the middle tile are none the faster
+// where there are few blocks, g_W 9.1 / 10.4).
+template <int BM, int BN, int WM, int WN, int STAGES, bool AK, bool BK, typename Epilogue>
 __global__ __launch_bounds__(WM *WN * 64, 2) void gemm_kernel(const GemmArgs g, const Epilogue epilogue) {
   constexpr bool WIDE = Epilogue::kWide;
   constexpr int NT = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
-  __shared__ uint4 a0[BM * 8], a1[BM * 8], b0[BN * 8], b1[BN * 8];
+  static_assert(STAGES == 2 || STAGES == 4, "the loop over steps");
+  // A's and B's tile of a stage.  Four stages' lie in an array each: of more arrays the compiler does not keep apart which loads fill which, and
+  // waits for all of them.  (Two stages' in one array each: 1 % slower, 16384 tokens, C = 4096, 65536 rows.)
+  constexpr int TA = BM * 8, TB = BN * 8;
+  constexpr bool FOUR = STAGES == 4;
+  __shared__ uint4 m0[FOUR ? TA + TB : TA], m1[FOUR ? TA + TB : TA], m2[FOUR ? TA + TB : 1], m3[FOUR ? TA + TB : 1];
+  __shared__ uint4 n0[FOUR ? 1 : TB], n1[FOUR ? 1 : TB];
+  struct Stage {
+    uint4 *a, *b;
+  };
+  const Stage s0{m0, FOUR ? m0 + TA : n0}, s1{m1, FOUR ? m1 + TA : n1}, s2{m2, m2 + TA}, s3{m3, m3 + TA};
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
   TileLoader<BM, NT, AK, WIDE> la;
   TileLoader<BN, NT, BK, WIDE> lb;
@@ -239,23 +252,26 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gemm_kernel(const GemmArgs g, 
   };
   constexpr int HM = FM / 2;
   const int at_a = lane_at<BM, AK, WIDE>(wm * FM), at_b = lane_at<BN, BK, WIDE>(wn * FN);
-  const auto piece_of = [&](uint4 *a, uint4 *b, int p) __attribute__((always_inline)) {
-    if (p < la.PER) la.piece(a, wave, p);
-    else if (p < la.PER + lb.PER) lb.piece(b, wave, p - la.PER);
+  const auto piece_of = [&](const Stage &st, int p) __attribute__((always_inline)) {
+    if (p < la.PER) la.piece(st.a, wave, p);
+    else if (p < la.PER + lb.PER) lb.piece(st.b, wave, p - la.PER);
   };
+  // The oldest of STAGES stages has arrived, whatever has been asked for since.
+  constexpr int PER = la.PER + lb.PER;
+  const auto wait_stage = [&]() __attribute__((always_inline)) { wait_all_but<(STAGES - 2) * PER>(); };
   // A step is four groups of products, (k half s, half hm of the rows), whose fragments are read one group ahead.  Once the last
   // group's have arrived the stage is free and the next one's tiles are needed: there the waves meet, and
   // the next step's first fragments are on their way while the last group multiplies.
   u32x4 fa[2][HM], fb[2][FN];
-  const auto read_a = [&](const uint4 *a, int s, int hm) __attribute__((always_inline)) {
+  const auto read_a = [&](const Stage &st, int s, int hm) __attribute__((always_inline)) {
     const int here = formed_here<AK>(at_a);
 #pragma unroll
-    for (int i = 0; i < HM; ++i) fa[hm][i] = fragment<BM, AK>(a, here, hm * HM + i, s);
+    for (int i = 0; i < HM; ++i) fa[hm][i] = fragment<BM, AK>(st.a, here, hm * HM + i, s);
   };
-  const auto read_b = [&](const uint4 *b, int s) __attribute__((always_inline)) {
+  const auto read_b = [&](const Stage &st, int s) __attribute__((always_inline)) {
     const int here = formed_here<BK>(at_b);
 #pragma unroll
-    for (int j = 0; j < FN; ++j) fb[s][j] = fragment<BN, BK>(b, here, j, s);
+    for (int j = 0; j < FN; ++j) fb[s][j] = fragment<BN, BK>(st.b, here, j, s);
   };
   // one row of fragments after the other, `between(i)` after row i
   const auto products = [&](int s, int hm, auto between) __attribute__((always_inline)) {
@@ -270,24 +286,24 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gemm_kernel(const GemmArgs g, 
     }
   };
   const auto nothing = [](int) {};
-  const auto step = [&](uint4 *a, uint4 *b, const uint4 *a_next, const uint4 *b_next) __attribute__((always_inline)) {
-    read_a(a, 0, 1);
+  const auto step = [&](const Stage &st, const Stage &st_next) __attribute__((always_inline)) {
+    read_a(st, 0, 1);
     products(0, 0, nothing);
-    read_b(b, 1);
-    read_a(a, 1, 0);
+    read_b(st, 1);
+    read_a(st, 1, 0);
     products(0, 1, nothing);
-    read_a(a, 1, 1);
+    read_a(st, 1, 1);
     products(1, 0, nothing);
-    wait_all();
+    wait_stage();
     barrier();
-    read_a(a_next, 0, 0);
-    read_b(b_next, 0);
+    read_a(st_next, 0, 0);
+    read_b(st_next, 0);
     aim();
     // the tiles after the next take this step's place
     products(1, 1, [&](int i) __attribute__((always_inline)) {
-      constexpr int EACH = (la.PER + lb.PER + HM - 1) / HM;
+      constexpr int EACH = (PER + HM - 1) / HM;
 #pragma unroll
-      for (int p = i * EACH; p < (i + 1) * EACH; ++p) piece_of(a, b, p);
+      for (int p = i * EACH; p < (i + 1) * EACH; ++p) piece_of(st, p);
     });
     next();
   };
@@ -295,15 +311,15 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gemm_kernel(const GemmArgs g, 
   // step's under the second one's.
   Eight ea[HM], eb[FN];
   Parts pa[HM], pb[FN];
-  const auto read_wide_a = [&](const uint4 *a, int hm) __attribute__((always_inline)) {
+  const auto read_wide_a = [&](const Stage &st, int hm) __attribute__((always_inline)) {
     const int here = formed_here<AK>(at_a);
 #pragma unroll
-    for (int i = 0; i < HM; ++i) ea[i] = wide_fragment<BM, AK>(a, here, hm * HM + i);
+    for (int i = 0; i < HM; ++i) ea[i] = wide_fragment<BM, AK>(st.a, here, hm * HM + i);
   };
-  const auto read_wide_b = [&](const uint4 *b) __attribute__((always_inline)) {
+  const auto read_wide_b = [&](const Stage &st) __attribute__((always_inline)) {
     const int here = formed_here<BK>(at_b);
 #pragma unroll
-    for (int j = 0; j < FN; ++j) eb[j] = wide_fragment<BN, BK>(b, here, j);
+    for (int j = 0; j < FN; ++j) eb[j] = wide_fragment<BN, BK>(st.b, here, j);
   };
   const auto wide_products = [&](int hm, auto between) __attribute__((always_inline)) {
     constexpr int A[6] = {1, 0, 2, 0, 1, 0}, B[6] = {1, 2, 0, 1, 0, 0};
@@ -316,80 +332,96 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gemm_kernel(const GemmArgs g, 
       between(k);
     }
   };
-  const auto wide_step = [&](uint4 *a, uint4 *b, const uint4 *a_next, const uint4 *b_next) __attribute__((always_inline)) {
+  const auto wide_step = [&](const Stage &st, const Stage &st_next) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < FN; ++j) pb[j] = parts_of(eb[j]);
 #pragma unroll
     for (int i = 0; i < HM; ++i) pa[i] = parts_of(ea[i]);
-    read_wide_a(a, 1);
+    read_wide_a(st, 1);
     wide_products(0, nothing);
 #pragma unroll
     for (int i = 0; i < HM; ++i) pa[i] = parts_of(ea[i]);
     __builtin_amdgcn_sched_barrier(0);
-    wait_all();
+    wait_stage();
     barrier();
-    read_wide_a(a_next, 0);
-    read_wide_b(b_next);
+    read_wide_a(st_next, 0);
+    read_wide_b(st_next);
     aim();
     wide_products(1, [&](int k) __attribute__((always_inline)) {
-      constexpr int EACH = (la.PER + lb.PER + 5) / 6;
+      constexpr int EACH = (PER + 5) / 6;
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int p = k * EACH; p < (k + 1) * EACH; ++p) piece_of(a, b, p);
+      for (int p = k * EACH; p < (k + 1) * EACH; ++p) piece_of(st, p);
       __builtin_amdgcn_sched_barrier(0);
     });
     next();
   };
-  const auto load = [&](uint4 *a, uint4 *b) __attribute__((always_inline)) {
+  const auto load = [&](const Stage &st) __attribute__((always_inline)) {
     aim();
 #pragma unroll
-    for (int p = 0; p < la.PER + lb.PER; ++p) piece_of(a, b, p);
+    for (int p = 0; p < PER; ++p) piece_of(st, p);
     next();
   };
-  begin();
-  load(a0, b0);
-  load(a1, b1);
+  const auto fill = [&]() __attribute__((always_inline)) {
+    begin();
+    load(s0);
+    load(s1);
+    if constexpr (STAGES == 4) {
+      load(s2);
+      load(s3);
+    }
+  };
+  const auto any_step = [&](const Stage &st, const Stage &st_next) __attribute__((always_inline)) {
+    if constexpr (WIDE) wide_step(st, st_next);
+    else step(st, st_next);
+  };
+  fill();
   bool stored = false;            // whether every wave's stores of the last epilogue were what stores<>() says at least
   for (;;) {
-    if (stored) wait_all_but<la.PER + lb.PER + Epilogue::template stores<FM, FN>()>();
-    else wait_all();
+    if (stored) wait_all_but<(STAGES - 1) * PER + Epilogue::template stores<FM, FN>()>();
+    else wait_all_but<(STAGES - 1) * PER>();
     barrier();
     if constexpr (WIDE) {
-      read_wide_a(a0, 0);
-      read_wide_b(b0);
+      read_wide_a(s0, 0);
+      read_wide_b(s0);
     } else {
-      read_a(a0, 0, 0);
-      read_b(b0, 0);
+      read_a(s0, 0, 0);
+      read_b(s0, 0);
     }
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // (steps in pairs, so that a stage's place is known where it is read; after an odd last one a step of zeros)
-    for (int left = to_do; left > 0; left -= 2) {
-      if constexpr (WIDE) {
-        wide_step(a0, b0, a1, b1);
-        wide_step(a1, b1, a0, b0);
-      } else {
-        step(a0, b0, a1, b1);
-        step(a1, b1, a0, b0);
+    // (a stage's place is known where it is read: the steps of two stages in pairs, after an odd last one a step of zeros)
+    if constexpr (STAGES == 2) {
+      for (int left = to_do; left > 0; left -= 2) {
+        any_step(s0, s1);
+        any_step(s1, s0);
       }
+    } else {
+      // (the last ones after the loop: left from its middle, it would wait for all loads at its head)
+      int left = to_do;
+      for (; left >= 4; left -= 4) {
+        any_step(s0, s1);
+        any_step(s1, s2);
+        any_step(s2, s3);
+        any_step(s3, s0);
+      }
+      if (left > 0) any_step(s0, s1);
+      if (left > 1) any_step(s1, s2);
+      if (left > 2) any_step(s2, s3);
     }
-    const int64_t m0 = static_cast<int64_t>(tm) * BM + wm * (FM * 16), n0 = static_cast<int64_t>(tn) * BN + wn * (FN * 16);
+    const int64_t first_m = static_cast<int64_t>(tm) * BM + wm * (FM * 16), first_n = static_cast<int64_t>(tn) * BN + wn * (FN * 16);
     const int this_split = split;
-    const auto held = epilogue.template hold<FN>(n0);
+    const auto held = epilogue.template hold<FN>(first_n);
     // the stages are free once the last loads (of zeros) have arrived and every wave has read its fragments
     wait_all();
     barrier();
     stored = epilogue.whole(static_cast<int64_t>(tm + 1) * BM, static_cast<int64_t>(tn + 1) * BN);
     tile += gridDim.x;
     const bool more = tile < tiles;
-    if (more) {
-      begin();
-      load(a0, b0);
-      load(a1, b1);
-    }
-    epilogue.template operator()<FM, FN>(acc, held, m0, n0, this_split);
+    if (more) fill();
+    epilogue.template operator()<FM, FN>(acc, held, first_m, first_n, this_split);
     if (!more) break;
   }
 }
@@ -802,12 +834,12 @@ hipError_t launch_gemm(const HeadTile &tile, const Operand &A, const Operand &B,
   const unsigned tiles = static_cast<unsigned>(g.tiles_m * g.tiles_n * splits), most = tile.bm == 256 ? kChipBlocks : 2 * kChipBlocks;
   const dim3 grid(tile.bn < 128 || tiles < most ? tiles : most);
   if (tile.bm == 256) {
-    if constexpr (!Epilogue::kWide) hipLaunchKernelGGL((gemm_kernel<256, 256, 2, 4, AK, BK, Epilogue>), grid, dim3(512), 0, s, g, e);
+    if constexpr (!Epilogue::kWide) hipLaunchKernelGGL((gemm_kernel<256, 256, 2, 4, 2, AK, BK, Epilogue>), grid, dim3(512), 0, s, g, e);
     else return hipErrorInvalidValue;
   } else if (tile.bn == 128) {
-    hipLaunchKernelGGL((gemm_kernel<128, 128, 2, 2, AK, BK, Epilogue>), grid, dim3(256), 0, s, g, e);
+    hipLaunchKernelGGL((gemm_kernel<128, 128, 2, 2, 2, AK, BK, Epilogue>), grid, dim3(256), 0, s, g, e);
   } else {
-    if constexpr (BK) hipLaunchKernelGGL((gemm_kernel<128, 32, 4, 1, AK, BK, Epilogue>), grid, dim3(256), 0, s, g, e);
+    if constexpr (BK) hipLaunchKernelGGL((gemm_kernel<128, 32, 4, 1, 4, AK, BK, Epilogue>), grid, dim3(256), 0, s, g, e);
     else return hipErrorInvalidValue;
   }
   return hipGetLastError();
