@@ -845,6 +845,12 @@ hipError_t launch_gemm(const HeadTile &tile, const Operand &A, const Operand &B,
   return hipGetLastError();
 }
 
+template <typename IO>
+hipError_t launch_slab_sum(const float *slabs, void *out, int count, int64_t elems, hipStream_t s) {
+  hipLaunchKernelGGL((slab_sum_kernel<IO>), dim3(blocks(elems, kBlock * 4)), dim3(kBlock), 0, s, slabs, out, count, elems);
+  return hipGetLastError();
+}
+
 // the largest tile of which there are enough for the chip (of fp32 operands the middle one: the largest one's registers do not hold their
 // numbers and parts besides the sums)
 // The smallest one for the few tokens of a step of decoding, or where the middle one leaves half the chip without work; `parts`: into how
@@ -852,6 +858,26 @@ hipError_t launch_gemm(const HeadTile &tile, const Operand &A, const Operand &B,
 HeadTile tile_for(int64_t M, int64_t N, int64_t parts, bool slim, bool big) {
   if (slim && (N <= 64 || ceil_div(M, 128) * ceil_div(N, 128) * parts < kChipBlocks / 2)) return kTileSlim;
   return big && ceil_div(M, 256) * ceil_div(N, 256) >= kChipBlocks ? kTileBig : kTileMid;
+}
+
+// Into how many parts the depth of a product of few tiles is split, each a slab of fp32 sums of its own: the number that is expected to end
+// first, in sixtieths of a step of two blocks on a compute unit.  A block alone there takes 0.7 of that for a step (fp32: 0.55), a part the like of
+// four steps for its first loads and its epilogue, a tile of a slab a sixtieth for being written and read again by every 256 units,
+// and the sum over slabs is a launch.  Parts of fewer than eight steps, or more than 64, are not taken.
+// (us, one part / this many.  g_W of 7043 tokens, C = 560, 955 rows, bf16, 40 tiles, 6: 83.7 / 25.0; of 7621 tokens, C = 3768, 1317 rows, fp32, 330
+// tiles, 3: 674 / 522.  g_h of 1000 tokens, C = 1024, 20000 rows, bf16, 64 tiles, 4 / 8: 69.1 / 52.9.)
+int splits_for(const HeadTile &tile, int64_t M, int64_t N, int64_t steps, bool wide) {
+  const int64_t tiles = ceil_div(M, tile.bm) * ceil_div(N, tile.bn);
+  int best = 1;
+  int64_t least = 0;
+  for (int k = 1; k == 1 || (k <= 64 && k <= steps / 8); ++k) {
+    const int64_t parts = tiles * k, rest = parts % (2 * kChipBlocks);
+    const int64_t step = tile.bm == 256 ? ceil_div(parts, kChipBlocks) * 60
+                                        : parts / (2 * kChipBlocks) * 60 + (rest == 0 ? 0 : rest > kChipBlocks ? 60 : wide ? 33 : 42);
+    const int64_t time = step * (ceil_div(steps, k) + 4) + (k > 1 ? parts + 160 : 0);
+    if (k == 1 || time < least) best = k, least = time;
+  }
+  return best;
 }
 
 }  // namespace
@@ -870,15 +896,9 @@ HeadPlan::HeadPlan(const mhcl_ends_desc &d, bool grad) {
   gw = tile_for(d.C, d.V, 1, false, !wide);
   ld = ceil_div(d.V, logits.bm) * logits.bm;   // (what the first product's tiles cover)
   granules = ld / logits.gran;
-  gh_splits = 1;
-  if (grad) {
-    // enough blocks for the chip, each with at least eight steps
-    const int64_t tiles = ceil_div(d.C, gh.bm) * ceil_div(tokens, gh.bn);
-    int64_t k = (2 * kChipBlocks) / (tiles > 0 ? tiles : 1);
-    if (k > steps / 8) k = steps / 8;
-    if (k > 64) k = 64;
-    gh_splits = k < 1 ? 1 : static_cast<int>(k);
-  }
+  gh_splits = grad ? splits_for(gh, d.C, tokens, steps, wide) : 1;
+  // (blocks of tokens add up in fp32 as they are)
+  gw_splits = grad && tokens == d.T ? splits_for(gw, d.C, d.V, ceil_div(tokens, wide ? 32 : 64), wide) : 1;
 }
 
 HeadWs::HeadWs(const mhcl_ends_desc &d, bool grad, void *ws) : plan(d, grad) {
@@ -889,7 +909,8 @@ HeadWs::HeadWs(const mhcl_ends_desc &d, bool grad, void *ws) : plan(d, grad) {
   stat = c.take<float2>(T * static_cast<size_t>(plan.granules));
   zt = c.take<float>(T);
   common = c.take<float>(1);
-  slabs = plan.gh_splits > 1 ? c.take<float>(static_cast<size_t>(plan.gh_splits) * T * C) : nullptr;
+  const size_t gh = plan.gh_splits > 1 ? static_cast<size_t>(plan.gh_splits) * T * C : 0, gw = plan.gw_splits > 1 ? static_cast<size_t>(plan.gw_splits) * V * C : 0;
+  slabs = gh + gw > 0 ? c.take<float>(gh > gw ? gh : gw) : nullptr;
   gW = grad && !plan.wide && plan.tokens < d.T ? c.take<float>(V * C) : nullptr;
   bytes = c.off;
 }
@@ -939,18 +960,18 @@ hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, const
       const StoreEpilogue<WIDE> ep{w.common, p.gh_splits > 1 ? w.slabs : (WIDE ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out),
                                    nullptr, C, T, T * C};
       if ((e = launch_gemm<false, true>(p.gh, Wm, gk, C, T, p.gh_splits, ep, s)) != hipSuccess) return e;
-      if (p.gh_splits > 1) {
-        hipLaunchKernelGGL((slab_sum_kernel<IO>), dim3(blocks(T * C, kBlock * 4)), dim3(kBlock), 0, s, w.slabs, out, p.gh_splits, T * C);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-      }
+      if (p.gh_splits > 1 && (e = launch_slab_sum<IO>(w.slabs, out, p.gh_splits, T * C, s)) != hipSuccess) return e;
     }
     // g_W [V, C]: m over C, n over the vocabulary, k over the tokens; the blocks of tokens add up in fp32
     {
       const Operand hm{w.hp, C, C, T}, gm{w.E, p.ld, p.ld, T};
       const bool last = t0 + T == d.T;
       float *sums = WIDE ? static_cast<float *>(g_W) : w.gW;
-      const StoreEpilogue<WIDE> ep{w.common, WIDE || !last ? sums : nullptr, static_cast<uint16_t *>(g_W), t0 > 0 ? sums : nullptr, C, V, 0};
-      if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, 1, ep, s)) != hipSuccess) return e;
+      const bool split = p.gw_splits > 1;
+      const StoreEpilogue<WIDE> ep{w.common, split ? w.slabs : (WIDE || !last ? sums : nullptr), static_cast<uint16_t *>(g_W), t0 > 0 ? sums : nullptr,
+                                   C, V, V * C};
+      if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, p.gw_splits, ep, s)) != hipSuccess) return e;
+      if (split && (e = launch_slab_sum<IO>(w.slabs, g_W, p.gw_splits, V * C, s)) != hipSuccess) return e;
     }
   }
   return hipSuccess;

@@ -367,6 +367,25 @@ def test_head_blocks_of_tokens(io, T, V):
     _check_head(h, W, targets, rows=128)
 
 
+def test_head_blocks_of_tokens_in_fp32():
+    h, W, targets = _head_inputs(16, 1100, 16, 2 ** 19 + 5, F)
+    d = mhcl.EndsDesc(16, 1100, 1, 2 ** 19 + 5, F, F)
+    assert mhcl.ends_workspace_bytes(d, mhcl.OP_HEAD_LOSS_GRAD) < 3 * 2 ** 30
+    _check_head(h, W, targets, rows=64)
+
+
+@pytest.mark.parametrize("io,T,C,V", [(BF, 7001, 64, 130), (BF, 1030, 136, 90), (F, 3003, 264, 190), (F, 2000, 1000, 700), (F, 33, 64, 9001)])
+def test_head_few_rows_of_the_vocabulary_or_few_tokens(io, T, C, V):
+    # products of few tiles and a long depth, which is split
+    _check_head(*_head_inputs(17, T, C, V, io))
+
+
+@pytest.mark.parametrize("io", [BF, F])
+@pytest.mark.parametrize("C", [8, 32, 40, 64, 96, 104, 128, 136, 192, 200, 256, 264, 328])
+def test_head_every_remainder_of_the_depth(io, C):
+    _check_head(*_head_inputs(C, 37, C, 270, io))
+
+
 # ---------------------------------------------------------------- how they are called
 
 
