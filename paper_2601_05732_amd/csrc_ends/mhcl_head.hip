@@ -44,7 +44,7 @@ struct GemmArgs {
 //   all 64 banks once.
 //  else, bf16: row k holds R / 8 pieces; the pairs of pieces (16 numbers, what a transposing read takes of a row) are exchanged
 //   by k: pair m16 of row k at m16 ^ (k % 4 + 4 (k / 8 % 2)), so that the eight rows that half a wave reads lie in all banks.
-//  else, fp32: row k holds R / 4 pieces; its units of four (16 numbers) are exchanged: unit m16 of row k at m16 ^ (k / 8), so that
+//  else, fp32: row k holds R / 4 pieces; its units of four (16 numbers) are exchanged: unit m16 of row k at m16 ^ (k / 4 % 4), so that
 //   the four rows that a read takes lie in all banks.
 // A thread's pieces lie the same distance apart; the loads' own range check gives zeros past the operand's end.  (Rows of m or n
 // outside of the operand give results that nobody reads.)
@@ -74,7 +74,7 @@ struct TileLoader {
       at = static_cast<uint32_t>((tid >> 3) * o.ld * ES + c * 16);
     } else if constexpr (WIDE) {
       const int slot = tid % PPR;
-      unit = (slot >> 2) << 6;
+      unit = ((slot >> 2) ^ (tid / PPR >> 2 & 3)) << 6;
       at = static_cast<uint32_t>(tid / PPR * o.ld * ES + (slot & 3) * 16);
     } else {
       const int kr = tid / PPR, slot = tid % PPR;
@@ -88,18 +88,19 @@ struct TileLoader {
   __device__ __forceinline__ void piece(uint4 *tile, int wave, int i) const {
     const int range = rest <= 0 ? 0 : (rest > 0x7fffffff ? 0x7fffffff : static_cast<int>(rest));
     uint32_t offset = from + i * apart;
-    if constexpr (!KINNER && WIDE) offset += unit ^ i << 6;
+    if constexpr (!KINNER && WIDE) offset += unit ^ (i & 1) << 7;   // (eight rows on: k / 4 is two more)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, range, 0x00020000),
                                              (lds_void *)(tile + i * NT + wave * 64), 16, offset, 0, 0, 0);
   }
 };
 
-// Fragments of 16 rows, k = 32 s + 8 q .. + 7 for lane (r, q).  lane_at: the lane's place in fragment 0 at s = 0, in bytes.
+// Fragments of 16 rows, k = 32 s + 8 q .. + 7 for lane (r, q); fp32: k = 4 q .. + 3 and 16 + 4 q .. + 3, in both operands alike, so that
+// a lane's first read is the one of bf16.  lane_at: the lane's place in fragment 0 at s = 0, in bytes.
 template <int R, bool KINNER, bool WIDE>
 __device__ __forceinline__ int lane_at() {
   const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-  if constexpr (KINNER) return r * 128 | ((WIDE ? 2 * q : q) ^ ((r >> 1) & 7)) << 4;
-  if constexpr (WIDE) return q * 8 * (R * 4) | q << 6 | r << 2;
+  if constexpr (KINNER) return r * 128 | (q ^ ((r >> 1) & 7)) << 4;
+  if constexpr (WIDE) return q * 4 * (R * 4) | q << 6 | r << 2;
   // 16 lanes read rows k .. k + 3, 32 bytes of each, and get a column of four each
   return (q * 8 + (r >> 2)) * (R * 2) | ((r >> 2) | (q & 1) << 2) << 5 | (r & 3) << 3;
 }
@@ -133,11 +134,11 @@ __device__ __forceinline__ Eight wide_fragment(const uint4 *tile, int at, int f)
   Eight e;
   if constexpr (KINNER) {
     e.v[0] = *reinterpret_cast<const f32x4 *>(p + at + f * 2048);
-    e.v[1] = *reinterpret_cast<const f32x4 *>(p + (at ^ 16) + f * 2048);
+    e.v[1] = *reinterpret_cast<const f32x4 *>(p + (at ^ 64) + f * 2048);
   } else {
     const char *from = p + (at ^ f << 6);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e.v[i / 4][i % 4] = *reinterpret_cast<const float *>(from + i * (R * 4));
+    for (int i = 0; i < 8; ++i) e.v[i / 4][i % 4] = *reinterpret_cast<const float *>(from + (i / 4 * 16 + i % 4) * (R * 4));
   }
   return e;
 }
