@@ -586,13 +586,13 @@ struct StoreEpilogue {
 // alone, so that equal weights do not round a whole gradient's scale (16384 tokens, the mean's 1 / 15560 in bf16: g_h, g_W off by 0.0030 of their
 // 2-norms with the weight in g, 0.0024 without).  The mean's: c = 1 / (targets that are not negative), weight / c = 1.  The caller's: c
 // the largest |weight| of a target that is not negative (1 where that is no positive number).
-template <typename ID>
-__global__ __launch_bounds__(1024) void common_weight_kernel(const ID *__restrict__ targets, const float *__restrict__ weight, int64_t T,
-                                                             float *__restrict__ common) {
-  __shared__ float red[16];
+// (A count and a maximum: the same bits whoever takes them.)
+template <int THREADS, typename ID>
+__device__ __forceinline__ float common_weight(const ID *__restrict__ targets, const float *__restrict__ weight, int64_t T) {
+  __shared__ float red[THREADS / 64];
   float most = 0.f;
   int count = 0;
-  for (int64_t t = threadIdx.x; t < T; t += 1024) {
+  for (int64_t t = threadIdx.x; t < T; t += THREADS) {
     const bool counts = targets[t] >= 0;
     count += counts ? 1 : 0;
     if (weight && counts) most = fmaxf(most, fabsf(weight[t]));
@@ -604,20 +604,28 @@ __global__ __launch_bounds__(1024) void common_weight_kernel(const ID *__restric
   }
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = weight ? most : __int_as_float(count);
   __syncthreads();
-  if (threadIdx.x == 0) {
-    int all = 0;
-    for (int i = 0; i < 16; ++i) {
-      most = fmaxf(most, weight ? red[i] : 0.f);
-      all += weight ? 0 : __float_as_int(red[i]);
-    }
-    if (!weight) most = all > 0 ? 1.f / static_cast<float>(all) : 0.f;
-    *common = most > 0.f && most <= 3.4028235e38f ? most : 1.f;
+  int all = 0;
+  for (int i = 0; i < THREADS / 64; ++i) {
+    most = fmaxf(most, weight ? red[i] : 0.f);
+    all += weight ? 0 : __float_as_int(red[i]);
   }
+  if (!weight) most = all > 0 ? 1.f / static_cast<float>(all) : 0.f;
+  return most > 0.f && most <= 3.4028235e38f ? most : 1.f;
+}
+// Up to so many tokens the rows' kernel takes it itself: each of its blocks, or the first alone where only the products need it.  (us,
+// 333 tokens, C = 520, 1003 rows, bf16, weights, the whole call with a launch for it / without: 31.0 / 29.5.)
+constexpr int64_t kCommonTokens = 1024;
+template <typename ID>
+__global__ __launch_bounds__(1024) void common_weight_kernel(const ID *__restrict__ targets, const float *__restrict__ weight, int64_t T,
+                                                             float *__restrict__ common) {
+  const float c = common_weight<1024>(targets, weight, T);
+  if (threadIdx.x == 0) *common = c;
 }
 
 struct RowArgs {
   const void *h;
-  const float *weight, *common;
+  const float *weight;
+  float *common;
   const float2 *stat;
   const float *zt;
   float *loss, *lse;
@@ -625,6 +633,7 @@ struct RowArgs {
   int64_t T, ld, granules;
   int32_t V;
   int C, gran_log2;
+  bool take_common;     // row_kernel: T is all tokens, and `common` is not there yet
 };
 
 // sum, and the largest, of a value over the WAVES waves of a token
@@ -698,7 +707,14 @@ __global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *
     a.lse[t] = base + logf(sum);
     a.loss[t] = loss;
   }
-  const float given = y < 0 ? 0.f : (a.weight ? a.weight[t] / *a.common : 1.f);
+  float common = 1.f;
+  if (a.take_common) {
+    if (a.weight || t == 0) common = common_weight<kBlock>(targets, a.weight, a.T);
+    if (t == 0 && tid == 0) *a.common = common;
+  } else if (a.weight) {
+    common = *a.common;
+  }
+  const float given = y < 0 ? 0.f : (a.weight ? a.weight[t] / common : 1.f);
   const bool counts = given != 0.f;
   const float weight = y < a.V ? given : bad;
   const float hit = weight * expm1f(-loss);      // p - 1 of the target
@@ -927,7 +943,8 @@ hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, const
   const bool grad = g_W != nullptr;
   const int64_t C = d.C, V = d.V, es = WIDE ? 4 : 2;
   hipError_t e;
-  if (grad) {
+  const bool take_common = d.T <= kCommonTokens && p.tokens == d.T;
+  if (grad && !take_common) {
     hipLaunchKernelGGL((common_weight_kernel<ID>), dim3(1), dim3(1024), 0, s, targets, weight, d.T, w.common);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
@@ -938,7 +955,8 @@ hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, const
     const void *hb = static_cast<const char *>(h) + t0 * C * es;
     const ID *y = targets + t0;
     const Operand Wk{W, C, V, C}, hk{hb, C, T, C};
-    const RowArgs a{hb, weight ? weight + t0 : nullptr, w.common, w.stat, w.zt, loss + t0, lse + t0, w.E, w.hp, T, p.ld, p.granules, d.V, d.C, gran_log2};
+    const RowArgs a{hb, weight ? weight + t0 : nullptr, w.common, w.stat, w.zt, loss + t0, lse + t0, w.E, w.hp, T, p.ld, p.granules, d.V, d.C, gran_log2,
+                    take_common};
     if (!grad) {
       const LogitsEpilogue<ID, false, WIDE> ep{y, w.stat, w.zt, w.E, T, V, p.ld, p.granules};
       if ((e = launch_gemm<true, true>(p.logits, Wk, hk, V, T, 1, ep, s)) != hipSuccess) return e;
