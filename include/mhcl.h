@@ -365,7 +365,8 @@ int mhcl_streams_norm_bwd(const mhcl_ends_desc *desc, const void *x, const float
 
 /* Softmax cross entropy of h W^T with the targets; logits never reach memory.  lse[t] = log sum_v exp(z[t][v]) is written for
  * every token, counted or not.  Logits and sums are fp32, of bf16 operands as they are; fp32 operands enter as three bf16
- * parts each (24 significant bits), six products of parts, so that an infinity among them makes NaN of the logits it meets.
+ * parts each (24 significant bits), six products of parts, so that an infinity among them makes NaN of the logits it meets, and so
+ * does a number past 3.3895e38, which rounds to one.
  * in : h [T,C] io, W [V,C] io, targets [T];  out: loss [T], lse [T] f32 */
 int mhcl_head_loss(const mhcl_ends_desc *desc, const void *h, const void *W, const void *targets, float *loss, float *lse,
                    void *ws, size_t ws_bytes, void *stream);
