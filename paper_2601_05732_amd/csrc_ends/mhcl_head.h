@@ -20,6 +20,7 @@ struct HeadPlan {
   int64_t ld;           // row of the softmax's numerators: V, filled up to whole tiles
   int64_t granules;     // partial sums of a row
   int gh_splits, gw_splits;   // parts of the vocabulary in the product for g_h, of the tokens in that for g_W
+  bool pair;            // the products for g_h and g_W in one launch
   HeadPlan(const mhcl_ends_desc &d, bool grad);
 };
 
@@ -30,7 +31,8 @@ struct HeadWs {
   float2 *stat;         // [tokens][granules] maximum and sum
   float *zt;            // [tokens] the targets' logits
   float *common;        // [1] what all weights are multiples of
-  float *slabs;         // [gh_splits][tokens][C], then [gw_splits][V][C]
+  float *slabs;         // [gh_splits][tokens][C]
+  float *gw_slabs;      // [gw_splits][V][C]
   float *gW;            // [V][C] sums over blocks of tokens
   size_t bytes;
   HeadWs(const mhcl_ends_desc &d, bool grad, void *ws);

@@ -8,6 +8,8 @@
 // exp(z - m) over the rows of the vocabulary that a wave holds (a "granule"), and for the gradients leaves exp(z - m) in 16
 // bits; a pass over a row then joins the granules, knows lse, and turns the numerators into g in place.  (Forming z again
 // instead, once lse is known, is a fourth product: 2 C operations for each number in place of 4 bytes.)
+#include <algorithm>
+
 #include "../csrc/mhcl_common.h"
 #include "mhcl_head.h"
 #include "../csrc/mhcl_mfma.h"
@@ -214,8 +216,9 @@ __device__ __forceinline__ void tile_of(const GemmArgs &g, int b, int &tm, int &
 // 128 x 128 of four waves: fp32, 2048 tokens, C = 768, 50257 rows 0.93 / 0.81 / 0.92 ms, 1.0 to 1.2 PFLOP/s of bf16 products;
 // matrix units busy for 49 % of the cycles, the vector ones, which take the parts, for 36 %.
 // 128 x 32: one token, C = 4096, 50257 rows 70 us, W at 5.9 TB/s.
+// block, blocks: its number of how many.
 template <int BM, int BN, int WM, int WN, int STAGES, bool AK, bool BK, typename Epilogue>
-__global__ __launch_bounds__(WM *WN * 64, 2) void gemm_kernel(const GemmArgs g, const Epilogue epilogue) {
+__device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &epilogue, int block, int blocks) {
   constexpr bool WIDE = Epilogue::kWide;
   constexpr int NT = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
   static_assert(STAGES == 2 || STAGES == 4, "the loop over steps");
@@ -235,7 +238,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gemm_kernel(const GemmArgs g, 
   const int64_t depth = g.A.depth < g.B.depth ? g.B.depth : g.A.depth;
   const int steps = static_cast<int>((depth + la.DEPTH - 1) / la.DEPTH);
   const int tiles = g.tiles_m * g.tiles_n * g.splits;
-  int tile = blockIdx.x, tm, tn, split;
+  int tile = block, tm, tn, split;
   int at, to_load, to_do;         // step of the next load; steps to load, and to multiply
   const auto begin = [&]() __attribute__((always_inline)) {
     tile_of(g, tile, tm, tn, split);
@@ -425,12 +428,28 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gemm_kernel(const GemmArgs g, 
     wait_all();
     barrier();
     stored = epilogue.whole(static_cast<int64_t>(tm + 1) * BM, static_cast<int64_t>(tn + 1) * BN);
-    tile += gridDim.x;
+    tile += blocks;
     const bool more = tile < tiles;
     if (more) fill();
     epilogue.template operator()<FM, FN>(acc, held, first_m, first_n, this_split);
     if (!more) break;
   }
+}
+
+template <int BM, int BN, int WM, int WN, int STAGES, bool AK, bool BK, typename Epilogue>
+__global__ __launch_bounds__(WM *WN * 64, 2) void gemm_kernel(const GemmArgs g, const Epilogue epilogue) {
+  gemm_tiles<BM, BN, WM, WN, STAGES, AK, BK>(g, epilogue, blockIdx.x, gridDim.x);
+}
+
+// The two gradients' products in one launch, where both have few parts: neither needs the other's result.  The first first_blocks blocks
+// take g_h, the others g_W, a part each.  Up to two blocks for a compute unit, though one is there at a time (more than that loses: 7043 tokens,
+// C = 560, 955 rows 79.2 / 90.1).  (us of the whole call with gradients, two launches / one: 333 tokens,
+// C = 520, 1003 rows, bf16 28.4 / 23.1; 8, 256, 600 21.7 / 16.1; 1000, 512, 1000 35.0 / 27.5; 2000, 256, 600, fp32 64.7 / 50.5.)
+template <bool SLIM, typename Epilogue>
+__global__ __launch_bounds__(256, 1) void gemm_pair_kernel(const GemmArgs gh, const Epilogue to_gh, const GemmArgs gw, const Epilogue to_gw, int first_blocks) {
+  const int block = blockIdx.x;
+  if (block < first_blocks) gemm_tiles<128, SLIM ? 32 : 128, SLIM ? 4 : 2, SLIM ? 1 : 2, SLIM ? 4 : 2, false, true>(gh, to_gh, block, first_blocks);
+  else gemm_tiles<128, 128, 2, 2, 2, false, false>(gw, to_gw, block - first_blocks, gridDim.x - first_blocks);
 }
 
 // Four 16-bit results of a lane (r, q) at 16 i + 4 q and as many at 16 (i + 1) + 4 q become eight, for one 16-byte store, at 16 (i + q % 2) +
@@ -850,9 +869,13 @@ hipError_t dispatch_id(int id_dtype, F &&f) {
   return f(int32_t{});
 }
 
+GemmArgs gemm_args(const HeadTile &tile, const Operand &A, const Operand &B, int64_t M, int64_t N, int splits) {
+  return {A, B, static_cast<int>(ceil_div(M, tile.bm)), static_cast<int>(ceil_div(N, tile.bn)), splits};
+}
+
 template <bool AK, bool BK, typename Epilogue>
 hipError_t launch_gemm(const HeadTile &tile, const Operand &A, const Operand &B, int64_t M, int64_t N, int splits, const Epilogue &e, hipStream_t s) {
-  const GemmArgs g{A, B, static_cast<int>(ceil_div(M, tile.bm)), static_cast<int>(ceil_div(N, tile.bn)), splits};
+  const GemmArgs g = gemm_args(tile, A, B, M, N, splits);
   // as many blocks as the chip holds (of the smallest tile, which waits for memory, one for every tile)
   const unsigned tiles = static_cast<unsigned>(g.tiles_m * g.tiles_n * splits), most = tile.bm == 256 ? kChipBlocks : 2 * kChipBlocks;
   const dim3 grid(tile.bn < 128 || tiles < most ? tiles : most);
@@ -886,22 +909,28 @@ HeadTile tile_for(int64_t M, int64_t N, int64_t parts, bool slim, bool big) {
 // Into how many parts the depth of a product of few tiles is split, each a slab of fp32 sums of its own: the number that is expected to end
 // first, in sixtieths of a step of two blocks on a compute unit.  A block alone there takes 0.7 of that for a step (fp32: 0.55), a part the like of
 // four steps for its first loads and its epilogue, a tile of a slab a sixtieth for being written and read again by every 256 units,
-// and the sum over slabs is a launch.  Parts of fewer than eight steps, or more than 64, are not taken.
+// and the sum over slabs is a launch, kSumTime.  Parts of fewer than eight steps, or more than 64, are not taken.
 // (us, one part / this many.  g_W of 7043 tokens, C = 560, 955 rows, bf16, 40 tiles, 6: 83.7 / 25.0; of 7621 tokens, C = 3768, 1317 rows, fp32, 330
 // tiles, 3: 674 / 522.  g_h of 1000 tokens, C = 1024, 20000 rows, bf16, 64 tiles, 4 / 8: 69.1 / 52.9.)
-int splits_for(const HeadTile &tile, int64_t M, int64_t N, int64_t steps, bool wide) {
-  const int64_t tiles = ceil_div(M, tile.bm) * ceil_div(N, tile.bn);
-  int best = 1;
-  int64_t least = 0;
-  for (int k = 1; k == 1 || (k <= 64 && k <= steps / 8); ++k) {
+constexpr int64_t kSumTime = 240;
+struct Split {
+  int64_t tiles, steps;
+  bool alone, wide;      // alone: a block of the tile fills a compute unit
+  Split(const HeadTile &tile, int64_t M, int64_t N, int64_t depth, bool w)
+      : tiles(ceil_div(M, tile.bm) * ceil_div(N, tile.bn)), steps(ceil_div(depth, w ? 32 : 64)), alone(tile.bm == 256), wide(w) {}
+  int64_t time(int k) const {   // without the sum
     const int64_t parts = tiles * k, rest = parts % (2 * kChipBlocks);
-    const int64_t step = tile.bm == 256 ? ceil_div(parts, kChipBlocks) * 60
-                                        : parts / (2 * kChipBlocks) * 60 + (rest == 0 ? 0 : rest > kChipBlocks ? 60 : wide ? 33 : 42);
-    const int64_t time = step * (ceil_div(steps, k) + 4) + (k > 1 ? parts + 160 : 0);
-    if (k == 1 || time < least) best = k, least = time;
+    const int64_t step = alone ? ceil_div(parts, kChipBlocks) * 60
+                               : parts / (2 * kChipBlocks) * 60 + (rest == 0 ? 0 : rest > kChipBlocks ? 60 : wide ? 33 : 42);
+    return step * (ceil_div(steps, k) + 4) + (k > 1 ? parts : 0);
   }
-  return best;
-}
+  int best() const {
+    int k_best = 1;
+    for (int k = 2; k <= 64 && k <= steps / 8; ++k)
+      if (time(k) + kSumTime < time(k_best) + (k_best > 1 ? kSumTime : 0)) k_best = k;
+    return k_best;
+  }
+};
 
 }  // namespace
 
@@ -913,15 +942,25 @@ HeadPlan::HeadPlan(const mhcl_ends_desc &d, bool grad) {
   const int64_t fit = static_cast<int64_t>(MHCL_HEAD_BLOCK_BYTES) / row_bytes / 256 * 256;
   if (tokens > fit) tokens = fit < 256 ? 256 : fit;
   if (tokens > d.T) tokens = d.T;
-  const int64_t steps = ceil_div(d.V, wide ? 32 : 64);   // of the product for g_h
   logits = tile_for(d.V, tokens, 1, true, !wide);
-  gh = tile_for(d.C, tokens, steps / 8 > 0 ? steps / 8 : 1, true, !wide);
+  gh = tile_for(d.C, tokens, std::max<int64_t>(1, ceil_div(d.V, wide ? 32 : 64) / 8), true, !wide);
   gw = tile_for(d.C, d.V, 1, false, !wide);
   ld = ceil_div(d.V, logits.bm) * logits.bm;   // (what the first product's tiles cover)
   granules = ld / logits.gran;
-  gh_splits = grad ? splits_for(gh, d.C, tokens, steps, wide) : 1;
-  // (blocks of tokens add up in fp32 as they are)
-  gw_splits = grad && tokens == d.T ? splits_for(gw, d.C, d.V, ceil_div(tokens, wide ? 32 : 64), wide) : 1;
+  gh_splits = gw_splits = 1;
+  pair = false;
+  if (grad) {
+    const Split h(gh, d.C, tokens, d.V, wide), w(gw, d.C, d.V, tokens, wide);
+    gh_splits = h.best();
+    if (tokens == d.T) gw_splits = w.best();   // (blocks of tokens add up in fp32 as they are)
+    pair = gh.bm < 256 && gw.bm < 256 && h.tiles * gh_splits + w.tiles * gw_splits <= 2 * kChipBlocks;
+    if (pair) {
+      // side by side the shorter one need not be split (us, 333 tokens, C = 520, 1003 rows, bf16, g_h in two parts / one: 23.1 / 20.5)
+      const auto time = [&](int i, int j) { return std::max(h.time(i), w.time(j)) + (i > 1 ? kSumTime : 0) + (j > 1 ? kSumTime : 0); };
+      if (time(1, gw_splits) <= time(gh_splits, gw_splits)) gh_splits = 1;
+      if (time(gh_splits, 1) <= time(gh_splits, gw_splits)) gw_splits = 1;
+    }
+  }
 }
 
 HeadWs::HeadWs(const mhcl_ends_desc &d, bool grad, void *ws) : plan(d, grad) {
@@ -932,8 +971,8 @@ HeadWs::HeadWs(const mhcl_ends_desc &d, bool grad, void *ws) : plan(d, grad) {
   stat = c.take<float2>(T * static_cast<size_t>(plan.granules));
   zt = c.take<float>(T);
   common = c.take<float>(1);
-  const size_t gh = plan.gh_splits > 1 ? static_cast<size_t>(plan.gh_splits) * T * C : 0, gw = plan.gw_splits > 1 ? static_cast<size_t>(plan.gw_splits) * V * C : 0;
-  slabs = gh + gw > 0 ? c.take<float>(gh > gw ? gh : gw) : nullptr;
+  slabs = plan.gh_splits > 1 ? c.take<float>(static_cast<size_t>(plan.gh_splits) * T * C) : nullptr;
+  gw_slabs = plan.gw_splits > 1 ? c.take<float>(static_cast<size_t>(plan.gw_splits) * V * C) : nullptr;
   gW = grad && !plan.wide && plan.tokens < d.T ? c.take<float>(V * C) : nullptr;
   bytes = c.off;
 }
@@ -978,26 +1017,28 @@ hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, const
     }
     hipLaunchKernelGGL((row_kernel<ID, IO>), dim3(static_cast<unsigned>(T)), dim3(kBlock), 0, s, a, y);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    // g_h [T, C]: m over C, k over the vocabulary
-    {
-      const Operand Wm{W, C, C, V}, gk{w.E, p.ld, T, p.ld};
-      void *out = static_cast<char *>(g_h) + t0 * C * es;
-      const StoreEpilogue<WIDE> ep{w.common, p.gh_splits > 1 ? w.slabs : (WIDE ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out),
-                                   nullptr, C, T, T * C};
-      if ((e = launch_gemm<false, true>(p.gh, Wm, gk, C, T, p.gh_splits, ep, s)) != hipSuccess) return e;
-      if (p.gh_splits > 1 && (e = launch_slab_sum<IO>(w.slabs, out, p.gh_splits, T * C, s)) != hipSuccess) return e;
+    // g_h [T, C]: m over C, n over the tokens, k over the vocabulary.  g_W [V, C]: m over C, n over the vocabulary, k over the tokens; the
+    // blocks of tokens add up in fp32.
+    const Operand Wm{W, C, C, V}, gk{w.E, p.ld, T, p.ld}, hm{w.hp, C, C, T}, gm{w.E, p.ld, p.ld, T};
+    void *gh_out = static_cast<char *>(g_h) + t0 * C * es;
+    float *sums = WIDE ? static_cast<float *>(g_W) : w.gW;
+    const StoreEpilogue<WIDE> to_gh{w.common, p.gh_splits > 1 ? w.slabs : (WIDE ? static_cast<float *>(gh_out) : nullptr),
+                                    static_cast<uint16_t *>(gh_out), nullptr, C, T, T * C};
+    const StoreEpilogue<WIDE> to_gw{w.common, p.gw_splits > 1 ? w.gw_slabs : (WIDE || t0 + T < d.T ? sums : nullptr), static_cast<uint16_t *>(g_W),
+                                    t0 > 0 ? sums : nullptr, C, V, V * C};
+    if (p.pair) {
+      const GemmArgs gh = gemm_args(p.gh, Wm, gk, C, T, p.gh_splits), gw = gemm_args(p.gw, hm, gm, C, V, p.gw_splits);
+      const int first = gh.tiles_m * gh.tiles_n * gh.splits;
+      const dim3 grid(first + gw.tiles_m * gw.tiles_n * gw.splits);
+      if (p.gh.bn < 128) hipLaunchKernelGGL((gemm_pair_kernel<true, StoreEpilogue<WIDE>>), grid, dim3(256), 0, s, gh, to_gh, gw, to_gw, first);
+      else hipLaunchKernelGGL((gemm_pair_kernel<false, StoreEpilogue<WIDE>>), grid, dim3(256), 0, s, gh, to_gh, gw, to_gw, first);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    } else {
+      if ((e = launch_gemm<false, true>(p.gh, Wm, gk, C, T, p.gh_splits, to_gh, s)) != hipSuccess) return e;
+      if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, p.gw_splits, to_gw, s)) != hipSuccess) return e;
     }
-    // g_W [V, C]: m over C, n over the vocabulary, k over the tokens; the blocks of tokens add up in fp32
-    {
-      const Operand hm{w.hp, C, C, T}, gm{w.E, p.ld, p.ld, T};
-      const bool last = t0 + T == d.T;
-      float *sums = WIDE ? static_cast<float *>(g_W) : w.gW;
-      const bool split = p.gw_splits > 1;
-      const StoreEpilogue<WIDE> ep{w.common, split ? w.slabs : (WIDE || !last ? sums : nullptr), static_cast<uint16_t *>(g_W), t0 > 0 ? sums : nullptr,
-                                   C, V, V * C};
-      if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, p.gw_splits, ep, s)) != hipSuccess) return e;
-      if (split && (e = launch_slab_sum<IO>(w.slabs, g_W, p.gw_splits, V * C, s)) != hipSuccess) return e;
-    }
+    if (p.gh_splits > 1 && (e = launch_slab_sum<IO>(w.slabs, gh_out, p.gh_splits, T * C, s)) != hipSuccess) return e;
+    if (p.gw_splits > 1 && (e = launch_slab_sum<IO>(w.gw_slabs, g_W, p.gw_splits, V * C, s)) != hipSuccess) return e;
   }
   return hipSuccess;
 }
