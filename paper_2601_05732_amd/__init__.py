@@ -21,4 +21,10 @@ from .ends import (  # noqa: F401,E402
     embed_tokens, embed_tokens_grad, streams_norm, streams_norm_grad, head_loss, head_loss_grad,
     TokenEmbedding, StreamsNorm, Head,
 )
-from .lm import LanguageModel  # noqa: F401,E402
+
+
+def __getattr__(name):
+    if name == "LanguageModel":     # imported when it is asked for: the module is also run by itself (python -m)
+        from .lm import LanguageModel
+        return LanguageModel
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
