@@ -899,10 +899,13 @@ hipError_t launch_slab_sum(const float *slabs, void *out, int count, int64_t ele
 
 // the largest tile of which there are enough for the chip (of fp32 operands the middle one: the largest one's registers do not hold their
 // numbers and parts besides the sums)
-// The smallest one for the few tokens of a step of decoding, or where the middle one leaves half the chip without work; `parts`: into how
-// many the depth can be split.  (us, 333 tokens, C = 520, 1003 rows, logits and g_h, middle / smallest: 16.4, 12.4 / 11.0, 7.8.)
+// The smallest one for the few tokens of a step of decoding, or where the middle one leaves a quarter of the chip without work; `parts`: into
+// how many the depth can be split.  (us, middle / smallest.  Logits and g_h of 333 tokens, C = 520, 1003 rows, bf16 16.4, 12.4 / 11.0, 7.8.  The
+// loss alone, bf16: 1000 tokens, C = 1024, 2000 rows, 128 tiles 22.1 / 17.5; 300, 2048, 8000, 189 tiles 30.5 / 29.5; 600, 256, 5000, 200
+// tiles 13.1 / 14.3; 140, 512, 16000, 250 tiles 14.0 / 15.5; 120, 1024, 30000, 235 tiles 22.7 / 24.3, but 158, 3776, 12304, 194 tiles 47.3 /
+// 36.2.  fp32: 300, 1024, 6000, 141 tiles 54.3 / 39.2.)
 HeadTile tile_for(int64_t M, int64_t N, int64_t parts, bool slim, bool big) {
-  if (slim && (N <= 64 || ceil_div(M, 128) * ceil_div(N, 128) * parts < kChipBlocks / 2)) return kTileSlim;
+  if (slim && (N <= 64 || ceil_div(M, 128) * ceil_div(N, 128) * parts < kChipBlocks * 3 / 4)) return kTileSlim;
   return big && ceil_div(M, 256) * ceil_div(N, 256) >= kChipBlocks ? kTileBig : kTileMid;
 }
 
