@@ -462,19 +462,21 @@ __device__ __forceinline__ uint4 join_pairs(uint2 lower, uint2 upper) {
 }
 
 // ---- epilogues
-// A number e in [0, 1] as 16 bits: 6 of the exponent, 10 of the mantissa (2^-61 .. 1 to 2^-11 of itself, what is less may be 0).  These are
-// bits 28 .. 13 of e 2^-64, which an exponential gives at once.
-constexpr float kCodeExp = -64.f, kCodeScale = 0x1p64f;
-__device__ __forceinline__ uint32_t encode2(float lo, float hi) {   // of two e 2^-64
-  return (__float_as_uint(lo) + 0x1000u) >> 13 | ((__float_as_uint(hi) + 0x1000u) << 3 & 0xffff0000u);
+// A number e in [0, 1] as 16 bits: 6 of the exponent, 10 of the mantissa (2^-62 .. 1 to 2^-11 of itself; what is less is off by up to 2^-63).  These are
+// bits 28 .. 13 of e 2^-64.
+constexpr float kCodeScale = 0x1p-64f;
+__device__ __forceinline__ uint32_t encode2(float lo, float hi) {
+  return (__float_as_uint(lo * kCodeScale) + 0x1000u) >> 13 | ((__float_as_uint(hi * kCodeScale) + 0x1000u) << 3 & 0xffff0000u);
 }
 __device__ __forceinline__ float decode(uint32_t code) { return code ? __uint_as_float((code << 13) + (64u << 23)) : 0.f; }
 
-// exp(x), x <= 0: the library's for fp32 operands; for bf16 ones 2^-64 exp(x) by the instruction (relative error 2^-23 |x|)
+// exp(x), x <= 0: the library's for fp32 operands; for bf16 ones by the instruction, to 2^-23 (1 + |x|) of itself, the rounding of
+// x log2(e) and its own.  (The codes' 2^-64 is a product after it: as a term of the exponent, -64 + x log2(e), it would leave that an ulp of
+// 2^-17 whatever x is, 2.6e-6 of every number and of the sums.)
 template <bool WIDE>
 __device__ __forceinline__ float exp_of(float x) {
   if constexpr (WIDE) return expf(x);
-  return __builtin_amdgcn_exp2f(fmaf(x, kLog2e, kCodeExp));
+  return __builtin_amdgcn_exp2f(x * kLog2e);
 }
 
 // m: vocabulary, n: tokens.  STORE: the numerators too.  WIDE: fp32 numerators.
@@ -558,7 +560,6 @@ struct LogitsEpilogue {
       }
       sum += __shfl_xor(sum, 16, 64);
       sum += __shfl_xor(sum, 32, 64);
-      if constexpr (!WIDE) sum *= kCodeScale;
       if (q == 0 && t < T) stat[t * granules + m0 / (FM * 16)] = make_float2(top, sum);
     }
   }
