@@ -535,6 +535,17 @@ __global__ __launch_bounds__(kBlock) void zero_kernel(uint32_t *__restrict__ p, 
 
 inline unsigned blocks(int64_t items, int64_t each) { return static_cast<unsigned>((items + each - 1) / each); }
 
+// f(first, count) for parts of `items` in turn, until one fails: a launch has to stay below 2^32 threads in x, and has at most half as
+// many here (of `threads` for each item, a power of two).
+constexpr int64_t kLaunchThreads = int64_t{1} << 31;
+template <typename F>
+hipError_t in_launches(int64_t items, int64_t threads, F &&f) {
+  const int64_t most = kLaunchThreads / threads;
+  hipError_t e = hipSuccess;
+  for (int64_t at = 0; at < items && e == hipSuccess; at += most) e = f(at, items - at < most ? items - at : most);
+  return e;
+}
+
 // threads for a row of `pieces` pieces, and for as many rows as a block then has threads for
 inline dim3 row_block(int pieces) {
   int x = 1;
@@ -581,10 +592,10 @@ hipError_t dispatch_streams(int n, F &&f) {
 int32_t EmbedBwdWs::embed_chunk(const mhcl_ends_desc &d) { return d.T < 16384 ? 8 : (d.T < 32768 ? 16 : 32); }
 
 hipError_t launch_zero(void *p, size_t bytes, hipStream_t s) {
-  const size_t words = bytes / 4;
-  if (words == 0) return hipSuccess;
-  hipLaunchKernelGGL(zero_kernel, dim3(blocks(words, kBlock)), dim3(kBlock), 0, s, static_cast<uint32_t *>(p), words);
-  return hipGetLastError();
+  return in_launches(static_cast<int64_t>(bytes / 4), 1, [&](int64_t at, int64_t words) {
+    hipLaunchKernelGGL(zero_kernel, dim3(blocks(words, kBlock)), dim3(kBlock), 0, s, static_cast<uint32_t *>(p) + at, static_cast<size_t>(words));
+    return hipGetLastError();
+  });
 }
 
 hipError_t launch_embed(const mhcl_ends_desc &d, const void *table, const void *ids, void *x, hipStream_t s) {
@@ -593,9 +604,11 @@ hipError_t launch_embed(const mhcl_ends_desc &d, const void *table, const void *
       using IO = decltype(io);
       using ID = decltype(id);
       const dim3 block = row_block(d.C / IO::kVec);
-      hipLaunchKernelGGL((embed_kernel<IO, decltype(w), ID>),
-                         dim3(blocks(d.T, block.y), blocks(d.C / IO::kVec, block.x)), block, 0, s, table, static_cast<const ID *>(ids), x, d.n, d.C, d.T, d.V, d.scale);
-      return hipGetLastError();
+      return in_launches(d.T, block.x, [&](int64_t t0, int64_t T) {
+        hipLaunchKernelGGL((embed_kernel<IO, decltype(w), ID>), dim3(blocks(T, block.y), blocks(d.C / IO::kVec, block.x)), block, 0, s, table,
+                           static_cast<const ID *>(ids) + t0, static_cast<char *>(x) + t0 * d.n * d.C * (16 / IO::kVec), d.n, d.C, T, d.V, d.scale);
+        return hipGetLastError();
+      });
     });
   });
 }
@@ -685,10 +698,14 @@ hipError_t launch_streams_norm(const mhcl_ends_desc &d, const void *x, const flo
     return dispatch_row(d.C / IO::kVec, [&](auto l, auto ch) {
       return dispatch_streams(d.n, [&](auto nn) {
         constexpr int L = decltype(l)::value, CH = decltype(ch)::value, N = decltype(nn)::value;
-        const bool once = d.T * d.n * d.C * static_cast<int64_t>(dtype_bytes(d.io_dtype)) > kLastLevelCache;
-        hipLaunchKernelGGL((once ? norm_kernel<IO, N, L, CH, true> : norm_kernel<IO, N, L, CH, false>), dim3(blocks(d.T, norm_tokens(L))),
-                           dim3(L * norm_tokens(L)), 0, s, x, gain, h, d.n, d.C, d.T, d.eps);
-        return hipGetLastError();
+        constexpr int ES = 16 / IO::kVec;
+        const bool once = d.T * d.n * d.C * ES > kLastLevelCache;
+        return in_launches(d.T, L, [&](int64_t t0, int64_t T) {
+          hipLaunchKernelGGL((once ? norm_kernel<IO, N, L, CH, true> : norm_kernel<IO, N, L, CH, false>), dim3(blocks(T, norm_tokens(L))),
+                             dim3(L * norm_tokens(L)), 0, s, static_cast<const char *>(x) + t0 * d.n * d.C * ES, gain,
+                             static_cast<char *>(h) + t0 * d.C * ES, d.n, d.C, T, d.eps);
+          return hipGetLastError();
+        });
       });
     });
   });
