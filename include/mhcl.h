@@ -381,13 +381,22 @@ int mhcl_head_loss(const mhcl_ends_desc *desc, const void *h, const void *W, con
 int mhcl_head_loss_grad(const mhcl_ends_desc *desc, const void *h, const void *W, const void *targets, const float *weight,
                         float *loss, float *lse, void *g_h, void *g_W, void *ws, size_t ws_bytes, void *stream);
 
+/* The same with g_h and g_W in fp32, not rounded to the operands' type: for gradients that are multiplied by a factor that is known
+ * only later (mhcl_scale_to), which are then rounded once.  Workspace as for mhcl_head_loss_grad.  out: g_h [T,C], g_W [V,C] f32 */
+int mhcl_head_loss_grad_unrounded(const mhcl_ends_desc *desc, const void *h, const void *W, const void *targets, const float *weight,
+                                  float *loss, float *lse, float *g_h, float *g_W, void *ws, size_t ws_bytes, void *stream);
+
 /* The sum of weight[t] loss[t] over the places that hold a target, those of weight 0 left out; weight NULL: their mean, 0 where there is none.
  * Added up in fp64, in a fixed order.  in : targets [T], loss [T] f32, weight [T] f32 or NULL;  out: total [1] f32 */
 int mhcl_head_total(const mhcl_ends_desc *desc, const void *targets, const float *loss, const float *weight, float *total, void *stream);
 
 /* p[i] *= *factor for `count` numbers of a type (MHCL_BF16 | MHCL_F32); `factor` is read on the device, and where it is 1 nothing else
- * is read or written: what a backward does with gradients that were taken for a factor of 1.  p is 16-byte aligned. */
+ * is read or written: what a backward does with gradients that were taken for a factor of 1.  p is 16-byte aligned.
+ * (Numbers of bf16 that a sum was rounded to are rounded once more, unless the factor is a power of two.) */
 int mhcl_scale(void *p, int dtype, int64_t count, const float *factor, void *stream);
+
+/* out[i] = in[i] * *factor, rounded to the type (MHCL_BF16 | MHCL_F32); in and out are 16-byte aligned and apart. */
+int mhcl_scale_to(const float *in, void *out, int dtype, int64_t count, const float *factor, void *stream);
 
 /* ---- measurement aids (no part of the method) --------------------------- */
 

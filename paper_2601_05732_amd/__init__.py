@@ -13,7 +13,7 @@ from .binding import (  # noqa: F401
     STATIC_SCRATCH_BYTES,
     I64, I32, OP_EMBED_BWD, OP_STREAMS_NORM_BWD, OP_HEAD_LOSS, OP_HEAD_LOSS_GRAD, EndsDesc, ends_workspace_bytes,
     mhcl_embed, mhcl_embed_bwd, mhcl_streams_norm, mhcl_streams_norm_bwd, mhcl_head_loss, mhcl_head_loss_grad,
-    mhcl_head_total, mhcl_scale,
+    mhcl_head_total, mhcl_scale, mhcl_scale_to,
 )
 from .layer import GpuLayer, desc_for, empty_stream, place_stream  # noqa: F401,E402
 from .autograd import HyperConnection, HyperConnectionStack, init_params  # noqa: F401,E402

@@ -29,7 +29,7 @@ _SYMBOLS = [
     "mhcl_logits", "mhcl_ds_chain", "mhcl_profile_next_call", "mhcl_debug_copy",
     "mhcl_fwd_coeffs_pre_static", "mhcl_coeffs_logits", "mhcl_coeffs_logits_layers", "mhcl_streams_in", "mhcl_streams_out",
     "mhcl_ends_workspace_bytes", "mhcl_embed", "mhcl_embed_bwd", "mhcl_streams_norm", "mhcl_streams_norm_bwd",
-    "mhcl_head_loss", "mhcl_head_loss_grad", "mhcl_head_total", "mhcl_scale",
+    "mhcl_head_loss", "mhcl_head_loss_grad", "mhcl_head_loss_grad_unrounded", "mhcl_head_total", "mhcl_scale", "mhcl_scale_to",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20   # MHCL_STATIC_SCRATCH_BYTES
 
@@ -151,9 +151,10 @@ def lib():
         L.mhcl_streams_norm.argtypes = [E] + [V] * 4
         L.mhcl_streams_norm_bwd.argtypes = [E] + [V] * 6 + [Z, V]
         L.mhcl_head_loss.argtypes = [E] + [V] * 6 + [Z, V]
-        L.mhcl_head_loss_grad.argtypes = [E] + [V] * 9 + [Z, V]
+        L.mhcl_head_loss_grad.argtypes = L.mhcl_head_loss_grad_unrounded.argtypes = [E] + [V] * 9 + [Z, V]
         L.mhcl_head_total.argtypes = [E] + [V] * 5
         L.mhcl_scale.argtypes = [V, ctypes.c_int, ctypes.c_int64, V, V]
+        L.mhcl_scale_to.argtypes = [V, V, ctypes.c_int, ctypes.c_int64, V, V]
         _lib = L
     return _lib
 
@@ -416,13 +417,17 @@ def mhcl_head_loss(d, h, W, targets, loss, lse, ws):
 
 
 def mhcl_head_loss_grad(d, h, W, targets, weight, loss, lse, g_h, g_W, ws):
+    """g_h and g_W of d's types, or both fp32: not rounded (mhcl_head_loss_grad_unrounded)."""
     f = torch.float32
     wp, wb = _ws(ws)
-    _check(lib().mhcl_head_loss_grad(
+    name, io, w = "mhcl_head_loss_grad", d.io, d.w
+    if g_h.dtype is f and d.io is not f:
+        name, io, w = "mhcl_head_loss_grad_unrounded", f, f
+    _check(getattr(lib(), name)(
         ctypes.byref(d.c), _ptr(h, d.io, (d.T, d.C), "h"), _ptr(W, d.w, (d.V, d.C), "W"),
         _ptr(targets, d.ids, (d.T,), "targets"), None if weight is None else _ptr(weight, f, (d.T,), "weight"),
-        _ptr(loss, f, (d.T,), "loss"), _ptr(lse, f, (d.T,), "lse"), _ptr(g_h, d.io, (d.T, d.C), "g_h"),
-        _ptr(g_W, d.w, (d.V, d.C), "g_W"), wp, wb, _stream()), "mhcl_head_loss_grad")
+        _ptr(loss, f, (d.T,), "loss"), _ptr(lse, f, (d.T,), "lse"), _ptr(g_h, io, (d.T, d.C), "g_h"),
+        _ptr(g_W, w, (d.V, d.C), "g_W"), wp, wb, _stream()), name)
 
 
 def mhcl_head_total(d, targets, loss, weight, total):
@@ -438,3 +443,11 @@ def mhcl_scale(t, factor):
         raise ValueError(f"dtype {t.dtype}: bfloat16 or float32")
     _check(lib().mhcl_scale(_ptr(t, t.dtype, t.shape, "t"), _DTYPE[t.dtype], t.numel(),
                             _ptr(factor.reshape(1), torch.float32, (1,), "factor"), _stream()), "mhcl_scale")
+
+
+def mhcl_scale_to(x, factor, out):
+    """out = x (fp32) * factor, a GPU tensor of one fp32 number, rounded to out's type."""
+    if out.dtype not in _DTYPE:
+        raise ValueError(f"dtype {out.dtype}: bfloat16 or float32")
+    _check(lib().mhcl_scale_to(_ptr(x, torch.float32, out.shape, "x"), _ptr(out, out.dtype, out.shape, "out"), _DTYPE[out.dtype], out.numel(),
+                               _ptr(factor.reshape(1), torch.float32, (1,), "factor"), _stream()), "mhcl_scale_to")

@@ -44,6 +44,24 @@ int check_ends(const mhcl_ends_desc *d, End end) {
     if ((expr) != hipSuccess) return MHCL_ERR_HIP;  \
   } while (0)
 
+// mhcl_head_loss_grad and its unrounded form
+int head_loss_grad(const mhcl_ends_desc *desc, const void *h, const void *W, const void *targets, const float *weight, float *loss,
+                   float *lse, void *g_h, void *g_W, bool unrounded, void *ws, size_t ws_bytes, void *stream) {
+  if (int e = check_ends(desc, End::kHead)) return e;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!all16(g_W)) return MHCL_ERR_INVALID_ARG;
+  if (desc->T == 0) {
+    MHCL_HIP(launch_zero(g_W, static_cast<size_t>(desc->V) * desc->C * (unrounded ? 4 : dtype_bytes(desc->w_dtype)), s));
+    return MHCL_OK;
+  }
+  if (!all16(h, W, (const void *)g_h) || !ids_ok(*desc, targets) || !aligned(loss, 4) || !aligned(lse, 4) ||
+      (weight && !aligned(weight, 4)))
+    return MHCL_ERR_INVALID_ARG;
+  if (!all16(ws) || ws_bytes < mhcl_ends_workspace_bytes(desc, MHCL_OP_HEAD_LOSS_GRAD)) return MHCL_ERR_WORKSPACE;
+  MHCL_HIP(launch_head(*desc, h, W, targets, weight, loss, lse, g_h, g_W, unrounded, HeadWs(*desc, true, ws), s));
+  return MHCL_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -113,26 +131,19 @@ int mhcl_head_loss(const mhcl_ends_desc *desc, const void *h, const void *W, con
   if (desc->T == 0) return MHCL_OK;
   if (!all16(h, W) || !ids_ok(*desc, targets) || !aligned(loss, 4) || !aligned(lse, 4)) return MHCL_ERR_INVALID_ARG;
   if (!all16(ws) || ws_bytes < mhcl_ends_workspace_bytes(desc, MHCL_OP_HEAD_LOSS)) return MHCL_ERR_WORKSPACE;
-  MHCL_HIP(launch_head(*desc, h, W, targets, nullptr, loss, lse, nullptr, nullptr, HeadWs(*desc, false, ws),
+  MHCL_HIP(launch_head(*desc, h, W, targets, nullptr, loss, lse, nullptr, nullptr, false, HeadWs(*desc, false, ws),
                        static_cast<hipStream_t>(stream)));
   return MHCL_OK;
 }
 
 int mhcl_head_loss_grad(const mhcl_ends_desc *desc, const void *h, const void *W, const void *targets, const float *weight,
                         float *loss, float *lse, void *g_h, void *g_W, void *ws, size_t ws_bytes, void *stream) {
-  if (int e = check_ends(desc, End::kHead)) return e;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  if (!all16(g_W)) return MHCL_ERR_INVALID_ARG;
-  if (desc->T == 0) {
-    MHCL_HIP(launch_zero(g_W, static_cast<size_t>(desc->V) * desc->C * dtype_bytes(desc->w_dtype), s));
-    return MHCL_OK;
-  }
-  if (!all16(h, W, (const void *)g_h) || !ids_ok(*desc, targets) || !aligned(loss, 4) || !aligned(lse, 4) ||
-      (weight && !aligned(weight, 4)))
-    return MHCL_ERR_INVALID_ARG;
-  if (!all16(ws) || ws_bytes < mhcl_ends_workspace_bytes(desc, MHCL_OP_HEAD_LOSS_GRAD)) return MHCL_ERR_WORKSPACE;
-  MHCL_HIP(launch_head(*desc, h, W, targets, weight, loss, lse, g_h, g_W, HeadWs(*desc, true, ws), s));
-  return MHCL_OK;
+  return head_loss_grad(desc, h, W, targets, weight, loss, lse, g_h, g_W, false, ws, ws_bytes, stream);
+}
+
+int mhcl_head_loss_grad_unrounded(const mhcl_ends_desc *desc, const void *h, const void *W, const void *targets, const float *weight,
+                                  float *loss, float *lse, float *g_h, float *g_W, void *ws, size_t ws_bytes, void *stream) {
+  return head_loss_grad(desc, h, W, targets, weight, loss, lse, g_h, g_W, true, ws, ws_bytes, stream);
 }
 
 int mhcl_head_total(const mhcl_ends_desc *desc, const void *targets, const float *loss, const float *weight, float *total,
@@ -154,6 +165,14 @@ int mhcl_scale(void *p, int dtype, int64_t count, const float *factor, void *str
   if (count == 0) return MHCL_OK;
   if (!all16(p)) return MHCL_ERR_INVALID_ARG;
   MHCL_HIP(launch_scale(p, dtype, count, factor, static_cast<hipStream_t>(stream)));
+  return MHCL_OK;
+}
+
+int mhcl_scale_to(const float *in, void *out, int dtype, int64_t count, const float *factor, void *stream) {
+  if (!dtype_ok(dtype) || count < 0 || !aligned(factor, 4)) return MHCL_ERR_INVALID_ARG;
+  if (count == 0) return MHCL_OK;
+  if (!all16((const void *)in, out)) return MHCL_ERR_INVALID_ARG;
+  MHCL_HIP(launch_scale_to(in, out, dtype, count, factor, static_cast<hipStream_t>(stream)));
   return MHCL_OK;
 }
 

@@ -38,12 +38,13 @@ struct HeadWs {
   HeadWs(const mhcl_ends_desc &d, bool grad, void *ws);
 };
 
-// g_h, g_W null: the loss alone.  weight null: that of the mean.
+// g_h, g_W null: the loss alone.  weight null: that of the mean.  unrounded: g_h and g_W are fp32, whatever the operands.
 hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, const void *targets, const float *weight,
-                       float *loss, float *lse, void *g_h, void *g_W, const HeadWs &w, hipStream_t s);
+                       float *loss, float *lse, void *g_h, void *g_W, bool unrounded, const HeadWs &w, hipStream_t s);
 
 hipError_t launch_head_total(const mhcl_ends_desc &d, const void *targets, const float *loss, const float *weight, float *total,
                              hipStream_t s);
 hipError_t launch_scale(void *p, int dtype, int64_t count, const float *factor, hipStream_t s);
+hipError_t launch_scale_to(const float *in, void *out, int dtype, int64_t count, const float *factor, hipStream_t s);
 
 }  // namespace mhcl

@@ -116,18 +116,26 @@ std::optional<std::tuple<Tensor, Tensor>> head(const Tensor &h, const Tensor &W,
 }
 
 std::optional<std::tuple<Tensor, Tensor, Tensor, Tensor>> head_grad(const Tensor &h, const Tensor &W, const Tensor &targets,
-                                                                    const std::optional<Tensor> &weight) {
+                                                                    const std::optional<Tensor> &weight, at::ScalarType dtype) {
   const int device = c10::hip::current_device();
   if (!head_ready(h, W, targets, device)) return std::nullopt;
+  const bool unrounded = dtype == at::kFloat && h.scalar_type() != at::kFloat;
+  if (!unrounded && dtype != h.scalar_type()) return std::nullopt;
   if (weight && (weight->dim() != 1 || weight->size(0) != h.size(0) || weight->scalar_type() != at::kFloat || !ready(*weight, device, 4)))
     return std::nullopt;
   const mhcl_ends_desc d =
       describe(1, h.size(1), h.size(0), W.size(0), *type_of(h.scalar_type()), *type_of(W.scalar_type()), &targets, 1., 0.);
-  const Tensor loss = floats(h, {d.T}), lse = floats(h, {d.T}), g_h = at::empty(h.sizes(), h.options()), g_W = at::empty(W.sizes(), W.options());
+  const Tensor loss = floats(h, {d.T}), lse = floats(h, {d.T}), g_h = at::empty(h.sizes(), h.options().dtype(dtype)), g_W = at::empty(W.sizes(), W.options().dtype(unrounded ? dtype : W.scalar_type()));
   const Tensor ws = workspace_of(d, MHCL_OP_HEAD_LOSS_GRAD, h);
-  check(mhcl_head_loss_grad(&d, ptr(h), ptr(W), ptr(targets), weight ? ptr<float>(*weight) : nullptr, ptr<float>(loss), ptr<float>(lse), ptr(g_h),
-                            ptr(g_W), ws.data_ptr(), ws.nbytes(), stream()),
-        "mhcl_head_loss_grad");
+  const float *const weights = weight ? ptr<float>(*weight) : nullptr;
+  if (unrounded)
+    check(mhcl_head_loss_grad_unrounded(&d, ptr(h), ptr(W), ptr(targets), weights, ptr<float>(loss), ptr<float>(lse), ptr<float>(g_h), ptr<float>(g_W),
+                                        ws.data_ptr(), ws.nbytes(), stream()),
+          "mhcl_head_loss_grad_unrounded");
+  else
+    check(mhcl_head_loss_grad(&d, ptr(h), ptr(W), ptr(targets), weights, ptr<float>(loss), ptr<float>(lse), ptr(g_h), ptr(g_W), ws.data_ptr(),
+                              ws.nbytes(), stream()),
+          "mhcl_head_loss_grad");
   return std::make_tuple(loss, lse, g_h, g_W);
 }
 
