@@ -178,17 +178,24 @@ class _HeadTotal(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, h, W, targets, weight):
-        loss, _, g_h, g_W = head_loss_grad(h, W, targets, weight, torch.float32)
-        ctx.grads, ctx.dtype = (g_h, g_W), h.dtype
-        return _total(h, W, targets, loss, weight)
+        if ctx.needs_input_grad[0] or ctx.needs_input_grad[1]:
+            loss, _, *grads = head_loss_grad(h, W, targets, weight, torch.float32)
+        else:
+            loss, grads = head_loss(h, W, targets)[0], [None, None]
+        total = _total(h, W, targets, loss, weight)
+        # (a place of weight 0 adds nothing, whatever it holds)
+        grads.append(loss.masked_fill((weight == 0) & ~loss.isfinite(), 0.0) if ctx.needs_input_grad[3] else None)
+        ctx.grads, ctx.dtypes = grads, (h.dtype, W.dtype, torch.float32)
+        return total
 
     @staticmethod
     def backward(ctx, g):
         if ctx.grads is None:
             raise RuntimeError("the head's gradients went out with its first backward: run the head again for another one")
         grads, ctx.grads = ctx.grads, None
-        g_h, g_W = (_times(t, g, ctx.dtype) if needed else None for t, needed in zip(grads, ctx.needs_input_grad))
-        return g_h, g_W, None, None
+        h, W, _, weight = ctx.needs_input_grad
+        g_h, g_W, g_weight = (_times(t, g, dtype) if needed else None for t, dtype, needed in zip(grads, ctx.dtypes, (h, W, weight)))
+        return g_h, g_W, None, g_weight
 
 
 def _times(t, factor, dtype):
@@ -235,7 +242,7 @@ class StreamsNorm(torch.nn.Module):
 
 class Head(torch.nn.Module):
     """The mean of the softmax cross entropy of h W^T with the next tokens [T] over those that are not negative, or, with weight [T],
-    the sum of weight times it.  W [V, C] is of h's type; `table`: the parameter of an embedding of that type, shared."""
+    the sum of weight times it, whose gradient on weight[t] is the token's cross entropy.  W [V, C] is of h's type; `table`: the parameter of an embedding of that type, shared."""
 
     def __init__(self, V: int, C: int, dtype=torch.bfloat16, std: float = 0.02, device="cuda", table=None):
         super().__init__()
@@ -244,7 +251,7 @@ class Head(torch.nn.Module):
         self.W = table if table is not None else torch.nn.Parameter(torch.empty(V, C, device=device, dtype=dtype).normal_(0.0, std))
 
     def forward(self, h, targets, weight=None):
-        if torch.is_grad_enabled() and (h.requires_grad or self.W.requires_grad):
+        if torch.is_grad_enabled() and (h.requires_grad or self.W.requires_grad or (weight is not None and weight.requires_grad)):
             return _HeadTotal.apply(h, self.W, targets, weight)
         return _total(h, self.W, targets, self.score(h, targets)[0], weight)
 
