@@ -177,14 +177,14 @@ class _HeadTotal(torch.autograd.Function):
     65536 rows, with bf16 gradients kept and multiplied / this: 20800 / 21500; 333, 520, 1003 75 / 81.)"""
 
     @staticmethod
-    def forward(ctx, h, W, targets, weight):
-        if ctx.needs_input_grad[0] or ctx.needs_input_grad[1]:
+    def forward(ctx, h, W, targets, weight, record):
+        if record and (ctx.needs_input_grad[0] or ctx.needs_input_grad[1]):
             loss, _, *grads = head_loss_grad(h, W, targets, weight, torch.float32)
         else:
             loss, grads = head_loss(h, W, targets)[0], [None, None]
         total = _total(h, W, targets, loss, weight)
         # (a place of weight 0 adds nothing, whatever it holds)
-        grads.append(loss.masked_fill((weight == 0) & ~loss.isfinite(), 0.0) if ctx.needs_input_grad[3] else None)
+        grads.append(loss.masked_fill((weight == 0) & ~loss.isfinite(), 0.0) if record and ctx.needs_input_grad[3] else None)
         ctx.grads, ctx.dtypes = grads, (h.dtype, W.dtype, torch.float32)
         return total
 
@@ -193,9 +193,9 @@ class _HeadTotal(torch.autograd.Function):
         if ctx.grads is None:
             raise RuntimeError("the head's gradients went out with its first backward: run the head again for another one")
         grads, ctx.grads = ctx.grads, None
-        h, W, _, weight = ctx.needs_input_grad
+        h, W, _, weight, _ = ctx.needs_input_grad
         g_h, g_W, g_weight = (_times(t, g, dtype) if needed else None for t, dtype, needed in zip(grads, ctx.dtypes, (h, W, weight)))
-        return g_h, g_W, None, g_weight
+        return g_h, g_W, None, g_weight, None
 
 
 def _times(t, factor, dtype):
@@ -251,9 +251,8 @@ class Head(torch.nn.Module):
         self.W = table if table is not None else torch.nn.Parameter(torch.empty(V, C, device=device, dtype=dtype).normal_(0.0, std))
 
     def forward(self, h, targets, weight=None):
-        if torch.is_grad_enabled() and (h.requires_grad or self.W.requires_grad or (weight is not None and weight.requires_grad)):
-            return _HeadTotal.apply(h, self.W, targets, weight)
-        return _total(h, self.W, targets, self.score(h, targets)[0], weight)
+        # (also where no gradient is asked for: a forward-mode tangent is refused there)
+        return _HeadTotal.apply(h, self.W, targets, weight, torch.is_grad_enabled())
 
     @torch.no_grad()
     def score(self, h, targets):

@@ -95,3 +95,28 @@ def test_a_weight_of_zero_keeps_what_a_place_holds_out_of_its_gradient():
     weight.grad = None
     head(h, targets, weight).backward()
     assert torch.isfinite(weight.grad).all() and float(weight.grad[at]) == 0.0    # ... unless that is no number
+
+
+@pytest.mark.parametrize("which", ["h", "W", "weight"])
+@pytest.mark.parametrize("grad", [False, True])
+def test_a_forward_mode_tangent_is_refused(which, grad):
+    head, h, targets, weight = _case()
+    head.W.requires_grad_(False)
+    with torch.autograd.forward_ad.dual_level(), torch.set_grad_enabled(grad):
+        dual = dict(h=h, W=head.W.detach(), weight=weight)
+        dual[which] = torch.autograd.forward_ad.make_dual(dual[which], torch.ones_like(dual[which]))
+        if which == "W":
+            del head.W
+            head.W = dual["W"]
+        with pytest.raises(NotImplementedError, match="jvp"):
+            head(dual["h"], targets, dual["weight"])
+
+
+def test_without_gradients_none_are_taken(monkeypatch):
+    head, h, targets, weight = _case()
+    h.requires_grad_()
+    monkeypatch.setattr(ends, "head_loss_grad", lambda *a: pytest.fail("gradients were taken"))
+    with torch.no_grad():
+        assert torch.allclose(head(h, targets, weight), _sum(targets, _losses(h, head.W, targets)[0], weight))
+    head.W.requires_grad_(False)
+    assert not head(h.detach(), targets).requires_grad
