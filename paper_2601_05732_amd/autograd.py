@@ -78,6 +78,28 @@ def _plain(*tensors) -> bool:
 _IO = {torch.bfloat16: mhcl.BF16, torch.float32: mhcl.F32}
 
 
+class _FirstOnly(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, what, count, *tensors):
+        ctx.what = what
+        return tensors[:count]
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(f"{ctx.what} has no second derivative")
+
+
+def first_only(what, grads, *on):
+    """What a backward returns: `grads` (a tuple), or, if it is itself recorded (create_graph=True), these tied to the tensors `on` that they
+    depend on, so that a derivative of theirs raises.  Untied they would be constants in it, in silence.  (torch's
+    once_differentiable ties them to the gradients that arrived alone, which a loss at the end of a network gets without a history.)"""
+    there = [g for g in grads if g is not None]
+    if not there or not torch.is_grad_enabled():
+        return grads
+    tied = iter(_FirstOnly.apply(what, len(there), *there, *on))
+    return tuple(None if g is None else next(tied) for g in grads)
+
+
 class _Link:
     """What the post node leaves for the coefficient node of the same layer."""
     __slots__ = ("y", "g_xout", "H_pre", "g_x_phase", "perm")

@@ -6,14 +6,15 @@ the formulas), which computes everything.  Tensors may be strided or at any addr
 gets copied first.  Calls with tensors that it can read go through the extension in C++ (``torch_ext/ends.cpp``: the same at less
 than half of the host time), where that is built.
 
-:class:`TokenEmbedding`, :class:`StreamsNorm` and :class:`Head` are the same under ``torch.autograd``.
+:class:`TokenEmbedding`, :class:`StreamsNorm` and :class:`Head` are the same under ``torch.autograd``: first derivatives; second ones and
+forward-mode tangents are refused.
 """
 from __future__ import annotations
 
 import torch
 
 from . import binding as mhcl
-from .autograd import _native
+from .autograd import _native, first_only
 from .layer import PHASE_G_X, PHASE_X, empty_stream
 
 
@@ -153,7 +154,7 @@ class _Embed(torch.autograd.Function):
     @staticmethod
     def backward(ctx, g_x):
         ids, = ctx.saved_tensors
-        return embed_tokens_grad(ids, g_x, ctx.V, ctx.scale, ctx.dtype), None, None, None, None
+        return *first_only("the embedding", (embed_tokens_grad(ids, g_x, ctx.V, ctx.scale, ctx.dtype),), g_x), None, None, None, None
 
 
 class _Norm(torch.autograd.Function):
@@ -166,7 +167,7 @@ class _Norm(torch.autograd.Function):
     @staticmethod
     def backward(ctx, g_h):
         x, gain = ctx.saved_tensors
-        return *streams_norm_grad(x, gain, g_h, ctx.eps), None
+        return *first_only("the norm of the streams", streams_norm_grad(x, gain, g_h, ctx.eps), x, gain, g_h), None
 
 
 class _HeadTotal(torch.autograd.Function):
@@ -183,6 +184,7 @@ class _HeadTotal(torch.autograd.Function):
         else:
             loss, grads = head_loss(h, W, targets)[0], [None, None]
         total = _total(h, W, targets, loss, weight)
+        ctx.save_for_backward(h, W, weight)     # (read by a recorded backward alone)
         # (a place of weight 0 adds nothing, whatever it holds)
         grads.append(loss.masked_fill((weight == 0) & ~loss.isfinite(), 0.0) if record and ctx.needs_input_grad[3] else None)
         ctx.grads, ctx.dtypes = grads, (h.dtype, W.dtype, torch.float32)
@@ -194,7 +196,10 @@ class _HeadTotal(torch.autograd.Function):
             raise RuntimeError("the head's gradients went out with its first backward: run the head again for another one")
         grads, ctx.grads = ctx.grads, None
         h, W, _, weight, _ = ctx.needs_input_grad
-        g_h, g_W, g_weight = (_times(t, g, dtype) if needed else None for t, dtype, needed in zip(grads, ctx.dtypes, (h, W, weight)))
+        grads = tuple(_times(t, g, dtype) if needed else None for t, dtype, needed in zip(grads, ctx.dtypes, (h, W, weight)))
+        if torch.is_grad_enabled():
+            grads = first_only("the head's loss", grads, *ctx.saved_tensors, g)
+        g_h, g_W, g_weight = grads
         return g_h, g_W, None, g_weight, None
 
 

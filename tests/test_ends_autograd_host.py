@@ -120,3 +120,64 @@ def test_without_gradients_none_are_taken(monkeypatch):
         assert torch.allclose(head(h, targets, weight), _sum(targets, _losses(h, head.W, targets)[0], weight))
     head.W.requires_grad_(False)
     assert not head(h.detach(), targets).requires_grad
+
+
+def _through_head(a):
+    head, h, targets, weight = _case()
+    return head(h @ a, targets, weight), [a, head.W]
+
+
+def _through_head_alone(a):            # nothing before it: the gradient that arrives is a constant
+    head, h, targets, weight = _case()
+    head.W.requires_grad_(False)
+    return head(a, targets[:8]), [a]
+
+
+def _through_norm(a):
+    norm = ends.StreamsNorm(8, device="cpu")
+    return (norm(a.unsqueeze(1)) * torch.arange(8.0)).sum(), [a, norm.gain]
+
+
+def _through_norm_s_gradient(a):       # linear in the gain, whose gradient depends on a
+    norm = ends.StreamsNorm(8, device="cpu")
+    return (norm(a.detach().unsqueeze(1)) * a).sum(), [norm.gain]
+
+
+def _through_embedding(a):
+    emb = ends.TokenEmbedding(9, 8, 2, dtype=torch.float32, device="cpu")
+    return (emb(torch.tensor([1, 3, -1, 3])) * a[:4].unsqueeze(1)).sum(), [emb.table]
+
+
+_PATHS = [_through_head, _through_head_alone, _through_norm, _through_norm_s_gradient, _through_embedding]
+
+
+@pytest.mark.parametrize("path", _PATHS)
+@pytest.mark.parametrize("only", [False, True])
+def test_a_second_derivative_is_refused(path, only):
+    a = torch.randn(8, 8, generator=torch.Generator().manual_seed(1)).requires_grad_()
+    value, wrt = path(a)
+    grads = torch.autograd.grad(value, wrt, create_graph=True)
+    penalty = sum(g.square().sum() for g in grads) + a.square().sum()
+    with pytest.raises(RuntimeError, match="no second derivative"):
+        torch.autograd.grad(penalty, [a]) if only else penalty.backward()
+
+
+@pytest.mark.parametrize("path", _PATHS)
+def test_a_recorded_backward_returns_the_same_gradients(path):
+    a = torch.randn(8, 8, generator=torch.Generator().manual_seed(1)).requires_grad_()
+    torch.manual_seed(2)
+    value, wrt = path(a)
+    recorded = torch.autograd.grad(value, wrt, create_graph=True)
+    torch.manual_seed(2)
+    value, wrt = path(a)
+    for x, y in zip(recorded, torch.autograd.grad(value, wrt)):
+        assert torch.equal(x, y) and x.shape == y.shape
+        (x.detach() + a.sum()).sum().backward()
+
+
+def test_a_place_without_gradients_in_a_recorded_backward():
+    head, h, targets, _ = _case()
+    head.W.requires_grad_(False)
+    h.requires_grad_()
+    head(h, targets).backward(create_graph=True)
+    assert h.grad is not None and head.W.grad is None
