@@ -23,6 +23,8 @@ update hands g_xout and y over to the node of the coefficients, whose backward
 runs the fused kernel and returns the whole g_x.  Autograd runs the post node
 first because h reaches x_out only through y.
 
+First derivatives only: a second one raises.
+
 Initialisation follows Sec. 4 ("Initialization"): W = 0, alpha = 0.01,
 b_res = -8 except 0 for the identity permutation (or the diagonal in the
 Sinkhorn-Knopp form), b_pre = b_post = -1 except +1 for one stream.
@@ -116,6 +118,9 @@ def _desc(x, res_mode, sk_iters, eps, perm=None):
     return mhcl.Desc(n, C, T, io, res_mode, sk_iters, eps, perm)
 
 
+_LAYER = "the hyper-connection layer"
+
+
 class _CoeffsPre(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, W, b, alpha, link, res_mode, sk_iters, eps):
@@ -151,8 +156,8 @@ class _CoeffsPre(torch.autograd.Function):
         ws = mhcl.new_workspace(d, mhcl.OP_BWD_FUSED, x.device)
         # g_y went out through the post node already: not asked for again
         mhcl.mhcl_bwd_fused(d, x, link.y, W, b, alpha, g_xout, g_h, g_x, None, g_W, g_b, g_alpha, ws)
-        link.y = link.g_xout = None
-        return g_x, g_W, g_b, g_alpha, None, None, None, None
+        y, link.y, link.g_xout = link.y, None, None
+        return *first_only(_LAYER, (g_x, g_W, g_b, g_alpha), x, W, b, alpha, g_h, g_xout, y), None, None, None, None
 
 
 class _Post(torch.autograd.Function):
@@ -177,7 +182,7 @@ class _Post(torch.autograd.Function):
         mhcl.mhcl_pre(d, g_xout, H_post, g_y)            # g_y = sum_i H_post[i] g_xout[i]
         # x and the coefficients get their gradients from the coefficient node (fused kernel), which
         # autograd runs once this node is done, also where no gradient reaches it through f
-        return None, g_y, None, None, None, None, None, None
+        return None, *first_only(_LAYER, (g_y,), g_xout, H_post), None, None, None, None, None, None
 
 
 def init_params(n: int, C: int, res_mode: int = mhcl.RES_LITE, one_index: int = 0, device="cuda",

@@ -5,6 +5,9 @@
 //
 // autograd.py decides which calls come here: plain GPU tensors outside of function transforms, tracing and
 // dispatch modes, with every shape, type and layout checked.  What the library itself refuses is raised as its status.
+#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
+
 #include <tuple>
 
 #include "native.h"
@@ -22,6 +25,8 @@ struct Link final : torch::CustomClassHolder {
   Tensor perm;                      // keeps d.perm alive
   int64_t g_x_phase;
   Tensor y, g_xout;                 // (y without its history: with it the link would hold itself)
+  std::weak_ptr<torch::autograd::Node> y_node;   // where a recorded backward found y's history, and which of the node's results y is
+  uint32_t y_nr = 0;
 };
 using LinkPtr = c10::intrusive_ptr<Link>;
 
@@ -35,6 +40,19 @@ LinkPtr kept(AutogradContext *ctx) {
 Tensor workspace(const mhcl_desc &d, int op, const Tensor &like) {
   return at::empty({static_cast<int64_t>(mhcl_workspace_bytes(&d, op))}, like.options().dtype(at::kByte));
 }
+
+// What a backward returns; if it is itself recorded (create_graph), tied to what it depends on by a node that raises, as autograd.first_only
+variable_list first_only(const char *what, variable_list grads, torch::autograd::edge_list on) {
+  bool any = false;
+  for (const auto &e : on) any = any || e.is_valid();
+  if (!at::GradMode::is_enabled() || !any) return grads;
+  const std::shared_ptr<torch::autograd::Error> node(new torch::autograd::Error(std::string(what) + " has no second derivative", std::move(on)),
+                                                     torch::autograd::deleteNode);
+  for (const Tensor &g : grads)
+    if (g.defined()) torch::autograd::set_history(g, node);
+  return grads;
+}
+constexpr const char *kLayer = "the hyper-connection layer", *kEnds = "the end of a hyper-connection stack";
 
 struct CoeffsPre : Function<CoeffsPre> {
   static variable_list forward(AutogradContext *ctx, Tensor x, Tensor W, Tensor b, Tensor alpha, LinkPtr link) {
@@ -69,7 +87,10 @@ struct CoeffsPre : Function<CoeffsPre> {
           "mhcl_bwd_fused");
     link->y.reset();
     link->g_xout.reset();
-    return {g_x, g_W, g_b, g_alpha, Tensor()};
+    auto on = torch::autograd::collect_next_edges(x, W, b, alpha, grads[0]);
+    on.emplace_back(link->y_node.lock(), link->y_nr);
+    link->y_node.reset();
+    return first_only(kLayer, {g_x, g_W, g_b, g_alpha, Tensor()}, std::move(on));
   }
 };
 
@@ -94,7 +115,12 @@ struct Post : Function<Post> {
     check(mhcl_pre(&d, ptr(g_xout), ptr<float>(saved[1]), ptr(g_y), stream()), "mhcl_pre");
     // x and the coefficients get their gradients from the coefficient node (fused kernel), which
     // autograd runs once this node is done, also where no gradient reaches it through f
-    return {Tensor(), g_y, Tensor(), Tensor(), Tensor()};
+    if (at::GradMode::is_enabled()) {
+      const torch::autograd::Edge y = torch::autograd::get_current_node()->next_edge(1);
+      link->y_node = y.function;
+      link->y_nr = y.input_nr;
+    }
+    return first_only(kLayer, {Tensor(), g_y, Tensor(), Tensor(), Tensor()}, torch::autograd::collect_next_edges(grads[0], saved[1]));
   }
 };
 
@@ -121,7 +147,7 @@ struct StreamsIn : Function<StreamsIn> {
     return copies(link->d, x0, 0);
   }
   static variable_list backward(AutogradContext *ctx, variable_list grads) {
-    return {sum(kept(ctx)->d, dense(grads[0])), Tensor()};
+    return first_only(kEnds, {sum(kept(ctx)->d, dense(grads[0])), Tensor()}, torch::autograd::collect_next_edges(grads[0]));
   }
 };
 struct StreamsOut : Function<StreamsOut> {
@@ -131,7 +157,7 @@ struct StreamsOut : Function<StreamsOut> {
   }
   static variable_list backward(AutogradContext *ctx, variable_list grads) {
     const LinkPtr link = kept(ctx);
-    return {copies(link->d, dense(grads[0]), link->g_x_phase), Tensor()};
+    return first_only(kEnds, {copies(link->d, dense(grads[0]), link->g_x_phase), Tensor()}, torch::autograd::collect_next_edges(grads[0]));
   }
 };
 
