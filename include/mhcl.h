@@ -363,7 +363,8 @@ int mhcl_streams_norm(const mhcl_ends_desc *desc, const void *x, const float *ga
 int mhcl_streams_norm_bwd(const mhcl_ends_desc *desc, const void *x, const float *gain, const void *g_h, void *g_x,
                           float *g_gain, void *ws, size_t ws_bytes, void *stream);
 
-/* Softmax cross entropy of h W^T with the targets; logits never reach memory.  lse[t] = log sum_v exp(z[t][v]) is written for
+/* Softmax cross entropy of h W^T with the targets; logits never reach memory (with gradients, their softmax's numerators do, a block of
+ * tokens at a time: below).  lse[t] = log sum_v exp(z[t][v]) is written for
  * every token, counted or not.  Logits and sums are fp32, of bf16 operands as they are; fp32 operands enter as three bf16
  * parts each (24 significant bits), six products of parts, so that an infinity among them makes NaN of the logits it meets, and so
  * does a number past 3.3895e38, which rounds to one.

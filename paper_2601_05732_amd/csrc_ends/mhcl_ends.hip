@@ -587,8 +587,10 @@ hipError_t dispatch_streams(int n, F &&f) {
 
 }  // namespace
 
-// About a thousand chunks, for the chip, of 8 to 32 tokens: shorter ones leave more rows to be joined. (us, sums and joins at 8 / 16 / 32:
-// 3001 tokens, n = 4, C = 768, f32 15.4 / 18.0 / 27.1; 16384, C = 1024, bf16 63.2 / 63.4 / 67.9; 32768, C = 4096 350 / 331 / 313.)
+// About a thousand chunks, for the chip, of 8 to 32 tokens: shorter ones leave more rows to be joined.  (us, sums and joins at 8 / 16 / 32, n = 4:
+// 3001 tokens, C = 768, fp32 18.6 / 23.1 / 37.5; bf16 8000, 4096 69.6 / 64.7 / 70.9; 16384, 1024 40.7 / 41.7 / 51.7; 16384, 4096 141 / 131 / 125; 32768,
+// 1024 72.5 / 65.6 / 71.5; 32768, 4096 284 / 262 / 246; 65536, 1024 144 / 128 / 119.  The rule knows the tokens alone; short rows have fewer threads
+// at work and would take shorter chunks: 16384, 256 21.0 / 28.0 / 43.5, 32768, 256 31.0 / 30.3 / 46.2.)
 int32_t EmbedBwdWs::embed_chunk(const mhcl_ends_desc &d) { return d.T < 16384 ? 8 : (d.T < 32768 ? 16 : 32); }
 
 hipError_t launch_zero(void *p, size_t bytes, hipStream_t s) {

@@ -211,11 +211,11 @@ __device__ __forceinline__ void tile_of(const GemmArgs &g, int b, int &tm, int &
 // (us, 333 tokens, C = 520, 1003 rows, logits / g_h: two 11.0 / 7.6, four 8.1 / 6.4; four of the middle tile are none the faster
 // where there are few blocks, g_W 9.1 / 10.4).
 // 256 x 256 tiles of eight waves, bound by the matrix units and the clock that they leave the chip (busy 64 to 68 % of the cycles at
-// 1.87 GHz): 16384 tokens, C = 4096, 65536 rows, bf16, logits / g_h / g_W 7.0 / 6.7 / 7.0 ms, 1.25 to 1.31 PFLOP/s (a wave of 128 x 128 and
-// four of them, raised wave priorities, barriers in the middle of a step, strips of 4 or 16 tiles: no faster).
-// 128 x 128 of four waves: fp32, 2048 tokens, C = 768, 50257 rows 0.93 / 0.81 / 0.92 ms, 1.0 to 1.2 PFLOP/s of bf16 products;
+// 1.87 GHz on one card, 62 to 66 % at 1.95 on another): 16384 tokens, C = 4096, 65536 rows, bf16, logits / g_h / g_W 7.0 / 6.7 / 7.0 ms
+// there, 6.7 / 6.4 / 6.8 here, 1.25 to 1.37 PFLOP/s (a wave of 128 x 128 and four of them, raised wave priorities, barriers in the middle of a step, strips of 4 or 16 tiles: no faster).
+// 128 x 128 of four waves: fp32, 2048 tokens, C = 768, 50257 rows 0.93 / 0.81 / 0.92 ms and 0.88 / 0.77 / 0.89, 1.0 to 1.2 PFLOP/s of bf16 products;
 // matrix units busy for 49 % of the cycles, the vector ones, which take the parts, for 36 %.
-// 128 x 32: one token, C = 4096, 50257 rows 70 us, W at 5.9 TB/s.
+// 128 x 32: one token, C = 4096, 50257 rows 70 to 80 us from card to card, W at 5.1 to 5.9 TB/s.
 // block, blocks: its number of how many.
 template <int BM, int BN, int WM, int WN, int STAGES, bool AK, bool BK, typename Epilogue>
 __device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &epilogue, int block, int blocks) {
@@ -716,7 +716,10 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * 64) void loss_kernel(
 }
 
 // The same, one block a token, and the row's numerators turned into g in their place, bf16 or (IO = F32) fp32; h's row into hp, zeros
-// where the weight is 0.  Bound by memory: 16384 tokens, 65536 rows, bf16 980 us, 4.4 TB/s; 2048, 50257, fp32 154 us, 5.4 TB/s.
+// where the weight is 0.  bf16: g is of the operands' type, which is what the matrix units multiply with W and h.  (Its rounding is the one of the
+// T V terms of a sum each, the gradient's own comes after it: off from 64 bits by 0.0023 of the 2-norm at 333 tokens and 0.0018 at 16384, where the
+// gradient's rounding alone is 0.0017.  Two bf16 parts of g instead would make each of the two products two: 13 ms more on 21 at 16384
+// tokens, C = 4096, 65536 rows.)  Bound by memory: 16384 tokens, 65536 rows, bf16 980 us, 4.4 TB/s; 2048, 50257, fp32 154 us, 5.4 TB/s.
 template <typename ID, typename IO>
 __global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *__restrict__ targets) {
   __shared__ float red[2][16];
