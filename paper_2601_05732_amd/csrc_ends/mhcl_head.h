@@ -1,21 +1,15 @@
 // Host-side declarations of the head's softmax cross entropy (mhcl_head.hip).
 #pragma once
 #include "mhcl_ends.h"
+#include "mhcl_tiles.h"
 
 namespace mhcl {
-
-// How the three products of the head are tiled: rows of the vocabulary and tokens of a block of threads, and the rows of one of its
-// waves, which is what a softmax's partial maximum and sum stand for.
-struct HeadTile {
-  int bm, bn, gran;
-};
-constexpr HeadTile kTileBig{256, 256, 128}, kTileMid{128, 128, 64}, kTileSlim{128, 32, 32};
 
 constexpr int32_t kHeadMostRows = (1 << 22) - 256;   // of the vocabulary
 
 struct HeadPlan {
   bool wide;            // fp32 operands
-  HeadTile logits, gh, gw;
+  ProductTile logits, gh, gw;
   int64_t tokens;       // of a block
   int64_t ld;           // row of the softmax's numerators: V, filled up to whole tiles
   int64_t granules;     // partial sums of a row
