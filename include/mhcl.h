@@ -399,6 +399,37 @@ int mhcl_scale(void *p, int dtype, int64_t count, const float *factor, void *str
 /* out[i] = in[i] * *factor, rounded to the type (MHCL_BF16 | MHCL_F32); in and out are 16-byte aligned and apart. */
 int mhcl_scale_to(const float *in, void *out, int dtype, int64_t count, const float *factor, void *stream);
 
+/* ---- the block between the layers ------------------------------------------ */
+/*
+ * The layers' f as a gated feed-forward block, for T rows of width C and H hidden ones:
+ *
+ *     y = (silu(x Wg^T) * (x Wu^T)) W_down^T,  silu(v) = v / (1 + exp(-v)),  Wg the first H rows of W_up, Wu the others
+ *
+ * Device pointers, no allocation, no synchronisation, the same bits from call to call, as above.  Sums are fp32 (fp32 operands enter as three
+ * bf16 parts each, as in mhcl_head_loss).  bf16: the hidden numbers silu(x Wg^T) * (x Wu^T) are rounded to bf16, once, before the second
+ * product, and so are `pre` and, in the backward, the gradients on it.
+ */
+typedef struct {
+  int32_t C;         /* width; a positive multiple of 8, at most 32768                    */
+  int32_t H;         /* hidden width; a positive multiple of 8, at most 131072, H C <= 2^28 */
+  int64_t T;         /* rows, 0 .. 2^30; T max(C, H) at most 2^41                          */
+  int32_t io_dtype;  /* MHCL_BF16 | MHCL_F32: every tensor                                */
+} mhcl_ffn_desc;
+
+enum { MHCL_OP_FFN = 0, MHCL_OP_FFN_GRAD = 1 };
+/* Bytes of workspace `op` needs for `desc`; 0 if desc or op is invalid or unsupported.  Host only. */
+size_t mhcl_ffn_workspace_bytes(const mhcl_ffn_desc *desc, int op);
+
+/* in : x [T,C], W_up [2H,C], W_down [C,H];  out: y [T,C], pre [T,2H] = x W_up^T for the backward, or NULL (what lies in a row's
+ * first H numbers belongs to Wg) */
+int mhcl_ffn(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, void *y, void *pre, void *ws, size_t ws_bytes,
+             void *stream);
+
+/* Backward of mhcl_ffn for the gradient g_y on its result.
+ * in : x, W_up, W_down, pre as of the forward, g_y [T,C];  out: g_x [T,C], g_W_up [2H,C], g_W_down [C,H] */
+int mhcl_ffn_grad(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, const void *pre, const void *g_y, void *g_x,
+                  void *g_W_up, void *g_W_down, void *ws, size_t ws_bytes, void *stream);
+
 /* ---- measurement aids (no part of the method) --------------------------- */
 
 /* Kernel stages that can be bracketed with events. */

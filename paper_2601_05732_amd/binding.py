@@ -21,6 +21,7 @@ RES_LITE, RES_SK, RES_SUBSET = 0, 1, 2
 OP_COEFFS, OP_COEFFS_BWD, OP_FWD_COEFFS_PRE, OP_BWD_FUSED, OP_COEFFS_LAYERS = 0, 1, 2, 3, 4
 I64, I32 = 0, 1
 OP_EMBED_BWD, OP_STREAMS_NORM_BWD, OP_HEAD_LOSS, OP_HEAD_LOSS_GRAD = 0, 1, 2, 3   # of the ends, ends_workspace_bytes
+OP_FFN, OP_FFN_GRAD = 0, 1   # of the block, ffn_workspace_bytes
 
 _SYMBOLS = [
     "mhcl_status_string", "mhcl_validate", "mhcl_logit_count", "mhcl_workspace_bytes",
@@ -30,6 +31,7 @@ _SYMBOLS = [
     "mhcl_fwd_coeffs_pre_static", "mhcl_coeffs_logits", "mhcl_coeffs_logits_layers", "mhcl_streams_in", "mhcl_streams_out",
     "mhcl_ends_workspace_bytes", "mhcl_embed", "mhcl_embed_bwd", "mhcl_streams_norm", "mhcl_streams_norm_bwd",
     "mhcl_head_loss", "mhcl_head_loss_grad", "mhcl_head_loss_grad_unrounded", "mhcl_head_total", "mhcl_scale", "mhcl_scale_to",
+    "mhcl_ffn_workspace_bytes", "mhcl_ffn", "mhcl_ffn_grad",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20   # MHCL_STATIC_SCRATCH_BYTES
 
@@ -53,6 +55,10 @@ class _CEndsDesc(ctypes.Structure):
                 ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
+class _CFfnDesc(ctypes.Structure):
+    _fields_ = [("C", ctypes.c_int32), ("H", ctypes.c_int32), ("T", ctypes.c_int64), ("io_dtype", ctypes.c_int32)]
+
+
 _DTYPE = {torch.bfloat16: BF16, torch.float32: F32}
 _ID_DTYPE = {torch.int64: I64, torch.int32: I32}
 
@@ -68,6 +74,19 @@ class EndsDesc:
             raise ValueError(f"n = {n}, C = {C}, V = {V}: out of range")
         self.n, self.C, self.T, self.V, self.io, self.w, self.ids = n, C, T, V, io, w, ids
         self.c = _CEndsDesc(n, C, T, V, _DTYPE[io], _DTYPE[w], _ID_DTYPE[ids], scale, eps)
+
+
+class FfnDesc:
+    """Mirror of ``mhcl_ffn_desc``, with torch's types."""
+    __slots__ = ("C", "H", "T", "io", "c")
+
+    def __init__(self, C, H, T, io=torch.bfloat16):
+        if io not in _DTYPE:
+            raise ValueError(f"type {io}: bfloat16 or float32")
+        if not (-2 ** 31 <= C < 2 ** 31 and -2 ** 31 <= H < 2 ** 31):
+            raise ValueError(f"C = {C}, H = {H}: out of range")
+        self.C, self.H, self.T, self.io = C, H, T, io
+        self.c = _CFfnDesc(C, H, T, _DTYPE[io])
 
 
 class Desc:
@@ -155,6 +174,11 @@ def lib():
         L.mhcl_head_total.argtypes = [E] + [V] * 5
         L.mhcl_scale.argtypes = [V, ctypes.c_int, ctypes.c_int64, V, V]
         L.mhcl_scale_to.argtypes = [V, V, ctypes.c_int, ctypes.c_int64, V, V]
+        B = ctypes.POINTER(_CFfnDesc)
+        L.mhcl_ffn_workspace_bytes.restype = Z
+        L.mhcl_ffn_workspace_bytes.argtypes = [B, ctypes.c_int]
+        L.mhcl_ffn.argtypes = [B] + [V] * 6 + [Z, V]
+        L.mhcl_ffn_grad.argtypes = [B] + [V] * 9 + [Z, V]
         _lib = L
     return _lib
 
@@ -451,3 +475,32 @@ def mhcl_scale_to(x, factor, out):
         raise ValueError(f"dtype {out.dtype}: bfloat16 or float32")
     _check(lib().mhcl_scale_to(_ptr(x, torch.float32, out.shape, "x"), _ptr(out, out.dtype, out.shape, "out"), _DTYPE[out.dtype], out.numel(),
                                _ptr(factor.reshape(1), torch.float32, (1,), "factor"), _stream()), "mhcl_scale_to")
+
+
+# ---- the block between the layers -------------------------------------------------------------
+
+
+def ffn_workspace_bytes(d: FfnDesc, op: int) -> int:
+    return lib().mhcl_ffn_workspace_bytes(ctypes.byref(d.c), op)
+
+
+def new_ffn_workspace(d: FfnDesc, op: int, device="cuda"):
+    return torch.empty(ffn_workspace_bytes(d, op), dtype=torch.uint8, device=device)
+
+
+def mhcl_ffn(d, x, W_up, W_down, y, pre, ws):
+    """pre: [T, 2 H], or None."""
+    wp, wb = _ws(ws)
+    _check(lib().mhcl_ffn(
+        ctypes.byref(d.c), _ptr(x, d.io, (d.T, d.C), "x"), _ptr(W_up, d.io, (2 * d.H, d.C), "W_up"),
+        _ptr(W_down, d.io, (d.C, d.H), "W_down"), _ptr(y, d.io, (d.T, d.C), "y"), _ptr(pre, d.io, (d.T, 2 * d.H), "pre"), wp, wb,
+        _stream()), "mhcl_ffn")
+
+
+def mhcl_ffn_grad(d, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, ws):
+    wp, wb = _ws(ws)
+    _check(lib().mhcl_ffn_grad(
+        ctypes.byref(d.c), _ptr(x, d.io, (d.T, d.C), "x"), _ptr(W_up, d.io, (2 * d.H, d.C), "W_up"),
+        _ptr(W_down, d.io, (d.C, d.H), "W_down"), _ptr(pre, d.io, (d.T, 2 * d.H), "pre"), _ptr(g_y, d.io, (d.T, d.C), "g_y"),
+        _ptr(g_x, d.io, (d.T, d.C), "g_x"), _ptr(g_W_up, d.io, (2 * d.H, d.C), "g_W_up"),
+        _ptr(g_W_down, d.io, (d.C, d.H), "g_W_down"), wp, wb, _stream()), "mhcl_ffn_grad")

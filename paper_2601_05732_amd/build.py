@@ -12,6 +12,7 @@ from concurrent.futures import ThreadPoolExecutor
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")             # the layers (bench.py's figures go by what lies there)
 CSRC_ENDS = os.path.join(_HERE, "csrc_ends")   # the ends of a language model
+CSRC_BLOCK = os.path.join(_HERE, "csrc_block") # the block between the layers
 LIB = os.path.join(_HERE, "libmhcl.so")
 OBJ_DIR = os.path.join(_HERE, "_build")
 PROBE_SRC = os.path.join(_HERE, "probe", "memsys_probe.hip")
@@ -29,7 +30,7 @@ FLAGS = [
 
 
 def sources():
-    return sorted(os.path.join(d, f) for d in (CSRC, CSRC_ENDS) for f in os.listdir(d) if f.endswith(".hip"))
+    return sorted(os.path.join(d, f) for d in (CSRC, CSRC_ENDS, CSRC_BLOCK) for f in os.listdir(d) if f.endswith(".hip"))
 
 
 def build_library(verbose: bool = False) -> str:

@@ -1,0 +1,31 @@
+// Host-side declarations of the gated feed-forward block (mhcl_ffn.hip).
+#pragma once
+#include "../csrc/mhcl_internal.h"
+#include "../csrc_ends/mhcl_tiles.h"
+
+namespace mhcl {
+
+constexpr int64_t kFfnMostWeights = int64_t{1} << 28;   // H C: the halves of W_up lie less than 2^31 bytes apart
+
+struct FfnPlan {
+  bool wide;                                  // fp32 operands
+  ProductTile up, down, act, gx, gup, gdown;
+  int down_splits, gx_splits, gup_splits, gdown_splits;
+  FfnPlan(const mhcl_ffn_desc &d, bool grad);
+};
+
+struct FfnWs {
+  FfnPlan plan;
+  char *a;              // [T][H] silu(gate) * up
+  char *g_pre;          // [T][2 H] gradients on gate | up
+  float *slabs;         // parts of the sums of one product after the other
+  size_t bytes;
+  FfnWs(const mhcl_ffn_desc &d, bool grad, void *ws);
+};
+
+// pre [T][2 H], may be null: gate | up
+hipError_t launch_ffn(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, void *y, void *pre, const FfnWs &w, hipStream_t s);
+hipError_t launch_ffn_grad(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, const void *pre, const void *g_y, void *g_x,
+                           void *g_W_up, void *g_W_down, const FfnWs &w, hipStream_t s);
+
+}  // namespace mhcl

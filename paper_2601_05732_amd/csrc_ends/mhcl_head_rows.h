@@ -30,7 +30,7 @@ __device__ __forceinline__ float exp_of(float x) {
 // m: vocabulary, n: tokens.  STORE: the numerators too.  WIDE: fp32 numerators.
 template <typename ID, bool STORE, bool WIDE>
 struct LogitsEpilogue {
-  static constexpr bool kWide = WIDE;
+  static constexpr bool kWide = WIDE, kPaired = false;
   const ID *targets;
   float2 *stat;
   float *zt;

@@ -2,6 +2,7 @@
 // choice of tiles and parts, launches.
 #pragma once
 #include <algorithm>
+#include <type_traits>
 
 #include "../csrc/mhcl_common.h"
 #include "../csrc/mhcl_mfma.h"
@@ -83,6 +84,40 @@ struct TileLoader {
     const int range = rest <= 0 ? 0 : (rest > 0x7fffffff ? 0x7fffffff : static_cast<int>(rest));
     uint32_t offset = from + i * apart;
     if constexpr (!KINNER && WIDE) offset += unit ^ (i & 1) << 7;   // (eight rows on: k / 4 is two more)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, range, 0x00020000),
+                                             (lds_void *)(tile + i * NT + wave * 64), 16, offset, 0, 0, 0);
+  }
+};
+
+// The same of an operand (KINNER) of two halves of rows / 2 rows, whose rows meet in a lane: the tile's rows are, for each wave, HALF of the first half
+// and the HALF of the second that go with them, so that the fragments FM / 2 on are the former ones' partners.  (Rows past the first half are
+// the second's first ones; they give results that nobody reads.)
+template <int R, int NT, int HALF, bool WIDE>
+struct PairedLoader {
+  static constexpr int PER = R * 8 / NT, ES = WIDE ? 4 : 2, DEPTH = 128 / ES, kRows = NT / 8;
+  static_assert(HALF == kRows || HALF * 2 == kRows, "a piece is of one half, or has both");
+  const char *base;
+  int64_t rest;
+  int step, apart;
+  uint32_t at, from;
+  uint32_t second;          // bytes from a row to its partner (less than 2^31: the host sees to it)
+  int depth;
+  __device__ __forceinline__ void init(const Operand &o, int64_t row0) {
+    const int tid = threadIdx.x, row = tid >> 3, c = (tid & 7) ^ ((tid >> 4) & 7);
+    const int64_t skip = row0 / 2 * o.ld * ES;
+    step = DEPTH * ES;
+    apart = static_cast<int>(HALF * o.ld * ES);
+    base = static_cast<const char *>(o.p) + skip;
+    rest = o.rows * o.ld * ES - skip;
+    second = static_cast<uint32_t>(o.rows / 2 * o.ld * ES);
+    depth = c * (16 / ES);
+    at = static_cast<uint32_t>(row % HALF * o.ld * ES + c * 16) + (row >= HALF ? second : 0u);
+  }
+  __device__ __forceinline__ void skip(int64_t bytes) { base += bytes, rest -= bytes; }
+  __device__ __forceinline__ void aim(int left) { from = depth < left ? at : 0x80000000u; }
+  __device__ __forceinline__ void piece(uint4 *tile, int wave, int i) const {
+    const int range = rest <= 0 ? 0 : (rest > 0x7fffffff ? 0x7fffffff : static_cast<int>(rest));
+    const uint32_t offset = HALF == kRows ? from + i / 2 * apart + (i % 2 ? second : 0u) : from + i * apart;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, range, 0x00020000),
                                              (lds_void *)(tile + i * NT + wave * 64), 16, offset, 0, 0, 0);
   }
@@ -208,7 +243,7 @@ __device__ __forceinline__ void tile_of(const GemmArgs &g, int b, int &tm, int &
 // 128 x 128 of four waves: fp32, 2048 tokens, C = 768, 50257 rows 0.93 / 0.81 / 0.92 ms and 0.88 / 0.77 / 0.89, 1.0 to 1.2 PFLOP/s of bf16 products;
 // matrix units busy for 49 % of the cycles, the vector ones, which take the parts, for 36 %.
 // 128 x 32: one token, C = 4096, 50257 rows 70 to 80 us from card to card, W at 5.1 to 5.9 TB/s.
-// block, blocks: its number of how many.
+// Epilogue::kPaired: A's rows are two halves (PairedLoader).  block, blocks: its number of how many.
 template <int BM, int BN, int WM, int WN, int STAGES, bool AK, bool BK, typename Epilogue>
 __device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &epilogue, int block, int blocks) {
   constexpr bool WIDE = Epilogue::kWide;
@@ -225,7 +260,8 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &ep
   };
   const Stage s0{m0, FOUR ? m0 + TA : n0}, s1{m1, FOUR ? m1 + TA : n1}, s2{m2, m2 + TA}, s3{m3, m3 + TA};
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
-  TileLoader<BM, NT, AK, WIDE> la;
+  std::conditional_t<Epilogue::kPaired, PairedLoader<BM, NT, FM * 8, WIDE>, TileLoader<BM, NT, AK, WIDE>> la;
+  static_assert(AK || !Epilogue::kPaired, "halves of rows");
   TileLoader<BN, NT, BK, WIDE> lb;
   const int64_t depth = g.A.depth < g.B.depth ? g.B.depth : g.A.depth;
   const int steps = static_cast<int>((depth + la.DEPTH - 1) / la.DEPTH);
@@ -452,18 +488,25 @@ __device__ __forceinline__ uint4 join_pairs(uint2 lower, uint2 upper) {
   const auto y = __builtin_amdgcn_permlane16_swap(lower.y, upper.y, false, false);
   return make_uint4(x[0], y[0], x[1], y[1]);
 }
+// and back
+__device__ __forceinline__ void split_pairs(uint4 eight, uint2 &lower, uint2 &upper) {
+  const auto x = __builtin_amdgcn_permlane16_swap(eight.x, eight.z, false, false);
+  const auto y = __builtin_amdgcn_permlane16_swap(eight.y, eight.w, false, false);
+  lower = make_uint2(x[0], y[0]);
+  upper = make_uint2(x[1], y[1]);
+}
 
-// out[n][m], m innermost, times *scale: fp32 slabs of splits (out32 != null), added to `add` if that is there; else rounded to bf16
+// out[n][m], m innermost, times *scale (null: 1): fp32 slabs of splits (out32 != null), added to `add` if that is there; else rounded to bf16
 template <bool WIDE>
 struct StoreEpilogue {
-  static constexpr bool kWide = WIDE;
+  static constexpr bool kWide = WIDE, kPaired = false;
   const float *scale;
   float *out32;
   uint16_t *out16;
   const float *add;
   int64_t M, N, slab;     // elements of a split's slab
   template <int FN>
-  __device__ __forceinline__ float hold(int64_t) const { return *scale; }
+  __device__ __forceinline__ float hold(int64_t) const { return scale ? *scale : 1.f; }
   template <int FM, int FN>
   static constexpr int stores() { return FN * (WIDE ? FM : FM / 2); }   // (into fp32 slabs twice as many)
   __device__ __forceinline__ bool whole(int64_t m_end, int64_t n_end) const { return m_end <= M && n_end <= N; }

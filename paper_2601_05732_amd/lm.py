@@ -6,7 +6,7 @@
     h    = norm(sum of the streams)               [T, C]
     loss = mean cross entropy of h W^T with the next tokens
 
-The blocks here are norm, two linear maps and a gate (what a user replaces by attention and the like); the paper does not say how
+The blocks here are norm and a gated feed-forward block (what a user replaces by attention and the like); the paper does not say how
 streams begin and end, so the ends are this package's choice.
 
 ``python -m paper_2601_05732_amd.lm`` trains one on a synthetic language, a fixed random successor for each token with some noise.
@@ -19,6 +19,7 @@ import torch
 
 from .autograd import HyperConnection
 from .ends import Head, StreamsNorm, TokenEmbedding
+from .ffn import apply_gated_ffn, takes
 
 
 class Block(torch.nn.Module):
@@ -31,8 +32,17 @@ class Block(torch.nn.Module):
         self.down = torch.nn.Linear(hidden, C, bias=False, device=device, dtype=dtype)
 
     def forward(self, h):
-        a, b = self.up(self.norm(h)).chunk(2, dim=-1)
+        h = self.norm(h)
+        if _plain_linear(self.up, h) and _plain_linear(self.down, h) and takes(self.up.in_features, self.down.in_features, h.dtype):
+            return apply_gated_ffn(h, self.up.weight, self.down.weight)
+        a, b = self.up(h).chunk(2, dim=-1)      # widths that the kernels do not take, or maps that a user put in place of these
         return self.down(torch.nn.functional.silu(a) * b)
+
+
+def _plain_linear(m, h) -> bool:
+    """Whether `m` is a linear map as Block makes it, and nothing looks at its call."""
+    return (type(m) is torch.nn.Linear and m.bias is None and m.weight.dtype is h.dtype and not torch.is_autocast_enabled("cuda")
+            and not (m._forward_hooks or m._forward_pre_hooks or m._backward_hooks or m._backward_pre_hooks))
 
 
 class LanguageModel(torch.nn.Module):

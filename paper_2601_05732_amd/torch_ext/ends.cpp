@@ -139,6 +139,49 @@ std::optional<std::tuple<Tensor, Tensor, Tensor, Tensor>> head_grad(const Tensor
   return std::make_tuple(loss, lse, g_h, g_W);
 }
 
+std::optional<mhcl_ffn_desc> ffn_ready(const Tensor &x, const Tensor &W_up, const Tensor &W_down, int device) {
+  const auto io = type_of(x.scalar_type());
+  if (!io || x.dim() != 2 || W_up.dim() != 2 || W_down.dim() != 2 || W_down.size(0) != x.size(1) || W_up.size(1) != x.size(1) ||
+      W_up.size(0) != 2 * W_down.size(1) || W_up.scalar_type() != x.scalar_type() || W_down.scalar_type() != x.scalar_type() ||
+      !ready(x, device, 16) || !ready(W_up, device, 16) || !ready(W_down, device, 16) || !fits(x.size(1)) || !fits(W_down.size(1)))
+    return std::nullopt;
+  mhcl_ffn_desc d{};
+  d.C = static_cast<int32_t>(x.size(1));
+  d.H = static_cast<int32_t>(W_down.size(1));
+  d.T = x.size(0);
+  d.io_dtype = *io;
+  return d;
+}
+
+Tensor ffn_workspace_of(const mhcl_ffn_desc &d, int op, const Tensor &like) {
+  return at::empty({static_cast<int64_t>(mhcl_ffn_workspace_bytes(&d, op))}, like.options().dtype(at::kByte));
+}
+
+std::optional<std::tuple<Tensor, std::optional<Tensor>>> ffn(const Tensor &x, const Tensor &W_up, const Tensor &W_down, bool keep) {
+  const auto d = ffn_ready(x, W_up, W_down, c10::hip::current_device());
+  if (!d) return std::nullopt;
+  const Tensor y = at::empty(x.sizes(), x.options());
+  std::optional<Tensor> pre;
+  if (keep) pre = at::empty({d->T, 2 * static_cast<int64_t>(d->H)}, x.options());
+  const Tensor ws = ffn_workspace_of(*d, MHCL_OP_FFN, x);
+  check(mhcl_ffn(&*d, ptr(x), ptr(W_up), ptr(W_down), ptr(y), pre ? ptr(*pre) : nullptr, ws.data_ptr(), ws.nbytes(), stream()), "mhcl_ffn");
+  return std::make_tuple(y, pre);
+}
+
+std::optional<std::tuple<Tensor, Tensor, Tensor>> ffn_grad(const Tensor &x, const Tensor &W_up, const Tensor &W_down, const Tensor &pre, const Tensor &g_y) {
+  const int device = c10::hip::current_device();
+  const auto d = ffn_ready(x, W_up, W_down, device);
+  if (!d || pre.dim() != 2 || pre.size(0) != x.size(0) || pre.size(1) != W_up.size(0) || pre.scalar_type() != x.scalar_type() ||
+      !ready(pre, device, 16) || g_y.sizes() != x.sizes() || g_y.scalar_type() != x.scalar_type() || !ready(g_y, device, 16))
+    return std::nullopt;
+  const Tensor g_x = at::empty(x.sizes(), x.options()), g_W_up = at::empty(W_up.sizes(), x.options()), g_W_down = at::empty(W_down.sizes(), x.options());
+  const Tensor ws = ffn_workspace_of(*d, MHCL_OP_FFN_GRAD, x);
+  check(mhcl_ffn_grad(&*d, ptr(x), ptr(W_up), ptr(W_down), ptr(pre), ptr(g_y), ptr(g_x), ptr(g_W_up), ptr(g_W_down), ws.data_ptr(), ws.nbytes(),
+                      stream()),
+        "mhcl_ffn_grad");
+  return std::make_tuple(g_x, g_W_up, g_W_down);
+}
+
 }  // namespace
 
 void bind_ends(py::module &m) {
@@ -149,6 +192,8 @@ void bind_ends(py::module &m) {
   m.def("norm_grad", wrap(&norm_grad));
   m.def("head", wrap(&head));
   m.def("head_grad", wrap(&head_grad));
+  m.def("ffn", wrap(&ffn));
+  m.def("ffn_grad", wrap(&ffn_grad));
 }
 
 }  // namespace native
