@@ -387,6 +387,43 @@ int mhcl_head_loss_grad(const mhcl_ends_desc *desc, const void *h, const void *W
 int mhcl_head_loss_grad_unrounded(const mhcl_ends_desc *desc, const void *h, const void *W, const void *targets, const float *weight,
                                   float *loss, float *lse, float *g_h, float *g_W, void *ws, size_t ws_bytes, void *stream);
 
+/* The head against a teacher's K likeliest rows of the vocabulary for each token, at a temperature tau:
+ *     p_k     = exp(logits[t][k] / tau) / sum_j exp(logits[t][j] / tau)      over the slots that hold one
+ *     loss[t] = sum_k p_k (log p_k - log q[ids[t][k]]),  q = softmax(h[t] W^T / tau),  lse[t] = log sum_v exp(z[t][v] / tau)
+ * and, where g_h and g_W are given, the gradients of sum_t weight[t] loss[t] on h and W: g = weight (q - p) / tau.  (Nothing is
+ * multiplied by tau^2: a caller who wants that has it in the weights.)
+ * A slot is empty where its id is negative or its logit -infinity; a token all of whose slots are empty does not count, as one without a
+ * target above (its loss is 0; weight NULL: the mean over those that count).  A slot that names row V or more, and a logit that is NaN or
+ * +infinity, is a mistake: the token's loss is NaN, and so are its g_h and all of g_W unless its weight is 0.  An id may stand in several slots: their
+ * probabilities add up.  The teacher's logits are constants.
+ * total: the sum of weight loss over the tokens that count, weights of 0 left out, or their mean, as mhcl_head_total; or NULL.
+ * g_h, g_W: both or neither; unrounded != 0: in fp32, whatever the operands, as mhcl_head_loss_grad_unrounded.
+ * K: 1 .. 256.  temperature: 1e-6 .. 1e6.  Roundings, blocks of tokens and the vocabulary's bound as in mhcl_head_loss_grad.
+ * in : h [T,C] io, W [V,C] io, ids [T,K] id_dtype, logits [T,K] f32, weight [T] f32 or NULL
+ * out: loss [T], lse [T], total [1] f32, g_h [T,C], g_W [V,C] */
+size_t mhcl_head_distill_workspace_bytes(const mhcl_ends_desc *desc, int32_t K, int grad);
+int mhcl_head_distill(const mhcl_ends_desc *desc, int32_t K, float temperature, const void *h, const void *W, const void *ids, const float *logits,
+                      const float *weight, float *loss, float *lse, float *total, void *g_h, void *g_W, int unrounded, void *ws, size_t ws_bytes,
+                      void *stream);
+
+/* Pairs of sequences packed into the T tokens, sequence s being tokens offsets[s] .. offsets[s + 1] - 1, the chosen one of pair p sequence 2 p
+ * and the rejected one 2 p + 1:
+ *     logp[s] = the sum over its targets that are not negative of their log probabilities           (0 of an empty sequence)
+ *     m[p]    = beta ((logp[2p] - reference[2p]) - (logp[2p+1] - reference[2p+1]))
+ *     loss[p] = (1 - smoothing) log(1 + exp(-m)) + smoothing log(1 + exp(m))
+ * and, where g_h and g_W are given, the gradients of sum_p weight[p] loss[p] on h and W (weight NULL: of the mean over the pairs).
+ * Log probabilities of tokens are fp32, their sums and all of a pair fp64, rounded to fp32 at the end.  Tokens outside of the sequences add nothing; their
+ * g_h is 0.  Offsets ascend from 0 or more to T or less; where they do not, which the host cannot see, the pair's loss and logp are NaN (and
+ * gradients unless its weight is 0); nothing is read or written out of bounds for it.  Past one block of tokens (MHCL_HEAD_BLOCK_BYTES) the
+ * logits are formed twice for gradients, since a pair's weight needs all of its tokens.
+ * total, g_h, g_W, unrounded: as in mhcl_head_distill.  pairs: 0 .. 2^22; beta finite; smoothing 0 .. 1.
+ * in : h [T,C] io, W [V,C] io, targets [T], offsets [2 pairs + 1] of offset_dtype, reference [2 pairs] f32 or NULL (zeros), weight [pairs] f32 or NULL
+ * out: loss [pairs], logp [2 pairs], total [1] f32, g_h [T,C], g_W [V,C] */
+size_t mhcl_head_preference_workspace_bytes(const mhcl_ends_desc *desc, int grad);
+int mhcl_head_preference(const mhcl_ends_desc *desc, int32_t pairs, float beta, float smoothing, const void *h, const void *W, const void *targets,
+                         const void *offsets, int offset_dtype, const float *reference, const float *weight, float *loss, float *logp, float *total,
+                         void *g_h, void *g_W, int unrounded, void *ws, size_t ws_bytes, void *stream);
+
 /* The sum of weight[t] loss[t] over the places that hold a target, those of weight 0 left out; weight NULL: their mean, 0 where there is none.
  * Added up in fp64, in a fixed order.  in : targets [T], loss [T] f32, weight [T] f32 or NULL;  out: total [1] f32 */
 int mhcl_head_total(const mhcl_ends_desc *desc, const void *targets, const float *loss, const float *weight, float *total, void *stream);
@@ -407,13 +444,13 @@ int mhcl_scale_to(const float *in, void *out, int dtype, int64_t count, const fl
  *
  * Device pointers, no allocation, no synchronisation, the same bits from call to call, as above.  Sums are fp32 (fp32 operands enter as three
  * bf16 parts each, as in mhcl_head_loss).  bf16: the hidden numbers silu(x Wg^T) * (x Wu^T) are rounded to bf16, once, before the second
- * product, and so are `pre` and, in the backward, the gradients on it.
+ * product, and so are, in the backward, they and the gradients on `pre`; `pre` itself is fp32.
  */
 typedef struct {
   int32_t C;         /* width; a positive multiple of 8, at most 32768                    */
   int32_t H;         /* hidden width; a positive multiple of 8, at most 131072, H C <= 2^28 */
   int64_t T;         /* rows, 0 .. 2^30; T max(C, H) at most 2^41                          */
-  int32_t io_dtype;  /* MHCL_BF16 | MHCL_F32: every tensor                                */
+  int32_t io_dtype;  /* MHCL_BF16 | MHCL_F32: every tensor but `pre`, which is fp32       */
 } mhcl_ffn_desc;
 
 enum { MHCL_OP_FFN = 0, MHCL_OP_FFN_GRAD = 1 };
@@ -422,12 +459,12 @@ size_t mhcl_ffn_workspace_bytes(const mhcl_ffn_desc *desc, int op);
 
 /* in : x [T,C], W_up [2H,C], W_down [C,H];  out: y [T,C], pre [T,2H] = x W_up^T for the backward, or NULL (what lies in a row's
  * first H numbers belongs to Wg) */
-int mhcl_ffn(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, void *y, void *pre, void *ws, size_t ws_bytes,
+int mhcl_ffn(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, void *y, float *pre, void *ws, size_t ws_bytes,
              void *stream);
 
 /* Backward of mhcl_ffn for the gradient g_y on its result.
  * in : x, W_up, W_down, pre as of the forward, g_y [T,C];  out: g_x [T,C], g_W_up [2H,C], g_W_down [C,H] */
-int mhcl_ffn_grad(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, const void *pre, const void *g_y, void *g_x,
+int mhcl_ffn_grad(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, const float *pre, const void *g_y, void *g_x,
                   void *g_W_up, void *g_W_down, void *ws, size_t ws_bytes, void *stream);
 
 /* ---- measurement aids (no part of the method) --------------------------- */

@@ -14,12 +14,14 @@ from .binding import (  # noqa: F401
     I64, I32, OP_EMBED_BWD, OP_STREAMS_NORM_BWD, OP_HEAD_LOSS, OP_HEAD_LOSS_GRAD, EndsDesc, ends_workspace_bytes,
     mhcl_embed, mhcl_embed_bwd, mhcl_streams_norm, mhcl_streams_norm_bwd, mhcl_head_loss, mhcl_head_loss_grad,
     mhcl_head_total, mhcl_scale, mhcl_scale_to,
+    mhcl_head_distill, head_distill_workspace_bytes, mhcl_head_preference, head_preference_workspace_bytes,
     OP_FFN, OP_FFN_GRAD, FfnDesc, ffn_workspace_bytes, mhcl_ffn, mhcl_ffn_grad,
 )
 from .layer import GpuLayer, desc_for, empty_stream, place_stream  # noqa: F401,E402
 from .autograd import HyperConnection, HyperConnectionStack, init_params  # noqa: F401,E402
 from .ends import (  # noqa: F401,E402
     embed_tokens, embed_tokens_grad, streams_norm, streams_norm_grad, head_loss, head_loss_grad,
+    head_distill, head_distill_grad, head_preference, head_preference_grad,
     TokenEmbedding, StreamsNorm, Head,
 )
 from .ffn import gated_ffn, gated_ffn_grad, GatedFeedForward  # noqa: F401,E402

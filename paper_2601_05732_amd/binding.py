@@ -31,6 +31,7 @@ _SYMBOLS = [
     "mhcl_fwd_coeffs_pre_static", "mhcl_coeffs_logits", "mhcl_coeffs_logits_layers", "mhcl_streams_in", "mhcl_streams_out",
     "mhcl_ends_workspace_bytes", "mhcl_embed", "mhcl_embed_bwd", "mhcl_streams_norm", "mhcl_streams_norm_bwd",
     "mhcl_head_loss", "mhcl_head_loss_grad", "mhcl_head_loss_grad_unrounded", "mhcl_head_total", "mhcl_scale", "mhcl_scale_to",
+    "mhcl_head_distill_workspace_bytes", "mhcl_head_distill", "mhcl_head_preference_workspace_bytes", "mhcl_head_preference",
     "mhcl_ffn_workspace_bytes", "mhcl_ffn", "mhcl_ffn_grad",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20   # MHCL_STATIC_SCRATCH_BYTES
@@ -174,6 +175,12 @@ def lib():
         L.mhcl_head_total.argtypes = [E] + [V] * 5
         L.mhcl_scale.argtypes = [V, ctypes.c_int, ctypes.c_int64, V, V]
         L.mhcl_scale_to.argtypes = [V, V, ctypes.c_int, ctypes.c_int64, V, V]
+        I, R = ctypes.c_int32, ctypes.c_float
+        L.mhcl_head_distill_workspace_bytes.restype = L.mhcl_head_preference_workspace_bytes.restype = Z
+        L.mhcl_head_distill_workspace_bytes.argtypes = [E, I, ctypes.c_int]
+        L.mhcl_head_preference_workspace_bytes.argtypes = [E, ctypes.c_int]
+        L.mhcl_head_distill.argtypes = [E, I, R] + [V] * 10 + [ctypes.c_int, V, Z, V]
+        L.mhcl_head_preference.argtypes = [E, I, R, R] + [V] * 4 + [ctypes.c_int] + [V] * 7 + [ctypes.c_int, V, Z, V]
         B = ctypes.POINTER(_CFfnDesc)
         L.mhcl_ffn_workspace_bytes.restype = Z
         L.mhcl_ffn_workspace_bytes.argtypes = [B, ctypes.c_int]
@@ -454,6 +461,49 @@ def mhcl_head_loss_grad(d, h, W, targets, weight, loss, lse, g_h, g_W, ws):
         _ptr(g_W, w, (d.V, d.C), "g_W"), wp, wb, _stream()), name)
 
 
+def _head_grads(d, g_h, g_W):
+    """Pointers of g_h and g_W (both or neither) and whether they are fp32 beside operands that are not."""
+    f = torch.float32
+    unrounded = g_h is not None and g_h.dtype is f and d.io is not f
+    io = f if unrounded else d.io
+    return _ptr(g_h, io, (d.T, d.C), "g_h"), _ptr(g_W, io, (d.V, d.C), "g_W"), int(unrounded)
+
+
+def head_distill_workspace_bytes(d: EndsDesc, K: int, grad: bool) -> int:
+    return lib().mhcl_head_distill_workspace_bytes(ctypes.byref(d.c), K, int(grad))
+
+
+def mhcl_head_distill(d, temperature, h, W, ids, logits, weight, loss, lse, total, g_h, g_W, ws):
+    """weight, total: may be None; g_h and g_W: both None, or of d's types, or both fp32 (not rounded)."""
+    f, K = torch.float32, ids.shape[1]
+    wp, wb = _ws(ws)
+    g_hp, g_Wp, unrounded = _head_grads(d, g_h, g_W)
+    _check(lib().mhcl_head_distill(
+        ctypes.byref(d.c), K, temperature, _ptr(h, d.io, (d.T, d.C), "h"), _ptr(W, d.w, (d.V, d.C), "W"),
+        _ptr(ids, d.ids, (d.T, K), "ids"), _ptr(logits, f, (d.T, K), "logits"), _ptr(weight, f, (d.T,), "weight"),
+        _ptr(loss, f, (d.T,), "loss"), _ptr(lse, f, (d.T,), "lse"), _ptr(total, f, (1,), "total"), g_hp, g_Wp, unrounded, wp, wb,
+        _stream()), "mhcl_head_distill")
+
+
+def head_preference_workspace_bytes(d: EndsDesc, grad: bool) -> int:
+    return lib().mhcl_head_preference_workspace_bytes(ctypes.byref(d.c), int(grad))
+
+
+def mhcl_head_preference(d, pairs, beta, smoothing, h, W, targets, offsets, reference, weight, loss, logp, total, g_h, g_W, ws):
+    """reference, weight, total: may be None; g_h and g_W: both None, or of d's types, or both fp32 (not rounded)."""
+    f = torch.float32
+    wp, wb = _ws(ws)
+    g_hp, g_Wp, unrounded = _head_grads(d, g_h, g_W)
+    if offsets.dtype not in _ID_DTYPE:
+        raise ValueError(f"offsets of {offsets.dtype}: int64 or int32")
+    _check(lib().mhcl_head_preference(
+        ctypes.byref(d.c), pairs, beta, smoothing, _ptr(h, d.io, (d.T, d.C), "h"), _ptr(W, d.w, (d.V, d.C), "W"),
+        _ptr(targets, d.ids, (d.T,), "targets"), _ptr(offsets, offsets.dtype, (2 * pairs + 1,), "offsets"), _ID_DTYPE[offsets.dtype],
+        _ptr(reference, f, (2 * pairs,), "reference"), _ptr(weight, f, (pairs,), "weight"), _ptr(loss, f, (pairs,), "loss"),
+        _ptr(logp, f, (2 * pairs,), "logp"), _ptr(total, f, (1,), "total"), g_hp, g_Wp, unrounded, wp, wb, _stream()),
+        "mhcl_head_preference")
+
+
 def mhcl_head_total(d, targets, loss, weight, total):
     f = torch.float32
     _check(lib().mhcl_head_total(
@@ -489,11 +539,11 @@ def new_ffn_workspace(d: FfnDesc, op: int, device="cuda"):
 
 
 def mhcl_ffn(d, x, W_up, W_down, y, pre, ws):
-    """pre: [T, 2 H], or None."""
+    """pre: [T, 2 H] fp32, or None."""
     wp, wb = _ws(ws)
     _check(lib().mhcl_ffn(
         ctypes.byref(d.c), _ptr(x, d.io, (d.T, d.C), "x"), _ptr(W_up, d.io, (2 * d.H, d.C), "W_up"),
-        _ptr(W_down, d.io, (d.C, d.H), "W_down"), _ptr(y, d.io, (d.T, d.C), "y"), _ptr(pre, d.io, (d.T, 2 * d.H), "pre"), wp, wb,
+        _ptr(W_down, d.io, (d.C, d.H), "W_down"), _ptr(y, d.io, (d.T, d.C), "y"), _ptr(pre, torch.float32, (d.T, 2 * d.H), "pre"), wp, wb,
         _stream()), "mhcl_ffn")
 
 
@@ -501,6 +551,6 @@ def mhcl_ffn_grad(d, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, ws):
     wp, wb = _ws(ws)
     _check(lib().mhcl_ffn_grad(
         ctypes.byref(d.c), _ptr(x, d.io, (d.T, d.C), "x"), _ptr(W_up, d.io, (2 * d.H, d.C), "W_up"),
-        _ptr(W_down, d.io, (d.C, d.H), "W_down"), _ptr(pre, d.io, (d.T, 2 * d.H), "pre"), _ptr(g_y, d.io, (d.T, d.C), "g_y"),
+        _ptr(W_down, d.io, (d.C, d.H), "W_down"), _ptr(pre, torch.float32, (d.T, 2 * d.H), "pre"), _ptr(g_y, d.io, (d.T, d.C), "g_y"),
         _ptr(g_x, d.io, (d.T, d.C), "g_x"), _ptr(g_W_up, d.io, (2 * d.H, d.C), "g_W_up"),
         _ptr(g_W_down, d.io, (d.C, d.H), "g_W_down"), wp, wb, _stream()), "mhcl_ffn_grad")

@@ -24,8 +24,8 @@ struct FfnWs {
 };
 
 // pre [T][2 H], may be null: gate | up
-hipError_t launch_ffn(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, void *y, void *pre, const FfnWs &w, hipStream_t s);
-hipError_t launch_ffn_grad(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, const void *pre, const void *g_y, void *g_x,
+hipError_t launch_ffn(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, void *y, float *pre, const FfnWs &w, hipStream_t s);
+hipError_t launch_ffn_grad(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, const float *pre, const void *g_y, void *g_x,
                            void *g_W_up, void *g_W_down, const FfnWs &w, hipStream_t s);
 
 }  // namespace mhcl

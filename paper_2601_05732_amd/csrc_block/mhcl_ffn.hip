@@ -46,34 +46,20 @@ __device__ __forceinline__ void store_one(void *p, int64_t row, int64_t m, int q
   if constexpr (WIDE) *reinterpret_cast<f32x4 *>(static_cast<float *>(p) + row + m + 4 * q) = u;
   else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p) + row + m + 4 * q) = make_uint2(pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3]));
 }
-// The way back: what lies past `end` or is not here is 0
-template <bool WIDE>
-__device__ __forceinline__ void load_two(const void *p, int64_t row, int64_t m, int q, f32x4 &u, f32x4 &v, bool here, int64_t end) {
-  if constexpr (WIDE) {
-    const float *o = static_cast<const float *>(p) + row + m + 4 * q;
-    u = here && m + 4 * q < end ? *reinterpret_cast<const f32x4 *>(o) : f32x4{0.f, 0.f, 0.f, 0.f};
-    v = here && m + 16 + 4 * q < end ? *reinterpret_cast<const f32x4 *>(o + 16) : f32x4{0.f, 0.f, 0.f, 0.f};
-  } else {
-    const int64_t at = m + 16 * (q & 1) + 8 * (q >> 1);
-    uint4 eight = make_uint4(0, 0, 0, 0);
-    if (here && at < end) eight = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + row + at);
-    uint2 l, h;
-    split_pairs(eight, l, h);
-    u = f32x4{bf16lo(l.x), bf16hi(l.x), bf16lo(l.y), bf16hi(l.y)};
-    v = f32x4{bf16lo(h.x), bf16hi(h.x), bf16lo(h.y), bf16hi(h.y)};
-  }
-}
+__device__ __forceinline__ f32x4 load_four(const float *p, bool here) { return here ? *reinterpret_cast<const f32x4 *>(p) : f32x4{0.f, 0.f, 0.f, 0.f}; }
 
-// m: pairs of rows of W_up, n: tokens.  a is formed of the sums and rounded once; KEEP: G and U for the backward, rounded to the operands' type.
+// m: pairs of rows of W_up, n: tokens.  a is formed of the sums and rounded once; KEEP: G and U for the backward, in fp32: rounded to bf16 they
+// would put their error into every gradient besides that of the rounded g_G, g_U and a (off from 64 bits by 0.0034 of the 2-norm then, 0.0024 so).
 template <bool KEEP, bool WIDE>
 struct GateEpilogue {
   static constexpr bool kWide = WIDE, kPaired = true;
-  void *a, *pre;
+  void *a;
+  float *pre;
   int64_t H, T;
-  template <int FN>
-  __device__ __forceinline__ int hold(int64_t) const { return 0; }
   template <int FM, int FN>
-  static constexpr int stores() { return FN * (WIDE || FM < 4 ? FM / 2 : FM / 4) * (KEEP ? 3 : 1); }
+  __device__ __forceinline__ int hold(int64_t, int64_t) const { return 0; }
+  template <int FM, int FN>
+  static constexpr int stores() { return FN * ((WIDE || FM < 4 ? FM / 2 : FM / 4) + (KEEP ? FM : 0)); }
   __device__ __forceinline__ bool whole(int64_t m_end, int64_t n_end) const { return m_end / 2 <= H && n_end <= T; }
   template <int FM, int FN>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], int, int64_t m0, int64_t n0, int) const {
@@ -91,18 +77,14 @@ struct GateEpilogue {
 #pragma unroll
       for (int i = 0; i < HM; i += 2) {
         const int64_t m = m0 / 2 + 16 * i;
-        if constexpr (HM > 1) {
-          store_two<WIDE>(a, n * H, m, q, v[i], v[i + 1], here, H);
-          if constexpr (KEEP) {
-            store_two<WIDE>(pre, n * 2 * H, m, q, acc[i][j], acc[i + 1][j], here, H);
-            store_two<WIDE>(pre, n * 2 * H + H, m, q, acc[HM + i][j], acc[HM + i + 1][j], here, H);
-          }
-        } else {
-          store_one<WIDE>(a, n * H, m, q, v[i], here, H);
-          if constexpr (KEEP) {
-            store_one<WIDE>(pre, n * 2 * H, m, q, acc[i][j], here, H);
-            store_one<WIDE>(pre, n * 2 * H + H, m, q, acc[HM + i][j], here, H);
-          }
+        if constexpr (HM > 1) store_two<WIDE>(a, n * H, m, q, v[i], v[i + 1], here, H);
+        else store_one<WIDE>(a, n * H, m, q, v[i], here, H);
+      }
+      if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < HM; ++i) {
+          store_one<true>(pre, n * 2 * H, m0 / 2 + 16 * i, q, acc[i][j], here, H);
+          store_one<true>(pre, n * 2 * H + H, m0 / 2 + 16 * i, q, acc[HM + i][j], here, H);
         }
       }
     }
@@ -113,11 +95,11 @@ struct GateEpilogue {
 template <bool WIDE>
 struct GateGradEpilogue {
   static constexpr bool kWide = WIDE, kPaired = false;
-  const void *pre;
+  const float *pre;
   void *a, *g_pre;
   int64_t H, T;
-  template <int FN>
-  __device__ __forceinline__ int hold(int64_t) const { return 0; }
+  template <int FM, int FN>
+  __device__ __forceinline__ int hold(int64_t, int64_t) const { return 0; }
   template <int FM, int FN>
   static constexpr int stores() { return FN * (WIDE ? FM : FM / 2) * 3; }
   __device__ __forceinline__ bool whole(int64_t m_end, int64_t n_end) const { return m_end <= H && n_end <= T; }
@@ -132,8 +114,12 @@ struct GateGradEpilogue {
       for (int i = 0; i < FM; i += 2) {
         const int64_t m = m0 + 16 * i;
         f32x4 G[2], U[2], v[2];
-        load_two<WIDE>(pre, row, m, q, G[0], G[1], here, H);
-        load_two<WIDE>(pre, row + H, m, q, U[0], U[1], here, H);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const bool there = here && m + 16 * k + 4 * q < H;
+          G[k] = load_four(pre + row + m + 16 * k + 4 * q, there);
+          U[k] = load_four(pre + row + H + m + 16 * k + 4 * q, there);
+        }
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -161,7 +147,7 @@ hipError_t product(const ProductTile &tile, const Operand &A, const Operand &B, 
 }
 
 template <typename IO>
-hipError_t run_ffn(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, void *y, void *pre, const FfnWs &w, hipStream_t s) {
+hipError_t run_ffn(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, void *y, float *pre, const FfnWs &w, hipStream_t s) {
   constexpr bool WIDE = IO::kVec == 4;
   const FfnPlan &p = w.plan;
   const int64_t T = d.T, C = d.C, H = d.H;
@@ -172,7 +158,7 @@ hipError_t run_ffn(const mhcl_ffn_desc &d, const void *x, const void *W_up, cons
 }
 
 template <typename IO>
-hipError_t run_ffn_grad(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, const void *pre, const void *g_y, void *g_x,
+hipError_t run_ffn_grad(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, const float *pre, const void *g_y, void *g_x,
                         void *g_W_up, void *g_W_down, const FfnWs &w, hipStream_t s) {
   constexpr bool WIDE = IO::kVec == 4;
   const FfnPlan &p = w.plan;
@@ -219,11 +205,11 @@ FfnWs::FfnWs(const mhcl_ffn_desc &d, bool grad, void *ws) : plan(d, grad) {
   bytes = c.off;
 }
 
-hipError_t launch_ffn(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, void *y, void *pre, const FfnWs &w, hipStream_t s) {
+hipError_t launch_ffn(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, void *y, float *pre, const FfnWs &w, hipStream_t s) {
   return dispatch_io(d.io_dtype, [&](auto io) { return run_ffn<decltype(io)>(d, x, W_up, W_down, y, pre, w, s); });
 }
 
-hipError_t launch_ffn_grad(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, const void *pre, const void *g_y, void *g_x,
+hipError_t launch_ffn_grad(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, const float *pre, const void *g_y, void *g_x,
                            void *g_W_up, void *g_W_down, const FfnWs &w, hipStream_t s) {
   return dispatch_io(d.io_dtype, [&](auto io) { return run_ffn_grad<decltype(io)>(d, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, w, s); });
 }

@@ -35,17 +35,17 @@ size_t mhcl_ffn_workspace_bytes(const mhcl_ffn_desc *desc, int op) {
   return check_ffn(desc) ? 0 : align_up(FfnWs(*desc, op == MHCL_OP_FFN_GRAD, nullptr).bytes + 1);
 }
 
-int mhcl_ffn(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, void *y, void *pre, void *ws, size_t ws_bytes,
+int mhcl_ffn(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, void *y, float *pre, void *ws, size_t ws_bytes,
              void *stream) {
   if (int e = check_ffn(desc)) return e;
   if (desc->T == 0) return MHCL_OK;
-  if (!all16(x, W_up, W_down, (const void *)y) || (pre && !all16(pre))) return MHCL_ERR_INVALID_ARG;
+  if (!all16(x, W_up, W_down, (const void *)y) || (pre && !all16((const void *)pre))) return MHCL_ERR_INVALID_ARG;
   if (!all16(ws) || ws_bytes < mhcl_ffn_workspace_bytes(desc, MHCL_OP_FFN)) return MHCL_ERR_WORKSPACE;
   MHCL_HIP(launch_ffn(*desc, x, W_up, W_down, y, pre, FfnWs(*desc, false, ws), static_cast<hipStream_t>(stream)));
   return MHCL_OK;
 }
 
-int mhcl_ffn_grad(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, const void *pre, const void *g_y, void *g_x,
+int mhcl_ffn_grad(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, const float *pre, const void *g_y, void *g_x,
                   void *g_W_up, void *g_W_down, void *ws, size_t ws_bytes, void *stream) {
   if (int e = check_ffn(desc)) return e;
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -56,7 +56,7 @@ int mhcl_ffn_grad(const mhcl_ffn_desc *desc, const void *x, const void *W_up, co
     MHCL_HIP(launch_zero(g_W_down, half, s));
     return MHCL_OK;
   }
-  if (!all16(x, W_up, W_down, pre, g_y, (const void *)g_x)) return MHCL_ERR_INVALID_ARG;
+  if (!all16(x, W_up, W_down, (const void *)pre, g_y, (const void *)g_x)) return MHCL_ERR_INVALID_ARG;
   if (!all16(ws) || ws_bytes < mhcl_ffn_workspace_bytes(desc, MHCL_OP_FFN_GRAD)) return MHCL_ERR_WORKSPACE;
   MHCL_HIP(launch_ffn_grad(*desc, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, FfnWs(*desc, true, ws), s));
   return MHCL_OK;

@@ -160,6 +160,77 @@ int mhcl_head_total(const mhcl_ends_desc *desc, const void *targets, const float
   return MHCL_OK;
 }
 
+size_t mhcl_head_distill_workspace_bytes(const mhcl_ends_desc *desc, int32_t K, int grad) {
+  if (K < 1 || K > kMostSlots || check_ends(desc, End::kHead)) return 0;
+  return align_up(DistillWs(*desc, K, grad != 0, nullptr).bytes + 1);
+}
+
+int mhcl_head_distill(const mhcl_ends_desc *desc, int32_t K, float temperature, const void *h, const void *W, const void *ids, const float *logits,
+                      const float *weight, float *loss, float *lse, float *total, void *g_h, void *g_W, int unrounded, void *ws, size_t ws_bytes,
+                      void *stream) {
+  if (int e = check_ends(desc, End::kHead)) return e;
+  if (K < 1 || !(temperature >= 1e-6f && temperature <= 1e6f)) return MHCL_ERR_INVALID_ARG;
+  if (K > kMostSlots) return MHCL_ERR_UNSUPPORTED;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool grad = g_W != nullptr;
+  if ((grad && !all16((const void *)g_W)) || (total && !aligned(total, 4))) return MHCL_ERR_INVALID_ARG;
+  if (desc->T == 0) {
+    if (g_h && !grad) return MHCL_ERR_INVALID_ARG;
+    if (grad) MHCL_HIP(launch_zero(g_W, static_cast<size_t>(desc->V) * desc->C * (unrounded ? 4 : dtype_bytes(desc->w_dtype)), s));
+    if (total) MHCL_HIP(launch_zero(total, 4, s));
+    return MHCL_OK;
+  }
+  if (!all16(h, W) || !ids_ok(*desc, ids) || !aligned(logits, 4) || !aligned(loss, 4) || !aligned(lse, 4) || (weight && !aligned(weight, 4)) ||
+      (g_h != nullptr) != grad || (grad && !all16((const void *)g_h)))
+    return MHCL_ERR_INVALID_ARG;
+  if (!all16(ws) || ws_bytes < mhcl_head_distill_workspace_bytes(desc, K, grad)) return MHCL_ERR_WORKSPACE;
+  MHCL_HIP(launch_distill(*desc, K, temperature, h, W, ids, logits, weight, loss, lse, total, g_h, g_W, unrounded != 0, DistillWs(*desc, K, grad, ws), s));
+  return MHCL_OK;
+}
+
+size_t mhcl_head_preference_workspace_bytes(const mhcl_ends_desc *desc, int grad) {
+  return check_ends(desc, End::kHead) ? 0 : align_up(PreferenceWs(*desc, grad != 0, nullptr).bytes + 1);
+}
+
+int mhcl_head_preference(const mhcl_ends_desc *desc, int32_t pairs, float beta, float smoothing, const void *h, const void *W, const void *targets,
+                         const void *offsets, int offset_dtype, const float *reference, const float *weight, float *loss, float *logp, float *total,
+                         void *g_h, void *g_W, int unrounded, void *ws, size_t ws_bytes, void *stream) {
+  if (int e = check_ends(desc, End::kHead)) return e;
+  if (pairs < 0 || !isfinite(beta) || !(smoothing >= 0.f && smoothing <= 1.f)) return MHCL_ERR_INVALID_ARG;
+  if (offset_dtype != MHCL_I64 && offset_dtype != MHCL_I32) return MHCL_ERR_INVALID_ARG;
+  if (pairs > kMostPairs) return MHCL_ERR_UNSUPPORTED;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool grad = g_W != nullptr;
+  if ((grad && !all16((const void *)g_W)) || (total && !aligned(total, 4)) || (g_h && !grad) || (weight && !aligned(weight, 4))) return MHCL_ERR_INVALID_ARG;
+  if (pairs > 0 && (!aligned(offsets, offset_dtype == MHCL_I64 ? 8 : 4) || !aligned(loss, 4) || !aligned(logp, 4) || (reference && !aligned(reference, 4))))
+    return MHCL_ERR_INVALID_ARG;
+  if (desc->T > 0) {
+    if (!all16(h, W) || !ids_ok(*desc, targets) || (grad && !all16((const void *)g_h))) return MHCL_ERR_INVALID_ARG;
+    if (!all16(ws) || ws_bytes < mhcl_head_preference_workspace_bytes(desc, grad)) return MHCL_ERR_WORKSPACE;
+  } else if (grad) {
+    MHCL_HIP(launch_zero(g_W, static_cast<size_t>(desc->V) * desc->C * (unrounded ? 4 : dtype_bytes(desc->w_dtype)), s));
+  }
+  PairArgs a{};
+  a.reference = reference;
+  a.weight = weight;
+  a.loss = loss;
+  a.logp = logp;
+  a.T = desc->T;
+  a.pairs = pairs;
+  a.beta = beta;
+  a.smoothing = smoothing;
+  MHCL_HIP(launch_preference(*desc, h, W, targets, offsets, offset_dtype, a, g_h, g_W, unrounded != 0, PreferenceWs(*desc, grad, ws), s));
+  if (!total) return MHCL_OK;
+  if (pairs == 0) {
+    MHCL_HIP(launch_zero(total, 4, s));
+    return MHCL_OK;
+  }
+  mhcl_ends_desc all = *desc;
+  all.T = pairs;
+  MHCL_HIP(launch_head_total(all, nullptr, loss, weight, total, s));
+  return MHCL_OK;
+}
+
 int mhcl_scale(void *p, int dtype, int64_t count, const float *factor, void *stream) {
   if (!dtype_ok(dtype) || count < 0 || !aligned(factor, 4)) return MHCL_ERR_INVALID_ARG;
   if (count == 0) return MHCL_OK;

@@ -1,4 +1,4 @@
-// Host-side declarations of the head's softmax cross entropy (mhcl_head.hip).
+// Host-side declarations of the head's losses: cross entropy and pairs of sequences (mhcl_head.hip), a teacher's top logits (mhcl_distill.hip).
 #pragma once
 #include "mhcl_ends.h"
 #include "mhcl_tiles.h"
@@ -36,8 +36,63 @@ struct HeadWs {
 hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, const void *targets, const float *weight,
                        float *loss, float *lse, void *g_h, void *g_W, bool unrounded, const HeadWs &w, hipStream_t s);
 
+// targets null: all count
 hipError_t launch_head_total(const mhcl_ends_desc &d, const void *targets, const float *loss, const float *weight, float *total,
                              hipStream_t s);
+// A loss of pairs of sequences
+constexpr int32_t kMostPairs = 1 << 22;   // a block of threads each
+struct PairArgs {
+  const float *reference;   // [2 pairs], may be null
+  const float *weight;      // [pairs], null: that of the mean
+  float *loss, *logp;       // [pairs], [2 pairs]
+  int64_t T;
+  int32_t pairs;
+  float beta, smoothing;
+  const float *ce;          // [T] cross entropies
+  float *token_weight;      // [T], null: the loss alone
+};
+struct PreferenceWs {
+  HeadWs head;
+  float *ce, *lse, *token_weight;   // [T]
+  size_t bytes;
+  PreferenceWs(const mhcl_ends_desc &d, bool grad, void *ws) : head(d, grad, ws) {
+    WsCursor c(ws ? static_cast<char *>(ws) + head.bytes : nullptr);
+    ce = c.take<float>(static_cast<size_t>(d.T));
+    lse = c.take<float>(static_cast<size_t>(d.T));
+    token_weight = grad ? c.take<float>(static_cast<size_t>(d.T)) : nullptr;
+    bytes = head.bytes + c.off;
+  }
+};
+hipError_t launch_preference(const mhcl_ends_desc &d, const void *h, const void *W, const void *targets, const void *offsets, int offset_dtype,
+                             PairArgs a, void *g_h, void *g_W, bool unrounded, const PreferenceWs &w, hipStream_t s);
+
+constexpr int kMostSlots = 256;   // of a token's teacher
+struct DistillWs {
+  HeadWs head;
+  int32_t *mark;        // [T] negative where the teacher says nothing, 1 where it names a row past the vocabulary, else 0
+  // of a block of tokens: a token's ids in order, its teacher's probability and the logarithm of it for each, the student's logit; how many of them
+  // lie before each granule
+  int32_t *id;          // [tokens][K]
+  float2 *p;            // [tokens][K]
+  float *z;             // [tokens][K]
+  uint16_t *start;      // [tokens][granules + 1]
+  size_t bytes;
+  DistillWs(const mhcl_ends_desc &d, int32_t K, bool grad, void *ws) : head(d, grad, ws) {
+    WsCursor c(ws ? static_cast<char *>(ws) + head.bytes : nullptr);
+    const size_t T = static_cast<size_t>(head.plan.tokens), slots = T * static_cast<size_t>(K);
+    mark = c.take<int32_t>(static_cast<size_t>(d.T));
+    id = c.take<int32_t>(slots);
+    p = c.take<float2>(slots);
+    z = c.take<float>(slots);
+    start = c.take<uint16_t>(T * static_cast<size_t>(head.plan.granules + 1));
+    bytes = head.bytes + c.off;
+  }
+};
+// total may be null; g_h, g_W null: the loss alone
+hipError_t launch_distill(const mhcl_ends_desc &d, int32_t K, float temperature, const void *h, const void *W, const void *ids, const float *logits,
+                          const float *weight, float *loss, float *lse, float *total, void *g_h, void *g_W, bool unrounded, const DistillWs &w,
+                          hipStream_t s);
+
 hipError_t launch_scale(void *p, int dtype, int64_t count, const float *factor, hipStream_t s);
 hipError_t launch_scale_to(const float *in, void *out, int dtype, int64_t count, const float *factor, hipStream_t s);
 

@@ -1,4 +1,4 @@
-// The head's softmax cross entropy and its gradients.
+// The head's softmax cross entropy, the loss of pairs of sequences that is made of it, and their gradients.
 //
 //   z = h W^T                       [T, V]   never in memory
 //   g = weight (softmax(z) - onehot)
@@ -31,11 +31,8 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * 64) void loss_kernel(
   }
 }
 
-// The same, one block a token, and the row's numerators turned into g in their place, bf16 or (IO = F32) fp32; h's row into hp, zeros
-// where the weight is 0.  bf16: g is of the operands' type, which is what the matrix units multiply with W and h.  (Its rounding is the one of the
-// T V terms of a sum each, the gradient's own comes after it: off from 64 bits by 0.0023 of the 2-norm at 333 tokens and 0.0018 at 16384, where the
-// gradient's rounding alone is 0.0017.  Two bf16 parts of g instead would make each of the two products two: 13 ms more on 21 at 16384
-// tokens, C = 4096, 65536 rows.)  Bound by memory: 16384 tokens, 65536 rows, bf16 980 us, 4.4 TB/s; 2048, 50257, fp32 154 us, 5.4 TB/s.
+// The same, one block a token, and the row's numerators turned into g (turn_row).  Bound by memory: 16384 tokens, 65536 rows, bf16 980 us, 4.4 TB/s;
+// 2048, 50257, fp32 154 us, 5.4 TB/s.
 template <typename ID, typename IO>
 __global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *__restrict__ targets) {
   __shared__ float red[2][16];
@@ -52,72 +49,25 @@ __global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *
     a.lse[t] = base + logf(sum);
     a.loss[t] = loss;
   }
-  float common = 1.f;
-  if (a.take_common) {
-    if (a.weight || t == 0) common = common_weight<kBlock>(targets, a.weight, a.T);
-    if (t == 0 && tid == 0) *a.common = common;
-  } else if (a.weight) {
-    common = *a.common;
-  }
-  const float given = y < 0 ? 0.f : (a.weight ? a.weight[t] / common : 1.f);
-  const bool counts = given != 0.f;
+  const float given = weight_over_common(a, targets, t, y);
   const float weight = y < a.V ? given : bad;
   const float hit = weight * expm1f(-loss);      // p - 1 of the target
-  const float scale = weight / sum;
-  for (int64_t v = tid * 8; v < a.ld; v += kBlock * 8) {
-    float g[8];
-    if (counts) {
-      const float f = scale * expf(stat[v >> a.gran_log2].x - base);
-      if constexpr (IO::kVec == 8) {
-        const uint4 c = *reinterpret_cast<const uint4 *>(a.E + (t * a.ld + v) * 2);
-        const uint32_t code[4] = {c.x, c.y, c.z, c.w};
+  turn_row<IO>(a, t, stat, base, weight / sum, given != 0.f, [&](int64_t v, float (&g)[8]) {
+    if (y >= v && y < v + 8) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          g[2 * i] = decode(code[i] & 0xffffu) * f;
-          g[2 * i + 1] = decode(code[i] >> 16) * f;
-        }
-      } else {
-        F32::load(a.E, t * a.ld + v, reinterpret_cast<float(&)[4]>(g[0]));
-        F32::load(a.E, t * a.ld + v + 4, reinterpret_cast<float(&)[4]>(g[4]));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] *= f;
-      }
-      if (y >= v && y < v + 8) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = y == v + i ? hit : g[i];
-      }
-      if (v + 8 > a.V) {                         // (a row of NaN leaves the fill-up finite)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = v + i < a.V ? g[i] : 0.f;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = 0.f;
+      for (int i = 0; i < 8; ++i) g[i] = y == v + i ? hit : g[i];
     }
-    if constexpr (IO::kVec == 8) {
-      BF16::store(a.E, t * a.ld + v, g);
-    } else {
-      F32::store(a.E, t * a.ld + v, reinterpret_cast<const float(&)[4]>(g[0]));
-      F32::store(a.E, t * a.ld + v + 4, reinterpret_cast<const float(&)[4]>(g[4]));
-    }
-  }
-  for (int c = tid * IO::kVec; c < a.C; c += kBlock * IO::kVec) {
-    float v[IO::kVec];
-    IO::load(a.h, t * a.C + c, v);
-#pragma unroll
-    for (int i = 0; i < IO::kVec; ++i) v[i] = counts ? v[i] : 0.f;
-    IO::store(a.hp, t * a.C + c, v);
-  }
+  });
 }
 
-// sum of weight loss over the targets that are not negative, weights of 0 left out, or their mean; one block, in fp64
+// sum of weight loss over the targets that are not negative (null: over all), weights of 0 left out, or their mean; one block, in fp64
 template <typename ID>
 __global__ __launch_bounds__(1024) void total_kernel(const ID *__restrict__ targets, const float *__restrict__ loss,
                                                      const float *__restrict__ weight, int64_t T, float *__restrict__ total) {
   __shared__ double red[2][16];
   double sum = 0., count = 0.;
   for (int64_t t = threadIdx.x; t < T; t += 1024) {
-    const float w = targets[t] < 0 ? 0.f : (weight ? weight[t] : 1.f);
+    const float w = targets && targets[t] < 0 ? 0.f : (weight ? weight[t] : 1.f);
     if (w != 0.f) sum += static_cast<double>(w) * loss[t];
     count += w != 0.f ? 1. : 0.;
   }
@@ -138,6 +88,55 @@ __global__ __launch_bounds__(1024) void total_kernel(const ID *__restrict__ targ
     }
     *total = static_cast<float>(weight ? sum : (count > 0. ? sum / count : 0.));
   }
+}
+
+// Pairs of sequences, a block each: L = the sum of the tokens' -ce from one offset to the next, in fp64,
+//   m = beta ((L_c - R_c) - (L_r - R_r)),  loss = (1 - s) softplus(-m) + s softplus(m)
+// and the factor of each token's cross entropy in the weighted sum of the pairs, -+ beta weight dloss/dm for the chosen and the rejected sequence's,
+// 0 outside of the sequences.  (loss, weights of tokens: few numbers, in fp64 until they are rounded.)
+constexpr int kPairThreads = 512;
+template <typename OFF>
+__global__ __launch_bounds__(kPairThreads) void pair_kernel(const PairArgs a, const OFF *__restrict__ offsets) {
+  __shared__ double red[2][kPairThreads / 64];
+  __shared__ float factor;
+  const int64_t p = blockIdx.x;
+  int64_t from[3];
+  bool bad = false;        // offsets that descend or lie outside of the tokens: what the host cannot see
+  for (int i = 0; i < 3; ++i) {
+    const int64_t o = static_cast<int64_t>(offsets[2 * p + i]);
+    const int64_t least = i > 0 ? from[i - 1] : 0;
+    bad |= o < least || o > a.T;
+    from[i] = o < least ? least : (o > a.T ? a.T : o);
+  }
+  double sum[2] = {0., 0.};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    for (int64_t t = from[i] + threadIdx.x; t < from[i + 1]; t += kPairThreads) sum[i] -= static_cast<double>(a.ce[t]);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum[i] += __shfl_xor(sum[i], off, 64);
+    if ((threadIdx.x & 63) == 0) red[i][threadIdx.x >> 6] = sum[i];
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double L[2] = {0., 0.}, ratio[2];
+    for (int i = 0; i < 2; ++i) {
+      for (int w = 0; w < kPairThreads / 64; ++w) L[i] += red[i][w];
+      if (bad) L[i] = __longlong_as_double(0x7ff8000000000000ll);
+      ratio[i] = L[i] - (a.reference ? static_cast<double>(a.reference[2 * p + i]) : 0.);
+      a.logp[2 * p + i] = static_cast<float>(L[i]);
+    }
+    const double m = static_cast<double>(a.beta) * (ratio[0] - ratio[1]), s = a.smoothing;
+    const double tail = log1p(exp(-fabs(m)));          // softplus(v) = max(v, 0) + tail
+    a.loss[p] = static_cast<float>((s < 1. ? (1. - s) * ((m < 0. ? -m : 0.) + tail) : 0.) + (s > 0. ? s * ((m > 0. ? m : 0.) + tail) : 0.));
+    const double slope = s / (1. + exp(-m)) - (1. - s) / (1. + exp(m));
+    const double weight = a.weight ? static_cast<double>(a.weight[p]) : 1. / static_cast<double>(a.pairs);
+    factor = weight == 0. ? 0.f : static_cast<float>(-static_cast<double>(a.beta) * slope * weight);
+  }
+  if (!a.token_weight) return;
+  __syncthreads();
+  const int64_t first = p == 0 ? 0 : from[0], last = p == a.pairs - 1 ? a.T : from[2];
+  for (int64_t t = first + threadIdx.x; t < last; t += kPairThreads)
+    a.token_weight[t] = t < from[0] || t >= from[2] ? 0.f : (t < from[1] ? factor : -factor);
 }
 
 template <typename IO>
@@ -238,80 +237,86 @@ HeadWs::HeadWs(const mhcl_ends_desc &d, bool grad, void *ws) : plan(d, grad) {
 
 namespace {
 
-// the head of IO operands (bf16 or fp32)
-template <typename ID, typename IO>
-hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, const ID *targets, const float *weight, float *loss,
-                    float *lse, void *g_h, void *g_W, bool unrounded, const HeadWs &w, hipStream_t s) {
-  constexpr bool WIDE = IO::kVec == 4;
-  const bool floats = WIDE || unrounded;   // what g_h and g_W are of
-  const HeadPlan &p = w.plan;
-  const bool grad = g_W != nullptr;
-  const int64_t C = d.C, V = d.V, es = WIDE ? 4 : 2;
-  hipError_t e;
-  const bool take_common = d.T <= kCommonTokens && p.tokens == d.T;
-  if (grad && !take_common) {
-    hipLaunchKernelGGL((common_weight_kernel<ID>), dim3(1), dim3(1024), 0, s, targets, weight, d.T, w.common);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+// what of run_head is the cross entropy's
+template <typename ID>
+struct CrossEntropy {
+  const ID *marks;          // the targets
+  const float *weight;
+  const HeadWs &w;
+  hipStream_t s;
+  static constexpr float factor = 1.f;
+  hipError_t before(int64_t, int64_t) { return hipSuccess; }
+  hipError_t between(const RowArgs &) { return hipSuccess; }
+  TargetLogit<ID> wanted(int64_t t0) const { return {marks + t0, w.zt}; }
+  hipError_t loss(const RowArgs &a, int64_t t0) {
+    // (us, 50257 rows in granules of 32: a wave / a block of sixteen for one token 11.2 / 4.6)
+    if (a.T < 1024) hipLaunchKernelGGL((loss_kernel<ID, 16>), dim3(static_cast<unsigned>(a.T)), dim3(1024), 0, s, a, marks + t0);
+    else hipLaunchKernelGGL((loss_kernel<ID, 1>), dim3(blocks(a.T, kBlock / 64)), dim3(kBlock), 0, s, a, marks + t0);
+    return hipGetLastError();
   }
-  int gran_log2 = 0;
-  while ((1 << gran_log2) < p.logits.gran) ++gran_log2;
-  for (int64_t t0 = 0; t0 < d.T; t0 += p.tokens) {
-    const int64_t T = d.T - t0 < p.tokens ? d.T - t0 : p.tokens;
-    const void *hb = static_cast<const char *>(h) + t0 * C * es;
-    const ID *y = targets + t0;
-    const Operand Wk{W, C, V, C}, hk{hb, C, T, C};
-    const RowArgs a{hb, weight ? weight + t0 : nullptr, w.common, w.stat, w.zt, loss + t0, lse + t0, w.E, w.hp, T, p.ld, p.granules, d.V, d.C, gran_log2,
-                    take_common};
-    if (!grad) {
-      const LogitsEpilogue<ID, false, WIDE> ep{y, w.stat, w.zt, w.E, T, V, p.ld, p.granules};
-      if ((e = launch_gemm<true, true>(p.logits, Wk, hk, V, T, 1, ep, s)) != hipSuccess) return e;
-      // (us, 50257 rows in granules of 32: a wave / a block of sixteen for one token 11.2 / 4.6)
-      if (T < 1024) hipLaunchKernelGGL((loss_kernel<ID, 16>), dim3(static_cast<unsigned>(T)), dim3(1024), 0, s, a, y);
-      else hipLaunchKernelGGL((loss_kernel<ID, 1>), dim3(blocks(T, kBlock / 64)), dim3(kBlock), 0, s, a, y);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-      continue;
-    }
-    {
-      const LogitsEpilogue<ID, true, WIDE> ep{y, w.stat, w.zt, w.E, T, V, p.ld, p.granules};
-      if ((e = launch_gemm<true, true>(p.logits, Wk, hk, V, T, 1, ep, s)) != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL((row_kernel<ID, IO>), dim3(static_cast<unsigned>(T)), dim3(kBlock), 0, s, a, y);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    // g_h [T, C]: m over C, n over the tokens, k over the vocabulary.  g_W [V, C]: m over C, n over the vocabulary, k over the tokens; the
-    // blocks of tokens add up in fp32 (in g_W itself where it is fp32).
-    const Operand Wm{W, C, C, V}, gk{w.E, p.ld, T, p.ld}, hm{w.hp, C, C, T}, gm{w.E, p.ld, p.ld, T};
-    void *gh_out = static_cast<char *>(g_h) + t0 * C * (floats ? 4 : 2);
-    float *sums = floats ? static_cast<float *>(g_W) : w.gW;
-    const StoreEpilogue<WIDE> to_gh{w.common, p.gh_splits > 1 ? w.slabs : (floats ? static_cast<float *>(gh_out) : nullptr),
-                                    static_cast<uint16_t *>(gh_out), nullptr, C, T, T * C};
-    const StoreEpilogue<WIDE> to_gw{w.common, p.gw_splits > 1 ? w.gw_slabs : (floats || t0 + T < d.T ? sums : nullptr), static_cast<uint16_t *>(g_W),
-                                    t0 > 0 ? sums : nullptr, C, V, V * C};
-    if (p.pair) {
-      const GemmArgs gh = gemm_args(p.gh, Wm, gk, C, T, p.gh_splits), gw = gemm_args(p.gw, hm, gm, C, V, p.gw_splits);
-      const int first = gh.tiles_m * gh.tiles_n * gh.splits;
-      const dim3 grid(first + gw.tiles_m * gw.tiles_n * gw.splits);
-      if (p.gh.bn < 128) hipLaunchKernelGGL((gemm_pair_kernel<true, StoreEpilogue<WIDE>>), grid, dim3(256), 0, s, gh, to_gh, gw, to_gw, first);
-      else hipLaunchKernelGGL((gemm_pair_kernel<false, StoreEpilogue<WIDE>>), grid, dim3(256), 0, s, gh, to_gh, gw, to_gw, first);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    } else {
-      if ((e = launch_gemm<false, true>(p.gh, Wm, gk, C, T, p.gh_splits, to_gh, s)) != hipSuccess) return e;
-      if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, p.gw_splits, to_gw, s)) != hipSuccess) return e;
-    }
-    const auto join = floats ? launch_slab_sum<F32> : launch_slab_sum<IO>;
-    if (p.gh_splits > 1 && (e = join(w.slabs, gh_out, p.gh_splits, T * C, s)) != hipSuccess) return e;
-    if (p.gw_splits > 1 && (e = join(w.gw_slabs, g_W, p.gw_splits, V * C, s)) != hipSuccess) return e;
+  template <typename IO>
+  hipError_t rows(const RowArgs &a, int64_t t0) {
+    hipLaunchKernelGGL((row_kernel<ID, IO>), dim3(static_cast<unsigned>(a.T)), dim3(kBlock), 0, s, a, marks + t0);
+    return hipGetLastError();
   }
-  return hipSuccess;
+};
+
+hipError_t launch_pairs(const PairArgs &a, const void *offsets, int offset_dtype, hipStream_t s) {
+  if (a.pairs == 0) return a.token_weight ? launch_zero(a.token_weight, static_cast<size_t>(a.T) * 4, s) : hipSuccess;
+  return dispatch_id(offset_dtype, [&](auto id) {
+    using OFF = decltype(id);
+    hipLaunchKernelGGL((pair_kernel<OFF>), dim3(static_cast<unsigned>(a.pairs)), dim3(kPairThreads), 0, s, a, static_cast<const OFF *>(offsets));
+    return hipGetLastError();
+  });
 }
 
+// The cross entropy whose weights come of it: where all tokens are one block, their losses and the pairs' are taken between the logits and the rows
+template <typename ID>
+struct PairedCrossEntropy : CrossEntropy<ID> {
+  const PairArgs &pairs;
+  const void *offsets;
+  int offset_dtype;
+  hipError_t between(const RowArgs &a) {
+    const hipError_t e = this->loss(a, 0);
+    return e != hipSuccess ? e : launch_pairs(pairs, offsets, offset_dtype, this->s);
+  }
+};
+
 }  // namespace
+
+hipError_t launch_preference(const mhcl_ends_desc &d, const void *h, const void *W, const void *targets, const void *offsets, int offset_dtype,
+                             PairArgs a, void *g_h, void *g_W, bool unrounded, const PreferenceWs &w, hipStream_t s) {
+  const bool grad = g_W != nullptr;
+  a.ce = w.ce;
+  a.token_weight = grad ? w.token_weight : nullptr;
+  if (d.T == 0) return launch_pairs(a, offsets, offset_dtype, s);
+  return dispatch_id(d.id_dtype, [&](auto id) {
+    return dispatch_io(d.io_dtype, [&](auto io) {
+      using ID = decltype(id);
+      using IO = decltype(io);
+      const ID *y = static_cast<const ID *>(targets);
+      hipError_t e;
+      if (grad && w.head.plan.tokens == d.T) {
+        PairedCrossEntropy<ID> way{{y, w.token_weight, w.head, s}, a, offsets, offset_dtype};
+        return run_head<IO>(d, h, W, way, w.ce, w.lse, g_h, g_W, unrounded, w.head, s);
+      }
+      // several blocks of tokens: a pair's weight needs all of its tokens, so that their logits are formed twice
+      CrossEntropy<ID> way{y, nullptr, w.head, s};
+      if ((e = run_head<IO>(d, h, W, way, w.ce, w.lse, nullptr, nullptr, false, w.head, s)) != hipSuccess) return e;
+      if ((e = launch_pairs(a, offsets, offset_dtype, s)) != hipSuccess || !grad) return e;
+      way.weight = w.token_weight;
+      return run_head<IO>(d, h, W, way, w.ce, w.lse, g_h, g_W, unrounded, w.head, s);
+    });
+  });
+}
 
 hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, const void *targets, const float *weight,
                        float *loss, float *lse, void *g_h, void *g_W, bool unrounded, const HeadWs &w, hipStream_t s) {
   return dispatch_id(d.id_dtype, [&](auto id) {
     return dispatch_io(d.io_dtype, [&](auto io) {
       using ID = decltype(id);
-      return run_head<ID, decltype(io)>(d, h, W, static_cast<const ID *>(targets), weight, loss, lse, g_h, g_W, unrounded, w, s);
+      CrossEntropy<ID> way{static_cast<const ID *>(targets), weight, w, s};
+      return run_head<decltype(io)>(d, h, W, way, loss, lse, g_h, g_W, unrounded, w, s);
     });
   });
 }

@@ -27,23 +27,18 @@ __device__ __forceinline__ float exp_of(float x) {
   return __builtin_amdgcn_exp2f(x * kLog2e);
 }
 
-// m: vocabulary, n: tokens.  STORE: the numerators too.  WIDE: fp32 numerators.
-template <typename ID, bool STORE, bool WIDE>
-struct LogitsEpilogue {
-  static constexpr bool kWide = WIDE, kPaired = false;
+// Which of a token's logits a loss reads as they are, taken from the sums: its target's.  (hold: what the epilogue reads, read ahead of it.)
+template <typename ID>
+struct TargetLogit {
   const ID *targets;
-  float2 *stat;
   float *zt;
-  char *E;
-  int64_t T, V, ld, granules;
-  // what the epilogue reads, read ahead of it
   template <int FN>
-  struct Targets {
+  struct Held {
     int64_t y[FN];
   };
-  template <int FN>
-  __device__ __forceinline__ Targets<FN> hold(int64_t n0) const {
-    Targets<FN> h;
+  template <int FM, int FN>
+  __device__ __forceinline__ Held<FN> hold(int64_t, int64_t n0, int64_t T) const {
+    Held<FN> h;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int64_t t = n0 + 16 * j + (threadIdx.x & 15);
@@ -51,13 +46,46 @@ struct LogitsEpilogue {
     }
     return h;
   }
+  __device__ __forceinline__ float factor() const { return 1.f; }
+  static constexpr bool kFactor = false;
+  template <int FM, int FN>
+  __device__ __forceinline__ void take(const f32x4 (&acc)[FM][FN], const Held<FN> &held, int j, int64_t t, int64_t m0, int q) const {
+    const int64_t y = held.y[j] - m0 - 4 * q;
+    if (__ballot(y >= 0 && y < FM * 16) != 0) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (y == 16 * i + e) zt[t] = acc[i][j][e];
+    }
+  }
+};
+
+// m: vocabulary, n: tokens.  STORE: the numerators too.  WIDE: fp32 numerators.
+template <typename Wanted, bool STORE, bool WIDE>
+struct LogitsEpilogue {
+  static constexpr bool kWide = WIDE, kPaired = false;
+  Wanted wanted;
+  float2 *stat;
+  char *E;
+  int64_t T, V, ld, granules;
+  template <int FM, int FN>
+  __device__ __forceinline__ auto hold(int64_t m0, int64_t n0) const {
+    return wanted.template hold<FM, FN>(m0, n0, T);
+  }
   // stores of a wave where all of a tile's tokens are there
   template <int FM, int FN>
   static constexpr int stores() { return FN * (1 + (!STORE ? 0 : (WIDE ? FM : FM / 2))); }
   __device__ __forceinline__ bool whole(int64_t, int64_t n_end) const { return n_end <= T; }
   template <int FM, int FN>
-  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], const Targets<FN> &held, int64_t m0, int64_t n0, int) const {
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], const typename Wanted::template Held<FN> &held, int64_t m0, int64_t n0, int) const {
     const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    if constexpr (Wanted::kFactor) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] *= wanted.factor();
+    }
     if (m0 + FM * 16 > V) {   // rows beyond the vocabulary
 #pragma unroll
       for (int i = 0; i < FM; ++i)
@@ -78,14 +106,7 @@ struct LogitsEpilogue {
         for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[i][j][e]);
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const int64_t y = held.y[j] - m0 - 4 * q;
-      if (__ballot(y >= 0 && y < FM * 16) != 0) {
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (y == 16 * i + e) zt[t] = acc[i][j][e];
-      }
+      wanted.take(acc, held, j, t, m0, q);
       const float base = top == -INFINITY ? 0.f : top;
       float sum = 0.f;
 #pragma unroll
@@ -118,7 +139,7 @@ struct LogitsEpilogue {
 // alone, so that equal weights do not round a whole gradient's scale (16384 tokens, the mean's 1 / 15560 in bf16: g_h, g_W off by 0.0030 of their
 // 2-norms with the weight in g, 0.0024 without).  The mean's: c = 1 / (targets that are not negative), weight / c = 1.  The caller's: c
 // the largest |weight| of a target that is not negative (1 where that is no positive number).
-// (A count and a maximum: the same bits whoever takes them.)
+// (A count and a maximum: the same bits whoever takes them.)  `factor`, what a loss multiplies every weight by, goes into c.
 template <int THREADS, typename ID>
 __device__ __forceinline__ float common_weight(const ID *__restrict__ targets, const float *__restrict__ weight, int64_t T) {
   __shared__ float red[THREADS / 64];
@@ -149,9 +170,9 @@ __device__ __forceinline__ float common_weight(const ID *__restrict__ targets, c
 constexpr int64_t kCommonTokens = 1024;
 template <typename ID>
 __global__ __launch_bounds__(1024) void common_weight_kernel(const ID *__restrict__ targets, const float *__restrict__ weight, int64_t T,
-                                                             float *__restrict__ common) {
+                                                             float factor, float *__restrict__ common) {
   const float c = common_weight<1024>(targets, weight, T);
-  if (threadIdx.x == 0) *common = c;
+  if (threadIdx.x == 0) *common = c * factor;
 }
 
 struct RowArgs {
@@ -165,7 +186,8 @@ struct RowArgs {
   int64_t T, ld, granules;
   int32_t V;
   int C, gran_log2;
-  bool take_common;     // row_kernel: T is all tokens, and `common` is not there yet
+  float factor;         // of all weights
+  bool take_common;     // row kernels: T is all tokens, and `common` is not there yet
 };
 
 // sum, and the largest, of a value over the WAVES waves of a token
@@ -205,10 +227,147 @@ __device__ __forceinline__ void join_granules(const float2 *stat, int64_t granul
   sum = rows_sum<WAVES>(sum, red[1]);
 }
 
+// A token's weight over what all have in common, which a block of threads leaves for the products where it is not there yet; y < 0: none
+template <typename ID>
+__device__ __forceinline__ float weight_over_common(const RowArgs &a, const ID *__restrict__ targets, int64_t t, int64_t y) {
+  float common = 1.f;
+  if (a.take_common) {
+    if (a.weight || t == 0) common = common_weight<kBlock>(targets, a.weight, a.T) * a.factor;
+    if (t == 0 && threadIdx.x == 0) *a.common = common;
+  } else if (a.weight) {
+    common = *a.common;
+  }
+  return y < 0 ? 0.f : (a.weight ? a.weight[t] * a.factor / common : 1.f);
+}
+
+// The row's numerators turned into scale exp(z - base) in their place, `replace(v, g)` having the last word on the eight from v on; zeros, and zeros
+// for h's row, where the token does not count.  bf16: g is of the operands' type, which is what the matrix units multiply with W and h.  (Its
+// rounding is the one of the T V terms of a sum each, the gradient's own comes after it: off from 64 bits by 0.0023 of the 2-norm at 333 tokens and
+// 0.0018 at 16384, where the gradient's rounding alone is 0.0017.  Two bf16 parts of g instead would make each of the two products two: 13 ms
+// more on 21 at 16384 tokens, C = 4096, 65536 rows.)
+template <typename IO, typename F>
+__device__ __forceinline__ void turn_row(const RowArgs &a, int64_t t, const float2 *stat, float base, float scale, bool counts, F &&replace) {
+  const int tid = threadIdx.x;
+  for (int64_t v = tid * 8; v < a.ld; v += kBlock * 8) {
+    float g[8];
+    if (counts) {
+      const float f = scale * expf(stat[v >> a.gran_log2].x - base);
+      if constexpr (IO::kVec == 8) {
+        const uint4 c = *reinterpret_cast<const uint4 *>(a.E + (t * a.ld + v) * 2);
+        const uint32_t code[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          g[2 * i] = decode(code[i] & 0xffffu) * f;
+          g[2 * i + 1] = decode(code[i] >> 16) * f;
+        }
+      } else {
+        F32::load(a.E, t * a.ld + v, reinterpret_cast<float(&)[4]>(g[0]));
+        F32::load(a.E, t * a.ld + v + 4, reinterpret_cast<float(&)[4]>(g[4]));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] *= f;
+      }
+      replace(v, g);
+      if (v + 8 > a.V) {                         // (a row of NaN leaves the fill-up finite)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = v + i < a.V ? g[i] : 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = 0.f;
+    }
+    if constexpr (IO::kVec == 8) {
+      BF16::store(a.E, t * a.ld + v, g);
+    } else {
+      F32::store(a.E, t * a.ld + v, reinterpret_cast<const float(&)[4]>(g[0]));
+      F32::store(a.E, t * a.ld + v + 4, reinterpret_cast<const float(&)[4]>(g[4]));
+    }
+  }
+  for (int c = tid * IO::kVec; c < a.C; c += kBlock * IO::kVec) {
+    float v[IO::kVec];
+    IO::load(a.h, t * a.C + c, v);
+#pragma unroll
+    for (int i = 0; i < IO::kVec; ++i) v[i] = counts ? v[i] : 0.f;
+    IO::store(a.hp, t * a.C + c, v);
+  }
+}
+
 template <typename F>
 hipError_t dispatch_id(int id_dtype, F &&f) {
   if (id_dtype == MHCL_I64) return f(int64_t{});
   return f(int32_t{});
+}
+
+// The head's products with a loss of the logits, of IO operands (bf16 or fp32).  The loss `way` gives
+//   before(t0, T)            what a block of tokens needs before its logits
+//   wanted(t0)               which logits it reads as they are
+//   loss(a, t0), rows(a, t0) the launches that form the losses of a block; and besides turn its numerators into gradients on the logits
+//   between(a)               what the first block needs between its logits and its rows
+//   marks, weight            ([all tokens]: negative where a token does not count) and its `factor`
+template <typename IO, typename Way>
+hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, Way &way, float *loss, float *lse, void *g_h, void *g_W, bool unrounded,
+                    const HeadWs &w, hipStream_t s) {
+  constexpr bool WIDE = IO::kVec == 4;
+  const bool floats = WIDE || unrounded;   // what g_h and g_W are of
+  const HeadPlan &p = w.plan;
+  const bool grad = g_W != nullptr;
+  const int64_t C = d.C, V = d.V, es = WIDE ? 4 : 2;
+  hipError_t e;
+  const bool take_common = d.T <= kCommonTokens && p.tokens == d.T;
+  int gran_log2 = 0;
+  while ((1 << gran_log2) < p.logits.gran) ++gran_log2;
+  for (int64_t t0 = 0; t0 < d.T; t0 += p.tokens) {
+    const int64_t T = d.T - t0 < p.tokens ? d.T - t0 : p.tokens;
+    const void *hb = static_cast<const char *>(h) + t0 * C * es;
+    const Operand Wk{W, C, V, C}, hk{hb, C, T, C};
+    const RowArgs a{hb, way.weight ? way.weight + t0 : nullptr, w.common, w.stat, w.zt, loss + t0, lse + t0, w.E, w.hp, T, p.ld, p.granules, d.V, d.C,
+                    gran_log2, way.factor, take_common};
+    if ((e = way.before(t0, T)) != hipSuccess) return e;
+    const auto wanted = way.wanted(t0);
+    using Wanted = std::decay_t<decltype(wanted)>;
+    if (!grad) {
+      const LogitsEpilogue<Wanted, false, WIDE> ep{wanted, w.stat, w.E, T, V, p.ld, p.granules};
+      if ((e = launch_gemm<true, true>(p.logits, Wk, hk, V, T, 1, ep, s)) != hipSuccess) return e;
+      if ((e = way.loss(a, t0)) != hipSuccess) return e;
+      continue;
+    }
+    {
+      const LogitsEpilogue<Wanted, true, WIDE> ep{wanted, w.stat, w.E, T, V, p.ld, p.granules};
+      if ((e = launch_gemm<true, true>(p.logits, Wk, hk, V, T, 1, ep, s)) != hipSuccess) return e;
+    }
+    if (t0 == 0) {
+      if ((e = way.between(a)) != hipSuccess) return e;
+      if (!take_common) {
+        using ID = std::remove_cv_t<std::remove_pointer_t<decltype(way.marks)>>;
+        hipLaunchKernelGGL((common_weight_kernel<ID>), dim3(1), dim3(1024), 0, s, way.marks, way.weight, d.T, way.factor, w.common);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
+    }
+    if ((e = way.template rows<IO>(a, t0)) != hipSuccess) return e;
+    // g_h [T, C]: m over C, n over the tokens, k over the vocabulary.  g_W [V, C]: m over C, n over the vocabulary, k over the tokens; the
+    // blocks of tokens add up in fp32 (in g_W itself where it is fp32).
+    const Operand Wm{W, C, C, V}, gk{w.E, p.ld, T, p.ld}, hm{w.hp, C, C, T}, gm{w.E, p.ld, p.ld, T};
+    void *gh_out = static_cast<char *>(g_h) + t0 * C * (floats ? 4 : 2);
+    float *sums = floats ? static_cast<float *>(g_W) : w.gW;
+    const StoreEpilogue<WIDE> to_gh{w.common, p.gh_splits > 1 ? w.slabs : (floats ? static_cast<float *>(gh_out) : nullptr),
+                                    static_cast<uint16_t *>(gh_out), nullptr, C, T, T * C};
+    const StoreEpilogue<WIDE> to_gw{w.common, p.gw_splits > 1 ? w.gw_slabs : (floats || t0 + T < d.T ? sums : nullptr), static_cast<uint16_t *>(g_W),
+                                    t0 > 0 ? sums : nullptr, C, V, V * C};
+    if (p.pair) {
+      const GemmArgs gh = gemm_args(p.gh, Wm, gk, C, T, p.gh_splits), gw = gemm_args(p.gw, hm, gm, C, V, p.gw_splits);
+      const int first = gh.tiles_m * gh.tiles_n * gh.splits;
+      const dim3 grid(first + gw.tiles_m * gw.tiles_n * gw.splits);
+      if (p.gh.bn < 128) hipLaunchKernelGGL((gemm_pair_kernel<true, StoreEpilogue<WIDE>>), grid, dim3(256), 0, s, gh, to_gh, gw, to_gw, first);
+      else hipLaunchKernelGGL((gemm_pair_kernel<false, StoreEpilogue<WIDE>>), grid, dim3(256), 0, s, gh, to_gh, gw, to_gw, first);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    } else {
+      if ((e = launch_gemm<false, true>(p.gh, Wm, gk, C, T, p.gh_splits, to_gh, s)) != hipSuccess) return e;
+      if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, p.gw_splits, to_gw, s)) != hipSuccess) return e;
+    }
+    const auto join = floats ? launch_slab_sum<F32> : launch_slab_sum<IO>;
+    if (p.gh_splits > 1 && (e = join(w.slabs, gh_out, p.gh_splits, T * C, s)) != hipSuccess) return e;
+    if (p.gw_splits > 1 && (e = join(w.gw_slabs, g_W, p.gw_splits, V * C, s)) != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

@@ -451,7 +451,7 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &ep
     }
     const int64_t first_m = static_cast<int64_t>(tm) * BM + wm * (FM * 16), first_n = static_cast<int64_t>(tn) * BN + wn * (FN * 16);
     const int this_split = split;
-    const auto held = epilogue.template hold<FN>(first_n);
+    const auto held = epilogue.template hold<FM, FN>(first_m, first_n);
     // the stages are free once the last loads (of zeros) have arrived and every wave has read its fragments
     wait_all();
     barrier();
@@ -488,13 +488,6 @@ __device__ __forceinline__ uint4 join_pairs(uint2 lower, uint2 upper) {
   const auto y = __builtin_amdgcn_permlane16_swap(lower.y, upper.y, false, false);
   return make_uint4(x[0], y[0], x[1], y[1]);
 }
-// and back
-__device__ __forceinline__ void split_pairs(uint4 eight, uint2 &lower, uint2 &upper) {
-  const auto x = __builtin_amdgcn_permlane16_swap(eight.x, eight.z, false, false);
-  const auto y = __builtin_amdgcn_permlane16_swap(eight.y, eight.w, false, false);
-  lower = make_uint2(x[0], y[0]);
-  upper = make_uint2(x[1], y[1]);
-}
 
 // out[n][m], m innermost, times *scale (null: 1): fp32 slabs of splits (out32 != null), added to `add` if that is there; else rounded to bf16
 template <bool WIDE>
@@ -505,8 +498,8 @@ struct StoreEpilogue {
   uint16_t *out16;
   const float *add;
   int64_t M, N, slab;     // elements of a split's slab
-  template <int FN>
-  __device__ __forceinline__ float hold(int64_t) const { return scale ? *scale : 1.f; }
+  template <int FM, int FN>
+  __device__ __forceinline__ float hold(int64_t, int64_t) const { return scale ? *scale : 1.f; }
   template <int FM, int FN>
   static constexpr int stores() { return FN * (WIDE ? FM : FM / 2); }   // (into fp32 slabs twice as many)
   __device__ __forceinline__ bool whole(int64_t m_end, int64_t n_end) const { return m_end <= M && n_end <= N; }

@@ -141,6 +141,91 @@ def head_loss_grad(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, weig
     return loss, lse, g_h, g_W
 
 
+def _constant(**tensors):
+    """The losses below take these as they are: a gradient that somebody waits for on them would be missing."""
+    for name, t in tensors.items():
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} is a constant of this loss: detach it")
+
+
+def _distill(h, W, ids, logits, weight, temperature, dtype, grad, total):
+    """``loss, lse, g_h, g_W, total``, with None for what is not asked for."""
+    logits = logits.float() if logits.dtype in (torch.bfloat16, torch.float16) else logits
+    native = _native()
+    if native is not None and (out := native.distill(h, W, ids, logits, weight, temperature, dtype if grad else None, total)) is not None:
+        return out
+    _same_device(h, W, ids, logits, weight)
+    _need(h.dim() == 2 and W.dim() == 2 and W.shape[1] == h.shape[1] and ids.dim() == 2 and ids.shape[0] == h.shape[0] and ids.shape == logits.shape,
+          f"h [T, C], W [V, C], ids [T, K] and logits [T, K], got {tuple(h.shape)}, {tuple(W.shape)}, {tuple(ids.shape)} and {tuple(logits.shape)}")
+    d = mhcl.EndsDesc(h.shape[1], h.shape[0], 1, W.shape[0], h.dtype, W.dtype, ids.dtype)
+    loss, lse = (torch.empty(d.T, device=h.device, dtype=torch.float32) for _ in range(2))
+    g_h, g_W = _head_grad_buffers(h, W, dtype, grad)
+    sum_ = torch.empty(1, device=h.device, dtype=torch.float32) if total else None
+    ws = torch.empty(mhcl.head_distill_workspace_bytes(d, ids.shape[1], grad), dtype=torch.uint8, device=h.device)
+    mhcl.mhcl_head_distill(d, temperature, _dense(h), _dense(W), ids.contiguous(), logits.contiguous(), None if weight is None else weight.contiguous(),
+                           loss, lse, sum_, g_h, g_W, ws)
+    return loss, lse, g_h, g_W, sum_
+
+
+def _head_grad_buffers(h, W, dtype, grad):
+    if not grad:
+        return None, None
+    _need(dtype in (h.dtype, torch.float32), f"gradients of {dtype}: {h.dtype} or float32")
+    return tuple(torch.empty(t.shape, device=h.device, dtype=dtype) for t in (h, W))
+
+
+def head_distill(h: torch.Tensor, W: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor, temperature: float = 1.0):
+    """``loss [T], lse [T]`` (fp32): the head against a teacher's likeliest rows, the divergence sum_k p_k (log p_k - log q[ids[t, k]]) of q, the
+    softmax of the logits h W^T / temperature, from p, that of the teacher's logits [T, K] / temperature over a token's slots; and the log-sum-exp of
+    the former.  A slot is empty where ids [T, K] (int64 or int32) is negative or the logit -inf; a token without any does not count: its
+    loss is 0.  h [T, C], W [V, C] of one type; the teacher's logits fp32, or of 16 bits (copied then); at most 256 slots."""
+    return _distill(h, W, ids, logits, None, temperature, None, False, False)[:2]
+
+
+def head_distill_grad(h: torch.Tensor, W: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor, weight=None, temperature: float = 1.0, dtype=None):
+    """``loss [T], lse [T], g_h [T, C], g_W [V, C]``: `head_distill` and the gradients of ``sum(weight * loss)``; weight [T] fp32, or None for the
+    mean over the tokens that count.  dtype as in `head_loss_grad`."""
+    return _distill(h, W, ids, logits, weight, temperature, dtype or h.dtype, True, False)[:4]
+
+
+def _preference(h, W, targets, offsets, reference, weight, beta, smoothing, dtype, grad, total):
+    """``loss, logp, g_h, g_W, total``, with None for what is not asked for."""
+    native = _native()
+    if native is not None and (out := native.preference(h, W, targets, offsets, reference, weight, beta, smoothing, dtype if grad else None,
+                                                        total)) is not None:
+        return out
+    _same_device(h, W, targets, offsets, reference, weight)
+    d = _head_desc(h, W, targets)
+    _need(offsets.dim() == 1 and offsets.shape[0] % 2 == 1, f"offsets [2 P + 1] of P pairs, got {tuple(offsets.shape)}")
+    pairs = offsets.shape[0] // 2
+    loss, logp = (torch.empty(n, device=h.device, dtype=torch.float32) for n in (pairs, 2 * pairs))
+    g_h, g_W = _head_grad_buffers(h, W, dtype, grad)
+    sum_ = torch.empty(1, device=h.device, dtype=torch.float32) if total else None
+    ws = torch.empty(mhcl.head_preference_workspace_bytes(d, grad), dtype=torch.uint8, device=h.device)
+    mhcl.mhcl_head_preference(d, pairs, beta, smoothing, _dense(h), _dense(W), targets.contiguous(), offsets.contiguous(),
+                              *(None if t is None else t.contiguous() for t in (reference, weight)), loss, logp, sum_, g_h, g_W, ws)
+    return loss, logp, g_h, g_W, sum_
+
+
+def head_preference(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, offsets: torch.Tensor, reference=None, beta: float = 0.1,
+                    smoothing: float = 0.0):
+    """``loss [P], logp [2 P]`` (fp32) of P pairs of packed sequences, tokens offsets[s] to offsets[s + 1] - 1 being sequence s, the chosen ones
+    even and the rejected ones odd: logp[s] is the sum of the log probabilities of its targets that are not negative, and
+
+        loss[p] = (1 - smoothing) log(1 + exp(-m)) + smoothing log(1 + exp(m)),  m = beta ((logp - reference)[2 p] - (logp - reference)[2 p + 1])
+
+    reference [2 P] fp32: those of a reference model (what this returns for it), or None for zeros.  offsets [2 P + 1] int64 or int32, ascending
+    within 0..T; tokens outside of them add nothing.  h [T, C], W [V, C] of one type."""
+    return _preference(h, W, targets, offsets, reference, None, beta, smoothing, None, False, False)[:2]
+
+
+def head_preference_grad(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, offsets: torch.Tensor, reference=None, weight=None,
+                         beta: float = 0.1, smoothing: float = 0.0, dtype=None):
+    """``loss [P], logp [2 P], g_h [T, C], g_W [V, C]``: `head_preference` and the gradients of ``sum(weight * loss)``; weight [P] fp32, or None for
+    the mean over the pairs.  dtype as in `head_loss_grad`."""
+    return _preference(h, W, targets, offsets, reference, weight, beta, smoothing, dtype or h.dtype, True, False)[:4]
+
+
 # ---- under torch.autograd --------------------------------------------------------------------
 
 
@@ -184,23 +269,64 @@ class _HeadTotal(torch.autograd.Function):
         else:
             loss, grads = head_loss(h, W, targets)[0], [None, None]
         total = _total(h, W, targets, loss, weight)
-        ctx.save_for_backward(h, W, weight)     # (read by a recorded backward alone)
-        # (a place of weight 0 adds nothing, whatever it holds)
-        grads.append(loss.masked_fill((weight == 0) & ~loss.isfinite(), 0.0) if record and ctx.needs_input_grad[3] else None)
-        ctx.grads, ctx.dtypes = grads, (h.dtype, W.dtype, torch.float32)
+        _keep_grads(ctx, h, W, weight, *grads, loss, record and ctx.needs_input_grad[3])
         return total
 
     @staticmethod
     def backward(ctx, g):
-        if ctx.grads is None:
-            raise RuntimeError("the head's gradients went out with its first backward: run the head again for another one")
-        grads, ctx.grads = ctx.grads, None
-        h, W, _, weight, _ = ctx.needs_input_grad
-        grads = tuple(_times(t, g, dtype) if needed else None for t, dtype, needed in zip(grads, ctx.dtypes, (h, W, weight)))
-        if torch.is_grad_enabled():
-            grads = first_only("the head's loss", grads, *ctx.saved_tensors, g)
-        g_h, g_W, g_weight = grads
+        g_h, g_W, g_weight = _kept_grads(ctx, g, "the head's loss")
         return g_h, g_W, None, g_weight, None
+
+
+class _DistillTotal(torch.autograd.Function):
+    """As _HeadTotal, of the loss against a teacher."""
+
+    @staticmethod
+    def forward(ctx, h, W, weight, ids, logits, temperature, record):
+        grad = record and (ctx.needs_input_grad[0] or ctx.needs_input_grad[1])
+        loss, _, g_h, g_W, total = _distill(h, W, ids, logits, weight, temperature, torch.float32, grad, True)
+        _keep_grads(ctx, h, W, weight, g_h, g_W, loss, record and ctx.needs_input_grad[2])
+        return total[0]
+
+    @staticmethod
+    def backward(ctx, g):
+        return *_kept_grads(ctx, g, "the head's loss against a teacher", 2), None, None, None, None
+
+
+class _PreferenceTotal(torch.autograd.Function):
+    """As _HeadTotal, of the loss of pairs; and the sequences' log probabilities, as numbers."""
+
+    @staticmethod
+    def forward(ctx, h, W, weight, targets, offsets, reference, beta, smoothing, record):
+        grad = record and (ctx.needs_input_grad[0] or ctx.needs_input_grad[1])
+        loss, logp, g_h, g_W, total = _preference(h, W, targets, offsets, reference, weight, beta, smoothing, torch.float32, grad, True)
+        _keep_grads(ctx, h, W, weight, g_h, g_W, loss, record and ctx.needs_input_grad[2])
+        ctx.mark_non_differentiable(logp)
+        return total[0], logp
+
+    @staticmethod
+    def backward(ctx, g, _):
+        return *_kept_grads(ctx, g, "the head's loss of pairs", 2), None, None, None, None, None, None
+
+
+def _keep_grads(ctx, h, W, weight, g_h, g_W, loss, weighed):
+    """What _kept_grads multiplies: the gradients for a factor of 1."""
+    ctx.save_for_backward(h, W, weight)     # (read by a recorded backward alone)
+    # (a place of weight 0 adds nothing, whatever it holds)
+    g_weight = loss.masked_fill((weight == 0) & ~loss.isfinite(), 0.0) if weighed else None
+    ctx.grads, ctx.dtypes = [g_h, g_W, g_weight], (h.dtype, W.dtype, torch.float32)
+
+
+def _kept_grads(ctx, g, what, weight_at=3):
+    """g_h, g_W and g_weight of a loss whose gradients were taken with it, for the gradient g on it."""
+    if ctx.grads is None:
+        raise RuntimeError("the head's gradients went out with its first backward: run the head again for another one")
+    grads, ctx.grads = ctx.grads, None
+    needed = (*ctx.needs_input_grad[:2], ctx.needs_input_grad[weight_at])
+    grads = tuple(_times(t, g, dtype) if need else None for t, dtype, need in zip(grads, ctx.dtypes, needed))
+    if torch.is_grad_enabled():
+        grads = first_only(what, grads, *ctx.saved_tensors, g)
+    return grads
 
 
 def _times(t, factor, dtype):
@@ -258,6 +384,16 @@ class Head(torch.nn.Module):
     def forward(self, h, targets, weight=None):
         # (also where no gradient is asked for: a forward-mode tangent is refused there)
         return _HeadTotal.apply(h, self.W, targets, weight, torch.is_grad_enabled())
+
+    def distill(self, h, ids, logits, weight=None, temperature: float = 1.0):
+        """The mean of `head_distill`'s loss over the tokens that count, or, with weight [T], the sum of weight times it."""
+        _constant(logits=logits)
+        return _DistillTotal.apply(h, self.W, weight, ids, logits, temperature, torch.is_grad_enabled())
+
+    def prefer(self, h, targets, offsets, reference=None, weight=None, beta: float = 0.1, smoothing: float = 0.0):
+        """The mean of `head_preference`'s loss over the pairs, or, with weight [P], the sum of weight times it; and logp [2 P], as numbers."""
+        _constant(reference=reference)
+        return _PreferenceTotal.apply(h, self.W, weight, targets, offsets, reference, beta, smoothing, torch.is_grad_enabled())
 
     @torch.no_grad()
     def score(self, h, targets):

@@ -24,14 +24,15 @@ def _desc(x, W_up, W_down):
 
 def gated_ffn(x: torch.Tensor, W_up: torch.Tensor, W_down: torch.Tensor, keep: bool = False):
     """``y [T, C] = (silu(x Wg^T) * (x Wu^T)) W_down^T`` of x [T, C], W_up [2 H, C] (Wg is its first half of rows, Wu the other) and
-    W_down [C, H], all of one type.  keep: ``y, kept`` with what `gated_ffn_grad` needs besides the operands, x W_up^T [T, 2 H]."""
+    W_down [C, H], all of one type.  keep: ``y, kept`` with what `gated_ffn_grad` needs besides the operands, x W_up^T [T, 2 H] in
+    fp32."""
     native = _native()
     if native is not None and (out := native.ffn(x, W_up, W_down, keep)) is not None:
         return out if keep else out[0]
     _same_device(x, W_up, W_down)
     d = _desc(x, W_up, W_down)
     y = torch.empty(d.T, d.C, device=x.device, dtype=x.dtype)
-    kept = torch.empty(d.T, 2 * d.H, device=x.device, dtype=x.dtype) if keep else None
+    kept = torch.empty(d.T, 2 * d.H, device=x.device, dtype=torch.float32) if keep else None
     ws = mhcl.new_ffn_workspace(d, mhcl.OP_FFN, x.device)
     mhcl.mhcl_ffn(d, _dense(x), _dense(W_up), _dense(W_down), y, kept, ws)
     return (y, kept) if keep else y

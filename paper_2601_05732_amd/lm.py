@@ -9,7 +9,11 @@
 The blocks here are norm and a gated feed-forward block (what a user replaces by attention and the like); the paper does not say how
 streams begin and end, so the ends are this package's choice.
 
-``python -m paper_2601_05732_amd.lm`` trains one on a synthetic language, a fixed random successor for each token with some noise.
+Besides the next tokens the head learns from a teacher's likeliest ones and from pairs of sequences (:meth:`LanguageModel.distill`,
+:meth:`LanguageModel.prefer`).
+
+``python -m paper_2601_05732_amd.lm`` trains one on a synthetic language, a fixed random successor for each token with some noise (``--teach K``
+and ``--pairs P``: and then in those ways).
 """
 from __future__ import annotations
 
@@ -69,6 +73,22 @@ class LanguageModel(torch.nn.Module):
         """The loss; negative ids hold no token, negative targets do not count."""
         return self.head(self.features(ids), targets, weight)
 
+    def distill(self, ids, teacher_ids, teacher_logits, weight=None, temperature: float = 1.0):
+        """The loss against a teacher's likeliest next tokens [T, K] of each token and their logits (`likeliest` of another model)."""
+        return self.head.distill(self.features(ids), teacher_ids, teacher_logits, weight, temperature)
+
+    def prefer(self, ids, targets, offsets, reference=None, weight=None, beta: float = 0.1, smoothing: float = 0.0):
+        """The loss of pairs of packed sequences, the chosen and the rejected one, and the sequences' log probabilities [2 P], which are
+        the `reference` of a later model.  offsets [2 P + 1]: where sequences begin; negative targets do not count.  (These blocks see one
+        token at a time: a model with attention keeps sequences apart itself.)"""
+        return self.head.prefer(self.features(ids), targets, offsets, reference, weight, beta, smoothing)
+
+    @torch.no_grad()
+    def likeliest(self, ids, k: int, rows: int = 4096):
+        """``ids [T, k], logits [T, k]`` of the k likeliest next tokens of each token, by torch's product and selection."""
+        out = [(h @ self.head.W.t()).float().topk(k, dim=1) for h in self.features(ids).split(rows)]
+        return torch.cat([o.indices for o in out]), torch.cat([o.values for o in out])
+
     @torch.no_grad()
     def score(self, ids, targets):
         """The negative log probability [T] of each target."""
@@ -87,19 +107,49 @@ def synthetic_tokens(V: int, count: int, noise: float = 0.1, seed: int = 0, devi
     return torch.tensor(tokens, device=device)
 
 
-def train(model, tokens, steps: int, batch: int, lr: float = 3e-3, report=None):
-    """AdamW on consecutive pieces of `batch` tokens; the losses."""
+def train(model, tokens, steps: int, batch: int, lr: float = 3e-3, report=None, teacher=None, k: int = 8, temperature: float = 1.0):
+    """AdamW on consecutive pieces of `batch` tokens; the losses.  teacher: a model whose k likeliest next tokens are learned instead of the
+    text's."""
     opt = torch.optim.AdamW(model.parameters(), lr=lr, weight_decay=0.0)
     losses = []
     for step in range(steps):
         at = step * batch % (len(tokens) - batch)
-        loss = model(tokens[at:at + batch], tokens[at + 1:at + batch + 1])
+        if teacher is None:
+            loss = model(tokens[at:at + batch], tokens[at + 1:at + batch + 1])
+        else:
+            loss = model.distill(tokens[at:at + batch], *teacher.likeliest(tokens[at:at + batch], k), temperature=temperature)
         opt.zero_grad(set_to_none=True)
         loss.backward()
         opt.step()
         losses.append(loss.detach())
         if report and step % report == 0:
             print(f"step {step}: loss {float(losses[-1]):.3f}", flush=True)
+    return torch.stack(losses)
+
+
+def train_on_pairs(model, tokens, steps: int, pairs: int, length: int, lr: float = 1e-3, beta: float = 0.1, report=None):
+    """AdamW on pairs of sequences of `length` tokens, the chosen ones out of the text and the rejected ones those in another order, measured against
+    the model as it is at the start; the losses."""
+    opt = torch.optim.AdamW(model.parameters(), lr=lr, weight_decay=0.0)
+    g = torch.Generator().manual_seed(0)
+    span, losses = pairs * (length + 1), []
+    offsets = torch.arange(2 * pairs + 1, device=tokens.device) * length
+    packed = []
+    for step in range(steps):
+        at = step * span % (len(tokens) - span)
+        chosen = tokens[at:at + span].view(pairs, length + 1)
+        both = torch.stack([chosen, chosen[:, torch.randperm(length + 1, generator=g).to(tokens.device)]], dim=1).view(2 * pairs, length + 1)
+        packed.append((both[:, :-1].reshape(-1), both[:, 1:].reshape(-1)))
+    with torch.no_grad():
+        references = [model.prefer(ids, targets, offsets)[1] for ids, targets in packed]
+    for step, ((ids, targets), reference) in enumerate(zip(packed, references)):
+        loss, _ = model.prefer(ids, targets, offsets, reference, beta=beta)
+        opt.zero_grad(set_to_none=True)
+        loss.backward()
+        opt.step()
+        losses.append(loss.detach())
+        if report and step % report == 0:
+            print(f"step {step}: loss of pairs {float(losses[-1]):.3f}", flush=True)
     return torch.stack(losses)
 
 
@@ -112,9 +162,17 @@ if __name__ == "__main__":
     ap.add_argument("--batch", type=int, default=2048)
     ap.add_argument("--steps", type=int, default=100)
     ap.add_argument("--tied", action="store_true")
+    ap.add_argument("--teach", type=int, default=0, metavar="K", help="then train a second model on the first one's K likeliest next tokens")
+    ap.add_argument("--pairs", type=int, default=0, metavar="P", help="then train on so many pairs of sequences a step")
     args = ap.parse_args()
     net = LanguageModel(args.V, args.C, args.n, args.layers, tied=args.tied)
     text = synthetic_tokens(args.V, 20 * args.batch + 1)
     train(net, text, args.steps, args.batch, report=10)
     held = synthetic_tokens(args.V, args.batch + 1)
     print(f"mean negative log probability: {float(net.score(held[:-1], held[1:]).mean()):.3f}")
+    if args.teach:
+        student = LanguageModel(args.V, args.C, args.n, args.layers, tied=args.tied)
+        train(student, text, args.steps, args.batch, report=10, teacher=net, k=args.teach)
+        print(f"the student's: {float(student.score(held[:-1], held[1:]).mean()):.3f}")
+    if args.pairs:
+        train_on_pairs(net, text, args.steps, args.pairs, 64, report=10)

@@ -139,6 +139,71 @@ std::optional<std::tuple<Tensor, Tensor, Tensor, Tensor>> head_grad(const Tensor
   return std::make_tuple(loss, lse, g_h, g_W);
 }
 
+bool floats_ready(const std::optional<Tensor> &t, int64_t count, int device) {
+  return !t || (t->dim() == 1 && t->size(0) == count && t->scalar_type() == at::kFloat && ready(*t, device, 4));
+}
+const float *floats_ptr(const std::optional<Tensor> &t) { return t ? ptr<float>(*t) : nullptr; }
+
+// the gradients' buffers: none without a type; `unrounded`: fp32 beside operands that are not
+struct HeadGrads {
+  std::optional<Tensor> h, W;
+  int unrounded = 0;
+  HeadGrads(const Tensor &like_h, const Tensor &like_W, std::optional<at::ScalarType> dtype) {
+    if (!dtype) return;
+    unrounded = *dtype == at::kFloat && like_h.scalar_type() != at::kFloat;
+    h = at::empty(like_h.sizes(), like_h.options().dtype(*dtype));
+    W = at::empty(like_W.sizes(), like_W.options().dtype(*dtype));
+  }
+  static bool fit(const Tensor &h, std::optional<at::ScalarType> dtype) { return !dtype || *dtype == at::kFloat || *dtype == h.scalar_type(); }
+  void *h_ptr() const { return h ? ptr(*h) : nullptr; }
+  void *W_ptr() const { return W ? ptr(*W) : nullptr; }
+};
+using HeadResults = std::tuple<Tensor, Tensor, std::optional<Tensor>, std::optional<Tensor>, std::optional<Tensor>>;
+
+std::optional<HeadResults> distill(const Tensor &h, const Tensor &W, const Tensor &ids, const Tensor &logits, const std::optional<Tensor> &weight,
+                                   double temperature, std::optional<at::ScalarType> dtype, bool total) {
+  const int device = c10::hip::current_device();
+  if (h.dim() != 2 || W.dim() != 2 || h.size(1) != W.size(1) || !type_of(h.scalar_type()) || W.scalar_type() != h.scalar_type() || ids.dim() != 2 ||
+      ids.size(0) != h.size(0) || logits.sizes() != ids.sizes() || logits.scalar_type() != at::kFloat || !ready(h, device, 16) ||
+      !ready(W, device, 16) || !ids_ready(ids, device) || !ready(logits, device, 4) || !fits(W.size(0)) || !fits(W.size(1)) || !fits(ids.size(1)) ||
+      !floats_ready(weight, h.size(0), device) || !HeadGrads::fit(h, dtype))
+    return std::nullopt;
+  const int32_t io = *type_of(h.scalar_type()), K = static_cast<int32_t>(ids.size(1));
+  const mhcl_ends_desc d = describe(1, h.size(1), h.size(0), W.size(0), io, io, &ids, 1., 0.);
+  const Tensor loss = floats(h, {d.T}), lse = floats(h, {d.T});
+  std::optional<Tensor> sum;
+  if (total) sum = floats(h, {1});
+  const HeadGrads g(h, W, dtype);
+  const Tensor ws = at::empty({static_cast<int64_t>(mhcl_head_distill_workspace_bytes(&d, K, dtype ? 1 : 0))}, h.options().dtype(at::kByte));
+  check(mhcl_head_distill(&d, K, static_cast<float>(temperature), ptr(h), ptr(W), ptr(ids), ptr<float>(logits), floats_ptr(weight), ptr<float>(loss),
+                          ptr<float>(lse), sum ? ptr<float>(*sum) : nullptr, g.h_ptr(), g.W_ptr(), g.unrounded, ws.data_ptr(), ws.nbytes(), stream()),
+        "mhcl_head_distill");
+  return HeadResults(loss, lse, g.h, g.W, sum);
+}
+
+std::optional<HeadResults> preference(const Tensor &h, const Tensor &W, const Tensor &targets, const Tensor &offsets, const std::optional<Tensor> &reference,
+                                      const std::optional<Tensor> &weight, double beta, double smoothing, std::optional<at::ScalarType> dtype, bool total) {
+  const int device = c10::hip::current_device();
+  if (!head_ready(h, W, targets, device) || W.scalar_type() != h.scalar_type() || offsets.dim() != 1 || offsets.size(0) % 2 != 1 ||
+      !ids_ready(offsets, device) || !fits(offsets.size(0)))
+    return std::nullopt;
+  const int64_t pairs = offsets.size(0) / 2;
+  if (!floats_ready(reference, 2 * pairs, device) || !floats_ready(weight, pairs, device) || !HeadGrads::fit(h, dtype)) return std::nullopt;
+  const int32_t io = *type_of(h.scalar_type());
+  const mhcl_ends_desc d = describe(1, h.size(1), h.size(0), W.size(0), io, io, &targets, 1., 0.);
+  const Tensor loss = floats(h, {pairs}), logp = floats(h, {2 * pairs});
+  std::optional<Tensor> sum;
+  if (total) sum = floats(h, {1});
+  const HeadGrads g(h, W, dtype);
+  const Tensor ws = at::empty({static_cast<int64_t>(mhcl_head_preference_workspace_bytes(&d, dtype ? 1 : 0))}, h.options().dtype(at::kByte));
+  check(mhcl_head_preference(&d, static_cast<int32_t>(pairs), static_cast<float>(beta), static_cast<float>(smoothing), ptr(h), ptr(W), ptr(targets),
+                             ptr(offsets), offsets.scalar_type() == at::kInt ? MHCL_I32 : MHCL_I64, floats_ptr(reference), floats_ptr(weight),
+                             ptr<float>(loss), ptr<float>(logp), sum ? ptr<float>(*sum) : nullptr, g.h_ptr(), g.W_ptr(), g.unrounded, ws.data_ptr(),
+                             ws.nbytes(), stream()),
+        "mhcl_head_preference");
+  return HeadResults(loss, logp, g.h, g.W, sum);
+}
+
 std::optional<mhcl_ffn_desc> ffn_ready(const Tensor &x, const Tensor &W_up, const Tensor &W_down, int device) {
   const auto io = type_of(x.scalar_type());
   if (!io || x.dim() != 2 || W_up.dim() != 2 || W_down.dim() != 2 || W_down.size(0) != x.size(1) || W_up.size(1) != x.size(1) ||
@@ -162,21 +227,21 @@ std::optional<std::tuple<Tensor, std::optional<Tensor>>> ffn(const Tensor &x, co
   if (!d) return std::nullopt;
   const Tensor y = at::empty(x.sizes(), x.options());
   std::optional<Tensor> pre;
-  if (keep) pre = at::empty({d->T, 2 * static_cast<int64_t>(d->H)}, x.options());
+  if (keep) pre = floats(x, {d->T, 2 * static_cast<int64_t>(d->H)});
   const Tensor ws = ffn_workspace_of(*d, MHCL_OP_FFN, x);
-  check(mhcl_ffn(&*d, ptr(x), ptr(W_up), ptr(W_down), ptr(y), pre ? ptr(*pre) : nullptr, ws.data_ptr(), ws.nbytes(), stream()), "mhcl_ffn");
+  check(mhcl_ffn(&*d, ptr(x), ptr(W_up), ptr(W_down), ptr(y), pre ? ptr<float>(*pre) : nullptr, ws.data_ptr(), ws.nbytes(), stream()), "mhcl_ffn");
   return std::make_tuple(y, pre);
 }
 
 std::optional<std::tuple<Tensor, Tensor, Tensor>> ffn_grad(const Tensor &x, const Tensor &W_up, const Tensor &W_down, const Tensor &pre, const Tensor &g_y) {
   const int device = c10::hip::current_device();
   const auto d = ffn_ready(x, W_up, W_down, device);
-  if (!d || pre.dim() != 2 || pre.size(0) != x.size(0) || pre.size(1) != W_up.size(0) || pre.scalar_type() != x.scalar_type() ||
+  if (!d || pre.dim() != 2 || pre.size(0) != x.size(0) || pre.size(1) != W_up.size(0) || pre.scalar_type() != at::kFloat ||
       !ready(pre, device, 16) || g_y.sizes() != x.sizes() || g_y.scalar_type() != x.scalar_type() || !ready(g_y, device, 16))
     return std::nullopt;
   const Tensor g_x = at::empty(x.sizes(), x.options()), g_W_up = at::empty(W_up.sizes(), x.options()), g_W_down = at::empty(W_down.sizes(), x.options());
   const Tensor ws = ffn_workspace_of(*d, MHCL_OP_FFN_GRAD, x);
-  check(mhcl_ffn_grad(&*d, ptr(x), ptr(W_up), ptr(W_down), ptr(pre), ptr(g_y), ptr(g_x), ptr(g_W_up), ptr(g_W_down), ws.data_ptr(), ws.nbytes(),
+  check(mhcl_ffn_grad(&*d, ptr(x), ptr(W_up), ptr(W_down), ptr<float>(pre), ptr(g_y), ptr(g_x), ptr(g_W_up), ptr(g_W_down), ws.data_ptr(), ws.nbytes(),
                       stream()),
         "mhcl_ffn_grad");
   return std::make_tuple(g_x, g_W_up, g_W_down);
@@ -192,6 +257,8 @@ void bind_ends(py::module &m) {
   m.def("norm_grad", wrap(&norm_grad));
   m.def("head", wrap(&head));
   m.def("head_grad", wrap(&head_grad));
+  m.def("distill", wrap(&distill));
+  m.def("preference", wrap(&preference));
   m.def("ffn", wrap(&ffn));
   m.def("ffn_grad", wrap(&ffn_grad));
 }

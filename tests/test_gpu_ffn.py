@@ -59,11 +59,9 @@ def _bounds(x, W_up, W_down, g_y):
     def e_a(e_G, e_U):
         return 1.1 * e_G * U.abs() + silu.abs() * e_U + (rel + last) * a.abs()
 
-    out = dict(kept=(pre, e_pre + last * pre.abs()))
+    out = dict(kept=(pre, e_pre))
     y = a @ Dn.t()
     out["y"] = (y, e_a(e_G, e_U) @ Dn.abs().t() + summed(H) * (a.abs() @ Dn.abs().t()) + last * y.abs())
-    # the backward reads G and U rounded
-    e_G, e_U = e_G + last * G.abs(), e_U + last * U.abs()
     ga = gy @ Dn
     e_ga = summed(C) * (gy.abs() @ Dn.abs())
     gU, gG = ga * silu, ga * U * slope
@@ -90,7 +88,7 @@ def _check(x, W_up, W_down, g_y):
     y, kept = mhcl.gated_ffn(x, W_up, W_down, keep=True)
     got = dict(zip(("y", "kept", "g_x", "g_W_up", "g_W_down"), (y, kept, *mhcl.gated_ffn_grad(x, W_up, W_down, kept, g_y))))
     for name, (ref, bound) in _bounds(x, W_up, W_down, g_y).items():
-        assert got[name].dtype is x.dtype
+        assert got[name].dtype is (F if name == "kept" else x.dtype)
         _within(got[name], ref, bound, name)
     assert torch.equal(y, mhcl.gated_ffn(x, W_up, W_down))
     assert all(torch.equal(a, b) for a, b in zip((got["g_x"], got["g_W_up"], got["g_W_down"]), mhcl.gated_ffn_grad(x, W_up, W_down, kept, g_y)))
@@ -173,7 +171,7 @@ def test_operands_that_do_not_fit_are_refused():
     for args in ((x, up[:-2], down), (x, up, down[:, :-8]), (x[:, :-8], up, down), (x.float(), up, down), (x, up.float(), down), (x[0], up, down)):
         with pytest.raises(ValueError):
             mhcl.gated_ffn(*args)
-    for args in ((kept[:-1], g_y), (kept[:, :-8], g_y), (kept.float(), g_y), (kept, g_y[:-1]), (kept, g_y.float()), (kept, g_y.cpu())):
+    for args in ((kept[:-1], g_y), (kept[:, :-8], g_y), (kept.to(BF), g_y), (kept, g_y[:-1]), (kept, g_y.float()), (kept, g_y.cpu())):
         with pytest.raises(ValueError):
             mhcl.gated_ffn_grad(x, up, down, *args)
     with pytest.raises(mhcl.MhclError):          # widths that are no multiple of 8

@@ -1,0 +1,278 @@
+"""The head's loss of pairs of sequences: against its definition in 64 bits element by element, at the lengths, masks and offsets where it can
+go wrong; its gradients against differences; under torch.autograd, captured.  Bounds: head_reference.py."""
+import math
+
+import pytest
+import torch
+
+import head_reference as ref
+import paper_2601_05732_amd as mhcl
+from paper_2601_05732_amd import ends
+
+pytestmark = pytest.mark.gpu
+
+BF, F = torch.bfloat16, torch.float32
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _normal(g, *shape, std=1.0, dtype=F):
+    return torch.empty(shape, device="cuda").normal_(0.0, std, generator=g).to(dtype)
+
+
+def _inputs(seed, T, C, V, pairs, io, lead=0, tail=0, holes=0.3, dtype=torch.int64):
+    """Ragged sequences, some empty, from `lead` to T - tail; a reference near the sequences' log probabilities."""
+    g = _gen(seed)
+    h, W = _normal(g, T, C, dtype=io), _normal(g, V, C, std=1.5 / math.sqrt(C), dtype=io)
+    targets = torch.randint(0, V, (T,), device="cuda", generator=g)
+    targets = torch.where(torch.rand(T, device="cuda", generator=g) < holes, -100, targets)
+    cuts = torch.sort(torch.randint(lead, T - tail + 1, (2 * pairs - 1,), device="cuda", generator=g))[0] if pairs else torch.empty(0, device="cuda").long()
+    offsets = torch.cat([torch.tensor([lead], device="cuda"), cuts] + ([torch.tensor([T - tail], device="cuda")] if pairs else []))
+    logp = torch.zeros(2 * pairs, device="cuda", dtype=torch.float64)
+    ce = torch.log_softmax(h.double() @ W.double().t(), dim=1).gather(1, targets.clamp(min=0).unsqueeze(1)).squeeze(1).masked_fill(targets < 0, 0.0)
+    for i in range(2 * pairs):
+        logp[i] = ce[int(offsets[i]):int(offsets[i + 1])].sum()
+    reference = (logp + 10 * _normal(g, 2 * pairs, dtype=torch.float64)).float()
+    return h, W, targets, offsets.to(dtype), reference
+
+
+def _check(h, W, targets, offsets, reference, weight=None, beta=0.1, smoothing=0.0, rows=1024):
+    refs = ref.preference(h, W, targets, offsets, reference, weight, beta, smoothing, rows)
+    got = dict(zip(("loss", "logp", "g_h", "g_W"), mhcl.head_preference_grad(h, W, targets, offsets, reference, weight, beta, smoothing)))
+    for name, (value, bound) in refs.items():
+        ref.within(got[name], value, bound, name)
+    alone = mhcl.head_preference(h, W, targets, offsets, reference, beta, smoothing)
+    ref.within(alone[0], *refs["loss"], "loss alone")
+    ref.within(alone[1], *refs["logp"], "logp alone")
+    again = mhcl.head_preference_grad(h, W, targets, offsets, reference, weight, beta, smoothing)
+    assert all(torch.equal(a, b) for a, b in zip(got.values(), again))
+    return got
+
+
+@pytest.mark.parametrize("io", [BF, F])
+@pytest.mark.parametrize("T,C,V,pairs", [
+    (1, 8, 1, 1), (2, 64, 2, 1), (2, 4096, 1000, 1), (16, 264, 127, 9), (33, 72, 1001, 3), (64, 512, 257, 2), (65, 136, 300, 40),
+    (130, 1024, 999, 1), (333, 520, 1003, 7), (1025, 64, 40, 2), (40, 128, 30011, 3), (500, 256, 4099, 5), (2049, 72, 8200, 300),
+])
+def test_preference(io, T, C, V, pairs):
+    _check(*_inputs(T + V, T, C, V, pairs, io, lead=T // 7, tail=T // 9), smoothing=0.1 if T % 2 else 0.0)
+
+
+def test_preference_in_the_largest_tiles():
+    _check(*_inputs(1, 4100, 72, 4200, 8, BF, tail=100))
+
+
+@pytest.mark.parametrize("io", [BF, F])
+@pytest.mark.parametrize("dtype", [torch.int64, torch.int32])
+def test_weights_types_and_no_reference(io, dtype):
+    h, W, targets, offsets, reference = _inputs(2, 700, 96, 500, 6, io, dtype=dtype)
+    weight = torch.rand(6, device="cuda", generator=_gen(3)) - 0.3
+    weight[2] = 0.0
+    _check(h, W, targets.to(torch.int32), offsets, reference, weight, 0.3, 0.25)
+    _check(h, W, targets, offsets.to(torch.int32 if dtype is torch.int64 else torch.int64), None, weight, 0.01)
+    _check(h, W, targets, offsets, reference, beta=0.0)
+    _check(h, W, targets, offsets, reference, beta=-0.2, smoothing=1.0)
+
+
+@pytest.mark.parametrize("io", [BF, F])
+def test_empty_sequences_and_pairs(io):
+    h, W, targets, offsets, reference = _inputs(4, 90, 64, 200, 3, io)
+    offsets = torch.tensor([10, 10, 40, 40, 40, 70, 70], device="cuda")
+    got = _check(h, W, targets, offsets, reference)
+    assert not got["logp"][[0, 2, 3, 5]].any()
+    outside = torch.ones(90, dtype=torch.bool, device="cuda")
+    outside[10:70] = False
+    assert not got["g_h"][outside].any()
+    # no pair at all, no token at all, no target at all
+    loss, logp, g_h, g_W = mhcl.head_preference_grad(h, W, targets, offsets[:1])
+    assert loss.shape == (0,) and logp.shape == (0,) and not g_h.any() and not g_W.any()
+    loss, logp, g_h, g_W = mhcl.head_preference_grad(h[:0], W, targets[:0], torch.zeros(5, device="cuda", dtype=torch.int64), reference[:4])
+    m = 0.1 * (reference[1:4:2] - reference[0:4:2]).double()
+    assert float((loss.double() - torch.nn.functional.softplus(-m)).abs().max()) <= 1e-5
+    assert not logp.any() and g_h.shape == (0, 64) and not g_W.any()
+    got = _check(h, W, torch.full_like(targets, -1), offsets, reference)
+    assert not got["g_h"].any() and not got["g_W"].any() and not got["logp"].any()
+
+
+@pytest.mark.parametrize("io", [BF, F])
+@pytest.mark.parametrize("T", [80, 1400])
+def test_places_that_do_not_count_may_hold_anything(io, T):
+    h, W, targets, offsets, reference = _inputs(5, T, 128, 300, 3, io, lead=5, tail=9)
+    weight = torch.tensor([1.0, 0.0, 0.5], device="cuda")
+    at = torch.arange(T, device="cuda")
+    bad = (targets < 0) | (at < offsets[0]) | (at >= offsets[-1]) | ((at >= offsets[2]) & (at < offsets[4]))
+    clean = h.clone()
+    clean[bad] = 0
+    h[bad] = math.nan
+    loss, logp, g_h, g_W = mhcl.head_preference_grad(h, W, targets, offsets, reference, weight)
+    want = mhcl.head_preference_grad(clean, W, targets, offsets, reference, weight)
+    assert torch.equal(g_h, want[2]) and torch.equal(g_W, want[3])
+    assert torch.equal(loss[[0, 2]], want[0][[0, 2]]) and torch.equal(logp[[0, 1, 4, 5]], want[1][[0, 1, 4, 5]])
+
+
+@pytest.mark.parametrize("io", [BF, F])
+def test_mistakes_are_loud_and_stay_in_their_pair(io):
+    h, W, targets, offsets, reference = _inputs(6, 120, 64, 200, 4, io, holes=0.0)
+    offsets = torch.tensor([0, 20, 40, 50, 60, 80, 90, 100, 120], device="cuda")
+    good = mhcl.head_preference(h, W, targets, offsets, reference)
+    weight = torch.ones(4, device="cuda")
+    for change in ("target", "past", "descends", "negative"):
+        y, o = targets.clone(), offsets.clone()
+        if change == "target":
+            y[45] = 200
+        elif change == "past":
+            o[-1] = 2 ** 40
+        elif change == "descends":
+            o[-1] = 95
+        else:
+            o[0] = -3
+        pair = dict(target=1, past=3, descends=3, negative=0)[change]
+        others = [p for p in range(4) if p != pair]
+        loss, logp, g_h, g_W = mhcl.head_preference_grad(h, W, y, o, reference, weight)
+        assert torch.isnan(loss[pair]) and torch.equal(loss[others], good[0][others]), change
+        assert torch.isnan(g_W).all(), change
+        weight[pair] = 0
+        _, _, g_h, g_W = mhcl.head_preference_grad(h, W, y, o, reference, weight)
+        assert torch.isfinite(g_h).all() and torch.isfinite(g_W).all(), change
+        weight[pair] = 1
+
+
+def test_large_margins():
+    h, W, targets, offsets, reference = _inputs(7, 400, 64, 300, 4, F)
+    reference += torch.tensor([1e4, 0, 0, 1e4, -3e4, 0, 0, -3e4], device="cuda")
+    got = _check(h, W, targets, offsets, reference, beta=0.5)
+    assert torch.isfinite(got["loss"]).all() and torch.isfinite(got["g_h"]).all()
+
+
+def test_blocks_of_tokens():
+    # a vocabulary so long that a block is of 256 tokens, and pairs that lie in two of them
+    V = 2 ** 22 - 256
+    g = _gen(8)
+    h, W = _normal(g, 300, 8, dtype=BF), _normal(g, V, 8, std=0.5, dtype=BF)
+    targets = torch.randint(0, V, (300,), device="cuda", generator=g)
+    offsets = torch.tensor([3, 150, 290], device="cuda")
+    loss, logp, g_h, g_W = mhcl.head_preference_grad(h, W, targets, offsets, torch.tensor([-2300.0, -2200.0], device="cuda"), beta=0.05)
+    ce = mhcl.head_loss(h, W, targets)[0].double()
+    L = -torch.stack([ce[3:150].sum(), ce[150:290].sum()])
+    m = 0.05 * ((L[0] + 2300) - (L[1] + 2200))
+    assert float((logp.double() - L).abs().max()) <= 1e-3 and abs(float(loss) - float(torch.nn.functional.softplus(-m))) <= 1e-4
+    w = torch.zeros(300, device="cuda")
+    w[3:150], w[150:290] = 0.05 * torch.sigmoid(-m).float(), -0.05 * torch.sigmoid(-m).float()
+    want = mhcl.head_loss_grad(h, W, targets, w)
+    for a, b in ((g_h, want[2]), (g_W, want[3])):
+        assert float((a.double() - b.double()).norm()) <= 1e-3 * float(b.double().norm())
+
+
+def test_gradients_against_differences():
+    h, W, targets, offsets, reference = _inputs(9, 12, 16, 30, 2, F, holes=0.1)
+    offsets = torch.tensor([0, 3, 5, 9, 12], device="cuda")
+    weight = torch.tensor([0.7, -0.4], device="cuda")
+
+    def value(h, W):
+        logp = torch.log_softmax(h @ W.t(), dim=1).gather(1, targets.clamp(min=0).unsqueeze(1)).squeeze(1).masked_fill(targets < 0, 0.0)
+        ratio = torch.stack([logp[a:b].sum() for a, b in ((0, 3), (3, 5), (5, 9), (9, 12))]) - reference.double()
+        m = 0.3 * (ratio[0::2] - ratio[1::2])
+        soft = torch.nn.functional.softplus
+        return float(((0.9 * soft(-m) + 0.1 * soft(m)) * weight.double()).sum())
+
+    _, _, g_h, g_W = mhcl.head_preference_grad(h, W, targets, offsets, reference, weight, 0.3, 0.1)
+    at = [h.double(), W.double()]
+    for k, grad in enumerate((g_h, g_W)):
+        for i in (0, grad.numel() // 3, grad.numel() - 1):
+            step = torch.zeros_like(at[k])
+            step.view(-1)[i] = 1e-5
+            up, down = (value(*(t + sign * step if j == k else t for j, t in enumerate(at))) for sign in (1, -1))
+            slope = (up - down) / 2e-5
+            assert abs(float(grad.reshape(-1)[i]) - slope) <= 1e-4 * max(1.0, abs(slope))
+
+
+def test_operands_that_do_not_fit_are_refused():
+    h, W, targets, offsets, reference = _inputs(10, 9, 64, 40, 2, BF)
+    weight = torch.ones(2, device="cuda")
+    for args in ((h, W, targets[:-1], offsets), (h, W, targets, offsets[:-1]), (h, W, targets, offsets.float()), (h, W, targets, offsets, reference[:-1]),
+                 (h, W, targets, offsets, reference.double()), (h, W, targets, offsets, reference, weight[:-1]), (h, W, targets, offsets.cpu()),
+                 (h[:, :-8], W, targets, offsets), (h, W, targets, offsets.view(1, -1))):
+        with pytest.raises(ValueError):
+            mhcl.head_preference_grad(*args)
+    for kw in (dict(beta=math.nan), dict(beta=math.inf), dict(smoothing=-0.1), dict(smoothing=1.1), dict(smoothing=math.nan)):
+        with pytest.raises(mhcl.MhclError):
+            mhcl.head_preference(h, W, targets, offsets, reference, **kw)
+    with pytest.raises(mhcl.MhclError):
+        mhcl.head_preference(h, W.float(), targets, offsets)
+
+
+@pytest.mark.parametrize("io", [BF, F])
+def test_python_and_native_calls_agree(monkeypatch, io):
+    h, W, targets, offsets, reference = _inputs(11, 45, 64, 136, 3, io)
+    weight = torch.rand(3, device="cuda", generator=_gen(1))
+
+    def calls():
+        return [*mhcl.head_preference(h, W, targets, offsets, reference, 0.2), *mhcl.head_preference_grad(h, W, targets, offsets, reference, weight),
+                *mhcl.head_preference_grad(h, W, targets, offsets, dtype=F)]
+
+    quick = calls()
+    monkeypatch.setattr(ends, "_native", lambda: None)
+    for a, b in zip(quick, calls()):
+        assert a.dtype is b.dtype and a.shape == b.shape and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("io", [BF, F])
+def test_under_autograd(io):
+    h, W, targets, offsets, reference = _inputs(12, 70, 64, 100, 3, io)
+    head = mhcl.Head(100, 64, dtype=io)
+    with torch.no_grad():
+        head.W.copy_(W)
+    h.requires_grad_()
+    weight = torch.rand(3, device="cuda", generator=_gen(2)).requires_grad_()
+    loss, logp, g_h, g_W = mhcl.head_preference_grad(h.detach(), W, targets, offsets, reference, weight.detach(), 0.2, 0.1)
+    total, held = head.prefer(h, targets, offsets, reference, weight, beta=0.2, smoothing=0.1)
+    assert torch.equal(held, logp) and not held.requires_grad
+    assert abs(float(total.detach()) - float((loss.double() * weight.detach().double()).sum())) <= 1e-6 * float(loss.abs().sum())
+    total.backward()
+    assert torch.equal(h.grad, g_h) and torch.equal(head.W.grad, g_W) and torch.equal(weight.grad, loss)
+    h.grad = head.W.grad = None
+    (0.25 * head.prefer(h, targets, offsets, reference, weight, beta=0.2, smoothing=0.1)[0]).backward()
+    assert torch.equal(h.grad, g_h * 0.25) and torch.equal(head.W.grad, g_W * 0.25)
+    with torch.no_grad():
+        mean, _ = head.prefer(h, targets, offsets, reference)
+    plain = mhcl.head_preference(h.detach(), W, targets, offsets, reference)[0].double().mean()
+    assert abs(float(mean) - float(plain)) <= 1e-6 * float(plain)
+    total, _ = head.prefer(h, targets, offsets, reference)
+    total.backward(retain_graph=True)
+    with pytest.raises(RuntimeError):
+        total.backward()
+    g, = torch.autograd.grad(head.prefer(h, targets, offsets, reference)[0], h, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.float().square().sum().backward()
+    with pytest.raises(ValueError):
+        head.prefer(h, targets, offsets, reference.requires_grad_())
+
+
+@pytest.mark.parametrize("T", [40, 1300])
+def test_captured_and_replayed(T):
+    h, W, targets, offsets, reference = _inputs(13, T, 64, 700, 3, BF)
+    h2, _, targets2, offsets2, reference2 = _inputs(14, T, 64, 700, 3, BF)
+
+    def step():
+        return mhcl.head_preference_grad(h, W, targets, offsets, reference)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for i in range(4):
+        for a, b in ((h, h2), (targets, targets2)):
+            a.copy_(b if i % 2 else b.flip(0))
+        if i == 2:
+            offsets.copy_(offsets2)
+            reference.copy_(reference2)
+        graph.replay()
+        eager = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, eager))
