@@ -11,6 +11,7 @@ struct FfnPlan {
   bool wide;                                  // fp32 operands
   ProductTile up, down, act, gx, gup, gdown;
   int down_splits, gx_splits, gup_splits, gdown_splits;
+  bool trio;                                  // the backward's three last products in one launch
   FfnPlan(const mhcl_ffn_desc &d, bool grad);
 };
 
@@ -18,7 +19,7 @@ struct FfnWs {
   FfnPlan plan;
   char *a;              // [T][H] silu(gate) * up
   char *g_pre;          // [T][2 H] gradients on gate | up
-  float *slabs;         // parts of the sums of one product after the other
+  float *slabs, *up_slabs, *down_slabs;   // parts of the sums of y and g_x, g_W_up, g_W_down; one and the same where they come one after the other
   size_t bytes;
   FfnWs(const mhcl_ffn_desc &d, bool grad, void *ws);
 };

@@ -6,18 +6,25 @@
 //   g = weight (q - p) / tau,  g_h = g W,  g_W = g^T h
 //
 // The cross entropy's products and passes (mhcl_head_rows.h) with K logits of a token in place of one: they are put in order of
-// their ids first, so that a wave of the first product finds by one look into a table which of them lie in its granule, and takes them
-// from its sums.  (A product of h with the K rows instead would read K C numbers a token again.)
+// their ids first, and a table says of each granule (the rows of a wave of the first product) which of them lie in it, so that the wave takes
+// them from its sums.  (A product of h with the K rows instead would read K C numbers a token again.)
+#include <string.h>
+
 #include "mhcl_head_rows.h"
 
 namespace mhcl {
 namespace {
 
+// What a granule holds of a token's slots in order: the first one, how many, and the first one's row in the granule
+__device__ __forceinline__ uint32_t slots_word(int first, int count, int row) { return row << 18 | count << 9 | first; }
+static_assert(kMostSlots < 512 && kTileBig.gran <= 1 << 14, "slots_word");
+
 // A token's slots, by a wave: a slot is empty where its id is negative or its logit is the lowest there is (-infinity).  LISTS: else the mark alone.
 template <typename ID, bool LISTS>
 __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ ids, const float *__restrict__ logits, int64_t T, int32_t K, int32_t V,
                                                          float inv, int gran_log2, int64_t granules, int32_t *__restrict__ mark,
-                                                         int32_t *__restrict__ id_out, float2 *__restrict__ p_out, uint16_t *__restrict__ start) {
+                                                         int32_t *__restrict__ id_out, float2 *__restrict__ p_out, uint32_t *__restrict__ table,
+                                                         int32_t *__restrict__ listed_out) {
   constexpr int WAVES = kBlock / 64, PER = kMostSlots / 64;
   __shared__ int32_t key[LISTS ? WAVES : 1][kMostSlots], sorted[LISTS ? WAVES : 1][kMostSlots];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -50,10 +57,9 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
   }
   if (lane == 0) mark[t] = held == 0 ? -1 : (past != 0 ? 1 : 0);
   if constexpr (LISTS) {
-    const int most = (K + 63) / 64;
-    for (int i = 0; i < most; ++i) key[wave][i * 64 + lane] = mine[i < PER ? i : 0];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
+      if (i * 64 < K) key[wave][i * 64 + lane] = mine[i];
       a[i] = mine[i] == 0x7fffffff && a[i] == -INFINITY ? -INFINITY : a[i] - top;   // (NaN where the largest is no number)
       sum += a[i] == -INFINITY ? 0.f : expf(a[i]);
     }
@@ -65,12 +71,12 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
     int listed = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      if (i >= most) break;
+      if (i * 64 >= K) break;
       const int k = i * 64 + lane;
       int rank = 0;
-      for (int j = 0; j < most * 64; ++j) rank += key[wave][j] < mine[i] || (key[wave][j] == mine[i] && j < k) ? 1 : 0;
-      sorted[wave][rank] = mine[i];      // (ranks are 0 .. 64 most - 1, each once)
-      if (mine[i] != 0x7fffffff) {
+      for (int j = 0; j < K; ++j) rank += key[wave][j] < mine[i] || (key[wave][j] == mine[i] && j < k) ? 1 : 0;
+      if (mine[i] != 0x7fffffff) {       // (the ranks of those are 0 .. listed - 1, each once)
+        sorted[wave][rank] = mine[i];
         id_out[t * K + rank] = mine[i];
         p_out[t * K + rank] = make_float2(expf(a[i]) / sum, a[i] - log_sum);
         ++listed;
@@ -78,35 +84,36 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) listed += __shfl_xor(listed, off, 64);
+    if (lane == 0) listed_out[t] = listed;
+    uint32_t *row = table + t * granules;
+    for (int64_t g = lane; g < granules; g += 64) row[g] = 0;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    for (int64_t g = lane; g <= granules; g += 64) {
-      const int64_t row = g << gran_log2;
-      int lo = 0, hi = listed;
-      while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (sorted[wave][mid] < row) lo = mid + 1;
-        else hi = mid;
-      }
-      start[t * (granules + 1) + g] = static_cast<uint16_t>(lo);
+    // the first slot of a granule writes its word, after the zeros of the same wave
+    for (int s = lane; s < listed; s += 64) {
+      const int32_t id = sorted[wave][s], g = id >> gran_log2;
+      if (s > 0 && sorted[wave][s - 1] >> gran_log2 == g) continue;
+      int end = s + 1;
+      while (end < listed && sorted[wave][end] >> gran_log2 == g) ++end;
+      row[g] = slots_word(s, end - s, id - (g << gran_log2));
     }
   }
 }
 
-// the logits at a teacher's ids, of logits over tau
+// the logits at a teacher's ids, of logits over tau.  (8192 tokens, C = 768, 50257 rows, 32 slots, us: the table's word read before the tile's first
+// step, and in it the row of the first slot, 693; its first slots by a prefix sum, read with the ids after the last step 743.)
 struct TeacherLogits {
   const int32_t *id;
-  const uint16_t *start;
+  const uint32_t *table;
   float *z;
-  int64_t granules;
-  float inv;
-  int32_t K;
+  int64_t granules, K;
+  int64_t inv;              // the factor's bits (a float beside the others would be put into LDS with them)
   template <int FN>
   struct Held {
-    int from[FN], to[FN];
+    uint32_t word[FN];
   };
-  static constexpr bool kFactor = true;
-  __device__ __forceinline__ float factor() const { return inv; }
+  static constexpr bool kFactor = true, kEarly = true;
+  __device__ __forceinline__ float factor() const { return __uint_as_float(static_cast<uint32_t>(inv)); }
   template <int FM, int FN>
   __device__ __forceinline__ Held<FN> hold(int64_t m0, int64_t n0, int64_t T) const {
     Held<FN> h;
@@ -114,16 +121,18 @@ struct TeacherLogits {
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int64_t t = n0 + 16 * j + (threadIdx.x & 15);
-      h.from[j] = t < T ? start[t * (granules + 1) + g] : 0;
-      h.to[j] = t < T ? start[t * (granules + 1) + g + 1] : 0;
+      h.word[j] = t < T ? table[t * granules + g] : 0u;
     }
     return h;
   }
   template <int FM, int FN>
   __device__ __forceinline__ void take(const f32x4 (&acc)[FM][FN], const Held<FN> &held, int j, int64_t t, int64_t m0, int q) const {
-    for (int s = held.from[j]; __ballot(s < held.to[j]) != 0; ++s) {
-      if (s < held.to[j]) {
-        const int y = id[t * K + s] - static_cast<int>(m0) - 4 * q;
+    const uint32_t word = held.word[j];
+    int s = word & 511, row = word >> 18;
+    const int end = s + (word >> 9 & 511);
+    while (__ballot(s < end) != 0) {
+      if (s < end) {
+        const int y = row - 4 * q;
         if (y >= 0 && (y & 12) == 0) {
           float v = 0.f;
 #pragma unroll
@@ -132,6 +141,7 @@ struct TeacherLogits {
             for (int e = 0; e < 4; ++e) v = y == 16 * i + e ? acc[i][j][e] : v;
           z[t * K + s] = v;
         }
+        if (++s < end) row = id[t * K + s] - static_cast<int>(m0);
       }
     }
   }
@@ -141,7 +151,7 @@ struct TeacherArgs {
   const int32_t *mark, *id;
   const float2 *p;
   const float *z;
-  const uint16_t *start;
+  const int32_t *listed;
   int32_t K;
 };
 
@@ -155,7 +165,6 @@ __device__ __forceinline__ float slots_loss(const TeacherArgs &a, int64_t t, int
   }
   return part;
 }
-__device__ __forceinline__ int slots_listed(const TeacherArgs &a, int64_t t, int64_t granules) { return a.start[t * (granules + 1) + granules]; }
 
 // loss and lse of a token: one wave each, or (WAVES > 1) a block each
 template <int WAVES>
@@ -166,7 +175,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * 64) void teacher_loss
   if (t >= a.T) return;
   float base, sum;
   join_granules<WAVES>(a.stat + t * a.granules, a.granules, red, base, sum);
-  const float loss = rows_sum<WAVES>(slots_loss<WAVES * 64>(b, t, slots_listed(b, t, a.granules), base, logf(sum)), red[2]);
+  const float loss = rows_sum<WAVES>(slots_loss<WAVES * 64>(b, t, b.listed[t], base, logf(sum)), red[2]);
   if (threadIdx.x % (WAVES * 64) == 0) {
     a.lse[t] = base + logf(sum);
     a.loss[t] = b.mark[t] < 0 ? 0.f : (b.mark[t] == 0 ? loss : __uint_as_float(0x7fc00000u));
@@ -182,7 +191,7 @@ __global__ __launch_bounds__(kBlock) void teacher_row_kernel(const RowArgs a, co
   const float2 *stat = a.stat + t * a.granules;
   float base, sum;
   join_granules<kBlock / 64>(stat, a.granules, red, base, sum);
-  const int listed = slots_listed(b, t, a.granules), mark = b.mark[t];
+  const int listed = b.listed[t], mark = b.mark[t];
   const float loss = rows_sum<kBlock / 64>(slots_loss<kBlock>(b, t, listed, base, logf(sum)), red[2]);
   const float bad = __uint_as_float(0x7fc00000u);
   if (threadIdx.x == 0) {
@@ -220,23 +229,27 @@ struct Teacher {
   int gran_log2;
   const DistillWs &w;
   hipStream_t s;
-  TeacherArgs args(int64_t t0) const { return {marks + t0, w.id, w.p, w.z, w.start, K}; }
+  TeacherArgs args(int64_t t0) const { return {marks + t0, w.id, w.p, w.z, w.listed, K}; }
   hipError_t before(int64_t t0, int64_t n) {
     const int64_t at = t0 * K, granules = w.head.plan.granules;
     constexpr int64_t kMostTokens = int64_t{1} << 24;      // of a launch, which has fewer than 2^32 threads
     for (int64_t t = 0; t0 == 0 && n < T && t < T; t += kMostTokens) {     // all marks, which the mean's weights need
       const int64_t some = T - t < kMostTokens ? T - t : kMostTokens;
       hipLaunchKernelGGL((teacher_kernel<ID, false>), dim3(blocks(some, kBlock / 64)), dim3(kBlock), 0, s, ids + t * K, logits + t * K, some, K, V,
-                         factor, gran_log2, granules, w.mark + t, nullptr, nullptr, nullptr);
+                         factor, gran_log2, granules, w.mark + t, nullptr, nullptr, nullptr, nullptr);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL((teacher_kernel<ID, true>), dim3(blocks(n, kBlock / 64)), dim3(kBlock), 0, s, ids + at, logits + at, n, K, V, factor, gran_log2,
-                       granules, w.mark + t0, w.id, w.p, w.start);
+                       granules, w.mark + t0, w.id, w.p, w.table, w.listed);
     return hipGetLastError();
   }
   hipError_t between(const RowArgs &) { return hipSuccess; }
-  TeacherLogits wanted(int64_t) const { return {w.id, w.start, w.z, w.head.plan.granules, factor, K}; }
+  TeacherLogits wanted(int64_t) const {
+    uint32_t bits;
+    memcpy(&bits, &factor, 4);
+    return {w.id, w.table, w.z, w.head.plan.granules, K, bits};
+  }
   hipError_t loss(const RowArgs &a, int64_t t0) {
     if (a.T < 1024) hipLaunchKernelGGL((teacher_loss_kernel<16>), dim3(static_cast<unsigned>(a.T)), dim3(1024), 0, s, a, args(t0));
     else hipLaunchKernelGGL((teacher_loss_kernel<1>), dim3(blocks(a.T, kBlock / 64)), dim3(kBlock), 0, s, a, args(t0));

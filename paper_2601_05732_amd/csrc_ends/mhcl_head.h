@@ -70,12 +70,13 @@ constexpr int kMostSlots = 256;   // of a token's teacher
 struct DistillWs {
   HeadWs head;
   int32_t *mark;        // [T] negative where the teacher says nothing, 1 where it names a row past the vocabulary, else 0
-  // of a block of tokens: a token's ids in order, its teacher's probability and the logarithm of it for each, the student's logit; how many of them
-  // lie before each granule
+  // of a block of tokens: a token's ids in order, its teacher's probability and the logarithm of it for each, the student's logit, how many there
+  // are; which of them lie in each granule
   int32_t *id;          // [tokens][K]
   float2 *p;            // [tokens][K]
   float *z;             // [tokens][K]
-  uint16_t *start;      // [tokens][granules + 1]
+  int32_t *listed;      // [tokens]
+  uint32_t *table;      // [tokens][granules]
   size_t bytes;
   DistillWs(const mhcl_ends_desc &d, int32_t K, bool grad, void *ws) : head(d, grad, ws) {
     WsCursor c(ws ? static_cast<char *>(ws) + head.bytes : nullptr);
@@ -84,7 +85,8 @@ struct DistillWs {
     id = c.take<int32_t>(slots);
     p = c.take<float2>(slots);
     z = c.take<float>(slots);
-    start = c.take<uint16_t>(T * static_cast<size_t>(head.plan.granules + 1));
+    listed = c.take<int32_t>(T);
+    table = c.take<uint32_t>(T * static_cast<size_t>(head.plan.granules));
     bytes = head.bytes + c.off;
   }
 };

@@ -47,7 +47,7 @@ struct TargetLogit {
     return h;
   }
   __device__ __forceinline__ float factor() const { return 1.f; }
-  static constexpr bool kFactor = false;
+  static constexpr bool kFactor = false, kEarly = false;
   template <int FM, int FN>
   __device__ __forceinline__ void take(const f32x4 (&acc)[FM][FN], const Held<FN> &held, int j, int64_t t, int64_t m0, int q) const {
     const int64_t y = held.y[j] - m0 - 4 * q;
@@ -64,7 +64,7 @@ struct TargetLogit {
 // m: vocabulary, n: tokens.  STORE: the numerators too.  WIDE: fp32 numerators.
 template <typename Wanted, bool STORE, bool WIDE>
 struct LogitsEpilogue {
-  static constexpr bool kWide = WIDE, kPaired = false;
+  static constexpr bool kWide = WIDE, kPaired = false, kEarly = Wanted::kEarly;
   Wanted wanted;
   float2 *stat;
   char *E;
@@ -81,10 +81,11 @@ struct LogitsEpilogue {
   __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], const typename Wanted::template Held<FN> &held, int64_t m0, int64_t n0, int) const {
     const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
     if constexpr (Wanted::kFactor) {
+      const float f = wanted.factor();
 #pragma unroll
       for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] *= wanted.factor();
+        for (int j = 0; j < FN; ++j) acc[i][j] *= f;
     }
     if (m0 + FM * 16 > V) {   // rows beyond the vocabulary
 #pragma unroll

@@ -231,6 +231,13 @@ __device__ __forceinline__ void tile_of(const GemmArgs &g, int b, int &tm, int &
   tn = i / width;
 }
 
+// The I-th array of N 16-byte pieces of LDS: one and the same for every product of a kernel that asks for it
+template <int N, int I>
+__device__ __forceinline__ uint4 *lds_array() {
+  __shared__ uint4 a[N];
+  return a;
+}
+
 // A block of WM x WN waves computes BM x BN tiles; wave (wm, wn) rows wm BM / WM of one and columns wn BN / WN on.
 // The epilogue gets acc[fm][fn]: lane (r, q) holds m = 16 fm + 4 q + 0..3 of the wave's rows, n = 16 fn + r of its columns.
 // The next tile's first loads are on their way during the epilogue, and the epilogue's stores during the next tile's first step.
@@ -243,8 +250,10 @@ __device__ __forceinline__ void tile_of(const GemmArgs &g, int b, int &tm, int &
 // 128 x 128 of four waves: fp32, 2048 tokens, C = 768, 50257 rows 0.93 / 0.81 / 0.92 ms and 0.88 / 0.77 / 0.89, 1.0 to 1.2 PFLOP/s of bf16 products;
 // matrix units busy for 49 % of the cycles, the vector ones, which take the parts, for 36 %.
 // 128 x 32: one token, C = 4096, 50257 rows 70 to 80 us from card to card, W at 5.1 to 5.9 TB/s.
-// Epilogue::kPaired: A's rows are two halves (PairedLoader).  block, blocks: its number of how many.
-template <int BM, int BN, int WM, int WN, int STAGES, bool AK, bool BK, typename Epilogue>
+// What an epilogue reads ahead it asks for after the last step, or (Epilogue::kEarly) before the first.
+// Epilogue::kPaired: A's rows are two halves (PairedLoader).  block, blocks: its number of how many.  LEAST: of the pieces of an array in LDS, where a
+// kernel has products of several tiles.
+template <int BM, int BN, int WM, int WN, int STAGES, bool AK, bool BK, int LEAST, typename Epilogue>
 __device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &epilogue, int block, int blocks) {
   constexpr bool WIDE = Epilogue::kWide;
   constexpr int NT = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
@@ -253,12 +262,12 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &ep
   // waits for all of them.  (Two stages' in one array each: 1 % slower, 16384 tokens, C = 4096, 65536 rows.)
   constexpr int TA = BM * 8, TB = BN * 8;
   constexpr bool FOUR = STAGES == 4;
-  __shared__ uint4 m0[FOUR ? TA + TB : TA], m1[FOUR ? TA + TB : TA], m2[FOUR ? TA + TB : 1], m3[FOUR ? TA + TB : 1];
-  __shared__ uint4 n0[FOUR ? 1 : TB], n1[FOUR ? 1 : TB];
+  constexpr int LM = std::max(FOUR ? TA + TB : TA, LEAST), LN = std::max(FOUR ? TA + TB : TB, LEAST);
   struct Stage {
     uint4 *a, *b;
   };
-  const Stage s0{m0, FOUR ? m0 + TA : n0}, s1{m1, FOUR ? m1 + TA : n1}, s2{m2, m2 + TA}, s3{m3, m3 + TA};
+  uint4 *const m0 = lds_array<LM, 0>(), *const m1 = lds_array<LM, 1>(), *const m2 = lds_array<LN, 2>(), *const m3 = lds_array<LN, 3>();
+  const Stage s0{m0, FOUR ? m0 + TA : m2}, s1{m1, FOUR ? m1 + TA : m3}, s2{m2, m2 + TA}, s3{m3, m3 + TA};
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
   std::conditional_t<Epilogue::kPaired, PairedLoader<BM, NT, FM * 8, WIDE>, TileLoader<BM, NT, AK, WIDE>> la;
   static_assert(AK || !Epilogue::kPaired, "halves of rows");
@@ -426,6 +435,9 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &ep
       read_a(s0, 0, 0);
       read_b(s0, 0);
     }
+    decltype(epilogue.template hold<FM, FN>(0, 0)) held;
+    if constexpr (Epilogue::kEarly)
+      held = epilogue.template hold<FM, FN>(static_cast<int64_t>(tm) * BM + wm * (FM * 16), static_cast<int64_t>(tn) * BN + wn * (FN * 16));
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -451,7 +463,7 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &ep
     }
     const int64_t first_m = static_cast<int64_t>(tm) * BM + wm * (FM * 16), first_n = static_cast<int64_t>(tn) * BN + wn * (FN * 16);
     const int this_split = split;
-    const auto held = epilogue.template hold<FM, FN>(first_m, first_n);
+    if constexpr (!Epilogue::kEarly) held = epilogue.template hold<FM, FN>(first_m, first_n);
     // the stages are free once the last loads (of zeros) have arrived and every wave has read its fragments
     wait_all();
     barrier();
@@ -466,18 +478,20 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &ep
 
 template <int BM, int BN, int WM, int WN, int STAGES, bool AK, bool BK, typename Epilogue>
 __global__ __launch_bounds__(WM *WN * 64, 2) void gemm_kernel(const GemmArgs g, const Epilogue epilogue) {
-  gemm_tiles<BM, BN, WM, WN, STAGES, AK, BK>(g, epilogue, blockIdx.x, gridDim.x);
+  gemm_tiles<BM, BN, WM, WN, STAGES, AK, BK, 0>(g, epilogue, blockIdx.x, gridDim.x);
 }
 
 // The two gradients' products in one launch, where both have few parts: neither needs the other's result.  The first first_blocks blocks
-// take g_h, the others g_W, a part each.  Up to two blocks for a compute unit, though one is there at a time (more than that loses: 7043 tokens,
+// take g_h, the others g_W, a part each.  Up to two blocks for a compute unit (more than that loses: 7043 tokens,
 // C = 560, 955 rows 79.2 / 90.1).  (us of the whole call with gradients, two launches / one: 333 tokens,
 // C = 520, 1003 rows, bf16 28.4 / 23.1; 8, 256, 600 21.7 / 16.1; 1000, 512, 1000 35.0 / 27.5; 2000, 256, 600, fp32 64.7 / 50.5.)
+constexpr int kSharedPieces = 128 * 8 + 32 * 8;   // of the smallest tile's arrays, which are the larger
 template <bool SLIM, typename Epilogue>
-__global__ __launch_bounds__(256, 1) void gemm_pair_kernel(const GemmArgs gh, const Epilogue to_gh, const GemmArgs gw, const Epilogue to_gw, int first_blocks) {
+__global__ __launch_bounds__(256, 2) void gemm_pair_kernel(const GemmArgs gh, const Epilogue to_gh, const GemmArgs gw, const Epilogue to_gw, int first_blocks) {
+  constexpr int LEAST = SLIM ? kSharedPieces : 0;
   const int block = blockIdx.x;
-  if (block < first_blocks) gemm_tiles<128, SLIM ? 32 : 128, SLIM ? 4 : 2, SLIM ? 1 : 2, SLIM ? 4 : 2, false, true>(gh, to_gh, block, first_blocks);
-  else gemm_tiles<128, 128, 2, 2, 2, false, false>(gw, to_gw, block - first_blocks, gridDim.x - first_blocks);
+  if (block < first_blocks) gemm_tiles<128, SLIM ? 32 : 128, SLIM ? 4 : 2, SLIM ? 1 : 2, SLIM ? 4 : 2, false, true, LEAST>(gh, to_gh, block, first_blocks);
+  else gemm_tiles<128, 128, 2, 2, 2, false, false, LEAST>(gw, to_gw, block - first_blocks, gridDim.x - first_blocks);
 }
 
 // Four 16-bit results of a lane (r, q) at 16 i + 4 q and as many at 16 (i + 1) + 4 q become eight, for one 16-byte store, at 16 (i + q % 2) +
@@ -492,7 +506,7 @@ __device__ __forceinline__ uint4 join_pairs(uint2 lower, uint2 upper) {
 // out[n][m], m innermost, times *scale (null: 1): fp32 slabs of splits (out32 != null), added to `add` if that is there; else rounded to bf16
 template <bool WIDE>
 struct StoreEpilogue {
-  static constexpr bool kWide = WIDE, kPaired = false;
+  static constexpr bool kWide = WIDE, kPaired = false, kEarly = false;
   const float *scale;
   float *out32;
   uint16_t *out16;

@@ -33,7 +33,8 @@ def _inputs(seed, T, C, H, io):
 def _bounds(x, W_up, W_down, g_y):
     """{name: (result, largest error)} of y, kept, g_x, g_W_up, g_W_down.
       * a sum of products over K: 2^-24 of the sum of their sizes for each of the ceil(K / 32) additions to the fp32 accumulator, six times
-        as many for fp32 operands, and 2^-23 for the products of their parts that are left out;
+        as many for fp32 operands, and 2^-23 for the products of their parts that are left out; or, of few rows, for each of the up to
+        eight additions to a lane's sum for every 512 of K (fp32: four for 256) and the six that join the lanes';
       * the sigmoid by the instructions: 2^-23 |G| for the exponent's rounding, an ulp each for exp2 and 1 / v, half a one for the sum, and a
         half for each product after it: 2^-21 + 2^-23 |G| of the result;
       * silu and its derivative have slopes of at most 1.1 and 0.5;
@@ -43,7 +44,8 @@ def _bounds(x, W_up, W_down, g_y):
     last = torch.finfo(x.dtype).eps / 2
 
     def summed(K):
-        return (-(-K // 32) + 1) * 2.0 ** -24 if bf else (6 * -(-K // 32) + 3) * 2.0 ** -24
+        by_tiles, by_lanes = (-(-K // 32) + 1 if bf else 6 * -(-K // 32) + 3), 8 * -(-K // 512) + 6
+        return max(by_tiles, by_lanes if len(x) <= 2 else 0) * 2.0 ** -24
 
     X, Up, Dn, gy = (t.double() for t in (x, W_up, W_down, g_y))
     T, (C, H) = len(X), Dn.shape
@@ -95,7 +97,7 @@ def _check(x, W_up, W_down, g_y):
     return got
 
 
-SIZES = [(1, 8, 8), (1, 4096, 1000), (2, 64, 24), (16, 264, 136), (31, 4096, 8), (33, 72, 1000), (64, 8, 2056), (65, 136, 520), (130, 1024, 264),
+SIZES = [(1, 8, 8), (2, 520, 2056), (2, 8200, 40), (2, 16392, 24), (4, 1032, 1000), (5, 136, 264), (16, 2056, 4104), (64, 520, 1000), (17, 2056, 24), (48, 1000, 520), (1, 4096, 1000), (2, 64, 24), (16, 264, 136), (31, 4096, 8), (33, 72, 1000), (64, 8, 2056), (65, 136, 520), (130, 1024, 264),
          (333, 520, 1000), (1000, 64, 40), (40, 128, 8200), (2049, 72, 264), (777, 2056, 16)]
 
 
