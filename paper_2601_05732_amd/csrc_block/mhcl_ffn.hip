@@ -498,6 +498,7 @@ FfnPlan::FfnPlan(const mhcl_ffn_desc &d, bool grad) {
   // is not before its longest part nor before all units have done their share.
   const Split *all[3] = {&x, &u, &w};
   int k[3] = {1, 1, 1};
+  const auto slim = [&](int i) { return i == 0 && gx.bn < 128; };     // (half a step's time, a quarter of a slab's)
   const auto part = [&](int i) { return (ceil_div(all[i]->steps, k[i]) + 4) * (i == 0 && gx.bn < 128 ? 30 : 60); };
   int64_t best = INT64_MAX;
   for (;;) {
@@ -508,7 +509,7 @@ FfnPlan::FfnPlan(const mhcl_ffn_desc &d, bool grad) {
       if (part(i) > longest) longest = part(i), which = i;
       work += count * part(i);
       parts += count;
-      slabs += k[i] > 1 ? count : 0;
+      slabs += k[i] > 1 ? count / (slim(i) ? 4 : 1) : 0;
     }
     const int64_t alone = parts <= kChipBlocks ? (wide ? 33 : 42) : 60;
     const int64_t time = std::max(longest * alone / 60, work / (2 * kChipBlocks)) + slabs + (slabs > 0 ? kSumTime : 0);
