@@ -155,16 +155,8 @@ struct TeacherArgs {
   int32_t K;
 };
 
-// a token's loss from its slots: the threads' parts of it
-template <int THREADS>
-__device__ __forceinline__ float slots_loss(const TeacherArgs &a, int64_t t, int listed, float base, float log_sum) {
-  float part = 0.f;
-  for (int s = threadIdx.x % THREADS; s < listed; s += THREADS) {
-    const float2 p = a.p[t * a.K + s];
-    if (p.x != 0.f) part += p.x * (p.y - ((a.z[t * a.K + s] - base) - log_sum));
-  }
-  return part;
-}
+// what a slot adds to its token's loss
+__device__ __forceinline__ float slot_loss(float2 p, float z, float base, float log_sum) { return p.x != 0.f ? p.x * (p.y - ((z - base) - log_sum)) : 0.f; }
 
 // loss and lse of a token: one wave each, or (WAVES > 1) a block each
 template <int WAVES>
@@ -175,7 +167,9 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * 64) void teacher_loss
   if (t >= a.T) return;
   float base, sum;
   join_granules<WAVES>(a.stat + t * a.granules, a.granules, red, base, sum);
-  const float loss = rows_sum<WAVES>(slots_loss<WAVES * 64>(b, t, b.listed[t], base, logf(sum)), red[2]);
+  float part = 0.f;
+  for (int s = threadIdx.x % (WAVES * 64); s < b.listed[t]; s += WAVES * 64) part += slot_loss(b.p[t * b.K + s], b.z[t * b.K + s], base, logf(sum));
+  const float loss = rows_sum<WAVES>(part, red[2]);
   if (threadIdx.x % (WAVES * 64) == 0) {
     a.lse[t] = base + logf(sum);
     a.loss[t] = b.mark[t] < 0 ? 0.f : (b.mark[t] == 0 ? loss : __uint_as_float(0x7fc00000u));
@@ -186,16 +180,23 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * 64) void teacher_loss
 // logits as they are; ids that a teacher names twice by the first of them.
 template <typename IO>
 __global__ __launch_bounds__(kBlock) void teacher_row_kernel(const RowArgs a, const TeacherArgs b) {
+  static_assert(kMostSlots <= kBlock, "a thread has a slot");
   __shared__ float red[3][16];
   const int64_t t = blockIdx.x;
+  const int s = threadIdx.x, listed = b.listed[t], mark = b.mark[t];
+  // (asked for before the row's sum is known; slots behind the last are in reach)
+  const int64_t slot = t * b.K + (s < b.K ? s : 0);
+  const float2 mine = b.p[slot];
+  const float z = b.z[slot];
+  const int32_t id = b.id[slot];
   const float2 *stat = a.stat + t * a.granules;
   float base, sum;
   join_granules<kBlock / 64>(stat, a.granules, red, base, sum);
-  const int listed = b.listed[t], mark = b.mark[t];
-  const float loss = rows_sum<kBlock / 64>(slots_loss<kBlock>(b, t, listed, base, logf(sum)), red[2]);
+  const float log_sum = logf(sum);
+  const float loss = rows_sum<kBlock / 64>(s < listed ? slot_loss(mine, z, base, log_sum) : 0.f, red[2]);
   const float bad = __uint_as_float(0x7fc00000u);
   if (threadIdx.x == 0) {
-    a.lse[t] = base + logf(sum);
+    a.lse[t] = base + log_sum;
     a.loss[t] = mark < 0 ? 0.f : (mark == 0 ? loss : bad);
   }
   const float given = weight_over_common(a, b.mark, t, mark);
@@ -203,17 +204,13 @@ __global__ __launch_bounds__(kBlock) void teacher_row_kernel(const RowArgs a, co
   const float weight = mark == 1 ? bad : given;
   turn_row<IO>(a, t, stat, base, weight / sum, counts, [](int64_t, float (&)[8]) {});
   __syncthreads();
-  if (!counts) return;
-  for (int s = threadIdx.x; s < listed; s += kBlock) {
-    const int32_t *id = b.id + t * b.K;
-    if (s > 0 && id[s - 1] == id[s]) continue;
-    float p = 0.f;
-    for (int i = s; i < listed && id[i] == id[s]; ++i) p += b.p[t * b.K + i].x;
-    const float g = weight * (expf(b.z[t * b.K + s] - base) / sum - p);
-    const int64_t at = t * a.ld + id[s];
-    if constexpr (IO::kVec == 8) reinterpret_cast<uint16_t *>(a.E)[at] = f32_to_bf16(g);
-    else reinterpret_cast<float *>(a.E)[at] = g;
-  }
+  if (!counts || s >= listed || (s > 0 && b.id[slot - 1] == id)) return;
+  float p = mine.x;
+  for (int i = s + 1; i < listed && b.id[t * b.K + i] == id; ++i) p += b.p[t * b.K + i].x;
+  const float g = weight * (expf(z - base) / sum - p);
+  const int64_t at = t * a.ld + id;
+  if constexpr (IO::kVec == 8) reinterpret_cast<uint16_t *>(a.E)[at] = f32_to_bf16(g);
+  else reinterpret_cast<float *>(a.E)[at] = g;
 }
 
 // what of run_head is the teacher's

@@ -133,6 +133,8 @@ def train_on_pairs(model, tokens, steps: int, pairs: int, length: int, lr: float
     opt = torch.optim.AdamW(model.parameters(), lr=lr, weight_decay=0.0)
     g = torch.Generator().manual_seed(0)
     span, losses = pairs * (length + 1), []
+    if pairs < 1 or length < 1 or len(tokens) <= span:
+        raise ValueError(f"{pairs} pairs of {length} tokens need more than {span} tokens, got {len(tokens)}")
     offsets = torch.arange(2 * pairs + 1, device=tokens.device) * length
     packed = []
     for step in range(steps):
