@@ -412,8 +412,8 @@ int mhcl_head_distill(const mhcl_ends_desc *desc, int32_t K, float temperature, 
  *     m[p]    = beta ((logp[2p] - reference[2p]) - (logp[2p+1] - reference[2p+1]))
  *     loss[p] = (1 - smoothing) log(1 + exp(-m)) + smoothing log(1 + exp(m))
  * and, where g_h and g_W are given, the gradients of sum_p weight[p] loss[p] on h and W (weight NULL: of the mean over the pairs).
- * Log probabilities of tokens are fp32, their sums and all of a pair fp64, rounded to fp32 at the end.  Tokens outside of the sequences add nothing; their
- * g_h is 0.  Offsets ascend from 0 or more to T or less; where they do not, which the host cannot see, the pair's loss and logp are NaN (and
+ * Log probabilities of tokens are fp32, their sums and all of a pair fp64, rounded to fp32 at the end.  Tokens outside of the sequences, and those
+ * without a target, add nothing; their g_h is 0, and large products leave them out.  Offsets ascend from 0 or more to T or less; where they do not, which the host cannot see, the pair's loss and logp are NaN (and
  * gradients unless its weight is 0); nothing is read or written out of bounds for it.  Past one block of tokens (MHCL_HEAD_BLOCK_BYTES) the
  * logits are formed twice for gradients, since a pair's weight needs all of its tokens.
  * total, g_h, g_W, unrounded: as in mhcl_head_distill.  pairs: 0 .. 2^22; beta finite; smoothing 0 .. 1.

@@ -52,7 +52,7 @@ __device__ __forceinline__ f32x4 load_four(const float *p, bool here) { return h
 // would put their error into every gradient besides that of the rounded g_G, g_U and a (off from 64 bits by 0.0034 of the 2-norm then, 0.0024 so).
 template <bool KEEP, bool WIDE>
 struct GateEpilogue {
-  static constexpr bool kWide = WIDE, kPaired = true, kEarly = false;
+  static constexpr bool kWide = WIDE, kPaired = true, kEarly = false, kCounted = false;
   void *a;
   float *pre;
   int64_t H, T;
@@ -94,7 +94,7 @@ struct GateEpilogue {
 // m: H, n: tokens.  The sums are g_a; g_G, g_U and a of them and of G and U, each rounded once.
 template <bool WIDE>
 struct GateGradEpilogue {
-  static constexpr bool kWide = WIDE, kPaired = false, kEarly = false;
+  static constexpr bool kWide = WIDE, kPaired = false, kEarly = false, kCounted = false;
   const float *pre;
   void *a, *g_pre;
   int64_t H, T;
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(kBlock) void slab_sums_kernel(const SlabSums a) {
 template <bool AK, bool BK, typename IO>
 hipError_t product(const ProductTile &tile, const Operand &A, const Operand &B, int64_t M, int64_t N, int splits, float *slabs, void *out, hipStream_t s) {
   constexpr bool WIDE = IO::kVec == 4;
-  const StoreEpilogue<WIDE> e{nullptr, splits > 1 ? slabs : (WIDE ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out), nullptr, M, N, M * N};
+  const StoreEpilogue<WIDE> e{nullptr, splits > 1 ? slabs : (WIDE ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out), nullptr, M, N, M * N, nullptr, {}, false, nullptr};
   const hipError_t err = launch_gemm<AK, BK>(tile, A, B, M, N, splits, e, s);
   return err != hipSuccess || splits == 1 ? err : launch_slab_sum<IO>(slabs, out, splits, M * N, s);
 }
@@ -443,8 +443,7 @@ hipError_t run_ffn_grad(const mhcl_ffn_desc &d, const void *x, const void *W_up,
   if ((e = launch_gemm<false, true>(p.act, Wd, gk, H, T, 1, GateGradEpilogue<WIDE>{pre, w.a, w.g_pre, H, T}, s)) != hipSuccess) return e;
   if (p.trio) {
     const auto to = [&](int splits, float *slabs, void *out, int64_t M, int64_t N) {
-      return StoreEpilogue<WIDE>{nullptr, splits > 1 ? slabs : (WIDE ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out), nullptr, M, N,
-                                 M * N};
+      return StoreEpilogue<WIDE>{nullptr, splits > 1 ? slabs : (WIDE ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out), nullptr, M, N, M * N, nullptr, {}, false, nullptr};
     };
     TrioArgs a{{gemm_args(p.gx, Wu, pk, C, T, p.gx_splits), gemm_args(p.gup, xm, pm, C, 2 * H, p.gup_splits), gemm_args(p.gdown, am, gm, H, C, p.gdown_splits)}, {}};
     const auto count = [&](int i) { return a.g[i].tiles_m * a.g[i].tiles_n * a.g[i].splits; };

@@ -24,12 +24,13 @@ template <typename ID, bool LISTS>
 __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ ids, const float *__restrict__ logits, int64_t T, int32_t K, int32_t V,
                                                          float inv, int gran_log2, int64_t granules, int32_t *__restrict__ mark,
                                                          int32_t *__restrict__ id_out, float2 *__restrict__ p_out, uint32_t *__restrict__ table,
-                                                         int32_t *__restrict__ listed_out) {
+                                                         int32_t *__restrict__ listed_out, const int32_t *__restrict__ row) {
   constexpr int WAVES = kBlock / 64, PER = kMostSlots / 64;
   __shared__ int32_t key[LISTS ? WAVES : 1][kMostSlots], sorted[LISTS ? WAVES : 1][kMostSlots];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * WAVES + wave;
   if (t >= T) return;      // (waves do not meet)
+  const int64_t from = row ? row[t] : t;      // the caller's
   float a[PER], top = -INFINITY, sum = 0.f;
   int32_t mine[PER];
   int held = 0, past = 0;
@@ -39,8 +40,8 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
     a[i] = -INFINITY;
     mine[i] = 0x7fffffff;
     if (k < K) {
-      const int64_t id = static_cast<int64_t>(ids[t * K + k]);
-      const float v = logits[t * K + k] * inv;
+      const int64_t id = static_cast<int64_t>(ids[from * K + k]);
+      const float v = logits[from * K + k] * inv;
       const bool there = id >= 0 && !(v == -INFINITY);
       if (there) a[i] = v;
       if (there && id < V) mine[i] = static_cast<int32_t>(id);
@@ -55,7 +56,7 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
     held += __shfl_xor(held, off, 64);
     past += __shfl_xor(past, off, 64);
   }
-  if (lane == 0) mark[t] = held == 0 ? -1 : (past != 0 ? 1 : 0);
+  if (lane == 0) mark[from] = held == 0 ? -1 : (past != 0 ? 1 : 0);
   if constexpr (LISTS) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -85,8 +86,8 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) listed += __shfl_xor(listed, off, 64);
     if (lane == 0) listed_out[t] = listed;
-    uint32_t *row = table + t * granules;
-    for (int64_t g = lane; g < granules; g += 64) row[g] = 0;
+    uint32_t *words = table + t * granules;
+    for (int64_t g = lane; g < granules; g += 64) words[g] = 0;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     // the first slot of a granule writes its word, after the zeros of the same wave
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
       if (s > 0 && sorted[wave][s - 1] >> gran_log2 == g) continue;
       int end = s + 1;
       while (end < listed && sorted[wave][end] >> gran_log2 == g) ++end;
-      row[g] = slots_word(s, end - s, id - (g << gran_log2));
+      words[g] = slots_word(s, end - s, id - (g << gran_log2));
     }
   }
 }
@@ -183,7 +184,8 @@ __global__ __launch_bounds__(kBlock) void teacher_row_kernel(const RowArgs a, co
   static_assert(kMostSlots <= kBlock, "a thread has a slot");
   __shared__ float red[3][16];
   const int64_t t = blockIdx.x;
-  const int s = threadIdx.x, listed = b.listed[t], mark = b.mark[t];
+  const int64_t u = a.token(t);
+  const int s = threadIdx.x, listed = b.listed[t], mark = b.mark[u];
   // (asked for before the row's sum is known; slots behind the last are in reach)
   const int64_t slot = t * b.K + (s < b.K ? s : 0);
   const float2 mine = b.p[slot];
@@ -196,9 +198,10 @@ __global__ __launch_bounds__(kBlock) void teacher_row_kernel(const RowArgs a, co
   const float loss = rows_sum<kBlock / 64>(s < listed ? slot_loss(mine, z, base, log_sum) : 0.f, red[2]);
   const float bad = __uint_as_float(0x7fc00000u);
   if (threadIdx.x == 0) {
-    a.lse[t] = base + log_sum;
-    a.loss[t] = mark < 0 ? 0.f : (mark == 0 ? loss : bad);
+    a.lse[u] = base + log_sum;
+    a.loss[u] = mark < 0 ? 0.f : (mark == 0 ? loss : bad);
   }
+  if (!a.counted(t)) return;
   const float given = weight_over_common(a, b.mark, t, mark);
   const bool counts = given != 0.f;
   const float weight = mark == 1 ? bad : given;
@@ -226,22 +229,31 @@ struct Teacher {
   int gran_log2;
   const DistillWs &w;
   hipStream_t s;
-  TeacherArgs args(int64_t t0) const { return {marks + t0, w.id, w.p, w.z, w.listed, K}; }
-  hipError_t before(int64_t t0, int64_t n) {
-    const int64_t at = t0 * K, granules = w.head.plan.granules;
+  TokenOrder order = {};
+  static constexpr bool kLeavesOut = false;   // lse is every token's
+  TeacherArgs args(int64_t t0) const { return {marks + (order.row ? 0 : t0), w.id, w.p, w.z, w.listed, K}; }
+  // all marks, which the mean's weights and the order need
+  hipError_t mark_all() {
     constexpr int64_t kMostTokens = int64_t{1} << 24;      // of a launch, which has fewer than 2^32 threads
-    for (int64_t t = 0; t0 == 0 && n < T && t < T; t += kMostTokens) {     // all marks, which the mean's weights need
+    for (int64_t t = 0; t < T; t += kMostTokens) {
       const int64_t some = T - t < kMostTokens ? T - t : kMostTokens;
       hipLaunchKernelGGL((teacher_kernel<ID, false>), dim3(blocks(some, kBlock / 64)), dim3(kBlock), 0, s, ids + t * K, logits + t * K, some, K, V,
-                         factor, gran_log2, granules, w.mark + t, nullptr, nullptr, nullptr, nullptr);
+                         factor, gran_log2, w.head.plan.granules, w.mark + t, nullptr, nullptr, nullptr, nullptr, nullptr);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((teacher_kernel<ID, true>), dim3(blocks(n, kBlock / 64)), dim3(kBlock), 0, s, ids + at, logits + at, n, K, V, factor, gran_log2,
-                       granules, w.mark + t0, w.id, w.p, w.table, w.listed);
+    return hipSuccess;
+  }
+  hipError_t before(int64_t t0, int64_t n) {
+    hipError_t e;
+    if (!order.row && t0 == 0 && n < T && (e = mark_all()) != hipSuccess) return e;
+    const int64_t shift = order.row ? 0 : t0;
+    hipLaunchKernelGGL((teacher_kernel<ID, true>), dim3(blocks(n, kBlock / 64)), dim3(kBlock), 0, s, ids + shift * K, logits + shift * K, n, K, V, factor,
+                       gran_log2, w.head.plan.granules, w.mark + shift, w.id, w.p, w.table, w.listed, order.row ? order.row + t0 : nullptr);
     return hipGetLastError();
   }
   hipError_t between(const RowArgs &) { return hipSuccess; }
+  template <bool ORDERED>
   TeacherLogits wanted(int64_t) const {
     uint32_t bits;
     memcpy(&bits, &factor, 4);
@@ -269,8 +281,14 @@ hipError_t launch_distill(const mhcl_ends_desc &d, int32_t K, float temperature,
       using ID = decltype(id);
       int gran_log2 = 0;
       while ((1 << gran_log2) < w.head.plan.logits.gran) ++gran_log2;
-      Teacher<ID> way{w.mark, weight, 1.f / temperature, static_cast<const ID *>(ids), logits, d.T, d.V, K, gran_log2, w, s};
-      const hipError_t e = run_head<decltype(io)>(d, h, W, way, loss, lse, g_h, g_W, unrounded, w.head, s);
+      Teacher<ID> way{w.mark, weight, 1.f / temperature, static_cast<const ID *>(ids), logits, d.T, d.V, K, gran_log2, w, s, w.order};
+      hipError_t e;
+      if (w.ordered) {
+        if ((e = way.mark_all()) != hipSuccess || (e = launch_order(way.marks, nullptr, MHCL_I64, 0, d.T, w.order, s)) != hipSuccess) return e;
+        e = run_head<decltype(io), true>(d, h, W, way, loss, lse, g_h, g_W, unrounded, w.head, s);
+      } else {
+        e = run_head<decltype(io), false>(d, h, W, way, loss, lse, g_h, g_W, unrounded, w.head, s);
+      }
       if (e != hipSuccess || !total) return e;
       mhcl_ends_desc marks = d;
       marks.id_dtype = MHCL_I32;

@@ -21,13 +21,13 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * 64) void loss_kernel(
   __shared__ float red[2][16];
   constexpr int TOKENS = WAVES == 1 ? kBlock / 64 : 1;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * TOKENS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
-  if (t >= a.T) return;
+  if (t >= a.T || !a.counted(t)) return;
   float base, sum;
   join_granules<WAVES>(a.stat + t * a.granules, a.granules, red, base, sum);
   if (threadIdx.x % (WAVES * 64) == 0) {
-    const int64_t y = static_cast<int64_t>(targets[t]);
-    a.lse[t] = base + logf(sum);
-    a.loss[t] = y < 0 ? 0.f : (y < a.V ? logf(sum) + (base - a.zt[t]) : __uint_as_float(0x7fc00000u));
+    const int64_t u = a.token(t), y = static_cast<int64_t>(targets[u]);
+    a.lse[u] = base + logf(sum);
+    a.loss[u] = y < 0 ? 0.f : (y < a.V ? logf(sum) + (base - a.zt[t]) : __uint_as_float(0x7fc00000u));
   }
 }
 
@@ -38,16 +38,17 @@ __global__ __launch_bounds__(kBlock) void row_kernel(const RowArgs a, const ID *
   __shared__ float red[2][16];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x;
+  if (!a.counted(t)) return;
   const float2 *stat = a.stat + t * a.granules;
   float base, sum;
   join_granules<kBlock / 64>(stat, a.granules, red, base, sum);
   // (not by way of lse, in which log(sum) is lost where the logits are large)
-  const int64_t y = static_cast<int64_t>(targets[t]);
+  const int64_t u = a.token(t), y = static_cast<int64_t>(targets[u]);
   const float bad = __uint_as_float(0x7fc00000u);
   const float loss = y < 0 ? 0.f : (y < a.V ? logf(sum) + (base - a.zt[t]) : bad);
   if (tid == 0) {
-    a.lse[t] = base + logf(sum);
-    a.loss[t] = loss;
+    a.lse[u] = base + logf(sum);
+    a.loss[u] = loss;
   }
   const float given = weight_over_common(a, targets, t, y);
   const float weight = y < a.V ? given : bad;
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(kBlock) void scale_to_kernel(const float *__restric
 
 }  // namespace
 
-HeadPlan::HeadPlan(const mhcl_ends_desc &d, bool grad) {
+HeadPlan::HeadPlan(const mhcl_ends_desc &d, bool grad, bool ordered) {
   wide = d.io_dtype == MHCL_F32;
   tokens = d.T;
   const int64_t row = ceil_div(d.V, 256) * 256;
@@ -210,6 +211,9 @@ HeadPlan::HeadPlan(const mhcl_ends_desc &d, bool grad) {
   if (grad) {
     const Split h(gh, d.C, tokens, d.V, wide), w(gw, d.C, d.V, tokens, wide);
     gh_splits = h.best();
+    // (the device chooses, up to this, once it knows how many tokens there are: where they fill the chip many times over there is little to gain)
+    if (ordered && h.tiles < 8 * (gh.bm == 256 ? kChipBlocks : 2 * kChipBlocks))
+      gh_splits = static_cast<int>(std::max<int64_t>(gh_splits, std::min<int64_t>(4, h.steps / 8)));
     if (tokens == d.T) gw_splits = w.best();   // (blocks of tokens add up in fp32 as they are)
     pair = gh.bm < 256 && gw.bm < 256 && h.tiles * gh_splits + w.tiles * gw_splits <= 2 * kChipBlocks;
     if (pair) {
@@ -221,7 +225,7 @@ HeadPlan::HeadPlan(const mhcl_ends_desc &d, bool grad) {
   }
 }
 
-HeadWs::HeadWs(const mhcl_ends_desc &d, bool grad, void *ws) : plan(d, grad) {
+HeadWs::HeadWs(const mhcl_ends_desc &d, bool grad, void *ws, bool ordered) : plan(d, grad, ordered) {
   WsCursor c(ws);
   const size_t T = static_cast<size_t>(plan.tokens), V = static_cast<size_t>(d.V), C = static_cast<size_t>(d.C), es = dtype_bytes(d.io_dtype);
   hp = grad ? c.take<char>(T * C * es) : nullptr;
@@ -244,11 +248,17 @@ struct CrossEntropy {
   const float *weight;
   const HeadWs &w;
   hipStream_t s;
+  TokenOrder order = {};
   static constexpr float factor = 1.f;
+  static constexpr bool kLeavesOut = true;    // (taken in an order for the pairs alone, who read nothing of a token that does not count)
   hipError_t before(int64_t, int64_t) { return hipSuccess; }
   hipError_t between(const RowArgs &) { return hipSuccess; }
-  TargetLogit<ID> wanted(int64_t t0) const { return {marks + t0, w.zt}; }
+  template <bool ORDERED>
+  TargetLogit<ID, ORDERED> wanted(int64_t t0) const {
+    return {marks + (ORDERED ? 0 : t0), w.zt, ORDERED ? order.row + t0 : nullptr};
+  }
   hipError_t loss(const RowArgs &a, int64_t t0) {
+    if (a.row) t0 = 0;
     // (us, 50257 rows in granules of 32: a wave / a block of sixteen for one token 11.2 / 4.6)
     if (a.T < 1024) hipLaunchKernelGGL((loss_kernel<ID, 16>), dim3(static_cast<unsigned>(a.T)), dim3(1024), 0, s, a, marks + t0);
     else hipLaunchKernelGGL((loss_kernel<ID, 1>), dim3(blocks(a.T, kBlock / 64)), dim3(kBlock), 0, s, a, marks + t0);
@@ -256,6 +266,7 @@ struct CrossEntropy {
   }
   template <typename IO>
   hipError_t rows(const RowArgs &a, int64_t t0) {
+    if (a.row) t0 = 0;
     hipLaunchKernelGGL((row_kernel<ID, IO>), dim3(static_cast<unsigned>(a.T)), dim3(kBlock), 0, s, a, marks + t0);
     return hipGetLastError();
   }
@@ -296,16 +307,21 @@ hipError_t launch_preference(const mhcl_ends_desc &d, const void *h, const void 
       using IO = decltype(io);
       const ID *y = static_cast<const ID *>(targets);
       hipError_t e;
+      if (w.ordered && (e = launch_order(y, offsets, offset_dtype, 2 * static_cast<int64_t>(a.pairs), d.T, w.order, s)) != hipSuccess) return e;
+      const auto run = [&](auto &way, void *to_h, void *to_W, bool floats) {
+        return w.ordered ? run_head<IO, true>(d, h, W, way, w.ce, w.lse, to_h, to_W, floats, w.head, s)
+                         : run_head<IO, false>(d, h, W, way, w.ce, w.lse, to_h, to_W, floats, w.head, s);
+      };
       if (grad && w.head.plan.tokens == d.T) {
-        PairedCrossEntropy<ID> way{{y, w.token_weight, w.head, s}, a, offsets, offset_dtype};
-        return run_head<IO>(d, h, W, way, w.ce, w.lse, g_h, g_W, unrounded, w.head, s);
+        PairedCrossEntropy<ID> way{{y, w.token_weight, w.head, s, w.order}, a, offsets, offset_dtype};
+        return run(way, g_h, g_W, unrounded);
       }
       // several blocks of tokens: a pair's weight needs all of its tokens, so that their logits are formed twice
-      CrossEntropy<ID> way{y, nullptr, w.head, s};
-      if ((e = run_head<IO>(d, h, W, way, w.ce, w.lse, nullptr, nullptr, false, w.head, s)) != hipSuccess) return e;
+      CrossEntropy<ID> way{y, nullptr, w.head, s, w.order};
+      if ((e = run(way, nullptr, nullptr, false)) != hipSuccess) return e;
       if ((e = launch_pairs(a, offsets, offset_dtype, s)) != hipSuccess || !grad) return e;
       way.weight = w.token_weight;
-      return run_head<IO>(d, h, W, way, w.ce, w.lse, g_h, g_W, unrounded, w.head, s);
+      return run(way, g_h, g_W, unrounded);
     });
   });
 }
@@ -316,7 +332,7 @@ hipError_t launch_head(const mhcl_ends_desc &d, const void *h, const void *W, co
     return dispatch_io(d.io_dtype, [&](auto io) {
       using ID = decltype(id);
       CrossEntropy<ID> way{static_cast<const ID *>(targets), weight, w, s};
-      return run_head<decltype(io)>(d, h, W, way, loss, lse, g_h, g_W, unrounded, w, s);
+      return run_head<decltype(io), false>(d, h, W, way, loss, lse, g_h, g_W, unrounded, w, s);
     });
   });
 }

@@ -28,10 +28,12 @@ __device__ __forceinline__ float exp_of(float x) {
 }
 
 // Which of a token's logits a loss reads as they are, taken from the sums: its target's.  (hold: what the epilogue reads, read ahead of it.)
-template <typename ID>
+// MAPPED: the product's token t is the caller's row[t].
+template <typename ID, bool MAPPED = false>
 struct TargetLogit {
   const ID *targets;
   float *zt;
+  const int32_t *row;
   template <int FN>
   struct Held {
     int64_t y[FN];
@@ -42,7 +44,7 @@ struct TargetLogit {
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int64_t t = n0 + 16 * j + (threadIdx.x & 15);
-      h.y[j] = t < T ? static_cast<int64_t>(targets[t]) : -1;
+      h.y[j] = t < T ? static_cast<int64_t>(targets[MAPPED ? row[t] : t]) : -1;
     }
     return h;
   }
@@ -61,25 +63,31 @@ struct TargetLogit {
   }
 };
 
-// m: vocabulary, n: tokens.  STORE: the numerators too.  WIDE: fp32 numerators.
-template <typename Wanted, bool STORE, bool WIDE>
+// m: vocabulary, n: tokens.  STORE: the numerators too.  WIDE: fp32 numerators.  COUNTED: `tokens` bounds them.
+template <typename Wanted, bool STORE, bool WIDE, bool COUNTED = false>
 struct LogitsEpilogue {
-  static constexpr bool kWide = WIDE, kPaired = false, kEarly = Wanted::kEarly;
+  static constexpr bool kWide = WIDE, kPaired = false, kEarly = Wanted::kEarly, kCounted = COUNTED;
   Wanted wanted;
   float2 *stat;
   char *E;
-  int64_t T, V, ld, granules;
+  int64_t most, V, ld, granules;     // `most`: tokens
+  TokenCount tokens;
+  __device__ __forceinline__ int64_t rows() const {
+    if constexpr (COUNTED) return tokens.of(most);
+    return most;
+  }
   template <int FM, int FN>
   __device__ __forceinline__ auto hold(int64_t m0, int64_t n0) const {
-    return wanted.template hold<FM, FN>(m0, n0, T);
+    return wanted.template hold<FM, FN>(m0, n0, rows());
   }
   // stores of a wave where all of a tile's tokens are there
   template <int FM, int FN>
   static constexpr int stores() { return FN * (1 + (!STORE ? 0 : (WIDE ? FM : FM / 2))); }
-  __device__ __forceinline__ bool whole(int64_t, int64_t n_end) const { return n_end <= T; }
+  __device__ __forceinline__ bool whole(int64_t, int64_t n_end) const { return n_end <= rows(); }
   template <int FM, int FN>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], const typename Wanted::template Held<FN> &held, int64_t m0, int64_t n0, int) const {
     const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    const int64_t T = rows();
     if constexpr (Wanted::kFactor) {
       const float f = wanted.factor();
 #pragma unroll
@@ -189,6 +197,12 @@ struct RowArgs {
   int C, gran_log2;
   float factor;         // of all weights
   bool take_common;     // row kernels: T is all tokens, and `common` is not there yet
+  // Tokens in an order of their own: token t is the caller's row[t], h's rows lie in hp already, and those past the count have no gradient (null: none of
+  // this)
+  const int32_t *row;
+  TokenCount tokens;
+  __device__ __forceinline__ int64_t token(int64_t t) const { return row ? row[t] : t; }
+  __device__ __forceinline__ bool counted(int64_t t) const { return !row || tokens.first + t < *tokens.count; }
 };
 
 // sum, and the largest, of a value over the WAVES waves of a token
@@ -248,7 +262,7 @@ __device__ __forceinline__ float weight_over_common(const RowArgs &a, const ID *
   } else if (a.weight) {
     common = *a.common;
   }
-  return y < 0 ? 0.f : (a.weight ? a.weight[t] * a.factor / common : 1.f);
+  return y < 0 ? 0.f : (a.weight ? a.weight[a.token(t)] * a.factor / common : 1.f);
 }
 
 // The row's numerators turned into scale exp(z - base) in their place, `replace(v, g)` having the last word on the eight from v on; zeros, and zeros
@@ -293,6 +307,7 @@ __device__ __forceinline__ void turn_row(const RowArgs &a, int64_t t, const floa
       F32::store(a.E, t * a.ld + v + 4, reinterpret_cast<const float(&)[4]>(g[4]));
     }
   }
+  if (a.row && counts) return;
   for (int c = tid * IO::kVec; c < a.C; c += kBlock * IO::kVec) {
     float v[IO::kVec];
     IO::load(a.h, t * a.C + c, v);
@@ -308,13 +323,134 @@ hipError_t dispatch_id(int id_dtype, F &&f) {
   return f(int32_t{});
 }
 
+// ---------------------------------------------------------------- order of the tokens
+// Tokens that count first, each kind in the caller's order: of kOrderTokens of them by a block of threads, which counts its own, and then, knowing
+// those of the blocks before, places them.  A token counts where its target is not negative and (offsets) it lies from the first offset to the last.
+constexpr int kOrderTokens = kBlock * 16;
+template <typename ID, typename OFF>
+struct Counting {
+  const ID *targets;
+  const OFF *offsets;       // null: all tokens
+  int64_t last;             // of the offsets
+  __device__ __forceinline__ uint32_t sixteen(int64_t t0, int64_t T) const {   // a bit each
+    const int64_t from = offsets ? static_cast<int64_t>(offsets[0]) : 0, to = offsets ? static_cast<int64_t>(offsets[last]) : T;
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int64_t t = t0 + i;
+      if (t < T && t >= from && t < to && targets[t] >= 0) bits |= 1u << i;
+    }
+    return bits;
+  }
+};
+template <typename ID, typename OFF>
+__global__ __launch_bounds__(kBlock) void order_count_kernel(const Counting<ID, OFF> c, int64_t T, int32_t *__restrict__ counts) {
+  __shared__ int red[kBlock / 64];
+  int n = __popc(c.sixteen((static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 16, T));
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) counts[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+}
+// counts null: every block counts all tokens itself
+template <typename ID, typename OFF>
+__global__ __launch_bounds__(kBlock) void order_place_kernel(const Counting<ID, OFF> c, int64_t T, const int32_t *__restrict__ counts, int32_t *__restrict__ row,
+                                                             int32_t *__restrict__ count) {
+  __shared__ int red[3][kBlock / 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0, all = 0;
+  if (counts) {
+    for (unsigned b = threadIdx.x; b < gridDim.x; b += kBlock) {
+      all += counts[b];
+      before += b < blockIdx.x ? counts[b] : 0;
+    }
+  } else {
+    for (unsigned b = 0; b < gridDim.x; ++b) {
+      const int n = __popc(c.sixteen((static_cast<int64_t>(b) * kBlock + threadIdx.x) * 16, T));
+      all += n;
+      before += b < blockIdx.x ? n : 0;
+    }
+  }
+  const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 16;
+  const uint32_t bits = c.sixteen(t0, T);
+  int mine = __popc(bits), upto = mine;     // of the lanes up to this one
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int other = __shfl_up(upto, off, 64);
+    upto += lane >= off ? other : 0;
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    before += __shfl_xor(before, off, 64);
+    all += __shfl_xor(all, off, 64);
+  }
+  if (lane == 63) red[0][wave] = upto;
+  if (lane == 0) {
+    red[1][wave] = before;
+    red[2][wave] = all;
+  }
+  __syncthreads();
+  int at = upto - mine;
+  before = all = 0;
+  for (int w = 0; w < kBlock / 64; ++w) {
+    at += w < wave ? red[0][w] : 0;
+    before += red[1][w];
+    all += red[2][w];
+  }
+  at += before;             // tokens that count before this thread's
+  if (blockIdx.x == 0 && threadIdx.x == 0) *count = all;
+  for (int i = 0; i < 16 && t0 + i < T; ++i) {
+    const bool counts_here = bits >> i & 1;
+    row[counts_here ? at : all + (t0 + i - at)] = static_cast<int32_t>(t0 + i);
+    at += counts_here ? 1 : 0;
+  }
+}
+
+// h's rows in the order of the tokens, a wave each; of those past the count, zeros in g_h and `ce` where they are (null: neither)
+template <typename IO>
+__global__ __launch_bounds__(kBlock) void gather_kernel(const void *__restrict__ h, char *__restrict__ hp, int64_t T, int C, const int32_t *__restrict__ row,
+                                                        TokenCount tokens, bool all, void *__restrict__ g_h, int g_pieces, float *__restrict__ ce) {
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
+  if (t >= T) return;
+  const int lane = threadIdx.x & 63, pieces = C / IO::kVec;
+  const int64_t from = row[t];
+  const bool counts = t < tokens.of(T);
+  if (counts || all)
+    for (int p = lane; p < pieces; p += 64) reinterpret_cast<uint4 *>(hp)[t * pieces + p] = static_cast<const uint4 *>(h)[from * pieces + p];
+  if (counts) return;
+  if (g_h)
+    for (int p = lane; p < g_pieces; p += 64) static_cast<uint4 *>(g_h)[from * g_pieces + p] = make_uint4(0, 0, 0, 0);
+  if (ce && lane == 0) ce[from] = 0.f;
+}
+
+template <typename ID>
+hipError_t launch_order(const ID *targets, const void *offsets, int offset_dtype, int64_t last, int64_t T, const TokenOrder &o, hipStream_t s) {
+  return dispatch_id(offset_dtype, [&](auto off) {
+    using OFF = decltype(off);
+    const Counting<ID, OFF> c{targets, static_cast<const OFF *>(offsets), last};
+    const dim3 grid(blocks(T, kOrderTokens));
+    const bool apart = grid.x > 16;      // (a launch of its own costs more than counting 65536 tokens sixteen times)
+    if (apart) {
+      hipLaunchKernelGGL((order_count_kernel<ID, OFF>), grid, dim3(kBlock), 0, s, c, T, o.counts);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((order_place_kernel<ID, OFF>), grid, dim3(kBlock), 0, s, c, T, apart ? o.counts : nullptr, o.row, o.count);
+    return hipGetLastError();
+  });
+}
+
 // The head's products with a loss of the logits, of IO operands (bf16 or fp32).  The loss `way` gives
 //   before(t0, T)            what a block of tokens needs before its logits
 //   wanted(t0)               which logits it reads as they are
 //   loss(a, t0), rows(a, t0) the launches that form the losses of a block; and besides turn its numerators into gradients on the logits
 //   between(a)               what the first block needs between its logits and its rows
 //   marks, weight            ([all tokens]: negative where a token does not count) and its `factor`
-template <typename IO, typename Way>
+// ORDERED: the tokens are taken in way.order's order, and those that do not count are left out of the gradients' products, and (way.kLeavesOut) of the
+// logits'.  (us, without / with: 8192 tokens, of which 5700 count, C = 4096, 65536 rows,
+// pairs 10230 / 7840, their loss alone 3194 / 2367, distillation 10255 / 8692; all 8192 count 10560 / 10730.)
+template <typename IO, bool ORDERED, typename Way>
 hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, Way &way, float *loss, float *lse, void *g_h, void *g_W, bool unrounded,
                     const HeadWs &w, hipStream_t s) {
   constexpr bool WIDE = IO::kVec == 4;
@@ -323,27 +459,36 @@ hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, Way &
   const bool grad = g_W != nullptr;
   const int64_t C = d.C, V = d.V, es = WIDE ? 4 : 2;
   hipError_t e;
-  const bool take_common = d.T <= kCommonTokens && p.tokens == d.T;
+  const bool take_common = !ORDERED && d.T <= kCommonTokens && p.tokens == d.T;
   int gran_log2 = 0;
   while ((1 << gran_log2) < p.logits.gran) ++gran_log2;
   for (int64_t t0 = 0; t0 < d.T; t0 += p.tokens) {
     const int64_t T = d.T - t0 < p.tokens ? d.T - t0 : p.tokens;
-    const void *hb = static_cast<const char *>(h) + t0 * C * es;
+    const TokenCount tokens{ORDERED ? way.order.count : nullptr, t0, 0, 0, 0, 0, 0};
+    const int32_t *row = ORDERED ? way.order.row + t0 : nullptr;
+    const int64_t shift = ORDERED ? 0 : t0;      // of what lies in the caller's order
+    const void *hb = ORDERED ? way.order.hp : static_cast<const char *>(h) + t0 * C * es;
     const Operand Wk{W, C, V, C}, hk{hb, C, T, C};
-    const RowArgs a{hb, way.weight ? way.weight + t0 : nullptr, w.common, w.stat, w.zt, loss + t0, lse + t0, w.E, w.hp, T, p.ld, p.granules, d.V, d.C,
-                    gran_log2, way.factor, take_common};
+    const RowArgs a{hb, way.weight ? way.weight + shift : nullptr, w.common, w.stat, w.zt, loss + shift, lse + shift, w.E, way.order.hp ? way.order.hp : w.hp,
+                    T, p.ld, p.granules, d.V, d.C, gran_log2, way.factor, take_common, row, tokens};
+    if constexpr (ORDERED) {
+      hipLaunchKernelGGL((gather_kernel<IO>), dim3(blocks(T, kBlock / 64)), dim3(kBlock), 0, s, h, way.order.hp, T, d.C, row, tokens, !Way::kLeavesOut,
+                         g_h, static_cast<int>(C * (floats ? 4 : 2) / 16), Way::kLeavesOut ? loss : nullptr);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     if ((e = way.before(t0, T)) != hipSuccess) return e;
-    const auto wanted = way.wanted(t0);
+    const auto wanted = way.template wanted<ORDERED>(t0);
     using Wanted = std::decay_t<decltype(wanted)>;
+    constexpr bool COUNTED = ORDERED && Way::kLeavesOut;
     if (!grad) {
-      const LogitsEpilogue<Wanted, false, WIDE> ep{wanted, w.stat, w.E, T, V, p.ld, p.granules};
-      if ((e = launch_gemm<true, true>(p.logits, Wk, hk, V, T, 1, ep, s)) != hipSuccess) return e;
+      const LogitsEpilogue<Wanted, false, WIDE, COUNTED> ep{wanted, w.stat, w.E, T, V, p.ld, p.granules, tokens};
+      if ((e = launch_gemm<true, true>(p.logits, Wk, hk, V, T, 1, ep, s, tokens)) != hipSuccess) return e;
       if ((e = way.loss(a, t0)) != hipSuccess) return e;
       continue;
     }
     {
-      const LogitsEpilogue<Wanted, true, WIDE> ep{wanted, w.stat, w.E, T, V, p.ld, p.granules};
-      if ((e = launch_gemm<true, true>(p.logits, Wk, hk, V, T, 1, ep, s)) != hipSuccess) return e;
+      const LogitsEpilogue<Wanted, true, WIDE, COUNTED> ep{wanted, w.stat, w.E, T, V, p.ld, p.granules, tokens};
+      if ((e = launch_gemm<true, true>(p.logits, Wk, hk, V, T, 1, ep, s, tokens)) != hipSuccess) return e;
     }
     if (t0 == 0) {
       if ((e = way.between(a)) != hipSuccess) return e;
@@ -356,26 +501,43 @@ hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, Way &
     if ((e = way.template rows<IO>(a, t0)) != hipSuccess) return e;
     // g_h [T, C]: m over C, n over the tokens, k over the vocabulary.  g_W [V, C]: m over C, n over the vocabulary, k over the tokens; the
     // blocks of tokens add up in fp32 (in g_W itself where it is fp32).
-    const Operand Wm{W, C, C, V}, gk{w.E, p.ld, T, p.ld}, hm{w.hp, C, C, T}, gm{w.E, p.ld, p.ld, T};
-    void *gh_out = static_cast<char *>(g_h) + t0 * C * (floats ? 4 : 2);
+    const Operand Wm{W, C, C, V}, gk{w.E, p.ld, T, p.ld}, hm{a.hp, C, C, T}, gm{w.E, p.ld, p.ld, T};
+    void *gh_out = static_cast<char *>(g_h) + shift * C * (floats ? 4 : 2);
     float *sums = floats ? static_cast<float *>(g_W) : w.gW;
-    const StoreEpilogue<WIDE> to_gh{w.common, p.gh_splits > 1 ? w.slabs : (floats ? static_cast<float *>(gh_out) : nullptr),
-                                    static_cast<uint16_t *>(gh_out), nullptr, C, T, T * C};
-    const StoreEpilogue<WIDE> to_gw{w.common, p.gw_splits > 1 ? w.gw_slabs : (floats || t0 + T < d.T ? sums : nullptr), static_cast<uint16_t *>(g_W),
-                                    t0 > 0 ? sums : nullptr, C, V, V * C};
+    const bool parts = p.gh_splits > 1;
+    using Store = StoreEpilogue<WIDE, ORDERED>;
+    TokenCount gh_tokens = tokens;
+    if (ORDERED && parts) {
+      gh_tokens.tiles_m = static_cast<int>(ceil_div(C, p.gh.bm));
+      gh_tokens.bn = p.gh.bn;
+      gh_tokens.steps = static_cast<int>(ceil_div(V, WIDE ? 32 : 64));
+      gh_tokens.alone = WIDE ? 33 : 42;
+      gh_tokens.most_parts = p.gh_splits;
+    }
+    const Store to_gh{w.common, parts && !ORDERED ? w.slabs : (floats ? static_cast<float *>(gh_out) : nullptr), static_cast<uint16_t *>(gh_out), nullptr, C, T,
+                      T * C, row, gh_tokens, false, ORDERED && parts ? w.slabs : nullptr};
+    const Store to_gw{w.common, p.gw_splits > 1 ? w.gw_slabs : (floats || t0 + T < d.T ? sums : nullptr), static_cast<uint16_t *>(g_W),
+                      t0 > 0 ? sums : nullptr, C, V, V * C, nullptr, tokens, true, nullptr};
     if (p.pair) {
-      const GemmArgs gh = gemm_args(p.gh, Wm, gk, C, T, p.gh_splits), gw = gemm_args(p.gw, hm, gm, C, V, p.gw_splits);
+      const GemmArgs gh = gemm_args(p.gh, Wm, gk, C, T, p.gh_splits, gh_tokens), gw = gemm_args(p.gw, hm, gm, C, V, p.gw_splits, tokens, true);
       const int first = gh.tiles_m * gh.tiles_n * gh.splits;
       const dim3 grid(first + gw.tiles_m * gw.tiles_n * gw.splits);
-      if (p.gh.bn < 128) hipLaunchKernelGGL((gemm_pair_kernel<true, StoreEpilogue<WIDE>>), grid, dim3(256), 0, s, gh, to_gh, gw, to_gw, first);
-      else hipLaunchKernelGGL((gemm_pair_kernel<false, StoreEpilogue<WIDE>>), grid, dim3(256), 0, s, gh, to_gh, gw, to_gw, first);
+      if (p.gh.bn < 128) hipLaunchKernelGGL((gemm_pair_kernel<true, Store>), grid, dim3(256), 0, s, gh, to_gh, gw, to_gw, first);
+      else hipLaunchKernelGGL((gemm_pair_kernel<false, Store>), grid, dim3(256), 0, s, gh, to_gh, gw, to_gw, first);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     } else {
-      if ((e = launch_gemm<false, true>(p.gh, Wm, gk, C, T, p.gh_splits, to_gh, s)) != hipSuccess) return e;
-      if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, p.gw_splits, to_gw, s)) != hipSuccess) return e;
+      if ((e = launch_gemm<false, true>(p.gh, Wm, gk, C, T, p.gh_splits, to_gh, s, gh_tokens)) != hipSuccess) return e;
+      if ((e = launch_gemm<false, false>(p.gw, hm, gm, C, V, p.gw_splits, to_gw, s, tokens, true)) != hipSuccess) return e;
     }
     const auto join = floats ? launch_slab_sum<F32> : launch_slab_sum<IO>;
-    if (p.gh_splits > 1 && (e = join(w.slabs, gh_out, p.gh_splits, T * C, s)) != hipSuccess) return e;
+    if (parts && ORDERED) {
+      const dim3 grid(blocks(T * C, kBlock * 4));
+      if (floats) hipLaunchKernelGGL((slab_sum_rows_kernel<F32>), grid, dim3(kBlock), 0, s, w.slabs, gh_out, T, C, row, gh_tokens);
+      else hipLaunchKernelGGL((slab_sum_rows_kernel<IO>), grid, dim3(kBlock), 0, s, w.slabs, gh_out, T, C, row, gh_tokens);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    } else if (parts && (e = join(w.slabs, gh_out, p.gh_splits, T * C, s)) != hipSuccess) {
+      return e;
+    }
     if (p.gw_splits > 1 && (e = join(w.gw_slabs, g_W, p.gw_splits, V * C, s)) != hipSuccess) return e;
   }
   return hipSuccess;

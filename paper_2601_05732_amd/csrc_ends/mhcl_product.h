@@ -28,10 +28,53 @@ struct Operand {
   int64_t rows, depth;
 };
 
+// How many tokens there are is known to the device alone: `count` of them less those of blocks before (`first`), at most as many as the host has sized the
+// product for.  They are D's rows n, or (deep) its depth.
+struct TokenCount {
+  const int32_t *count;
+  int64_t first;
+  __device__ __forceinline__ int64_t of(int64_t most) const {
+    const int64_t n = static_cast<int64_t>(*count) - first;
+    return n < 0 ? 0 : (n < most ? n : most);
+  }
+  // Parts of the depth of a product over n, up to `most_parts` (0: as the host says): the number that ends first, by Split's model, of tiles_m tiles for
+  // every bn tokens; `alone`: a step's time of a tile that has a compute unit for itself (60: the largest, which always has).  (us, 8192 tokens, of which 5700 count, C = 4096, 65536 rows, pairs, the whole call: one part 8471,
+  // so 7840; all 8192 count 10600 and 10730.)
+  int tiles_m, bn, steps, alone, most_parts;
+  __device__ __forceinline__ int parts(int64_t rows) const {
+    const int tiles = tiles_m * static_cast<int>((rows + bn - 1) / bn), slab = bn >= 256 ? 4 : 1;
+    int best = 1, least = 0x7fffffff;
+    for (int k = 1; k <= most_parts; ++k) {
+      const int parts = tiles * k, rest = parts % 512;
+      const int step = bn >= 256 ? (parts + 255) / 256 * 60 : parts / 512 * 60 + (rest == 0 ? 0 : (rest > 256 ? 60 : alone));
+      const int time = step * ((steps + k - 1) / k + 4) + (k > 1 ? parts * slab + 240 : 0);
+      if (time < least) least = time, best = k;
+    }
+    return best;
+  }
+};
 struct GemmArgs {
   Operand A, B;
   int tiles_m, tiles_n, splits;
+  TokenCount tokens;      // read with epilogues that are kCounted
+  bool deep;
 };
+template <int BN, typename Epilogue>
+__device__ __forceinline__ std::conditional_t<Epilogue::kCounted, GemmArgs, const GemmArgs &> counted(const GemmArgs &given) {
+  if constexpr (Epilogue::kCounted) {
+    GemmArgs g = given;
+    if (g.deep) {
+      g.A.depth = g.B.depth = g.tokens.of(given.A.depth);
+    } else {
+      g.B.rows = g.tokens.of(given.B.rows);
+      g.tiles_n = static_cast<int>((g.B.rows + BN - 1) / BN);
+      if (g.tokens.most_parts > 1) g.splits = g.tokens.parts(g.B.rows);
+    }
+    return g;
+  } else {
+    return given;
+  }
+}
 
 // One operand's tile of R rows by 128 bytes in LDS, in 16-byte pieces, as the loads that go straight to LDS leave it (piece i at
 // 16 i), so that a piece's place is chosen by which piece of memory a thread asks for.
@@ -254,8 +297,9 @@ __device__ __forceinline__ uint4 *lds_array() {
 // Epilogue::kPaired: A's rows are two halves (PairedLoader).  block, blocks: its number of how many.  LEAST: of the pieces of an array in LDS, where a
 // kernel has products of several tiles.
 template <int BM, int BN, int WM, int WN, int STAGES, bool AK, bool BK, int LEAST, typename Epilogue>
-__device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &epilogue, int block, int blocks) {
+__device__ __forceinline__ void gemm_tiles(const GemmArgs &given, const Epilogue &epilogue, int block, int blocks) {
   constexpr bool WIDE = Epilogue::kWide;
+  const std::conditional_t<Epilogue::kCounted, GemmArgs, const GemmArgs &> g = counted<BN, Epilogue>(given);
   constexpr int NT = WM * WN * 64, FM = BM / WM / 16, FN = BN / WN / 16;
   static_assert(STAGES == 2 || STAGES == 4, "the loop over steps");
   // A's and B's tile of a stage.  Four stages' lie in an array each: of more arrays the compiler does not keep apart which loads fill which, and
@@ -275,6 +319,7 @@ __device__ __forceinline__ void gemm_tiles(const GemmArgs &g, const Epilogue &ep
   const int64_t depth = g.A.depth < g.B.depth ? g.B.depth : g.A.depth;
   const int steps = static_cast<int>((depth + la.DEPTH - 1) / la.DEPTH);
   const int tiles = g.tiles_m * g.tiles_n * g.splits;
+  if (Epilogue::kCounted && block >= tiles) return;
   int tile = block, tm, tn, split;
   int at, to_load, to_do;         // step of the next load; steps to load, and to multiply
   const auto begin = [&]() __attribute__((always_inline)) {
@@ -503,42 +548,61 @@ __device__ __forceinline__ uint4 join_pairs(uint2 lower, uint2 upper) {
   return make_uint4(x[0], y[0], x[1], y[1]);
 }
 
-// out[n][m], m innermost, times *scale (null: 1): fp32 slabs of splits (out32 != null), added to `add` if that is there; else rounded to bf16
-template <bool WIDE>
+// out[n][m], m innermost, times *scale (null: 1): fp32 slabs of splits (out32 != null), added to `add` if that is there; else rounded to bf16.
+// COUNTED: row n goes to row[n] (null: n), and `tokens` bounds them.
+template <bool WIDE, bool COUNTED = false>
 struct StoreEpilogue {
-  static constexpr bool kWide = WIDE, kPaired = false, kEarly = false;
+  static constexpr bool kWide = WIDE, kPaired = false, kEarly = false, kCounted = COUNTED;
   const float *scale;
   float *out32;
   uint16_t *out16;
   const float *add;
   int64_t M, N, slab;     // elements of a split's slab
+  const int32_t *row;
+  TokenCount tokens;
+  bool deep;
+  float *slabs;           // COUNTED: of several parts, in rows as they are; one part goes where the rest says
+  __device__ __forceinline__ int64_t rows() const {
+    if constexpr (COUNTED) return deep ? N : tokens.of(N);
+    return N;
+  }
   template <int FM, int FN>
   __device__ __forceinline__ float hold(int64_t, int64_t) const { return scale ? *scale : 1.f; }
   template <int FM, int FN>
   static constexpr int stores() { return FN * (WIDE ? FM : FM / 2); }   // (into fp32 slabs twice as many)
-  __device__ __forceinline__ bool whole(int64_t m_end, int64_t n_end) const { return m_end <= M && n_end <= N; }
+  __device__ __forceinline__ bool whole(int64_t m_end, int64_t n_end) const { return m_end <= M && n_end <= rows(); }
   template <int FM, int FN>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], float factor, int64_t m0, int64_t n0, int split) const {
     const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+    const int64_t end = rows();
+    float *to32 = out32;
+    const int32_t *map = row;
+    if constexpr (COUNTED) {
+      if (slabs && tokens.parts(end) > 1) to32 = slabs, map = nullptr;
+    }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int64_t n = n0 + 16 * j + r;
+      int64_t to = n;
+      if constexpr (COUNTED) {
+        if (map && n < end) to = map[n];
+      }
 #pragma unroll
       for (int i = 0; i < FM; i += 2) {
         uint2 part[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const int64_t m = m0 + 16 * (i + k) + 4 * q, elem = n * M + m;      // (M is a multiple of 8)
-          const bool there = n < N && m < M;
+          const int64_t m = m0 + 16 * (i + k) + 4 * q, elem = to * M + m;      // (M is a multiple of 8)
+          const bool there = n < end && m < M;
           f32x4 v = acc[i + k][j] * factor;
           if (add && there) v += *reinterpret_cast<const f32x4 *>(add + elem);
-          if (out32 && there) *reinterpret_cast<f32x4 *>(out32 + split * slab + elem) = v;
+          if (to32 && there) *reinterpret_cast<f32x4 *>(to32 + split * slab + elem) = v;
           part[k] = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
         }
-        if (!out32) {
+        if (!to32) {
           const uint4 eight = join_pairs(part[0], part[1]);
           const int64_t m = m0 + 16 * (i + (q & 1)) + 8 * (q >> 1);
-          if (n < N && m < M) *reinterpret_cast<uint4 *>(out16 + n * M + m) = eight;
+          if (n < end && m < M) *reinterpret_cast<uint4 *>(out16 + to * M + m) = eight;
         }
       }
     }
@@ -557,18 +621,35 @@ __global__ __launch_bounds__(kBlock) void slab_sum_kernel(const float *__restric
   else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + i) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
 }
 
+// The same of rows of M numbers, row n to row[n], as many as there are tokens, and parts where there are several
+template <typename IO>
+__global__ __launch_bounds__(kBlock) void slab_sum_rows_kernel(const float *__restrict__ in, void *__restrict__ out, int64_t N, int64_t M,
+                                                               const int32_t *__restrict__ row, TokenCount tokens) {
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 4, n = i / M, count = N * M, rows = tokens.of(N);
+  if (n >= rows) return;
+  const int slabs = tokens.parts(rows);
+  if (slabs == 1) return;
+  f32x4 s = *reinterpret_cast<const f32x4 *>(in + i);
+#pragma unroll 4
+  for (int k = 1; k < slabs; ++k) s += *reinterpret_cast<const f32x4 *>(in + k * count + i);
+  const int64_t to = row[n] * M + i % M;
+  if constexpr (IO::kVec == 4) *reinterpret_cast<f32x4 *>(static_cast<float *>(out) + to) = s;
+  else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + to) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
+}
+
 constexpr int64_t kChipBlocks = 256;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 unsigned blocks(int64_t items, int64_t each) { return static_cast<unsigned>(ceil_div(items, each)); }
 
-GemmArgs gemm_args(const ProductTile &tile, const Operand &A, const Operand &B, int64_t M, int64_t N, int splits) {
-  return {A, B, static_cast<int>(ceil_div(M, tile.bm)), static_cast<int>(ceil_div(N, tile.bn)), splits};
+GemmArgs gemm_args(const ProductTile &tile, const Operand &A, const Operand &B, int64_t M, int64_t N, int splits, TokenCount tokens = {}, bool deep = false) {
+  return {A, B, static_cast<int>(ceil_div(M, tile.bm)), static_cast<int>(ceil_div(N, tile.bn)), splits, tokens, deep};
 }
 
 template <bool AK, bool BK, typename Epilogue>
-hipError_t launch_gemm(const ProductTile &tile, const Operand &A, const Operand &B, int64_t M, int64_t N, int splits, const Epilogue &e, hipStream_t s) {
-  const GemmArgs g = gemm_args(tile, A, B, M, N, splits);
+hipError_t launch_gemm(const ProductTile &tile, const Operand &A, const Operand &B, int64_t M, int64_t N, int splits, const Epilogue &e, hipStream_t s,
+                       TokenCount tokens = {}, bool deep = false) {
+  const GemmArgs g = gemm_args(tile, A, B, M, N, splits, tokens, deep);
   // as many blocks as the chip holds (of the smallest tile, which waits for memory, one for every tile)
   const unsigned tiles = static_cast<unsigned>(g.tiles_m * g.tiles_n * splits), most = tile.bm == 256 ? kChipBlocks : 2 * kChipBlocks;
   const dim3 grid(tile.bn < 128 || tiles < most ? tiles : most);

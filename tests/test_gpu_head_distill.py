@@ -62,6 +62,25 @@ def test_distill_in_the_largest_tiles():
     _check(*_inputs(1, 4100, 72, 4200, 48, BF), tau=2.0)
 
 
+@pytest.mark.parametrize("io,T,C,V,holes", [(BF, 4200, 2048, 16400, 0.4), (F, 4200, 2048, 16400, 0.0), (BF, 500, 4096, 70000, 0.2), (F, 2049, 4096, 16500, 0.7),
+                                            (BF, 2049, 4096, 16500, 1.1)])
+def test_products_that_are_large_enough_leave_tokens_out(io, T, C, V, holes):
+    h, W, ids, logits = _inputs(T, T, C, V, 17, io, holes=holes)
+    weight = torch.rand(T, device="cuda", generator=_gen(4))
+    weight[::5] = 0.0
+    none = ~(ids >= 0).any(dim=1)
+    _check(h, W, ids, logits, None, 2.0)
+    got = _check(h, W, ids, logits, weight, 2.0)
+    assert not got["g_h"][none].any() and not got["loss"][none].any()
+    h[none] = math.nan
+    again = mhcl.head_distill_grad(h, W, ids.to(torch.int32), logits, weight, 2.0)
+    for name, b in zip(got, again):
+        if name == "lse":
+            assert torch.equal(got[name][~none], b[~none])
+        else:
+            assert torch.equal(got[name], b)
+
+
 @pytest.mark.parametrize("io", [BF, F])
 def test_weights_and_types_of_ids_and_logits(io):
     h, W, ids, logits = _inputs(2, 200, 96, 500, 12, io, ids_dtype=torch.int32)
@@ -158,11 +177,11 @@ def test_large_logits_and_temperatures():
         _check(h, W, ids, 20 * logits, tau=tau)
 
 
-@pytest.mark.parametrize("io", [BF, F])
-def test_blocks_of_tokens(io):
-    # a vocabulary so long that a block is of 256 tokens: marks of all of them, lists of a block's
+@pytest.mark.parametrize("io,C", [(BF, 8), (F, 8), (BF, 128)])
+def test_blocks_of_tokens(io, C):
+    # a vocabulary so long that a block is of 256 tokens: marks of all of them, lists of a block's; C = 128: in an order of their own
     V = 2 ** 22 - 256
-    h, W, ids, logits = _inputs(10, 300, 8, V, 4, io)
+    h, W, ids, logits = _inputs(10, 300, C, V, 4, io)
     ids[:, 0] = torch.where(ids[:, 0] >= 0, V - 1, -1)
     got = dict(zip(("loss", "lse", "g_h", "g_W"), mhcl.head_distill_grad(h, W, ids, logits)))
     W64 = W.double()

@@ -65,6 +65,24 @@ def test_preference_in_the_largest_tiles():
 
 
 @pytest.mark.parametrize("io", [BF, F])
+@pytest.mark.parametrize("T,C,V,pairs,holes", [(2100, 1024, 8200, 5, 0.3), (5000, 264, 13100, 40, 0.7), (300, 4096, 16000, 2, 0.0), (9000, 72, 27000, 3, 0.3),
+                                               (2049, 1032, 8200, 3, 1.1)])
+def test_products_that_are_large_enough_leave_tokens_out(io, T, C, V, pairs, holes):
+    h, W, targets, offsets, reference = _inputs(T, T, C, V, pairs, io, lead=T // 7, tail=T // 9, holes=holes)
+    weight = torch.rand(pairs, device="cuda", generator=_gen(4))
+    weight[0] = 0.0
+    bad = targets < 0
+    bad[:T // 7] = bad[T - T // 9:] = True
+    got = _check(h, W, targets, offsets, reference, weight, smoothing=0.1)
+    assert not got["g_h"][bad].any()
+    h[bad] = math.nan
+    again = mhcl.head_preference_grad(h, W, targets.to(torch.int32), offsets.to(torch.int32), reference, weight, 0.1, 0.1)
+    assert all(torch.equal(a, b) for a, b in zip(got.values(), again))
+    h[bad] = math.inf
+    assert torch.equal(mhcl.head_preference(h, W, targets, offsets, reference, smoothing=0.1)[1], mhcl.head_preference_grad(h, W, targets, offsets)[1])
+
+
+@pytest.mark.parametrize("io", [BF, F])
 @pytest.mark.parametrize("dtype", [torch.int64, torch.int32])
 def test_weights_types_and_no_reference(io, dtype):
     h, W, targets, offsets, reference = _inputs(2, 700, 96, 500, 6, io, dtype=dtype)
@@ -146,17 +164,20 @@ def test_large_margins():
     assert torch.isfinite(got["loss"]).all() and torch.isfinite(got["g_h"]).all()
 
 
-def test_blocks_of_tokens():
-    # a vocabulary so long that a block is of 256 tokens, and pairs that lie in two of them
+@pytest.mark.parametrize("C,holes", [(8, 0.0), (16, 0.0), (16, 0.1), (16, 0.5)])
+def test_blocks_of_tokens(C, holes):
+    # a vocabulary so long that a block is of 256 tokens, and pairs that lie in two of them, or (tokens left out) all in one
     V = 2 ** 22 - 256
     g = _gen(8)
-    h, W = _normal(g, 300, 8, dtype=BF), _normal(g, V, 8, std=0.5, dtype=BF)
+    h, W = _normal(g, 300, C, dtype=BF), _normal(g, V, C, std=0.5, dtype=BF)
     targets = torch.randint(0, V, (300,), device="cuda", generator=g)
+    targets = torch.where(torch.rand(300, device="cuda", generator=g) < holes, -1, targets)
     offsets = torch.tensor([3, 150, 290], device="cuda")
-    loss, logp, g_h, g_W = mhcl.head_preference_grad(h, W, targets, offsets, torch.tensor([-2300.0, -2200.0], device="cuda"), beta=0.05)
     ce = mhcl.head_loss(h, W, targets)[0].double()
     L = -torch.stack([ce[3:150].sum(), ce[150:290].sum()])
-    m = 0.05 * ((L[0] + 2300) - (L[1] + 2200))
+    reference = (L + torch.tensor([20.0, -10.0], device="cuda")).float()
+    loss, logp, g_h, g_W = mhcl.head_preference_grad(h, W, targets, offsets, reference, beta=0.05)
+    m = 0.05 * ((L[0] - reference[0].double()) - (L[1] - reference[1].double()))
     assert float((logp.double() - L).abs().max()) <= 1e-3 and abs(float(loss) - float(torch.nn.functional.softplus(-m))) <= 1e-4
     w = torch.zeros(300, device="cuda")
     w[3:150], w[150:290] = 0.05 * torch.sigmoid(-m).float(), -0.05 * torch.sigmoid(-m).float()
