@@ -260,7 +260,7 @@ struct Teacher {
     return {w.id, w.table, w.z, w.head.plan.granules, K, bits};
   }
   hipError_t loss(const RowArgs &a, int64_t t0) {
-    if (a.T < 1024) hipLaunchKernelGGL((teacher_loss_kernel<16>), dim3(static_cast<unsigned>(a.T)), dim3(1024), 0, s, a, args(t0));
+    if (a.T < 1024 && a.granules > kWaveGranules) hipLaunchKernelGGL((teacher_loss_kernel<16>), dim3(static_cast<unsigned>(a.T)), dim3(1024), 0, s, a, args(t0));
     else hipLaunchKernelGGL((teacher_loss_kernel<1>), dim3(blocks(a.T, kBlock / 64)), dim3(kBlock), 0, s, a, args(t0));
     return hipGetLastError();
   }

@@ -249,6 +249,7 @@ struct CrossEntropy {
   const HeadWs &w;
   hipStream_t s;
   TokenOrder order = {};
+  bool pairs = false;
   static constexpr float factor = 1.f;
   static constexpr bool kLeavesOut = true;    // (taken in an order for the pairs alone, who read nothing of a token that does not count)
   hipError_t before(int64_t, int64_t) { return hipSuccess; }
@@ -260,7 +261,8 @@ struct CrossEntropy {
   hipError_t loss(const RowArgs &a, int64_t t0) {
     if (a.row) t0 = 0;
     // (us, 50257 rows in granules of 32: a wave / a block of sixteen for one token 11.2 / 4.6)
-    if (a.T < 1024) hipLaunchKernelGGL((loss_kernel<ID, 16>), dim3(static_cast<unsigned>(a.T)), dim3(1024), 0, s, a, marks + t0);
+    // (or, of pairs, where a wave holds a row's granules in registers: 300 tokens, 32 granules 4.5 / 3.8; the cross entropy alone keeps its bits)
+    if (a.T < 1024 && !(pairs && a.granules <= kWaveGranules)) hipLaunchKernelGGL((loss_kernel<ID, 16>), dim3(static_cast<unsigned>(a.T)), dim3(1024), 0, s, a, marks + t0);
     else hipLaunchKernelGGL((loss_kernel<ID, 1>), dim3(blocks(a.T, kBlock / 64)), dim3(kBlock), 0, s, a, marks + t0);
     return hipGetLastError();
   }
@@ -313,11 +315,11 @@ hipError_t launch_preference(const mhcl_ends_desc &d, const void *h, const void 
                          : run_head<IO, false>(d, h, W, way, w.ce, w.lse, to_h, to_W, floats, w.head, s);
       };
       if (grad && w.head.plan.tokens == d.T) {
-        PairedCrossEntropy<ID> way{{y, w.token_weight, w.head, s, w.order}, a, offsets, offset_dtype};
+        PairedCrossEntropy<ID> way{{y, w.token_weight, w.head, s, w.order, true}, a, offsets, offset_dtype};
         return run(way, g_h, g_W, unrounded);
       }
       // several blocks of tokens: a pair's weight needs all of its tokens, so that their logits are formed twice
-      CrossEntropy<ID> way{y, nullptr, w.head, s, w.order};
+      CrossEntropy<ID> way{y, nullptr, w.head, s, w.order, true};
       if ((e = run(way, nullptr, nullptr, false)) != hipSuccess) return e;
       if ((e = launch_pairs(a, offsets, offset_dtype, s)) != hipSuccess || !grad) return e;
       way.weight = w.token_weight;

@@ -231,9 +231,10 @@ __device__ __forceinline__ float rows_max(float v, float *red) {
 
 // a row's maximum (0 where there is none) and the sum of exp(z - that) from its granules; the first ones of a lane stay in registers from the one to the
 // other (us, 50257 rows in granules of 128, 8192 tokens a wave each: read twice 10.7, so 9.4)
+constexpr int64_t kWaveGranules = 512;     // that a wave holds
 template <int WAVES>
 __device__ __forceinline__ void join_granules(const float2 *stat, int64_t granules, float (*red)[16], float &base, float &sum) {
-  constexpr int STRIDE = WAVES * 64, HELD = WAVES == 1 ? 8 : (WAVES <= 4 ? 4 : 1);
+  constexpr int STRIDE = WAVES * 64, HELD = WAVES == 1 ? kWaveGranules / 64 : (WAVES <= 4 ? 4 : 1);
   const int tid = threadIdx.x % STRIDE;
   float2 held[HELD];
   float top = -INFINITY;
@@ -325,28 +326,31 @@ hipError_t dispatch_id(int id_dtype, F &&f) {
 
 // ---------------------------------------------------------------- order of the tokens
 // Tokens that count first, each kind in the caller's order: of kOrderTokens of them by a block of threads, which counts its own, and then, knowing
-// those of the blocks before, places them.  A token counts where its target is not negative and (offsets) it lies from the first offset to the last.
+// those of the blocks before, places them; a wave has 16 times 64.  A token counts where its target is not negative and (offsets) it lies from the first
+// offset to the last.
 constexpr int kOrderTokens = kBlock * 16;
 template <typename ID, typename OFF>
 struct Counting {
   const ID *targets;
   const OFF *offsets;       // null: all tokens
   int64_t last;             // of the offsets
-  __device__ __forceinline__ uint32_t sixteen(int64_t t0, int64_t T) const {   // a bit each
+  // a bit each for the lane's tokens t0 + 64 i
+  __device__ __forceinline__ uint32_t sixteen(int64_t t0, int64_t T) const {
     const int64_t from = offsets ? static_cast<int64_t>(offsets[0]) : 0, to = offsets ? static_cast<int64_t>(offsets[last]) : T;
+    ID y[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = targets[t0 + 64 * i < T ? t0 + 64 * i : T - 1];     // (a load under a condition would wait for the one before)
     uint32_t bits = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int64_t t = t0 + i;
-      if (t < T && t >= from && t < to && targets[t] >= 0) bits |= 1u << i;
-    }
+    for (int i = 0; i < 16; ++i) bits |= t0 + 64 * i < T && t0 + 64 * i >= from && t0 + 64 * i < to && y[i] >= 0 ? 1u << i : 0u;
     return bits;
   }
 };
+__device__ __forceinline__ int64_t order_token(int64_t block) { return block * kOrderTokens + (threadIdx.x >> 6) * 1024 + (threadIdx.x & 63); }
 template <typename ID, typename OFF>
 __global__ __launch_bounds__(kBlock) void order_count_kernel(const Counting<ID, OFF> c, int64_t T, int32_t *__restrict__ counts) {
   __shared__ int red[kBlock / 64];
-  int n = __popc(c.sixteen((static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 16, T));
+  int n = __popc(c.sixteen(order_token(blockIdx.x), T));
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
@@ -359,7 +363,9 @@ __global__ __launch_bounds__(kBlock) void order_place_kernel(const Counting<ID, 
                                                              int32_t *__restrict__ count) {
   __shared__ int red[3][kBlock / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int before = 0, all = 0;
+  const int64_t t0 = order_token(blockIdx.x);
+  const uint32_t bits = c.sixteen(t0, T);
+  int mine = __popc(bits), before = 0, all = 0;
   if (counts) {
     for (unsigned b = threadIdx.x; b < gridDim.x; b += kBlock) {
       all += counts[b];
@@ -367,43 +373,38 @@ __global__ __launch_bounds__(kBlock) void order_place_kernel(const Counting<ID, 
     }
   } else {
     for (unsigned b = 0; b < gridDim.x; ++b) {
-      const int n = __popc(c.sixteen((static_cast<int64_t>(b) * kBlock + threadIdx.x) * 16, T));
+      const int n = __popc(c.sixteen(order_token(b), T));
       all += n;
       before += b < blockIdx.x ? n : 0;
     }
   }
-  const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 16;
-  const uint32_t bits = c.sixteen(t0, T);
-  int mine = __popc(bits), upto = mine;     // of the lanes up to this one
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int other = __shfl_up(upto, off, 64);
-    upto += lane >= off ? other : 0;
-  }
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) {
+    mine += __shfl_xor(mine, off, 64);
     before += __shfl_xor(before, off, 64);
     all += __shfl_xor(all, off, 64);
   }
-  if (lane == 63) red[0][wave] = upto;
   if (lane == 0) {
+    red[0][wave] = mine;
     red[1][wave] = before;
     red[2][wave] = all;
   }
   __syncthreads();
-  int at = upto - mine;
-  before = all = 0;
+  int at = 0;               // tokens that count before the wave's next 64
+  all = 0;
   for (int w = 0; w < kBlock / 64; ++w) {
-    at += w < wave ? red[0][w] : 0;
-    before += red[1][w];
+    at += red[1][w] + (w < wave ? red[0][w] : 0);
     all += red[2][w];
   }
-  at += before;             // tokens that count before this thread's
   if (blockIdx.x == 0 && threadIdx.x == 0) *count = all;
-  for (int i = 0; i < 16 && t0 + i < T; ++i) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
     const bool counts_here = bits >> i & 1;
-    row[counts_here ? at : all + (t0 + i - at)] = static_cast<int32_t>(t0 + i);
-    at += counts_here ? 1 : 0;
+    const uint64_t there = __ballot(counts_here);
+    const int64_t t = t0 + 64 * i;
+    const int here = at + __popcll(there & ((uint64_t{1} << lane) - 1));
+    if (t < T) row[counts_here ? here : all + (t - here)] = static_cast<int32_t>(t);
+    at += __popcll(there);
   }
 }
 

@@ -297,3 +297,28 @@ def test_captured_and_replayed(T):
         eager = step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, eager))
+
+
+@pytest.mark.parametrize("io", [BF, F])
+def test_many_tokens_in_an_order_of_their_own(io):
+    # more tokens than a block of threads places and than one launch counts, in few distinct rows: sums that are known
+    T, C, V = 70001, 8, 64000
+    g = _gen(20)
+    W = _normal(g, V, C, std=0.3, dtype=io)
+    h = _normal(g, 7, C, dtype=io).repeat(T // 7 + 1, 1)[:T].contiguous()
+    targets = torch.randint(0, V, (T,), device="cuda", generator=g)
+    targets = torch.where(torch.rand(T, device="cuda", generator=g) < 0.4, -1, targets)
+    offsets = torch.tensor([100, 30000, 33333, 33333, 69000], device="cuda", dtype=torch.int32)
+    loss, logp, g_h, g_W = mhcl.head_preference_grad(h, W, targets, offsets)
+    ce = mhcl.head_loss(h, W, targets)[0].double()
+    want = -torch.stack([ce[a:b].sum() for a, b in ((100, 30000), (30000, 33333), (33333, 33333), (33333, 69000))])
+    assert float((logp.double() - want).abs().max()) <= 1e-5 * float(want.abs().max())
+    m = 0.1 * (want[0::2] - want[1::2])
+    w = torch.zeros(T, device="cuda", dtype=torch.float64)
+    for i, (a, b) in enumerate(((100, 30000), (30000, 33333), (33333, 33333), (33333, 69000))):
+        w[a:b] = (0.1 if i % 2 == 0 else -0.1) * torch.sigmoid(-m[i // 2]) / 2
+    ref_h, ref_W = mhcl.head_loss_grad(h, W, targets, w.float())[2:]
+    out = (targets < 0) | (w == 0)
+    assert not g_h[out].any()
+    for a, b in ((g_h, ref_h), (g_W, ref_W)):
+        assert float((a.double() - b.double()).norm()) <= (0.006 if io is BF else 1e-4) * float(b.double().norm())
