@@ -122,8 +122,10 @@ struct TeacherLogits {
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int64_t t = n0 + 16 * j + (threadIdx.x & 15);
-      h.word[j] = t < T ? table[t * granules + g] : 0u;
+      h.word[j] = table[(t < T ? t : T - 1) * granules + g];
     }
+#pragma unroll
+    for (int j = 0; j < FN; ++j) h.word[j] = n0 + 16 * j + (threadIdx.x & 15) < T ? h.word[j] : 0u;
     return h;
   }
   template <int FM, int FN>

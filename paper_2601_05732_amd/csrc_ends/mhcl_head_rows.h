@@ -43,9 +43,11 @@ struct TargetLogit {
     Held<FN> h;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
-      const int64_t t = n0 + 16 * j + (threadIdx.x & 15);
-      h.y[j] = t < T ? static_cast<int64_t>(targets[MAPPED ? row[t] : t]) : -1;
+      const int64_t t = n0 + 16 * j + (threadIdx.x & 15), from = t < T ? t : T - 1;    // (loads under a condition would wait for each other)
+      h.y[j] = static_cast<int64_t>(targets[MAPPED ? row[from] : from]);
     }
+#pragma unroll
+    for (int j = 0; j < FN; ++j) h.y[j] = n0 + 16 * j + (threadIdx.x & 15) < T ? h.y[j] : -1;
     return h;
   }
   __device__ __forceinline__ float factor() const { return 1.f; }
