@@ -41,7 +41,7 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
     mine[i] = 0x7fffffff;
     if (k < K) {
       const int64_t id = static_cast<int64_t>(ids[from * K + k]);
-      const float v = logits[from * K + k] * inv;
+      const float v = logits[from * K + k];
       const bool there = id >= 0 && !(v == -INFINITY);
       if (there) a[i] = v;
       if (there && id < V) mine[i] = static_cast<int32_t>(id);
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       if (i * 64 < K) key[wave][i * 64 + lane] = mine[i];
-      a[i] = mine[i] == 0x7fffffff && a[i] == -INFINITY ? -INFINITY : a[i] - top;   // (NaN where the largest is no number)
+      a[i] = mine[i] == 0x7fffffff && a[i] == -INFINITY ? -INFINITY : (a[i] - top) * inv;   // (NaN where the largest is no number)
       sum += a[i] == -INFINITY ? 0.f : expf(a[i]);
     }
 #pragma unroll

@@ -70,8 +70,9 @@ def within(got, ref, bound, what):
 
 
 def distill(h, W, ids, logits, weight, tau, rows=1024):
-    """{name: (result, largest error)}; weight [T] or None.  The teacher's probabilities, of logits a / tau: 2^-22 of the largest |a / tau| and
-    2^-20 of themselves (exp, a sum of at most ten additions, a division); their logarithms as much and 2^-21 of their own."""
+    """{name: (result, largest error)}; weight [T] or None.  The teacher's probabilities, of logits a / tau: 2^-21 of the largest |a / tau| (the
+    difference from the largest one is at most twice that, and has three roundings of 2^-24: its own, the factor's, the product's) and 2^-20 of themselves (exp, a sum of at most ten additions, a division);
+    their logarithms as much and 2^-21 of their own."""
     held = (ids >= 0) & (logits > -float("inf"))
     counts = held.any(dim=1)
     w = torch.full((len(h),), 1.0 / max(1, int(counts.sum())), device=h.device, dtype=torch.float64) if weight is None else weight.double()
@@ -86,7 +87,7 @@ def distill(h, W, ids, logits, weight, tau, rows=1024):
         p = torch.softmax(a, dim=1).masked_fill(~on, 0.0)
         top = a.abs().masked_fill(~on, 0.0).amax(dim=1, keepdim=True)
         log_p = torch.where(p > 0, p, 1.0).log()
-        rel_p = 2.0 ** -22 * top + 2.0 ** -20
+        rel_p = 2.0 ** -21 * top + 2.0 ** -20
         z = L.z.gather(1, at)
         log_q = z - L.lse.unsqueeze(1)
         terms = log_p - log_q

@@ -126,6 +126,18 @@ def test_slots_without_a_number(io):
     clean = mhcl.head_distill_grad(h, W, ids, logits)
     assert all(torch.equal(a, b) for a, b in zip(got.values(), clean))
     assert not got["loss"][4:6].any() and not got["g_h"][4:6].any()
+    # the lowest numbers as a mask: of some slots, and of all, which are then alike, at any temperature
+    low = logits.clone()
+    low[7, 2:], low[8] = torch.finfo(F).min, torch.finfo(F).min
+    for tau in (1.0, 0.5):
+        loss, _, g_h, _ = mhcl.head_distill_grad(h, W, ids, low, temperature=tau)
+        few, even = low.clone(), low.clone()
+        few[7, 2:], even[8] = -math.inf, 0.0
+        want = mhcl.head_distill_grad(h, W, ids, few, temperature=tau)
+        assert abs(float(loss[7] - want[0][7])) <= 1e-6 * float(loss[7])
+        assert float((g_h[7] - want[2][7]).double().norm()) <= 0.01 * float(want[2][7].double().norm())
+        want = mhcl.head_distill_grad(h, W, ids, even, temperature=tau)
+        assert torch.equal(loss[8], want[0][8]) and torch.equal(g_h[8], want[2][8]) and torch.isfinite(loss[8])
     # mistakes: NaN, infinity, a row past the vocabulary
     logits[10, 2], logits[11, 0], ids[12, 9], ids[13, 9] = math.nan, math.inf, 200, 2 ** 40
     weight = torch.ones(90, device="cuda")
@@ -308,10 +320,10 @@ def test_under_autograd(io):
         head.distill(fwd.make_dual(h.detach(), torch.ones_like(h)), ids, logits.detach())
 
 
-@pytest.mark.parametrize("T", [40, 1300])
-def test_captured_and_replayed(T):
-    h, W, ids, logits = _inputs(17, T, 64, 700, 9, BF)
-    h2, _, ids2, logits2 = _inputs(18, T, 64, 700, 9, BF)
+@pytest.mark.parametrize("T,C,V", [(40, 64, 700), (1300, 64, 700), (2100, 2048, 33000)])
+def test_captured_and_replayed(T, C, V):
+    h, W, ids, logits = _inputs(17, T, C, V, 9, BF)
+    h2, _, ids2, logits2 = _inputs(18, T, C, V, 9, BF, holes=0.5)
 
     def step():
         return mhcl.head_distill_grad(h, W, ids, logits)
@@ -327,6 +339,8 @@ def test_captured_and_replayed(T):
     for i in range(4):
         for a, b in ((h, h2), (ids, ids2), (logits, logits2)):
             a.copy_(b if i % 2 else b.flip(0))
+        if i == 3:
+            ids[T // 4:] = -1          # far fewer tokens than when it was captured
         graph.replay()
         eager = step()
         torch.cuda.synchronize()

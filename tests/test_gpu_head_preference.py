@@ -271,10 +271,10 @@ def test_under_autograd(io):
         head.prefer(h, targets, offsets, reference.requires_grad_())
 
 
-@pytest.mark.parametrize("T", [40, 1300])
-def test_captured_and_replayed(T):
-    h, W, targets, offsets, reference = _inputs(13, T, 64, 700, 3, BF)
-    h2, _, targets2, offsets2, reference2 = _inputs(14, T, 64, 700, 3, BF)
+@pytest.mark.parametrize("T,C,V", [(40, 64, 700), (1300, 64, 700), (2100, 520, 33000)])
+def test_captured_and_replayed(T, C, V):
+    h, W, targets, offsets, reference = _inputs(13, T, C, V, 3, BF)
+    h2, _, targets2, offsets2, reference2 = _inputs(14, T, C, V, 3, BF)
 
     def step():
         return mhcl.head_preference_grad(h, W, targets, offsets, reference)
@@ -293,6 +293,8 @@ def test_captured_and_replayed(T):
         if i == 2:
             offsets.copy_(offsets2)
             reference.copy_(reference2)
+        if i == 3:
+            targets[T // 4:] = -1          # far fewer tokens than when it was captured
         graph.replay()
         eager = step()
         torch.cuda.synchronize()
