@@ -1,5 +1,6 @@
 """The two ends of a language model around a stack of hyper-connection layers: token embedding into the streams, the norm of
-the streams' sum, and the head's softmax cross entropy, each with its gradients.
+the streams' sum, and the head's softmax cross entropy, each with its gradients; and what the head learns from besides next tokens, a teacher's
+likeliest ones and pairs of sequences.
 
 The functions here allocate the results and make one call into ``libmhcl.so`` (``mhcl_embed`` and so on; include/mhcl.h has
 the formulas), which computes everything.  Tensors may be strided or at any address: what the library cannot read as it is
