@@ -35,14 +35,23 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
   float a[PER], top = -INFINITY, sum = 0.f;
   int32_t mine[PER];
   int held = 0, past = 0;
+  ID given[PER];
+  float value[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {      // (a load under a lane's condition would wait for the one before)
+    if (i * 64 >= K) break;
+    const int k = i * 64 + lane < K ? i * 64 + lane : 0;
+    given[i] = ids[from * K + k];
+    value[i] = logits[from * K + k];
+  }
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int k = i * 64 + lane;
     a[i] = -INFINITY;
     mine[i] = 0x7fffffff;
     if (k < K) {
-      const int64_t id = static_cast<int64_t>(ids[from * K + k]);
-      const float v = logits[from * K + k];
+      const int64_t id = static_cast<int64_t>(given[i]);
+      const float v = value[i];
       const bool there = id >= 0 && !(v == -INFINITY);
       if (there) a[i] = v;
       if (there && id < V) mine[i] = static_cast<int32_t>(id);

@@ -244,7 +244,7 @@ __device__ __forceinline__ float rows_max(float v, float *red) {
 }
 
 // a row's maximum (0 where there is none) and the sum of exp(z - that) from its granules; the first ones of a lane stay in registers from the one to the
-// other (us, 50257 rows in granules of 128, 8192 tokens a wave each: read twice 10.7, so 9.4)
+// other (us, 50257 rows in granules of 128, 8192 tokens a wave each, with 32 slots: read twice 11.5, so 8.3)
 constexpr int64_t kWaveGranules = 512;     // that a wave holds
 template <int WAVES>
 __device__ __forceinline__ void join_granules(const float2 *stat, int64_t granules, float (*red)[16], float &base, float &sum) {
@@ -253,9 +253,9 @@ __device__ __forceinline__ void join_granules(const float2 *stat, int64_t granul
   float2 held[HELD];
   float top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < HELD; ++i) held[i] = tid + i * STRIDE < granules ? stat[tid + i * STRIDE] : make_float2(-INFINITY, 0.f);
+  for (int i = 0; i < HELD; ++i) held[i] = stat[tid + i * STRIDE < granules ? tid + i * STRIDE : granules - 1];   // (again: not under a condition)
 #pragma unroll
-  for (int i = 0; i < HELD; ++i) top = fmaxf(top, held[i].x);
+  for (int i = 0; i < HELD; ++i) top = fmaxf(top, held[i].x);      // (the last one's once more is no other maximum)
   for (int64_t p = tid + HELD * STRIDE; p < granules; p += STRIDE) top = fmaxf(top, stat[p].x);
   top = rows_max<WAVES>(top, red[0]);
   base = top == -INFINITY ? 0.f : top;
