@@ -283,7 +283,8 @@ __device__ __forceinline__ float weight_over_common(const RowArgs &a, const ID *
 // The row's numerators turned into scale exp(z - base) in their place, `replace(v, g)` having the last word on the eight from v on; zeros, and zeros
 // for h's row, where the token does not count.  bf16: g is of the operands' type, which is what the matrix units multiply with W and h.  (Its
 // rounding is the one of the T V terms of a sum each, the gradient's own comes after it: off from 64 bits by 0.0023 of the 2-norm at 333 tokens and
-// 0.0018 at 16384, where the gradient's rounding alone is 0.0017.  Two bf16 parts of g instead would make each of the two products two: 13 ms
+// 0.0018 at 16384, where the gradient's rounding alone is 0.0017.  Where few entries outweigh the rest their roundings do not
+// average, and the sum may be as far off as one of them, 2^-8.  Two bf16 parts of g instead would make each of the two products two: 13 ms
 // more on 21 at 16384 tokens, C = 4096, 65536 rows.)
 template <typename IO, typename F>
 __device__ __forceinline__ void turn_row(const RowArgs &a, int64_t t, const float2 *stat, float base, float scale, bool counts, F &&replace) {
