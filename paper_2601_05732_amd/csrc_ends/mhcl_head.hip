@@ -91,35 +91,50 @@ __global__ __launch_bounds__(1024) void total_kernel(const ID *__restrict__ targ
   }
 }
 
+// Whether a pair's three offsets ascend within 0 .. T, which the host cannot see
+template <typename OFF>
+__device__ __forceinline__ bool ascends(const OFF *__restrict__ offsets, int64_t p, int64_t T) {
+  const int64_t o[3] = {static_cast<int64_t>(offsets[2 * p]), static_cast<int64_t>(offsets[2 * p + 1]), static_cast<int64_t>(offsets[2 * p + 2])};
+  return o[0] >= 0 && o[0] <= o[1] && o[1] <= o[2] && o[2] <= T;
+}
+
 // Pairs of sequences, a block each: L = the sum of the tokens' -ce from one offset to the next, in fp64,
 //   m = beta ((L_c - R_c) - (L_r - R_r)),  loss = (1 - s) softplus(-m) + s softplus(m)
 // and the factor of each token's cross entropy in the weighted sum of the pairs, -+ beta weight dloss/dm for the chosen and the rejected sequence's,
 // 0 outside of the sequences.  (loss, weights of tokens: few numbers, in fp64 until they are rounded.)  16 pairs of 8192 tokens 5.7 us, 2 of 300 3.6: a
 // launch and two dependent reads.
+// A token's weight is written by one block whatever the offsets are.  Those of pairs that ascend are taken as they are, so that a mistake stays in its pair;
+// E, the furthest end of the ascending pairs before, is where their tokens end.  A pair writes from there on; it is a mistake as well where it begins
+// before, and one that does not ascend writes nothing.  (Where all offsets ascend E is the pair's first one, and 0 for the first pair.)
 constexpr int kPairThreads = 512;
 template <typename OFF>
 __global__ __launch_bounds__(kPairThreads) void pair_kernel(const PairArgs a, const OFF *__restrict__ offsets) {
   __shared__ double red[2][kPairThreads / 64];
+  __shared__ int32_t ends[kPairThreads / 64];
   __shared__ float factor;
   const int64_t p = blockIdx.x;
-  int64_t from[3];
-  bool bad = false;        // offsets that descend or lie outside of the tokens: what the host cannot see
-  for (int i = 0; i < 3; ++i) {
-    const int64_t o = static_cast<int64_t>(offsets[2 * p + i]);
-    const int64_t least = i > 0 ? from[i - 1] : 0;
-    bad |= o < least || o > a.T;
-    from[i] = o < least ? least : (o > a.T ? a.T : o);
-  }
+  const int64_t from[3] = {static_cast<int64_t>(offsets[2 * p]), static_cast<int64_t>(offsets[2 * p + 1]), static_cast<int64_t>(offsets[2 * p + 2])};
+  const bool right = ascends(offsets, p, a.T);
+  const auto weighs = [&](int64_t i) { return !(a.weight && a.weight[i] == 0.f); };
+  int32_t end = 0;          // E: a pair for each thread, or what pair_ends_kernel left
+  if (a.pairs > kPairThreads) end = __float_as_int(a.loss[p]);
+  else if (threadIdx.x < p && ascends(offsets, threadIdx.x, a.T)) end = static_cast<int32_t>(offsets[2 * threadIdx.x + 2]);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) end = max(end, __shfl_xor(end, off, 64));
+  if ((threadIdx.x & 63) == 0) ends[threadIdx.x >> 6] = end;
   double sum[2] = {0., 0.};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    for (int64_t t = from[i] + threadIdx.x; t < from[i + 1]; t += kPairThreads) sum[i] -= static_cast<double>(a.ce[t]);
+    for (int64_t t = from[i] + threadIdx.x; right && t < from[i + 1]; t += kPairThreads) sum[i] -= static_cast<double>(a.ce[t]);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum[i] += __shfl_xor(sum[i], off, 64);
     if ((threadIdx.x & 63) == 0) red[i][threadIdx.x >> 6] = sum[i];
   }
   __syncthreads();
+  for (int w = 0; w < kPairThreads / 64; ++w) end = max(end, ends[w]);
+  const int64_t before = end;
   if (threadIdx.x == 0) {
+    const bool bad = !right || (from[0] < before && from[0] < from[2]);
     double L[2] = {0., 0.}, ratio[2];
     for (int i = 0; i < 2; ++i) {
       for (int w = 0; w < kPairThreads / 64; ++w) L[i] += red[i][w];
@@ -136,9 +151,41 @@ __global__ __launch_bounds__(kPairThreads) void pair_kernel(const PairArgs a, co
   }
   if (!a.token_weight) return;
   __syncthreads();
-  const int64_t first = p == 0 ? 0 : from[0], last = p == a.pairs - 1 ? a.T : from[2];
-  for (int64_t t = first + threadIdx.x; t < last; t += kPairThreads)
-    a.token_weight[t] = t < from[0] || t >= from[2] ? 0.f : (t < from[1] ? factor : -factor);
+  // tokens that no pair's offsets claim any more: NaN where the pair that should have is a mistake that counts
+  const float nan = __uint_as_float(0x7fc00000u);
+  if (right) {
+    const float gap = p > 0 && !ascends(offsets, p - 1, a.T) && weighs(p - 1) ? nan : 0.f;
+    for (int64_t t = before + threadIdx.x; t < from[2]; t += kPairThreads) a.token_weight[t] = t < from[0] ? gap : (t < from[1] ? factor : -factor);
+  }
+  if (p == a.pairs - 1) {
+    const float rest = !right && weighs(p) ? nan : 0.f;
+    for (int64_t t = (right && from[2] > before ? from[2] : before) + threadIdx.x; t < a.T; t += kPairThreads) a.token_weight[t] = rest;
+  }
+}
+
+// E of more pairs than a block of those has threads, left in the bits of `loss` until they replace it: a thread for every so many pairs in a row
+template <typename OFF>
+__global__ __launch_bounds__(1024) void pair_ends_kernel(const PairArgs a, const OFF *__restrict__ offsets) {
+  __shared__ int32_t ends[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int each = (a.pairs + 1023) / 1024, first = min(static_cast<int>(threadIdx.x) * each, a.pairs), last = min(first + each, a.pairs);
+  int32_t end = 0;
+  for (int p = first; p < last; ++p)
+    if (ascends(offsets, p, a.T)) end = max(end, static_cast<int32_t>(offsets[2 * static_cast<int64_t>(p) + 2]));
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int32_t other = __shfl_up(end, off, 64);
+    end = lane >= off ? max(end, other) : end;
+  }
+  if (lane == 63) ends[wave] = end;
+  end = __shfl_up(end, 1, 64);
+  if (lane == 0) end = 0;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) end = max(end, ends[w]);
+  for (int p = first; p < last; ++p) {
+    a.loss[p] = __int_as_float(end);
+    if (ascends(offsets, p, a.T)) end = max(end, static_cast<int32_t>(offsets[2 * static_cast<int64_t>(p) + 2]));
+  }
 }
 
 template <typename IO>
@@ -279,6 +326,11 @@ hipError_t launch_pairs(const PairArgs &a, const void *offsets, int offset_dtype
   if (a.pairs == 0) return a.token_weight ? launch_zero(a.token_weight, static_cast<size_t>(a.T) * 4, s) : hipSuccess;
   return dispatch_id(offset_dtype, [&](auto id) {
     using OFF = decltype(id);
+    if (a.pairs > kPairThreads) {
+      hipLaunchKernelGGL((pair_ends_kernel<OFF>), dim3(1), dim3(1024), 0, s, a, static_cast<const OFF *>(offsets));
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
     hipLaunchKernelGGL((pair_kernel<OFF>), dim3(static_cast<unsigned>(a.pairs)), dim3(kPairThreads), 0, s, a, static_cast<const OFF *>(offsets));
     return hipGetLastError();
   });

@@ -157,6 +157,82 @@ def test_mistakes_are_loud_and_stay_in_their_pair(io):
         weight[pair] = 1
 
 
+# offsets [9] of 4 pairs of 120 tokens, and which pairs are mistakes
+OUT_OF_ORDER = [
+    ([0, 50, 30, 40, 60, 80, 90, 100, 120], [0]),           # pair 1 begins before the middle of pair 0
+    ([70, 10, 20, 30, 40, 80, 90, 100, 120], [0]),          # the first one lies inside a later pair
+    ([0, 20, 40, 50, 60, 80, 90, 100, 30], [3]),            # the last one before earlier pairs' ends
+    ([0, 20, 40, 50, 60, 80, 90, 100, 0], [3]),
+    ([5, 20, 40, 50, 60, 80, 90, 100, -5], [3]),
+    ([0, 20, 40, 35, 30, 50, 80, 100, 120], [1, 2]),        # pair 2 begins before the end of pair 0
+    ([0, 20, 40, 35, 30, 30, 30, 100, 120], [1, 3]),        # pair 2 is empty, and pair 3 begins there
+    ([10, 20, 40, 200, 50, 70, 60, 100, 115], [1, 2]),
+    ([-9, 20, 2 ** 33, 50, 60, 80, -2 ** 40, 7, 2 ** 62], [0, 1, 2, 3]),
+]
+
+
+@pytest.mark.parametrize("io", [BF, F])
+@pytest.mark.parametrize("offsets,bad", OUT_OF_ORDER)
+def test_offsets_out_of_order_leave_the_other_pairs_alone(io, offsets, bad):
+    _out_of_order(*_inputs(15, 120, 64, 200, 4, io, holes=0.2), offsets, bad)
+
+
+def _out_of_order(h, W, targets, _, reference, offsets, bad):
+    good = [p for p in range(4) if p not in bad]
+    # the same pairs by themselves, where there is a gap before them one of weight 0
+    held, clean, at = [], [0], 0
+    for p in good:
+        empty = offsets[2 * p] == offsets[2 * p + 2]       # (wherever it lies)
+        if offsets[2 * p] != at and not empty:
+            clean += [at, offsets[2 * p]]
+            held.append(None)
+        held.append(p)
+        clean += [at, at] if empty else offsets[2 * p + 1:2 * p + 3]
+        at = clean[-1]
+    where = [held.index(p) for p in good]
+    rows = torch.zeros(len(h), dtype=torch.bool, device="cuda")
+    for p in good:
+        rows[offsets[2 * p]:offsets[2 * p + 2]] = True
+
+    def of(values, empty):
+        return torch.tensor([empty if p is None else values[p] for p in held], device="cuda", dtype=F)
+
+    halves = reference.view(4, 2)
+    weight = [0.3 + p for p in range(4)]
+    own = [torch.stack([of(halves[:, i].tolist(), 0.0) for i in range(2)], dim=1).view(-1), of(weight, 0.0)]
+    want = mhcl.head_preference_grad(h, W, targets, torch.tensor(clean, device="cuda"), *own, smoothing=0.1)
+    refs = ref.preference(h, W, targets, torch.tensor(clean, device="cuda"), *own, 0.1, 0.1)
+    for name, value in zip(("loss", "logp", "g_h", "g_W"), want):
+        ref.within(value, *refs[name], name)
+    o = torch.tensor(offsets, device="cuda")
+    for on in (0.0, 1.0):
+        w = torch.tensor([on if p in bad else weight[p] for p in range(4)], device="cuda")
+        loss, logp, g_h, g_W = got = mhcl.head_preference_grad(h, W, targets, o, reference, w, smoothing=0.1)
+        assert torch.isnan(loss[bad]).all() and torch.isnan(logp.view(4, 2)[bad]).all()
+        assert torch.equal(loss[good], want[0][where]) and torch.equal(logp.view(4, 2)[good], want[1].view(-1, 2)[where])
+        assert torch.equal(g_h[rows], want[2][rows])
+        if on == 0:
+            assert torch.equal(g_h, want[2]) and torch.equal(g_W, want[3])
+        alone = mhcl.head_preference(h, W, targets, o, reference, smoothing=0.1)
+        for a, b in zip((*got, *alone), (*mhcl.head_preference_grad(h, W, targets, o, reference, w, smoothing=0.1), loss, logp)):
+            assert torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0)) and torch.equal(a.isnan(), b.isnan())
+
+
+def test_many_pairs_with_one_out_of_order():
+    # more pairs than a block has threads, and than a thread has of them
+    for pairs in (513, 1500):
+        h, W, targets, offsets, reference = _inputs(16, 2000, 72, 90, pairs, F, lead=3, tail=5)
+        weight = torch.rand(pairs, device="cuda", generator=_gen(5))
+        weight[pairs // 2] = 0.0
+        want = _check(h, W, targets, offsets, reference, weight)
+        broken = offsets.clone()
+        broken[2 * (pairs // 2) + 1] = 1999        # its middle behind its end
+        loss, logp, g_h, g_W = mhcl.head_preference_grad(h, W, targets, broken, reference, weight)
+        assert torch.isnan(loss[pairs // 2]) and torch.equal(g_h, want["g_h"]) and torch.equal(g_W, want["g_W"])
+        rest = torch.arange(pairs, device="cuda") != pairs // 2
+        assert torch.equal(loss[rest], want["loss"][rest]) and torch.equal(logp.view(-1, 2)[rest], want["logp"].view(-1, 2)[rest])
+
+
 def test_large_margins():
     h, W, targets, offsets, reference = _inputs(7, 400, 64, 300, 4, F)
     reference += torch.tensor([1e4, 0, 0, 1e4, -3e4, 0, 0, -3e4], device="cuda")
