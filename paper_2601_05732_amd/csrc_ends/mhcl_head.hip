@@ -91,13 +91,6 @@ __global__ __launch_bounds__(1024) void total_kernel(const ID *__restrict__ targ
   }
 }
 
-// Whether a pair's three offsets ascend within 0 .. T, which the host cannot see
-template <typename OFF>
-__device__ __forceinline__ bool ascends(const OFF *__restrict__ offsets, int64_t p, int64_t T) {
-  const int64_t o[3] = {static_cast<int64_t>(offsets[2 * p]), static_cast<int64_t>(offsets[2 * p + 1]), static_cast<int64_t>(offsets[2 * p + 2])};
-  return o[0] >= 0 && o[0] <= o[1] && o[1] <= o[2] && o[2] <= T;
-}
-
 // Pairs of sequences, a block each: L = the sum of the tokens' -ce from one offset to the next, in fp64,
 //   m = beta ((L_c - R_c) - (L_r - R_r)),  loss = (1 - s) softplus(-m) + s softplus(m)
 // and the factor of each token's cross entropy in the weighted sum of the pairs, -+ beta weight dloss/dm for the chosen and the rejected sequence's,
@@ -362,7 +355,7 @@ hipError_t launch_preference(const mhcl_ends_desc &d, const void *h, const void 
       using IO = decltype(io);
       const ID *y = static_cast<const ID *>(targets);
       hipError_t e;
-      if (w.ordered && (e = launch_order(y, offsets, offset_dtype, 2 * static_cast<int64_t>(a.pairs), d.T, w.order, s)) != hipSuccess) return e;
+      if (w.ordered && (e = launch_order(y, offsets, offset_dtype, a.pairs, d.T, w.order, s)) != hipSuccess) return e;
       const auto run = [&](auto &way, void *to_h, void *to_W, bool floats) {
         return w.ordered ? run_head<IO, true>(d, h, W, way, w.ce, w.lse, to_h, to_W, floats, w.head, s)
                          : run_head<IO, false>(d, h, W, way, w.ce, w.lse, to_h, to_W, floats, w.head, s);

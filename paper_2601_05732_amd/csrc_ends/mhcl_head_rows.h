@@ -339,25 +339,52 @@ hipError_t dispatch_id(int id_dtype, F &&f) {
   return f(int32_t{});
 }
 
+// Whether a pair's three offsets ascend within 0 .. T, which the host cannot see
+template <typename OFF>
+__device__ __forceinline__ bool ascends(const OFF *__restrict__ offsets, int64_t p, int64_t T) {
+  const int64_t o[3] = {static_cast<int64_t>(offsets[2 * p]), static_cast<int64_t>(offsets[2 * p + 1]), static_cast<int64_t>(offsets[2 * p + 2])};
+  return o[0] >= 0 && o[0] <= o[1] && o[1] <= o[2] && o[2] <= T;
+}
+
 // ---------------------------------------------------------------- order of the tokens
 // Tokens that count first, each kind in the caller's order: of kOrderTokens of them by a block of threads, which counts its own, and then, knowing
 // those of the blocks before, places them; a wave has 16 times 64.  A token counts where its target is not negative and (offsets) it lies from the first
-// offset to the last.
+// offset to the last, if all of them ascend within 0 .. T: where they do not, the ends say nothing about the pairs between them.
 constexpr int kOrderTokens = kBlock * 16;
 template <typename ID, typename OFF>
 struct Counting {
   const ID *targets;
   const OFF *offsets;       // null: all tokens
-  int64_t last;             // of the offsets
-  // a bit each for the lane's tokens t0 + 64 i
+  int64_t pairs;
+  struct Range {
+    int64_t from, to;
+  };
+  // by a block of threads
+  __device__ __forceinline__ Range range(int64_t T) const {
+    if (!offsets) return {0, T};
+    if (pairs == 0) return {0, 0};
+    __shared__ int red[kBlock / 64];
+    bool wrong = false;
+    for (int64_t p = threadIdx.x; p < pairs; p += kBlock) wrong |= !ascends(offsets, p, T);
+    const bool any = __ballot(wrong) != 0;
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = any ? 1 : 0;
+    const int64_t from = static_cast<int64_t>(offsets[0]), to = static_cast<int64_t>(offsets[2 * pairs]);
+    __syncthreads();
+    return red[0] + red[1] + red[2] + red[3] == 0 ? Range{from, to} : Range{0, T};
+  }
+  // a bit each for the lane's tokens t0 + 64 i whose targets are not negative, and those of them in a range
   __device__ __forceinline__ uint32_t sixteen(int64_t t0, int64_t T) const {
-    const int64_t from = offsets ? static_cast<int64_t>(offsets[0]) : 0, to = offsets ? static_cast<int64_t>(offsets[last]) : T;
     ID y[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = targets[t0 + 64 * i < T ? t0 + 64 * i : T - 1];     // (a load under a condition would wait for the one before)
     uint32_t bits = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) bits |= t0 + 64 * i < T && t0 + 64 * i >= from && t0 + 64 * i < to && y[i] >= 0 ? 1u << i : 0u;
+    for (int i = 0; i < 16; ++i) bits |= t0 + 64 * i < T && y[i] >= 0 ? 1u << i : 0u;
+    return bits;
+  }
+  __device__ __forceinline__ uint32_t within(uint32_t bits, int64_t t0, Range r) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) bits &= t0 + 64 * i >= r.from && t0 + 64 * i < r.to ? ~0u : ~(1u << i);
     return bits;
   }
 };
@@ -365,7 +392,9 @@ __device__ __forceinline__ int64_t order_token(int64_t block) { return block * k
 template <typename ID, typename OFF>
 __global__ __launch_bounds__(kBlock) void order_count_kernel(const Counting<ID, OFF> c, int64_t T, int32_t *__restrict__ counts) {
   __shared__ int red[kBlock / 64];
-  int n = __popc(c.sixteen(order_token(blockIdx.x), T));
+  const int64_t t0 = order_token(blockIdx.x);
+  const uint32_t bits = c.sixteen(t0, T);
+  int n = __popc(c.within(bits, t0, c.range(T)));
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
@@ -379,7 +408,9 @@ __global__ __launch_bounds__(kBlock) void order_place_kernel(const Counting<ID, 
   __shared__ int red[3][kBlock / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t t0 = order_token(blockIdx.x);
-  const uint32_t bits = c.sixteen(t0, T);
+  uint32_t bits = c.sixteen(t0, T);
+  const auto range = c.range(T);
+  bits = c.within(bits, t0, range);
   int mine = __popc(bits), before = 0, all = 0;
   if (counts) {
     for (unsigned b = threadIdx.x; b < gridDim.x; b += kBlock) {
@@ -388,7 +419,7 @@ __global__ __launch_bounds__(kBlock) void order_place_kernel(const Counting<ID, 
     }
   } else {
     for (unsigned b = 0; b < gridDim.x; ++b) {
-      const int n = __popc(c.sixteen(order_token(b), T));
+      const int n = __popc(c.within(c.sixteen(order_token(b), T), order_token(b), range));
       all += n;
       before += b < blockIdx.x ? n : 0;
     }
@@ -442,10 +473,10 @@ __global__ __launch_bounds__(kBlock) void gather_kernel(const void *__restrict__
 }
 
 template <typename ID>
-hipError_t launch_order(const ID *targets, const void *offsets, int offset_dtype, int64_t last, int64_t T, const TokenOrder &o, hipStream_t s) {
+hipError_t launch_order(const ID *targets, const void *offsets, int offset_dtype, int64_t pairs, int64_t T, const TokenOrder &o, hipStream_t s) {
   return dispatch_id(offset_dtype, [&](auto off) {
     using OFF = decltype(off);
-    const Counting<ID, OFF> c{targets, static_cast<const OFF *>(offsets), last};
+    const Counting<ID, OFF> c{targets, static_cast<const OFF *>(offsets), pairs};
     const dim3 grid(blocks(T, kOrderTokens));
     const bool apart = grid.x > 16;      // (a launch of its own costs more than counting 65536 tokens sixteen times)
     if (apart) {
