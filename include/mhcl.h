@@ -414,8 +414,9 @@ int mhcl_head_distill(const mhcl_ends_desc *desc, int32_t K, float temperature, 
  * and, where g_h and g_W are given, the gradients of sum_p weight[p] loss[p] on h and W (weight NULL: of the mean over the pairs).
  * Log probabilities of tokens are fp32, their sums and all of a pair fp64, rounded to fp32 at the end.  Tokens outside of the sequences, and those
  * without a target, add nothing; their g_h is 0, and large products leave them out.  Offsets ascend from 0 or more to T or less.  A pair whose own three
- * do not, which the host cannot see, or that begins before the end of an earlier pair whose own do, is a mistake: its loss and logp are NaN (and
- * gradients unless its weight is 0), the other pairs' are what they are without it, and nothing is read or written out of bounds for it.
+ * do not, which the host cannot see, or that begins before the end of an earlier pair whose own do, is a mistake: its loss and logp are NaN, the
+ * other pairs' are what they are without it, and nothing is read or written out of bounds for it.  A pair whose loss is NaN, of whatever cause, makes
+ * all of g_W NaN (where there are tokens) and g_h of the tokens that are its alone, unless its weight is 0.
  * Past one block of tokens (MHCL_HEAD_BLOCK_BYTES) the logits are formed twice for gradients, since a pair's weight needs all of its tokens.
  * total, g_h, g_W, unrounded: as in mhcl_head_distill.  pairs: 0 .. 2^22; beta finite; smoothing 0 .. 1.
  * in : h [T,C] io, W [V,C] io, targets [T], offsets [2 pairs + 1] of offset_dtype, reference [2 pairs] f32 or NULL (zeros), weight [pairs] f32 or NULL

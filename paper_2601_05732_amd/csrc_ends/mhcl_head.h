@@ -24,7 +24,7 @@ struct HeadWs {
   char *E;              // [tokens][ld] numerators in 16 bits, then g in bf16 in their place; fp32: 32 bits each
   float2 *stat;         // [tokens][granules] maximum and sum
   float *zt;            // [tokens] the targets' logits
-  float *common;        // [1] what all weights are multiples of
+  float *common;        // [2] what all weights are multiples of, in g_h and in g_W
   float *slabs;         // [gh_splits][tokens][C]
   float *gw_slabs;      // [gw_splits][V][C]
   float *gW;            // [V][C] sums over blocks of tokens

@@ -273,7 +273,7 @@ HeadWs::HeadWs(const mhcl_ends_desc &d, bool grad, void *ws, bool ordered) : pla
   E = grad ? c.take<char>(T * static_cast<size_t>(plan.ld) * es) : nullptr;
   stat = c.take<float2>(T * static_cast<size_t>(plan.granules));
   zt = c.take<float>(T);
-  common = c.take<float>(1);
+  common = c.take<float>(2);
   slabs = plan.gh_splits > 1 ? c.take<float>(static_cast<size_t>(plan.gh_splits) * T * C) : nullptr;
   gw_slabs = plan.gw_splits > 1 ? c.take<float>(static_cast<size_t>(plan.gw_splits) * V * C) : nullptr;
   gW = grad && !plan.wide && plan.tokens < d.T ? c.take<float>(V * C) : nullptr;
@@ -290,11 +290,12 @@ struct CrossEntropy {
   const HeadWs &w;
   hipStream_t s;
   TokenOrder order = {};
-  bool pairs = false;
+  const PairArgs *pairs = nullptr;
   static constexpr float factor = 1.f;
   static constexpr bool kLeavesOut = true;    // (taken in an order for the pairs alone, who read nothing of a token that does not count)
   hipError_t before(int64_t, int64_t) { return hipSuccess; }
   hipError_t between(const RowArgs &) { return hipSuccess; }
+  PairLosses losses() const { return pairs ? PairLosses{pairs->loss, pairs->weight, pairs->pairs} : PairLosses{}; }
   template <bool ORDERED>
   TargetLogit<ID, ORDERED> wanted(int64_t t0) const {
     return {marks + (ORDERED ? 0 : t0), w.zt, ORDERED ? order.row + t0 : nullptr};
@@ -332,12 +333,11 @@ hipError_t launch_pairs(const PairArgs &a, const void *offsets, int offset_dtype
 // The cross entropy whose weights come of it: where all tokens are one block, their losses and the pairs' are taken between the logits and the rows
 template <typename ID>
 struct PairedCrossEntropy : CrossEntropy<ID> {
-  const PairArgs &pairs;
   const void *offsets;
   int offset_dtype;
   hipError_t between(const RowArgs &a) {
     const hipError_t e = this->loss(a, 0);
-    return e != hipSuccess ? e : launch_pairs(pairs, offsets, offset_dtype, this->s);
+    return e != hipSuccess ? e : launch_pairs(*this->pairs, offsets, offset_dtype, this->s);
   }
 };
 
@@ -361,11 +361,11 @@ hipError_t launch_preference(const mhcl_ends_desc &d, const void *h, const void 
                          : run_head<IO, false>(d, h, W, way, w.ce, w.lse, to_h, to_W, floats, w.head, s);
       };
       if (grad && w.head.plan.tokens == d.T) {
-        PairedCrossEntropy<ID> way{{y, w.token_weight, w.head, s, w.order, true}, a, offsets, offset_dtype};
+        PairedCrossEntropy<ID> way{{y, w.token_weight, w.head, s, w.order, &a}, offsets, offset_dtype};
         return run(way, g_h, g_W, unrounded);
       }
       // several blocks of tokens: a pair's weight needs all of its tokens, so that their logits are formed twice
-      CrossEntropy<ID> way{y, nullptr, w.head, s, w.order, true};
+      CrossEntropy<ID> way{y, nullptr, w.head, s, w.order, &a};
       if ((e = run(way, nullptr, nullptr, false)) != hipSuccess) return e;
       if ((e = launch_pairs(a, offsets, offset_dtype, s)) != hipSuccess || !grad) return e;
       way.weight = w.token_weight;

@@ -191,11 +191,33 @@ __device__ __forceinline__ float common_weight(const ID *__restrict__ targets, c
 // Up to so many tokens the rows' kernel takes it itself: each of its blocks, or the first alone where only the products need it.  (us,
 // 333 tokens, C = 520, 1003 rows, bf16, weights, the whole call with a launch for it / without: 31.0 / 29.5.)
 constexpr int64_t kCommonTokens = 1024;
+
+// Losses of pairs and their weights.  Where one is NaN all of g_W is, unless its weight is 0: by way of g_W's common weight, since a pair whose
+// offsets are a mistake may have no token to be NaN in.
+struct PairLosses {
+  const float *loss, *weight;
+  int32_t count;
+  template <int THREADS>
+  __device__ __forceinline__ float times(float common) const {
+    if (count == 0) return common;
+    __shared__ int red[THREADS / 64];
+    bool lost = false;
+    for (int p = threadIdx.x; p < count; p += THREADS) lost |= isnan(loss[p]) && !(weight && weight[p] == 0.f);
+    const bool any = __ballot(lost) != 0;
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = any ? 1 : 0;
+    __syncthreads();
+    for (int w = 0; w < THREADS / 64; ++w) common = red[w] ? __uint_as_float(0x7fc00000u) : common;
+    return common;
+  }
+};
 template <typename ID>
 __global__ __launch_bounds__(1024) void common_weight_kernel(const ID *__restrict__ targets, const float *__restrict__ weight, int64_t T,
-                                                             float factor, float *__restrict__ common) {
-  const float c = common_weight<1024>(targets, weight, T);
-  if (threadIdx.x == 0) *common = c * factor;
+                                                             float factor, const PairLosses pairs, float *__restrict__ common) {
+  const float c = common_weight<1024>(targets, weight, T) * factor, of_W = pairs.times<1024>(c);
+  if (threadIdx.x == 0) {
+    common[0] = c;
+    common[1] = of_W;
+  }
 }
 
 struct RowArgs {
@@ -211,6 +233,7 @@ struct RowArgs {
   int C, gran_log2;
   float factor;         // of all weights
   bool take_common;     // row kernels: T is all tokens, and `common` is not there yet
+  PairLosses pairs;
   // Tokens in an order of their own: token t is the caller's row[t], h's rows lie in hp already, and those past the count have no gradient (null: none of
   // this)
   const int32_t *row;
@@ -273,7 +296,13 @@ __device__ __forceinline__ float weight_over_common(const RowArgs &a, const ID *
   float common = 1.f;
   if (a.take_common) {
     if (a.weight || t == 0) common = common_weight<kBlock>(targets, a.weight, a.T) * a.factor;
-    if (t == 0 && threadIdx.x == 0) *a.common = common;
+    if (t == 0) {
+      const float of_W = a.pairs.times<kBlock>(common);
+      if (threadIdx.x == 0) {
+        a.common[0] = common;
+        a.common[1] = of_W;
+      }
+    }
   } else if (a.weight) {
     common = *a.common;
   }
@@ -495,6 +524,7 @@ hipError_t launch_order(const ID *targets, const void *offsets, int offset_dtype
 //   loss(a, t0), rows(a, t0) the launches that form the losses of a block; and besides turn its numerators into gradients on the logits
 //   between(a)               what the first block needs between its logits and its rows
 //   marks, weight            ([all tokens]: negative where a token does not count) and its `factor`
+//   losses()                 of pairs, if its weights come of them
 // ORDERED: the tokens are taken in way.order's order, and those that do not count are left out of the gradients' products, and (way.kLeavesOut) of the
 // logits'.  (us, without / with: 8192 tokens, of which 5700 count, C = 4096, 65536 rows,
 // pairs 10230 / 7840, their loss alone 3194 / 2367, distillation 10255 / 8692; all 8192 count 10560 / 10730.)
@@ -518,7 +548,7 @@ hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, Way &
     const void *hb = ORDERED ? way.order.hp : static_cast<const char *>(h) + t0 * C * es;
     const Operand Wk{W, C, V, C}, hk{hb, C, T, C};
     const RowArgs a{hb, way.weight ? way.weight + shift : nullptr, w.common, w.stat, w.zt, loss + shift, lse + shift, w.E, way.order.hp ? way.order.hp : w.hp,
-                    T, p.ld, p.granules, d.V, d.C, gran_log2, way.factor, take_common, row, tokens};
+                    T, p.ld, p.granules, d.V, d.C, gran_log2, way.factor, take_common, way.losses(), row, tokens};
     if constexpr (ORDERED) {
       hipLaunchKernelGGL((gather_kernel<IO>), dim3(blocks(T, kBlock / 64)), dim3(kBlock), 0, s, h, way.order.hp, T, d.C, row, tokens, !Way::kLeavesOut,
                          g_h, static_cast<int>(C * (floats ? 4 : 2) / 16), Way::kLeavesOut ? loss : nullptr);
@@ -542,7 +572,7 @@ hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, Way &
       if ((e = way.between(a)) != hipSuccess) return e;
       if (!take_common) {
         using ID = std::remove_cv_t<std::remove_pointer_t<decltype(way.marks)>>;
-        hipLaunchKernelGGL((common_weight_kernel<ID>), dim3(1), dim3(1024), 0, s, way.marks, way.weight, d.T, way.factor, w.common);
+        hipLaunchKernelGGL((common_weight_kernel<ID>), dim3(1), dim3(1024), 0, s, way.marks, way.weight, d.T, way.factor, way.losses(), w.common);
         if ((e = hipGetLastError()) != hipSuccess) return e;
       }
     }
@@ -564,7 +594,7 @@ hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, Way &
     }
     const Store to_gh{w.common, parts && !ORDERED ? w.slabs : (floats ? static_cast<float *>(gh_out) : nullptr), static_cast<uint16_t *>(gh_out), nullptr, C, T,
                       T * C, row, gh_tokens, false, ORDERED && parts ? w.slabs : nullptr};
-    const Store to_gw{w.common, p.gw_splits > 1 ? w.gw_slabs : (floats || t0 + T < d.T ? sums : nullptr), static_cast<uint16_t *>(g_W),
+    const Store to_gw{w.common + 1, p.gw_splits > 1 ? w.gw_slabs : (floats || t0 + T < d.T ? sums : nullptr), static_cast<uint16_t *>(g_W),
                       t0 > 0 ? sums : nullptr, C, V, V * C, nullptr, tokens, true, nullptr};
     if (p.pair) {
       const GemmArgs gh = gemm_args(p.gh, Wm, gk, C, T, p.gh_splits, gh_tokens), gw = gemm_args(p.gw, hm, gm, C, V, p.gw_splits, tokens, true);

@@ -220,12 +220,27 @@ def _out_of_order(h, W, targets, _, reference, offsets, bad, same_bits=True):
         there = rows if on else slice(None)
         ref.within(g_h[there], *(t[there] for t in refs["g_h"]), "g_h")
         assert not same_bits or torch.equal(g_h[there], want[2][there])
+        assert on == 0 or torch.isnan(g_W).all()
         if on == 0:
             ref.within(g_W, *refs["g_W"], "g_W")
             assert not same_bits or torch.equal(g_W, want[3])
         alone = mhcl.head_preference(h, W, targets, o, reference, smoothing=0.1)
         for a, b in zip((*got, *alone), (*mhcl.head_preference_grad(h, W, targets, o, reference, w, smoothing=0.1), loss, logp)):
             assert torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0)) and torch.equal(a.isnan(), b.isnan())
+
+
+@pytest.mark.parametrize("io", [BF, F])
+@pytest.mark.parametrize("T,C,V", [(120, 64, 200), (1500, 64, 200), (4200, 1024, 8200)])
+@pytest.mark.parametrize("offsets,others", [([5, 3, 2], []), ([40, 40, 20], []), ([9, 5, -1, 0, 0], [0.0]), ([20, 10, 0, 0, 60], [1.0])])
+def test_a_mistake_without_tokens_is_in_the_gradient(io, T, C, V, offsets, others):
+    pairs = len(offsets) // 2
+    h, W, targets, _, reference = _inputs(18, T, C, V, pairs, io)
+    o = torch.tensor(offsets, device="cuda", dtype=torch.int32)
+    for weight in (None, torch.tensor([0.5, 0.0][:pairs], device="cuda")):
+        loss, _, g_h, g_W = mhcl.head_preference_grad(h, W, targets, o, reference, weight)
+        assert torch.isnan(loss[0]) and torch.isnan(g_W).all()
+    loss, _, g_h, g_W = mhcl.head_preference_grad(h, W, targets, o, reference, torch.tensor([0.0] + others, device="cuda"))
+    assert torch.isnan(loss[0]) and torch.isfinite(g_h).all() and torch.isfinite(g_W).all()
 
 
 def test_many_pairs_with_one_out_of_order():
