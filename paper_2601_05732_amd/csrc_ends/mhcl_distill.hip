@@ -34,7 +34,7 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
   const int64_t from = row ? row[t] : t;      // the caller's
   float a[PER], top = -INFINITY, sum = 0.f;
   int32_t mine[PER];
-  int held = 0, past = 0;
+  int held = 0, bad = 0;
   ID given[PER];
   float value[PER];
 #pragma unroll
@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
       if (there) a[i] = v;
       if (there && id < V) mine[i] = static_cast<int32_t>(id);
       held += there ? 1 : 0;
-      past += there && id >= V ? 1 : 0;
+      bad += there && (id >= V || !(v < INFINITY)) ? 1 : 0;      // (or NaN)
     }
     top = fmaxf(top, a[i]);
   }
@@ -64,9 +64,9 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
   for (int off = 32; off > 0; off >>= 1) {
     top = fmaxf(top, __shfl_xor(top, off, 64));
     held += __shfl_xor(held, off, 64);
-    past += __shfl_xor(past, off, 64);
+    bad += __shfl_xor(bad, off, 64);
   }
-  if (lane == 0) mark[from] = held == 0 ? -1 : (past != 0 ? 1 : 0);
+  if (lane == 0) mark[from] = held == 0 ? -1 : (bad != 0 ? 1 : 0);
   if constexpr (LISTS) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {

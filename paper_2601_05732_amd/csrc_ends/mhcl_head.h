@@ -96,7 +96,7 @@ hipError_t launch_preference(const mhcl_ends_desc &d, const void *h, const void 
 constexpr int kMostSlots = 256;   // of a token's teacher
 struct DistillWs {
   HeadWs head;
-  int32_t *mark;        // [T] negative where the teacher says nothing, 1 where it names a row past the vocabulary, else 0
+  int32_t *mark;        // [T] negative where the teacher says nothing, 1 where it is a mistake (a row past the vocabulary, NaN, infinity), else 0
   // of a block of tokens: a token's ids in order, its teacher's probability and the logarithm of it for each, the student's logit, how many there
   // are; which of them lie in each granule
   int32_t *id;          // [tokens][K]

@@ -151,6 +151,27 @@ def test_slots_without_a_number(io):
 
 
 @pytest.mark.parametrize("io", [BF, F])
+@pytest.mark.parametrize("T,C,V", [(90, 64, 200), (1500, 64, 200), (2100, 1024, 65000)])
+@pytest.mark.parametrize("mistake", ["nan", "inf", "row"])
+def test_each_mistake_alone_is_in_all_of_the_gradient(io, T, C, V, mistake):
+    # (the last size takes the tokens in an order of their own)
+    h, W, ids, logits = _inputs(12, T, C, V, 10, io, short=0.0)
+    at = int((ids >= 0).all(dim=1).nonzero()[3])
+    if mistake == "row":
+        ids[at, 2] = V
+    else:
+        logits[at, 2] = math.nan if mistake == "nan" else math.inf
+    for weight in (None, torch.ones(T, device="cuda")):
+        loss, _, g_h, g_W = mhcl.head_distill_grad(h, W, ids, logits, weight)
+        assert torch.isnan(loss[at]) and torch.isnan(g_h[at]).all() and torch.isnan(g_W).all()
+        rest = torch.arange(T, device="cuda") != at
+        assert torch.isfinite(loss[rest]).all() and torch.isfinite(g_h[rest]).all()
+    weight[at] = 0.0
+    _, _, g_h, g_W = mhcl.head_distill_grad(h, W, ids, logits, weight)
+    assert torch.isfinite(g_h).all() and torch.isfinite(g_W).all()
+
+
+@pytest.mark.parametrize("io", [BF, F])
 @pytest.mark.parametrize("T", [50, 1500])
 def test_places_that_do_not_count_may_hold_anything(io, T):
     h, W, ids, logits = _inputs(7, T, 128, 300, 6, io)
