@@ -20,6 +20,7 @@ from __future__ import annotations
 import argparse
 
 import torch
+from torch.nn.modules.module import _has_any_global_hook
 
 from .autograd import HyperConnection
 from .ends import Head, StreamsNorm, TokenEmbedding
@@ -37,16 +38,25 @@ class Block(torch.nn.Module):
 
     def forward(self, h):
         h = self.norm(h)
-        if _plain_linear(self.up, h) and _plain_linear(self.down, h) and takes(self.up.in_features, self.down.in_features, h.dtype):
-            return apply_gated_ffn(h, self.up.weight, self.down.weight)
+        if _plain_linear(self.up, h) and _plain_linear(self.down, h):
+            W_up, W_down = self.up.weight, self.down.weight
+            C, H = W_down.shape
+            if W_up.shape == (2 * H, C) and takes(C, H, h.dtype):
+                return apply_gated_ffn(h, W_up, W_down)
         a, b = self.up(h).chunk(2, dim=-1)      # widths that the kernels do not take, or maps that a user put in place of these
         return self.down(torch.nn.functional.silu(a) * b)
 
 
+_LINEAR = torch.nn.Linear.forward
+
+
 def _plain_linear(m, h) -> bool:
-    """Whether `m` is a linear map as Block makes it, and nothing looks at its call."""
-    return (type(m) is torch.nn.Linear and m.bias is None and m.weight.dtype is h.dtype and not torch.is_autocast_enabled("cuda")
-            and not (m._forward_hooks or m._forward_pre_hooks or m._backward_hooks or m._backward_pre_hooks))
+    """Whether `m` is a linear map as Block makes it, and nothing takes the place of its call or looks at it: a `forward` of its own (offloading,
+    adapters), a weight of a tensor subclass, hooks of it or of all modules, a compiled call."""
+    return (type(m) is torch.nn.Linear and "forward" not in vars(m) and torch.nn.Linear.forward is _LINEAR and m._compiled_call_impl is None
+            and not (m._forward_hooks or m._forward_pre_hooks or m._backward_hooks or m._backward_pre_hooks or _has_any_global_hook())
+            and m.bias is None and type(m.weight) in (torch.nn.Parameter, torch.Tensor) and m.weight.dtype is h.dtype
+            and not torch.is_autocast_enabled("cuda"))
 
 
 class LanguageModel(torch.nn.Module):

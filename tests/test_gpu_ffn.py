@@ -312,3 +312,12 @@ def test_blocks_that_the_kernels_do_not_take_run_as_they_are():
     block.down.register_forward_hook(lambda *args: seen.append(1))
     block(h)
     assert seen == [1]
+
+
+def test_a_map_s_own_forward_is_called():
+    h = _normal(_gen(14), 50, 64, dtype=BF)
+    block = lm.Block(64, 40, BF, "cuda")
+    before, ours = block(h), block.down.forward
+    block.down.forward = lambda x: ours(x) + 1.0
+    a, b = block.up(block.norm(h)).chunk(2, dim=-1)
+    assert torch.equal(block(h), block.down(torch.nn.functional.silu(a) * b)) and float((block(h) - before).float().mean()) > 0.9
