@@ -469,6 +469,10 @@ int mhcl_ffn(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const v
 int mhcl_ffn_grad(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, const float *pre, const void *g_y, void *g_x,
                   void *g_W_up, void *g_W_down, void *ws, size_t ws_bytes, void *stream);
 
+/* The same where any of g_x, g_W_up and g_W_down may be NULL, but (of one row or more) not all of them: their products are left out, and the others' bits are the same. */
+int mhcl_ffn_grad_of(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, const float *pre, const void *g_y, void *g_x,
+                     void *g_W_up, void *g_W_down, void *ws, size_t ws_bytes, void *stream);
+
 /* ---- measurement aids (no part of the method) --------------------------- */
 
 /* Kernel stages that can be bracketed with events. */

@@ -15,7 +15,7 @@ from .binding import (  # noqa: F401
     mhcl_embed, mhcl_embed_bwd, mhcl_streams_norm, mhcl_streams_norm_bwd, mhcl_head_loss, mhcl_head_loss_grad,
     mhcl_head_total, mhcl_scale, mhcl_scale_to,
     mhcl_head_distill, head_distill_workspace_bytes, mhcl_head_preference, head_preference_workspace_bytes,
-    OP_FFN, OP_FFN_GRAD, FfnDesc, ffn_workspace_bytes, mhcl_ffn, mhcl_ffn_grad,
+    OP_FFN, OP_FFN_GRAD, FfnDesc, ffn_workspace_bytes, mhcl_ffn, mhcl_ffn_grad, mhcl_ffn_grad_of,
 )
 from .layer import GpuLayer, desc_for, empty_stream, place_stream  # noqa: F401,E402
 from .autograd import HyperConnection, HyperConnectionStack, init_params  # noqa: F401,E402

@@ -32,7 +32,7 @@ _SYMBOLS = [
     "mhcl_ends_workspace_bytes", "mhcl_embed", "mhcl_embed_bwd", "mhcl_streams_norm", "mhcl_streams_norm_bwd",
     "mhcl_head_loss", "mhcl_head_loss_grad", "mhcl_head_loss_grad_unrounded", "mhcl_head_total", "mhcl_scale", "mhcl_scale_to",
     "mhcl_head_distill_workspace_bytes", "mhcl_head_distill", "mhcl_head_preference_workspace_bytes", "mhcl_head_preference",
-    "mhcl_ffn_workspace_bytes", "mhcl_ffn", "mhcl_ffn_grad",
+    "mhcl_ffn_workspace_bytes", "mhcl_ffn", "mhcl_ffn_grad", "mhcl_ffn_grad_of",
 ]
 STATIC_SCRATCH_BYTES = 16 << 20   # MHCL_STATIC_SCRATCH_BYTES
 
@@ -185,7 +185,7 @@ def lib():
         L.mhcl_ffn_workspace_bytes.restype = Z
         L.mhcl_ffn_workspace_bytes.argtypes = [B, ctypes.c_int]
         L.mhcl_ffn.argtypes = [B] + [V] * 6 + [Z, V]
-        L.mhcl_ffn_grad.argtypes = [B] + [V] * 9 + [Z, V]
+        L.mhcl_ffn_grad.argtypes = L.mhcl_ffn_grad_of.argtypes = [B] + [V] * 9 + [Z, V]
         _lib = L
     return _lib
 
@@ -547,10 +547,19 @@ def mhcl_ffn(d, x, W_up, W_down, y, pre, ws):
         _stream()), "mhcl_ffn")
 
 
-def mhcl_ffn_grad(d, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, ws):
+def _ffn_grad(name, d, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, ws):
     wp, wb = _ws(ws)
-    _check(lib().mhcl_ffn_grad(
+    _check(getattr(lib(), name)(
         ctypes.byref(d.c), _ptr(x, d.io, (d.T, d.C), "x"), _ptr(W_up, d.io, (2 * d.H, d.C), "W_up"),
         _ptr(W_down, d.io, (d.C, d.H), "W_down"), _ptr(pre, torch.float32, (d.T, 2 * d.H), "pre"), _ptr(g_y, d.io, (d.T, d.C), "g_y"),
         _ptr(g_x, d.io, (d.T, d.C), "g_x"), _ptr(g_W_up, d.io, (2 * d.H, d.C), "g_W_up"),
-        _ptr(g_W_down, d.io, (d.C, d.H), "g_W_down"), wp, wb, _stream()), "mhcl_ffn_grad")
+        _ptr(g_W_down, d.io, (d.C, d.H), "g_W_down"), wp, wb, _stream()), name)
+
+
+def mhcl_ffn_grad(d, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, ws):
+    _ffn_grad("mhcl_ffn_grad", d, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, ws)
+
+
+def mhcl_ffn_grad_of(d, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, ws):
+    """g_x, g_W_up, g_W_down: None for what is not asked for."""
+    _ffn_grad("mhcl_ffn_grad_of", d, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, ws)

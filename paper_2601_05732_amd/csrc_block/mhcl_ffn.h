@@ -26,6 +26,7 @@ struct FfnWs {
 
 // pre [T][2 H], may be null: gate | up
 hipError_t launch_ffn(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, void *y, float *pre, const FfnWs &w, hipStream_t s);
+// g_x, g_W_up, g_W_down: those that are null are not formed
 hipError_t launch_ffn_grad(const mhcl_ffn_desc &d, const void *x, const void *W_up, const void *W_down, const float *pre, const void *g_y, void *g_x,
                            void *g_W_up, void *g_W_down, const FfnWs &w, hipStream_t s);
 

@@ -95,7 +95,8 @@ struct GateEpilogue {
 // m: H, n: tokens.  The sums are g_a; g_G, g_U and a of them and of G and U, each rounded once.  16384 rows, C = 4096, H = 8192 1220 us, 0.90 PFLOP/s;
 // without the reads 1010, without the stores 998: 1.9 GB at the memory's rate between the main loops of 830 us in all.  (Reads two or three fragments ahead
 // 1214 and 1228; half of the blocks half a tile later 1249; tiles of 128 x 128, two to a unit, 1366.)
-template <bool WIDE>
+// ACT: a too, which g_W_down alone reads.
+template <bool WIDE, bool ACT>
 struct GateGradEpilogue {
   static constexpr bool kWide = WIDE, kPaired = false, kEarly = false, kCounted = false;
   const float *pre;
@@ -104,7 +105,7 @@ struct GateGradEpilogue {
   template <int FM, int FN>
   __device__ __forceinline__ int hold(int64_t, int64_t) const { return 0; }
   template <int FM, int FN>
-  static constexpr int stores() { return FN * (WIDE ? FM : FM / 2) * 3; }
+  static constexpr int stores() { return FN * (WIDE ? FM : FM / 2) * (ACT ? 3 : 2); }
   __device__ __forceinline__ bool whole(int64_t m_end, int64_t n_end) const { return m_end <= H && n_end <= T; }
   template <int FM, int FN>
   __device__ __forceinline__ void operator()(f32x4 (&acc)[FM][FN], int, int64_t m0, int64_t n0, int) const {
@@ -132,13 +133,27 @@ struct GateGradEpilogue {
             G[k][e] = ga * u * (s * (1.f + g * (1.f - s)));
             U[k][e] = ga * silu;
           }
-        store_two<WIDE>(a, n * H, m, q, v[0], v[1], here, H);
+        if constexpr (ACT) store_two<WIDE>(a, n * H, m, q, v[0], v[1], here, H);
         store_two<WIDE>(g_pre, row, m, q, G[0], G[1], here, H);
         store_two<WIDE>(g_pre, row + H, m, q, U[0], U[1], here, H);
       }
     }
   }
 };
+
+// a of G and U, where nothing but g_W_down is asked for: blocks take rows in turn.  Bound by memory.
+template <typename IO>
+__global__ __launch_bounds__(kBlock) void gate_kernel(const float *__restrict__ pre, void *__restrict__ a, int64_t T, int64_t H) {
+  constexpr bool WIDE = IO::kVec == 4;
+  for (int64_t t = blockIdx.x; t < T; t += gridDim.x)
+    for (int64_t m = threadIdx.x * 4; m < H; m += kBlock * 4) {
+      const f32x4 G = load_four(pre + t * 2 * H + m, true), U = load_four(pre + t * 2 * H + H + m, true);
+      f32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = G[e] * sigmoid<WIDE>(G[e]) * U[e];
+      store_one<WIDE>(a, t * H + m, 0, 0, v, true, H);
+    }
+}
 
 // ---------------------------------------------------------------- few rows
 // y = W x for up to 64 rows of x, as in a step of decoding: W is read once, straight into the fragments of its 16 rows a block, and the waves
@@ -443,13 +458,22 @@ hipError_t run_ffn_grad(const mhcl_ffn_desc &d, const void *x, const void *W_up,
   const Operand Wd{W_down, H, H, C}, gk{g_y, C, T, C}, Wu{W_up, C, C, 2 * H}, pk{w.g_pre, 2 * H, T, 2 * H};
   const Operand xm{x, C, C, T}, pm{w.g_pre, 2 * H, 2 * H, T}, am{w.a, H, H, T}, gm{g_y, C, C, T};
   hipError_t e;
-  if ((e = launch_gemm<false, true>(p.act, Wd, gk, H, T, 1, GateGradEpilogue<WIDE>{pre, w.a, w.g_pre, H, T}, s)) != hipSuccess) return e;
+  if (!g_x && !g_W_up) {
+    hipLaunchKernelGGL((gate_kernel<IO>), dim3(static_cast<unsigned>(std::min<int64_t>(T, 8 * kChipBlocks))), dim3(kBlock), 0, s, pre, w.a, T, H);
+    e = hipGetLastError();
+  } else if (g_W_down) {
+    e = launch_gemm<false, true>(p.act, Wd, gk, H, T, 1, GateGradEpilogue<WIDE, true>{pre, w.a, w.g_pre, H, T}, s);
+  } else {
+    e = launch_gemm<false, true>(p.act, Wd, gk, H, T, 1, GateGradEpilogue<WIDE, false>{pre, nullptr, w.g_pre, H, T}, s);
+  }
+  if (e != hipSuccess) return e;
+  void *const out[3] = {g_x, g_W_up, g_W_down};     // (as many parts of each whichever are asked for: the same bits)
   if (p.trio) {
     const auto to = [&](int splits, float *slabs, void *out, int64_t M, int64_t N) {
       return StoreEpilogue<WIDE>{nullptr, splits > 1 ? slabs : (WIDE ? static_cast<float *>(out) : nullptr), static_cast<uint16_t *>(out), nullptr, M, N, M * N, nullptr, {}, false, nullptr};
     };
     TrioArgs a{{gemm_args(p.gx, Wu, pk, C, T, p.gx_splits), gemm_args(p.gup, xm, pm, C, 2 * H, p.gup_splits), gemm_args(p.gdown, am, gm, H, C, p.gdown_splits)}, {}};
-    const auto count = [&](int i) { return a.g[i].tiles_m * a.g[i].tiles_n * a.g[i].splits; };
+    const auto count = [&](int i) { return !out[i] ? 0 : a.g[i].tiles_m * a.g[i].tiles_n * a.g[i].splits; };
     a.blocks[0] = count(0);
     a.blocks[1] = count(0) + count(1);
     const dim3 grid(a.blocks[1] + count(2));
@@ -458,16 +482,16 @@ hipError_t run_ffn_grad(const mhcl_ffn_desc &d, const void *x, const void *W_up,
     if (p.gx.bn < 128) hipLaunchKernelGGL((trio_kernel<true, WIDE>), grid, dim3(256), 0, s, a, e0, e1, e2);
     else hipLaunchKernelGGL((trio_kernel<false, WIDE>), grid, dim3(256), 0, s, a, e0, e1, e2);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    SlabSums sums{{w.slabs, w.up_slabs, w.down_slabs}, {g_x, g_W_up, g_W_down}, {p.gx_splits, p.gup_splits, p.gdown_splits}, {T * C, 2 * H * C, H * C}, {}};
+    SlabSums sums{{w.slabs, w.up_slabs, w.down_slabs}, {out[0], out[1], out[2]}, {p.gx_splits, p.gup_splits, p.gdown_splits}, {T * C, 2 * H * C, H * C}, {}};
     int64_t total = 0;
-    for (int i = 0; i < 3; ++i) sums.end[i] = total += sums.slabs[i] > 1 ? ceil_div(sums.count[i], kBlock * 4) : 0;
+    for (int i = 0; i < 3; ++i) sums.end[i] = total += out[i] && sums.slabs[i] > 1 ? ceil_div(sums.count[i], kBlock * 4) : 0;
     if (total == 0) return hipSuccess;
     hipLaunchKernelGGL((slab_sums_kernel<IO>), dim3(static_cast<unsigned>(total)), dim3(kBlock), 0, s, sums);
     return hipGetLastError();
   }
-  if ((e = product<false, true, IO>(p.gx, Wu, pk, C, T, p.gx_splits, w.slabs, g_x, s)) != hipSuccess) return e;
-  if ((e = product<false, false, IO>(p.gup, xm, pm, C, 2 * H, p.gup_splits, w.slabs, g_W_up, s)) != hipSuccess) return e;
-  return product<false, false, IO>(p.gdown, am, gm, H, C, p.gdown_splits, w.slabs, g_W_down, s);
+  if (g_x && (e = product<false, true, IO>(p.gx, Wu, pk, C, T, p.gx_splits, w.slabs, g_x, s)) != hipSuccess) return e;
+  if (g_W_up && (e = product<false, false, IO>(p.gup, xm, pm, C, 2 * H, p.gup_splits, w.slabs, g_W_up, s)) != hipSuccess) return e;
+  return !g_W_down ? hipSuccess : product<false, false, IO>(p.gdown, am, gm, H, C, p.gdown_splits, w.slabs, g_W_down, s);
 }
 
 }  // namespace

@@ -21,10 +21,27 @@ bool all16(P... p) {
   return ((p != nullptr && reinterpret_cast<uintptr_t>(p) % 16 == 0) && ...);
 }
 
+bool none_or16(const void *p) { return p == nullptr || all16(p); }
+
 #define MHCL_HIP(expr)                              \
   do {                                              \
     if ((expr) != hipSuccess) return MHCL_ERR_HIP;  \
   } while (0)
+
+// mhcl_ffn_grad and mhcl_ffn_grad_of, which has seen to it that of g_x, g_W_up and g_W_down those are there that have to be
+int ffn_grad(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, const float *pre, const void *g_y, void *g_x,
+             void *g_W_up, void *g_W_down, void *ws, size_t ws_bytes, hipStream_t s) {
+  if (desc->T == 0) {
+    const size_t half = static_cast<size_t>(desc->H) * desc->C * dtype_bytes(desc->io_dtype);
+    if (g_W_up) MHCL_HIP(launch_zero(g_W_up, 2 * half, s));
+    if (g_W_down) MHCL_HIP(launch_zero(g_W_down, half, s));
+    return MHCL_OK;
+  }
+  if (!all16(x, W_up, W_down, (const void *)pre, g_y)) return MHCL_ERR_INVALID_ARG;
+  if (!all16(ws) || ws_bytes < mhcl_ffn_workspace_bytes(desc, MHCL_OP_FFN_GRAD)) return MHCL_ERR_WORKSPACE;
+  MHCL_HIP(launch_ffn_grad(*desc, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, FfnWs(*desc, true, ws), s));
+  return MHCL_OK;
+}
 
 }  // namespace
 
@@ -48,18 +65,16 @@ int mhcl_ffn(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const v
 int mhcl_ffn_grad(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, const float *pre, const void *g_y, void *g_x,
                   void *g_W_up, void *g_W_down, void *ws, size_t ws_bytes, void *stream) {
   if (int e = check_ffn(desc)) return e;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  if (!all16(g_W_up, g_W_down)) return MHCL_ERR_INVALID_ARG;
-  if (desc->T == 0) {
-    const size_t half = static_cast<size_t>(desc->H) * desc->C * dtype_bytes(desc->io_dtype);
-    MHCL_HIP(launch_zero(g_W_up, 2 * half, s));
-    MHCL_HIP(launch_zero(g_W_down, half, s));
-    return MHCL_OK;
-  }
-  if (!all16(x, W_up, W_down, (const void *)pre, g_y, (const void *)g_x)) return MHCL_ERR_INVALID_ARG;
-  if (!all16(ws) || ws_bytes < mhcl_ffn_workspace_bytes(desc, MHCL_OP_FFN_GRAD)) return MHCL_ERR_WORKSPACE;
-  MHCL_HIP(launch_ffn_grad(*desc, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, FfnWs(*desc, true, ws), s));
-  return MHCL_OK;
+  if (!all16(g_W_up, g_W_down) || (desc->T > 0 && !all16((const void *)g_x))) return MHCL_ERR_INVALID_ARG;
+  return ffn_grad(desc, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, ws, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+int mhcl_ffn_grad_of(const mhcl_ffn_desc *desc, const void *x, const void *W_up, const void *W_down, const float *pre, const void *g_y, void *g_x,
+                     void *g_W_up, void *g_W_down, void *ws, size_t ws_bytes, void *stream) {
+  if (int e = check_ffn(desc)) return e;
+  if (!none_or16(g_x) || !none_or16(g_W_up) || !none_or16(g_W_down) || (desc->T > 0 && !g_x && !g_W_up && !g_W_down))
+    return MHCL_ERR_INVALID_ARG;
+  return ffn_grad(desc, x, W_up, W_down, pre, g_y, g_x, g_W_up, g_W_down, ws, ws_bytes, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

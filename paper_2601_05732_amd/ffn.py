@@ -1,6 +1,6 @@
 """The gated feed-forward block between the layers, ``y = (silu(x Wg^T) * (x Wu^T)) W_down^T``, with its gradients.
 
-As in :mod:`.ends`: the functions allocate the results and make one call into ``libmhcl.so`` (``mhcl_ffn``, ``mhcl_ffn_grad``; include/mhcl.h
+As in :mod:`.ends`: the functions allocate the results and make one call into ``libmhcl.so`` (``mhcl_ffn``, ``mhcl_ffn_grad_of``; include/mhcl.h
 has the formulas), through the extension in C++ where the library can read the tensors as they are; others are copied first.
 :class:`GatedFeedForward` is the same under ``torch.autograd``: first derivatives; second ones and forward-mode tangents are refused.
 """
@@ -38,16 +38,19 @@ def gated_ffn(x: torch.Tensor, W_up: torch.Tensor, W_down: torch.Tensor, keep: b
     return (y, kept) if keep else y
 
 
-def gated_ffn_grad(x: torch.Tensor, W_up: torch.Tensor, W_down: torch.Tensor, kept: torch.Tensor, g_y: torch.Tensor):
-    """``g_x [T, C], g_W_up [2 H, C], g_W_down [C, H]`` of `gated_ffn` for the gradient g_y [T, C] on its result; `kept` as it gave it."""
+def gated_ffn_grad(x: torch.Tensor, W_up: torch.Tensor, W_down: torch.Tensor, kept: torch.Tensor, g_y: torch.Tensor, wanted=(True, True, True)):
+    """``g_x [T, C], g_W_up [2 H, C], g_W_down [C, H]`` of `gated_ffn` for the gradient g_y [T, C] on its result; `kept` as it gave it.
+    wanted: which of the three (one at least); those that are not wanted are None, and their products are left out."""
+    wanted = tuple(bool(w) for w in wanted)
+    _need(len(wanted) == 3 and any(wanted), f"wanted: which of the three gradients, got {wanted}")
     native = _native()
-    if native is not None and (g := native.ffn_grad(x, W_up, W_down, kept, g_y)) is not None:
+    if native is not None and (g := native.ffn_grad(x, W_up, W_down, kept, g_y, *wanted)) is not None:
         return g
     _same_device(x, W_up, W_down, kept, g_y)
     d = _desc(x, W_up, W_down)
-    g_x, g_W_up, g_W_down = (torch.empty(t.shape, device=t.device, dtype=t.dtype) for t in (x, W_up, W_down))
+    g_x, g_W_up, g_W_down = (torch.empty(t.shape, device=t.device, dtype=t.dtype) if w else None for t, w in zip((x, W_up, W_down), wanted))
     ws = mhcl.new_ffn_workspace(d, mhcl.OP_FFN_GRAD, x.device)
-    mhcl.mhcl_ffn_grad(d, _dense(x), _dense(W_up), _dense(W_down), _dense(kept), _dense(g_y), g_x, g_W_up, g_W_down, ws)
+    mhcl.mhcl_ffn_grad_of(d, _dense(x), _dense(W_up), _dense(W_down), _dense(kept), _dense(g_y), g_x, g_W_up, g_W_down, ws)
     return g_x, g_W_up, g_W_down
 
 
@@ -69,7 +72,8 @@ class _Ffn(torch.autograd.Function):
     @staticmethod
     def backward(ctx, g_y):
         x, W_up, W_down, kept = ctx.saved_tensors
-        return *first_only("the feed-forward block", gated_ffn_grad(x, W_up, W_down, kept, g_y), x, W_up, W_down, g_y), None
+        grads = gated_ffn_grad(x, W_up, W_down, kept, g_y, ctx.needs_input_grad[:3])      # (frozen weights need no products)
+        return *first_only("the feed-forward block", grads, x, W_up, W_down, g_y), None
 
 
 def apply_gated_ffn(x, W_up, W_down):

@@ -233,18 +233,22 @@ std::optional<std::tuple<Tensor, std::optional<Tensor>>> ffn(const Tensor &x, co
   return std::make_tuple(y, pre);
 }
 
-std::optional<std::tuple<Tensor, Tensor, Tensor>> ffn_grad(const Tensor &x, const Tensor &W_up, const Tensor &W_down, const Tensor &pre, const Tensor &g_y) {
+using FfnGrads = std::tuple<std::optional<Tensor>, std::optional<Tensor>, std::optional<Tensor>>;
+std::optional<FfnGrads> ffn_grad(const Tensor &x, const Tensor &W_up, const Tensor &W_down, const Tensor &pre, const Tensor &g_y, bool of_x, bool of_W_up,
+                                 bool of_W_down) {
   const int device = c10::hip::current_device();
   const auto d = ffn_ready(x, W_up, W_down, device);
   if (!d || pre.dim() != 2 || pre.size(0) != x.size(0) || pre.size(1) != W_up.size(0) || pre.scalar_type() != at::kFloat ||
       !ready(pre, device, 16) || g_y.sizes() != x.sizes() || g_y.scalar_type() != x.scalar_type() || !ready(g_y, device, 16))
     return std::nullopt;
-  const Tensor g_x = at::empty(x.sizes(), x.options()), g_W_up = at::empty(W_up.sizes(), x.options()), g_W_down = at::empty(W_down.sizes(), x.options());
+  const auto buffer = [&](bool wanted, const Tensor &like) { return wanted ? std::optional<Tensor>(at::empty(like.sizes(), x.options())) : std::nullopt; };
+  const auto g_x = buffer(of_x, x), g_W_up = buffer(of_W_up, W_up), g_W_down = buffer(of_W_down, W_down);
+  const auto out = [](const std::optional<Tensor> &t) { return t ? ptr(*t) : nullptr; };
   const Tensor ws = ffn_workspace_of(*d, MHCL_OP_FFN_GRAD, x);
-  check(mhcl_ffn_grad(&*d, ptr(x), ptr(W_up), ptr(W_down), ptr<float>(pre), ptr(g_y), ptr(g_x), ptr(g_W_up), ptr(g_W_down), ws.data_ptr(), ws.nbytes(),
-                      stream()),
-        "mhcl_ffn_grad");
-  return std::make_tuple(g_x, g_W_up, g_W_down);
+  check(mhcl_ffn_grad_of(&*d, ptr(x), ptr(W_up), ptr(W_down), ptr<float>(pre), ptr(g_y), out(g_x), out(g_W_up), out(g_W_down), ws.data_ptr(), ws.nbytes(),
+                         stream()),
+        "mhcl_ffn_grad_of");
+  return FfnGrads(g_x, g_W_up, g_W_down);
 }
 
 }  // namespace

@@ -3,6 +3,7 @@ go wrong; its gradients against differences; under torch.autograd, captured, on 
 
 The bounds (_bounds) are carried through the formulas from the roundings and were fixed before the first run.
 """
+import itertools
 import math
 
 import pytest
@@ -321,3 +322,45 @@ def test_a_map_s_own_forward_is_called():
     block.down.forward = lambda x: ours(x) + 1.0
     a, b = block.up(block.norm(h)).chunk(2, dim=-1)
     assert torch.equal(block(h), block.down(torch.nn.functional.silu(a) * b)) and float((block(h) - before).float().mean()) > 0.9
+
+
+ASKED = [w for w in itertools.product((False, True), repeat=3) if any(w)]
+
+
+@pytest.mark.parametrize("io,T,C,H", [(io, *s) for io in (BF, F) for s in [(1, 64, 24), (5, 136, 264), (65, 136, 520), (333, 520, 1000), (2049, 72, 264), (40, 128, 8200)]]
+                         + [(BF, 4104, 72, 4104), (BF, 300, 4104, 4104), (BF, 4104, 4104, 72)])
+def test_gradients_that_are_asked_for(monkeypatch, io, T, C, H):
+    x, up, down, g_y = _inputs(T + H, T, C, H, io)
+    _, kept = mhcl.gated_ffn(x, up, down, keep=True)
+    every = mhcl.gated_ffn_grad(x, up, down, kept, g_y)
+    again = mhcl.gated_ffn_grad(x, up, down, kept, g_y, (True, True, True))
+    assert all(torch.equal(a, b) for a, b in zip(every, again))
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(ffn, "_native", lambda: None)
+        for wanted in ASKED:
+            some = mhcl.gated_ffn_grad(x, up, down, kept, g_y, wanted)
+            assert all(torch.equal(a, b) if w else b is None for a, b, w in zip(every, some, wanted)), wanted
+
+
+@pytest.mark.parametrize("io", [BF, F])
+def test_gradients_of_frozen_weights(io):
+    T, C, H = 70, 64, 40
+    x, up, down, g_y = _inputs(15, T, C, H, io)
+    _, kept = mhcl.gated_ffn(x, up, down, keep=True)
+    every = mhcl.gated_ffn_grad(x, up, down, kept, g_y)
+    for wanted in ASKED:
+        net = mhcl.GatedFeedForward(C, H, dtype=io)
+        with torch.no_grad():
+            net.W_up.copy_(up)
+            net.W_down.copy_(down)
+        net.W_up.requires_grad_(wanted[1])
+        net.W_down.requires_grad_(wanted[2])
+        own = x.clone().requires_grad_(wanted[0])
+        net(own).backward(g_y)
+        for got, want, w in zip((own.grad, net.W_up.grad, net.W_down.grad), every, wanted):
+            assert torch.equal(got, want) if w else got is None, wanted
+    none = x[:0]
+    for wanted in ASKED:
+        g = mhcl.gated_ffn_grad(none, up, down, kept[:0], none, wanted)
+        assert all((t is None) if not w else not t.any() for t, w in zip(g, wanted))
