@@ -364,3 +364,10 @@ def test_gradients_of_frozen_weights(io):
     for wanted in ASKED:
         g = mhcl.gated_ffn_grad(none, up, down, kept[:0], none, wanted)
         assert all((t is None) if not w else not t.any() for t, w in zip(g, wanted))
+
+
+# few rows against more outputs than a unit has blocks of sixteen for: of the second product (C > 4096), and in fp32 of the first one (H > 4096)
+@pytest.mark.parametrize("io,T,C,H", [(io, *s) for io in (BF, F) for s in [(31, 4104, 136), (64, 4104, 1000), (33, 8200, 264), (3, 4104, 72), (17, 32768, 8)]]
+                         + [(F, 20, 4096, 4104), (F, 64, 4096, 4104), (F, 64, 4104, 4104), (F, 16, 520, 4112)])
+def test_few_rows_and_many_outputs(io, T, C, H):
+    _check(*_inputs(T + C, T, C, H, io))
