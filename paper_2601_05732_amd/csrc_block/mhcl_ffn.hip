@@ -18,7 +18,8 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// 1 / (1 + exp(-x)): by the instructions for bf16 operands, to 2^-22 + 2^-24 |x| of itself, the library's for fp32 ones
+// 1 / (1 + exp(-x)): by the instructions for bf16 operands, to 1.25 * 2^-22 + 1.22 * 2^-24 |x| of itself, the library's for fp32 ones.  (An ulp, 2^-23, each
+// for the exponential and the reciprocal, half a one for the sum; in the exponent the product's 2^-24 and the constant's 2^-26.2 of |x|.)
 template <bool WIDE>
 __device__ __forceinline__ float sigmoid(float x) {
   if constexpr (WIDE) return 1.f / (1.f + expf(-x));
@@ -370,9 +371,14 @@ hipError_t launch_few(const FewArgs &a, hipStream_t s) {
   const unsigned count = blocks(a.M, 16);
   const auto go = [&](auto fn) {
     constexpr int FN = decltype(fn)::value;
-    // (the waves of a unit: where it has one block, as many as it holds)
-    if (count <= kChipBlocks) hipLaunchKernelGGL((few_kernel<FN, GATE, WIDE, 16>), dim3(count), dim3(1024), 0, s, a);
-    else hipLaunchKernelGGL((few_kernel<FN, GATE, WIDE, 8>), dim3(count), dim3(512), 0, s, a);
+    // (the waves of a unit: where it has one block, as many as it holds, which is so of all of bf16's first products: few_for takes up to 2812 rows of Wg)
+    if constexpr (!GATE || WIDE) {
+      if (count > kChipBlocks) {
+        hipLaunchKernelGGL((few_kernel<FN, GATE, WIDE, 8>), dim3(count), dim3(512), 0, s, a);
+        return hipGetLastError();
+      }
+    }
+    hipLaunchKernelGGL((few_kernel<FN, GATE, WIDE, 16>), dim3(count), dim3(1024), 0, s, a);
     return hipGetLastError();
   };
   if (a.T <= 16) return go(std::integral_constant<int, 1>{});
