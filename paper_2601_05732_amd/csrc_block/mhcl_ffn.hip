@@ -543,7 +543,7 @@ FfnPlan::FfnPlan(const mhcl_ffn_desc &d, bool grad) {
       parts += count;
       slabs += k[i] > 1 ? count / (slim(i) ? 4 : 1) : 0;
     }
-    const int64_t alone = parts <= kChipBlocks ? (wide ? 33 : 42) : 60;
+    const int64_t alone = parts <= kChipBlocks ? alone_time(wide) : 60;
     const int64_t time = std::max(longest * alone / 60, work / (2 * kChipBlocks)) + slabs + (slabs > 0 ? kSumTime : 0);
     if (time < best) {
       best = time;

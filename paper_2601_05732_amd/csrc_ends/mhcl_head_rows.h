@@ -589,7 +589,7 @@ hipError_t run_head(const mhcl_ends_desc &d, const void *h, const void *W, Way &
       gh_tokens.tiles_m = static_cast<int>(ceil_div(C, p.gh.bm));
       gh_tokens.bn = p.gh.bn;
       gh_tokens.steps = static_cast<int>(ceil_div(V, WIDE ? 32 : 64));
-      gh_tokens.alone = WIDE ? 33 : 42;
+      gh_tokens.alone = alone_time(WIDE);
       gh_tokens.most_parts = p.gh_splits;
     }
     const Store to_gh{w.common, parts && !ORDERED ? w.slabs : (floats ? static_cast<float *>(gh_out) : nullptr), static_cast<uint16_t *>(gh_out), nullptr, C, T,

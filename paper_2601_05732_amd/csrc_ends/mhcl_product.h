@@ -28,6 +28,19 @@ struct Operand {
   int64_t rows, depth;
 };
 
+// The time of a product of few tiles whose depth is split into parts, in sixtieths of a step of two blocks on a compute unit: `each` steps of a
+// part, whose first loads and epilogue are the like of four more, `parts` of them at once.  filling: a block of the tile fills a compute unit; alone: a step's time
+// of one that does not and has a unit for itself.  (Split on the host, TokenCount on the device.)
+constexpr int64_t kChipBlocks = 256, kSumTime = 240;      // the sum over slabs, a launch
+constexpr int alone_time(bool wide) { return wide ? 33 : 42; }
+template <typename I>
+__host__ __device__ constexpr I parts_time(I parts, I each, bool filling, I alone) {
+  constexpr I UNITS = static_cast<I>(kChipBlocks);
+  const I rest = parts % (2 * UNITS);
+  const I step = filling ? (parts + UNITS - 1) / UNITS * 60 : parts / (2 * UNITS) * 60 + (rest == 0 ? 0 : (rest > UNITS ? 60 : alone));
+  return step * (each + 4);
+}
+
 // How many tokens there are is known to the device alone: `count` of them less those of blocks before (`first`), at most as many as the host has sized the
 // product for.  They are D's rows n, or (deep) its depth.
 struct TokenCount {
@@ -37,17 +50,15 @@ struct TokenCount {
     const int64_t n = static_cast<int64_t>(*count) - first;
     return n < 0 ? 0 : (n < most ? n : most);
   }
-  // Parts of the depth of a product over n, up to `most_parts` (0: as the host says): the number that ends first, by Split's model, of tiles_m tiles for
-  // every bn tokens; `alone`: a step's time of a tile that has a compute unit for itself (60: the largest, which always has).  (us, 8192 tokens, of which 5700 count, C = 4096, 65536 rows, pairs, the whole call: one part 8471,
+  // Parts of the depth of a product over n, up to `most_parts` (0: as the host says): the number that ends first, of tiles_m tiles for
+  // every bn tokens (a slab of the largest tile counting four times).  (us, 8192 tokens, of which 5700 count, C = 4096, 65536 rows, pairs, the whole call: one part 8471,
   // so 7840; all 8192 count 10600 and 10730.)
   int tiles_m, bn, steps, alone, most_parts;
   __device__ __forceinline__ int parts(int64_t rows) const {
     const int tiles = tiles_m * static_cast<int>((rows + bn - 1) / bn), slab = bn >= 256 ? 4 : 1;
     int best = 1, least = 0x7fffffff;
     for (int k = 1; k <= most_parts; ++k) {
-      const int parts = tiles * k, rest = parts % 512;
-      const int step = bn >= 256 ? (parts + 255) / 256 * 60 : parts / 512 * 60 + (rest == 0 ? 0 : (rest > 256 ? 60 : alone));
-      const int time = step * ((steps + k - 1) / k + 4) + (k > 1 ? parts * slab + 240 : 0);
+      const int time = parts_time(tiles * k, (steps + k - 1) / k, bn >= 256, alone) + (k > 1 ? tiles * k * slab + static_cast<int>(kSumTime) : 0);
       if (time < least) least = time, best = k;
     }
     return best;
@@ -637,8 +648,6 @@ __global__ __launch_bounds__(kBlock) void slab_sum_rows_kernel(const float *__re
   else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + to) = make_uint2(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]));
 }
 
-constexpr int64_t kChipBlocks = 256;
-
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 unsigned blocks(int64_t items, int64_t each) { return static_cast<unsigned>(ceil_div(items, each)); }
 
@@ -684,22 +693,17 @@ ProductTile tile_for(int64_t M, int64_t N, int64_t parts, bool slim, bool big) {
 }
 
 // Into how many parts the depth of a product of few tiles is split, each a slab of fp32 sums of its own: the number that is expected to end
-// first, in sixtieths of a step of two blocks on a compute unit.  A block alone there takes 0.7 of that for a step (fp32: 0.55), a part the like of
-// four steps for its first loads and its epilogue, a tile of a slab a sixtieth for being written and read again by every 256 units,
-// and the sum over slabs is a launch, kSumTime.  Parts of fewer than eight steps, or more than 64, are not taken.
+// first, by parts_time (a block alone on a compute unit takes 0.7 of a step of two, fp32 0.55), a tile of a slab taking a sixtieth of a step for being
+// written and read again by every 256 units, and the sum over slabs being a launch, kSumTime.  Parts of fewer than eight steps, or more than 64, are not taken.
 // (us, one part / this many.  g_W of 7043 tokens, C = 560, 955 rows, bf16, 40 tiles, 6: 83.7 / 25.0; of 7621 tokens, C = 3768, 1317 rows, fp32, 330
 // tiles, 3: 674 / 522.  g_h of 1000 tokens, C = 1024, 20000 rows, bf16, 64 tiles, 4 / 8: 69.1 / 52.9.)
-constexpr int64_t kSumTime = 240;
 struct Split {
   int64_t tiles, steps;
   bool alone, wide;      // alone: a block of the tile fills a compute unit
   Split(const ProductTile &tile, int64_t M, int64_t N, int64_t depth, bool w)
       : tiles(ceil_div(M, tile.bm) * ceil_div(N, tile.bn)), steps(ceil_div(depth, w ? 32 : 64)), alone(tile.bm == 256), wide(w) {}
   int64_t time(int k) const {   // without the sum
-    const int64_t parts = tiles * k, rest = parts % (2 * kChipBlocks);
-    const int64_t step = alone ? ceil_div(parts, kChipBlocks) * 60
-                               : parts / (2 * kChipBlocks) * 60 + (rest == 0 ? 0 : rest > kChipBlocks ? 60 : wide ? 33 : 42);
-    return step * (ceil_div(steps, k) + 4) + (k > 1 ? parts : 0);
+    return parts_time<int64_t>(tiles * k, ceil_div(steps, k), alone, alone_time(wide)) + (k > 1 ? tiles * k : 0);
   }
   int best() const {
     int k_best = 1;
