@@ -156,28 +156,41 @@ __global__ __launch_bounds__(kPairThreads) void pair_kernel(const PairArgs a, co
   }
 }
 
-// E of more pairs than a block of those has threads, left in the bits of `loss` until they replace it: a thread for every so many pairs in a row
+// E of more pairs than a block of those has threads, left in the bits of `loss` until they replace it: a wave for a sixteenth of the pairs, 64 of them
+// at a time, first for the furthest end of all and then, from that of the waves before on, pair by pair.
 template <typename OFF>
 __global__ __launch_bounds__(1024) void pair_ends_kernel(const PairArgs a, const OFF *__restrict__ offsets) {
   __shared__ int32_t ends[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int each = (a.pairs + 1023) / 1024, first = min(static_cast<int>(threadIdx.x) * each, a.pairs), last = min(first + each, a.pairs);
+  const int each = ((a.pairs + 15) / 16 + 63) / 64 * 64, first = min(wave * each, a.pairs), last = min(first + each, a.pairs);
+  // (not under a condition: the loads of several pairs are side by side)
+  const auto end_of = [&](int p) __attribute__((always_inline)) {
+    const int64_t from = p < last ? p : a.pairs - 1;
+    const bool right = ascends(offsets, from, a.T);
+    const int64_t end = static_cast<int64_t>(offsets[2 * from + 2]);
+    return right && p < last ? static_cast<int32_t>(end) : 0;
+  };
   int32_t end = 0;
-  for (int p = first; p < last; ++p)
-    if (ascends(offsets, p, a.T)) end = max(end, static_cast<int32_t>(offsets[2 * static_cast<int64_t>(p) + 2]));
+#pragma unroll 8
+  for (int p = first + lane; p < last; p += 64) end = max(end, end_of(p));
 #pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int32_t other = __shfl_up(end, off, 64);
-    end = lane >= off ? max(end, other) : end;
-  }
-  if (lane == 63) ends[wave] = end;
-  end = __shfl_up(end, 1, 64);
-  if (lane == 0) end = 0;
+  for (int off = 32; off > 0; off >>= 1) end = max(end, __shfl_xor(end, off, 64));
+  if (lane == 0) ends[wave] = end;
   __syncthreads();
-  for (int w = 0; w < wave; ++w) end = max(end, ends[w]);
-  for (int p = first; p < last; ++p) {
-    a.loss[p] = __int_as_float(end);
-    if (ascends(offsets, p, a.T)) end = max(end, static_cast<int32_t>(offsets[2 * static_cast<int64_t>(p) + 2]));
+  int32_t before = 0;
+  for (int w = 0; w < wave; ++w) before = max(before, ends[w]);
+  int32_t next = first < last ? end_of(first + lane) : 0;
+  for (int p0 = first; p0 < last; p0 += 64) {
+    int32_t upto = next;
+    next = end_of(p0 + 64 + lane);
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int32_t other = __shfl_up(upto, off, 64);
+      upto = lane >= off ? max(upto, other) : upto;
+    }
+    const int32_t here = __shfl_up(upto, 1, 64);
+    if (p0 + lane < last) a.loss[p0 + lane] = __int_as_float(lane > 0 ? max(before, here) : before);
+    before = max(before, __shfl(upto, 63, 64));
   }
 }
 

@@ -202,7 +202,11 @@ struct PairLosses {
     if (count == 0) return common;
     __shared__ int red[THREADS / 64];
     bool lost = false;
-    for (int p = threadIdx.x; p < count; p += THREADS) lost |= isnan(loss[p]) && !(weight && weight[p] == 0.f);
+#pragma unroll 8
+    for (int p = threadIdx.x; p < count; p += THREADS) {
+      const float w = weight ? weight[p] : 1.f;
+      lost |= isnan(loss[p]) & (w != 0.f);
+    }
     const bool any = __ballot(lost) != 0;
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = any ? 1 : 0;
     __syncthreads();
@@ -372,7 +376,7 @@ hipError_t dispatch_id(int id_dtype, F &&f) {
 template <typename OFF>
 __device__ __forceinline__ bool ascends(const OFF *__restrict__ offsets, int64_t p, int64_t T) {
   const int64_t o[3] = {static_cast<int64_t>(offsets[2 * p]), static_cast<int64_t>(offsets[2 * p + 1]), static_cast<int64_t>(offsets[2 * p + 2])};
-  return o[0] >= 0 && o[0] <= o[1] && o[1] <= o[2] && o[2] <= T;
+  return (o[0] >= 0) & (o[0] <= o[1]) & (o[1] <= o[2]) & (o[2] <= T);
 }
 
 // ---------------------------------------------------------------- order of the tokens
@@ -394,6 +398,7 @@ struct Counting {
     if (pairs == 0) return {0, 0};
     __shared__ int red[kBlock / 64];
     bool wrong = false;
+#pragma unroll 8
     for (int64_t p = threadIdx.x; p < pairs; p += kBlock) wrong |= !ascends(offsets, p, T);
     const bool any = __ballot(wrong) != 0;
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = any ? 1 : 0;

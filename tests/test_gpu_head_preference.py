@@ -258,6 +258,49 @@ def test_many_pairs_with_one_out_of_order():
         assert torch.equal(loss[rest], want["loss"][rest]) and torch.equal(logp.view(-1, 2)[rest], want["logp"].view(-1, 2)[rest])
 
 
+@pytest.mark.parametrize("pairs,near", [(6, 9), (60, 0), (400, 5), (512, 40), (700, 5), (5000, 9), (5000, 300)])
+def test_offsets_in_any_order(pairs, near):
+    # mostly ascending by little, with some that lie anywhere: which pairs are mistakes, and one writer for every weight
+    T = 500
+    h, W, targets, _, reference = _inputs(19, T, 64, 90, pairs, F)
+    g = torch.Generator().manual_seed(pairs + near)
+    offsets = torch.sort(torch.randint(0, T + 1, (2 * pairs + 1,), generator=g))[0]
+    away = torch.rand(2 * pairs + 1, generator=g) < near / (2 * pairs + 1)
+    offsets = torch.where(away, torch.randint(-5, T + 6, (2 * pairs + 1,), generator=g), offsets)
+    o, end, bad, owner = offsets.tolist(), 0, [], torch.full((T,), -1)
+    for p in range(pairs):
+        a, b, c = o[2 * p:2 * p + 3]
+        ascends = 0 <= a <= b <= c <= T
+        if not ascends or (a < end and a < c):
+            bad.append(p)
+        elif a < c:
+            owner[a:c] = p
+        end = max(end, c) if ascends else end
+    weight = torch.rand(pairs, generator=g) + 0.1
+    weight[bad] = 0.0
+    args = (h, W, targets, offsets.cuda(), reference, weight.cuda())
+    loss, _, g_h, g_W = got = mhcl.head_preference_grad(*args)
+    isnan = torch.zeros(pairs, dtype=torch.bool)
+    isnan[bad] = True
+    assert torch.equal(loss.isnan().cpu(), isnan) and torch.isfinite(g_h).all() and torch.isfinite(g_W).all()
+    nobody = (owner < 0).cuda() | (targets < 0)
+    assert not g_h[nobody].any()
+    # the weight of each token is that of the pair that holds it: its cross entropy's factor
+    w = torch.zeros(T, dtype=torch.float64)
+    m = 0.1 * (got[1].view(-1, 2)[:, 0] - got[1].view(-1, 2)[:, 1] - reference[0::2] + reference[1::2]).double().cpu()
+    for t in range(T):
+        p = int(owner[t])
+        if p >= 0:
+            w[t] = (0.1 if t < o[2 * p + 1] else -0.1) * torch.sigmoid(-m[p]) * weight[p]
+    want = mhcl.head_loss_grad(h, W, targets, w.float().cuda())
+    # (m here is of fp32 numbers of up to some hundreds, 2^-24 of them each: 1e-5 of a weight)
+    for a, b in zip((g_h, g_W), want[2:]):
+        assert float((a.double() - b.double()).norm()) <= 1e-4 * float(b.double().norm())
+    assert all(torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0)) for a, b in zip(got, mhcl.head_preference_grad(*args)))
+    again = mhcl.head_preference_grad(*args[:5], torch.ones(pairs, device="cuda"))
+    assert bool(torch.isnan(again[3]).all()) == bool(bad) and torch.equal(again[0].isnan().cpu(), isnan)
+
+
 def test_large_margins():
     h, W, targets, offsets, reference = _inputs(7, 400, 64, 300, 4, F)
     reference += torch.tensor([1e4, 0, 0, 1e4, -3e4, 0, 0, -3e4], device="cuda")
