@@ -416,7 +416,7 @@ int mhcl_head_distill(const mhcl_ends_desc *desc, int32_t K, float temperature, 
  * without a target, add nothing; their g_h is 0, and large products leave them out.  Offsets ascend from 0 or more to T or less.  A pair whose own three
  * do not, which the host cannot see, or that begins before the end of an earlier pair whose own do, is a mistake: its loss and logp are NaN, the
  * other pairs' are what they are without it, and nothing is read or written out of bounds for it.  A pair whose loss is NaN, of whatever cause, makes
- * all of g_W NaN (where there are tokens) and g_h of the tokens that are its alone, unless its weight is 0.
+ * all of g_W NaN (where there are tokens) unless its weight is 0, and g_h of its tokens (of a mistake's: of tokens that no other pair holds).
  * Past one block of tokens (MHCL_HEAD_BLOCK_BYTES) the logits are formed twice for gradients, since a pair's weight needs all of its tokens.
  * total, g_h, g_W, unrounded: as in mhcl_head_distill.  pairs: 0 .. 2^22; beta finite; smoothing 0 .. 1.
  * in : h [T,C] io, W [V,C] io, targets [T], offsets [2 pairs + 1] of offset_dtype, reference [2 pairs] f32 or NULL (zeros), weight [pairs] f32 or NULL

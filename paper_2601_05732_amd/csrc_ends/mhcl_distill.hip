@@ -111,8 +111,8 @@ __global__ __launch_bounds__(kBlock) void teacher_kernel(const ID *__restrict__ 
   }
 }
 
-// the logits at a teacher's ids, of logits over tau.  (8192 tokens, C = 768, 50257 rows, 32 slots, us: the table's word read before the tile's first
-// step, and in it the row of the first slot, 693; its first slots by a prefix sum, read with the ids after the last step 743.)
+// the logits at a teacher's ids, of logits over tau.  (8192 tokens, C = 768, 50257 rows, 32 slots: the table's word, and in it the row of the first
+// slot, read before the tile's first step is 50 us less than first slots by a prefix sum, read with the ids after the last step; the call takes 600.)
 struct TeacherLogits {
   const int32_t *id;
   const uint32_t *table;

@@ -216,7 +216,7 @@ def head_preference(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, off
         loss[p] = (1 - smoothing) log(1 + exp(-m)) + smoothing log(1 + exp(m)),  m = beta ((logp - reference)[2 p] - (logp - reference)[2 p + 1])
 
     reference [2 P] fp32: those of a reference model (what this returns for it), or None for zeros.  offsets [2 P + 1] int64 or int32, ascending
-    within 0..T; tokens outside of them add nothing.  h [T, C], W [V, C] of one type."""
+    within 0..T (a pair whose are not has a loss of NaN); tokens outside of them add nothing.  h [T, C], W [V, C] of one type."""
     return _preference(h, W, targets, offsets, reference, None, beta, smoothing, None, False, False)[:2]
 
 
