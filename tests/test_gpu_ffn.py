@@ -371,3 +371,18 @@ def test_gradients_of_frozen_weights(io):
                          + [(F, 20, 4096, 4104), (F, 64, 4096, 4104), (F, 64, 4104, 4104), (F, 16, 520, 4112)])
 def test_few_rows_and_many_outputs(io, T, C, H):
     _check(*_inputs(T + C, T, C, H, io))
+
+
+@pytest.mark.parametrize("io", [BF, F])
+@pytest.mark.parametrize("T", [0, 40, 700])
+def test_the_call_that_forms_every_gradient(io, T):
+    x, up, down, g_y = _inputs(16, T, 72, 136, io)
+    _, kept = mhcl.gated_ffn(x, up, down, keep=True)
+    d = mhcl.FfnDesc(72, 136, T, io)
+    got = [torch.full_like(t, math.nan) for t in (x, up, down)]
+    ws = torch.empty(mhcl.ffn_workspace_bytes(d, mhcl.OP_FFN_GRAD), dtype=torch.uint8, device="cuda")
+    mhcl.mhcl_ffn_grad(d, x, up, down, kept, g_y, *got, ws)
+    assert all(torch.equal(a, b) for a, b in zip(got, mhcl.gated_ffn_grad(x, up, down, kept, g_y)))
+    if T:
+        with pytest.raises(mhcl.MhclError):
+            mhcl.mhcl_ffn_grad(d, x, up, down, kept, g_y, None, *got[1:], ws)
