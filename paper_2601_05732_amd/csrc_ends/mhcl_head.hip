@@ -94,7 +94,7 @@ __global__ __launch_bounds__(1024) void total_kernel(const ID *__restrict__ targ
 // Pairs of sequences, a block each: L = the sum of the tokens' -ce from one offset to the next, in fp64,
 //   m = beta ((L_c - R_c) - (L_r - R_r)),  loss = (1 - s) softplus(-m) + s softplus(m)
 // and the factor of each token's cross entropy in the weighted sum of the pairs, -+ beta weight dloss/dm for the chosen and the rejected sequence's,
-// 0 outside of the sequences.  (loss, weights of tokens: few numbers, in fp64 until they are rounded.)  16 pairs of 8192 tokens 6.2 us, 2 of 300 4.3: a
+// 0 outside of the sequences.  (loss, weights of tokens: few numbers, in fp64 until they are rounded.)  16 pairs of 8192 tokens 6.2 us, 2 of 300 4.0: a
 // launch and two dependent reads.
 // A token's weight is written by one block whatever the offsets are.  Those of pairs that ascend are taken as they are, so that a mistake stays in its pair;
 // E, the furthest end of the ascending pairs before, is where their tokens end.  A pair writes from there on; it is a mistake as well where it begins

@@ -488,7 +488,7 @@ __global__ __launch_bounds__(kBlock) void order_place_kernel(const Counting<ID, 
   }
 }
 
-// us: the order of 16384 tokens 7.4, of 8192 of 16 pairs 7.6; gathering 16384 rows, C = 4096 44, 6 TB/s, of 8192 the 5560 that count 21.
+// us: the order of 16384 tokens 7.4, of 8192 of 16 pairs 7.2; gathering 16384 rows, C = 4096 44, 6 TB/s, of 8192 the 5560 that count 21.
 // h's rows in the order of the tokens, a wave each; of those past the count, zeros in g_h and `ce` where they are (null: neither)
 template <typename IO>
 __global__ __launch_bounds__(kBlock) void gather_kernel(const void *__restrict__ h, char *__restrict__ hp, int64_t T, int C, const int32_t *__restrict__ row,
